@@ -111,6 +111,10 @@ typedef int32_t rq_status;
 #define RQ_BF16 1
 #define RQ_F32 2              /* gradients of rq_sensitivity only            */
 
+/* Code formats of the block-scaled cache (rq_block_cache). */
+#define RQ_INT8 0
+#define RQ_E4M3 1
+
 #define RQ_MAX_KV_HEADS 32
 
 /* Floats of the TurboQuant codebook table filled by rq_turbo_codebook. */
@@ -355,6 +359,152 @@ rq_status rq_cap_weights(int32_t n, double* w, double factor);
  * finite beta, r2 and r2_min.  Host only. */
 rq_status rq_fallback_beta(int32_t n, double* beta, const double* r2,
                            double r2_min);
+
+/* ------------------------------------------------------------------------
+ * The block-scaled 8-bit cache: a second kind of cache beside rq_cache, for
+ * serving at one width.  K and V are held in 8 bits with one fp32 scale for
+ * every block of 32 tokens of a kv-head; lengths live on the device, one a
+ * sequence, so calls can be captured into a graph and replayed as the
+ * sequences grow; several new tokens a sequence can attend at once; and a
+ * cache that keeps its tokens' accumulated attention weight can be shrunk to
+ * the heaviest ones.
+ *
+ * A block of 32 tokens x head_dim values x of one side (K or V) becomes
+ *   s = fp32(max|x| * fp32(1 / M)), M = 127 (RQ_INT8) or 448 (RQ_E4M3),
+ *       and 0 where that is below 2^-126;
+ *   code = round(x * fp32(1 / s)), half-even to a whole number or to an
+ *       e4m3 number (1 sign, 4 exponent, 3 mantissa bits, no infinities);
+ *       0 where s = 0.  The product is rounded to fp32 before.
+ * It stands for code * s.  The tokens of a sequence's unfinished last block
+ * stay in 16 bits until the block is full: with L tokens cached, the first
+ * floor(L / 32) * 32 are coded, the rest lie in the tail.
+ *
+ * Buffers (the caller allocates the sizes reported by rq_block_sizes, each
+ * aligned to 16 bytes; contents of a new cache do not matter):
+ *  codes      8-bit [n_layers][batch][n_kv_heads][2][capacity][head_dim]
+ *  scales     fp32  [n_layers][batch][n_kv_heads][2][capacity / 32]
+ *  tail       16-bit, in dtype [n_layers][batch][n_kv_heads][2][32][head_dim]
+ *             (token t of the unfinished block in row t mod 32)
+ *  positions  int32 [n_layers][batch][n_kv_heads][capacity]: each slot's
+ *             position in its sequence, ascending
+ *  weights    fp32  [n_layers][batch][n_kv_heads][capacity]: accumulated
+ *             attention weight of each slot; NULL if none is kept
+ * (2: K, then V).  Entries behind a sequence's last token are neither read
+ * for a result nor written.
+ *
+ * Device arrays of lengths (int32 [batch]) are read by the kernels.  What
+ * they hold cannot be checked on the host: a value outside the range that a
+ * call states is taken as the nearest one inside, and no call reads or
+ * writes outside its buffers.  Keys, values and queries must be finite and
+ * below 2^56 in magnitude; rows that a call does not use may hold anything. */
+typedef struct rq_block_cache {
+  int32_t format;        /* RQ_INT8 or RQ_E4M3                             */
+  int32_t dtype;         /* RQ_F16 or RQ_BF16: type of K, V, q, the tail   */
+  int32_t n_layers;
+  int32_t batch;         /* batch * n_kv_heads <= 32767                    */
+  int32_t n_kv_heads;    /* <= RQ_MAX_KV_HEADS                             */
+  int32_t n_q_heads;     /* multiple of n_kv_heads, ratio <= 16            */
+  int32_t head_dim;      /* 64 or 128                                      */
+  int32_t capacity;      /* slots per sequence, % 32 == 0, <= 2^24         */
+  void* codes;
+  float* scales;
+  void* tail;
+  int32_t* positions;
+  float* weights;
+} rq_block_cache;
+
+/* A device tensor [batch][heads][tokens][head_dim] whose rows are contiguous
+ * and may begin at any element; strides in elements. */
+typedef struct rq_block_rows {
+  void* data;
+  int64_t stride_batch, stride_head, stride_token;
+} rq_block_rows;
+
+/* Validate a descriptor (its pointers may be NULL here) and report the
+ * buffer sizes in bytes.  Any output pointer may be NULL.  Host only. */
+rq_status rq_block_sizes(const rq_block_cache* c, uint64_t* codes_bytes,
+                         uint64_t* scales_bytes, uint64_t* tail_bytes,
+                         uint64_t* positions_bytes, uint64_t* weights_bytes);
+
+/* Append tokens to one layer.  past: device int32 [batch], tokens each
+ * sequence holds (0..capacity).  k, v: [batch][n_kv_heads][n_new][head_dim]
+ * in dtype.  new_len: device int32 [batch], how many of the n_new rows each
+ * sequence takes (0..n_new; the rest is padding), or NULL: all.  Tokens that
+ * do not fit the capacity are dropped.  Codes every block that becomes full,
+ * keeps the rest in the tail, sets the new slots' positions (one more than
+ * the slot before; 0 in an empty sequence) and their weights to 0.  The
+ * caller adds the new tokens to its lengths.  Asynchronous. */
+rq_status rq_block_append(const rq_block_cache* c, int32_t layer,
+                          const int32_t* past, int32_t n_new,
+                          const int32_t* new_len, const rq_block_rows* k,
+                          const rq_block_rows* v, rq_stream stream);
+
+/* What an attention call asks of one layer. */
+typedef struct rq_block_query {
+  int32_t n_new;           /* query tokens a sequence, >= 1                */
+  int32_t max_tokens;      /* bound on past + new, n_new..capacity         */
+  const int32_t* past;     /* device [batch]: tokens before the query's
+                              own, 0..max_tokens - new                     */
+  const int32_t* new_len;  /* device [batch]: query tokens of each sequence
+                              (0..n_new), or NULL: n_new                   */
+  rq_block_rows q;         /* [batch][n_q_heads][n_new][head_dim] in dtype */
+  rq_block_rows out;       /* the same shape in out_dtype                  */
+  int32_t out_dtype;       /* RQ_F32, RQ_F16 or RQ_BF16                    */
+  float scale;             /* of the scores                                */
+  float cap;               /* scores become cap * tanh(score / cap); 0: no */
+  int32_t window;          /* a query sees keys less than window positions
+                              before it; 0: all                            */
+  const float* slopes;     /* device [n_q_heads]: slope * (distance in
+                              positions) is subtracted; NULL: none         */
+  int32_t accumulate;      /* add to the cache's weights                   */
+} rq_block_query;
+
+/* Workspace bytes of rq_block_attention for n_new, max_tokens, window and
+ * accumulate of *a (its pointers may be NULL).  Host only. */
+rq_status rq_block_attention_workspace(const rq_block_cache* c,
+                                       const rq_block_query* a,
+                                       uint64_t* bytes);
+
+/* Attention of the last new tokens of every sequence, which the cache holds
+ * already (rq_block_append with the same past and new_len), over the tokens
+ * up to each:
+ *   out[b][j][i] = softmax(x) V_hat,
+ *   x_t = f(scale * q[b][j][i] . K_hat_t) - slope_j * (p - p_t)
+ * for the slots t <= past + i with p - p_t < window, p being the position of
+ * slot past + i; query head j reads kv-head j / (n_q_heads / n_kv_heads).
+ * Rows i >= new_len of out are left as they were.  With accumulate, each
+ * slot's weight grows by its softmax probabilities summed over the call's
+ * query tokens and the kv-head's query heads.
+ * Accuracy: scores, softmax and sums are fp32 on exact operands (queries as
+ * fp16 relative to their row's largest element); probabilities times the
+ * value scale are rounded to 22 bits relative to the largest.
+ * ws: device scratch, 16-byte aligned, contents arbitrary; calls that share
+ * it must not overlap.  Asynchronous. */
+rq_status rq_block_attention(const rq_block_cache* c, int32_t layer,
+                             const rq_block_query* a, void* ws,
+                             uint64_t ws_bytes, rq_stream stream);
+
+/* Workspace bytes of rq_block_evict.  Host only. */
+rq_status rq_block_evict_workspace(const rq_block_cache* src, int32_t keep,
+                                   uint64_t* bytes);
+
+/* Shrink one layer of src into the same layer of dst, another cache of the
+ * same format, dtype, layers, batch, heads and head_dim with a capacity of
+ * at least keep.  A sequence of L = lengths[b] tokens (device int32 [batch],
+ * 0..src capacity) keeps min(L, keep) of them in each kv-head: the first
+ * n_sink, the last n_recent (>= 1) and of the others those with the largest
+ * weights (ties: the lowest slot; weights must not be NaN), in order, with
+ * their positions and weights.  Kept values are code * scale in fp32 (or the
+ * tail's 16-bit numbers), quantized again in dst's blocks, and rounded to
+ * dtype where they land in dst's tail.  new_lengths: device int32 [batch],
+ * receives min(L, keep).  n_sink + n_recent <= keep.  ws: device scratch,
+ * 16-byte aligned, contents arbitrary.  src is left as it was.
+ * Asynchronous. */
+rq_status rq_block_evict(const rq_block_cache* src, const rq_block_cache* dst,
+                         int32_t layer, const int32_t* lengths, int32_t keep,
+                         int32_t n_sink, int32_t n_recent,
+                         int32_t* new_lengths, void* ws, uint64_t ws_bytes,
+                         rq_stream stream);
 
 #ifdef __cplusplus
 }

@@ -19,6 +19,7 @@ RQ_OK, RQ_EINVAL, RQ_EINFEASIBLE, RQ_EUNSUPPORTED, RQ_EDEVICE, RQ_ESMALLWS = (
     0, -1, -2, -3, -4, -5)
 RQ_KIVI, RQ_QUAROT, RQ_TURBO, RQ_RTN, RQ_KIVI_RTN = 0, 1, 2, 3, 4
 RQ_F16, RQ_BF16, RQ_F32 = 0, 1, 2
+RQ_INT8, RQ_E4M3 = 0, 1
 RQ_MAX_KV_HEADS = 32
 
 EXPORTS = ("rq_version", "rq_last_error", "rq_cache_sizes", "rq_region_offset",
@@ -27,7 +28,9 @@ EXPORTS = ("rq_version", "rq_last_error", "rq_cache_sizes", "rq_region_offset",
            "rq_fit_distortion", "rq_allocate_bits", "rq_turbo_codebook",
            "rq_sensitivity_workspace", "rq_sensitivity", "rq_cap_weights",
            "rq_fallback_beta", "rq_decode_static_bytes",
-           "rq_decode_attention_static", "rq_read_probe", "rq_decode_step")
+           "rq_decode_attention_static", "rq_read_probe", "rq_decode_step",
+           "rq_block_sizes", "rq_block_append", "rq_block_attention_workspace",
+           "rq_block_attention", "rq_block_evict_workspace", "rq_block_evict")
 RQ_TURBO_TABLE_FLOATS = 8 * 2 * 256
 
 
@@ -46,6 +49,30 @@ class RqCache(C.Structure):
                 ("codes", C.c_void_p), ("meta", C.c_void_p),
                 ("resid", C.c_void_p), ("rotation", C.c_void_p),
                 ("codebook", C.c_void_p)]
+
+
+class RqBlockCache(C.Structure):
+    _fields_ = [("format", C.c_int32), ("dtype", C.c_int32),
+                ("n_layers", C.c_int32), ("batch", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("n_q_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("capacity", C.c_int32),
+                ("codes", C.c_void_p), ("scales", C.c_void_p),
+                ("tail", C.c_void_p), ("positions", C.c_void_p),
+                ("weights", C.c_void_p)]
+
+
+class RqBlockRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_batch", C.c_int64),
+                ("stride_head", C.c_int64), ("stride_token", C.c_int64)]
+
+
+class RqBlockQuery(C.Structure):
+    _fields_ = [("n_new", C.c_int32), ("max_tokens", C.c_int32),
+                ("past", C.c_void_p), ("new_len", C.c_void_p),
+                ("q", RqBlockRows), ("out", RqBlockRows),
+                ("out_dtype", C.c_int32), ("scale", C.c_float),
+                ("cap", C.c_float), ("window", C.c_int32),
+                ("slopes", C.c_void_p), ("accumulate", C.c_int32)]
 
 
 _lib = None
@@ -93,6 +120,17 @@ def lib():
             "rq_decode_step": (i32, [pc, i32, i32, vp, vp, vp, vp, C.c_float,
                                      vp, u64, vp]),
         }
+        pb, pr, pq = (C.POINTER(t) for t in (RqBlockCache, RqBlockRows,
+                                             RqBlockQuery))
+        sig.update({
+            "rq_block_sizes": (i32, [pb, pu64, pu64, pu64, pu64, pu64]),
+            "rq_block_append": (i32, [pb, i32, vp, i32, vp, pr, pr, vp]),
+            "rq_block_attention_workspace": (i32, [pb, pq, pu64]),
+            "rq_block_attention": (i32, [pb, i32, pq, vp, u64, vp]),
+            "rq_block_evict_workspace": (i32, [pb, i32, pu64]),
+            "rq_block_evict": (i32, [pb, pb, i32, vp, i32, i32, i32, vp, vp,
+                                     u64, vp]),
+        })
         for name, (res, args) in sig.items():
             f = getattr(L, name)
             f.restype, f.argtypes = res, args
@@ -446,3 +484,285 @@ class KVCache:
         rq_decode_attention_static(self.desc, layer, self.n_tokens[layer], q,
                                    out, scale, stream)
         return out
+
+
+# ------------------------------------------------- block-scaled 8-bit cache
+def make_block_cache(format, dtype, n_layers, batch, n_kv_heads, n_q_heads,
+                     head_dim, capacity, codes=None, scales=None, tail=None,
+                     positions=None, weights=None):
+    """Fill an RqBlockCache descriptor.  The device tensors must have the
+    sizes rq_block_sizes reports; they are kept alive on the returned
+    object."""
+    c = RqBlockCache(format, dtype, n_layers, batch, n_kv_heads, n_q_heads,
+                     head_dim, capacity)
+    buffers = (codes, scales, tail, positions, weights)
+    given = [t for t in buffers if t is not None]
+    if given:
+        sizes = rq_block_sizes(c)
+        for name, t, size in zip(("codes", "scales", "tail", "positions",
+                                  "weights"), buffers, sizes):
+            if t is None:
+                continue
+            if not t.is_cuda or t.device != given[0].device:
+                raise ValueError(f"{name} must be on the cache's device")
+            if t.numel() * t.element_size() < size:
+                raise ValueError(f"{name} has {t.numel() * t.element_size()} "
+                                 f"bytes, needs {size}")
+            setattr(c, name, _tptr(t))
+        c._device = given[0].device
+    c._buffers = buffers
+    return c
+
+
+def rq_block_sizes(cache):
+    """Bytes of (codes, scales, tail, positions, weights)."""
+    v = [C.c_uint64() for _ in range(5)]
+    _check(lib().rq_block_sizes(C.byref(cache), *(C.byref(x) for x in v)))
+    return tuple(x.value for x in v)
+
+
+def _block_stream(cache, stream):
+    """The stream of a call: the given one, or the current one of the cache's
+    device."""
+    import torch
+    s = torch.cuda.current_stream(cache._device) if stream is None else stream
+    if s.device != cache._device:
+        raise ValueError(f"the stream is on {s.device}, the cache on {cache._device}")
+    return C.c_void_p(s.cuda_stream)
+
+
+def _block_call(cache, f, *args):
+    """Launch with the cache's device current."""
+    import torch
+    if torch.cuda.current_device() == cache._device.index:
+        _check(f(*args))
+    else:
+        with torch.cuda.device(cache._device):
+            _check(f(*args))
+
+
+def _block_rows(cache, t, what, heads, n, dtypes):
+    """RqBlockRows of t [batch][heads][n][head_dim] (any strides, contiguous
+    rows)."""
+    shape = (cache.batch, heads, n, cache.head_dim)
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {shape}")
+    if t.device != cache._device:
+        raise ValueError(f"{what} is on {t.device}, the cache on {cache._device}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what} has dtype {t.dtype}, expected {dtypes[0]}")
+    sb, sh, st, sd = t.stride()
+    if sd != 1:
+        raise ValueError(f"the rows of {what} must be contiguous")
+    return RqBlockRows(t.data_ptr(), sb, sh, st)
+
+
+def _block_lengths(cache, t, what):
+    import torch
+    if t is None:
+        return None
+    if t.device != cache._device or t.dtype != torch.int32 \
+            or tuple(t.shape) != (cache.batch,) or not t.is_contiguous():
+        raise ValueError(f"{what} must be int32 [{cache.batch}] on the cache's device")
+    return C.c_void_p(t.data_ptr())
+
+
+def _block_dtype(cache):
+    import torch
+    return torch.bfloat16 if cache.dtype == RQ_BF16 else torch.float16
+
+
+def rq_block_append(cache, layer, past, k, v, new_len=None, stream=None):
+    """k, v: torch [batch][n_kv_heads][n_new][head_dim] in the cache's dtype
+    (any strides, contiguous rows); past, new_len: device int32 [batch]."""
+    n = k.shape[2] if k.dim() == 4 else -1
+    dt = (_block_dtype(cache),)
+    rk = _block_rows(cache, k, "k", cache.n_kv_heads, n, dt)
+    rv = _block_rows(cache, v, "v", cache.n_kv_heads, n, dt)
+    if past is None:
+        raise ValueError("past is missing")
+    _block_call(cache, lib().rq_block_append, C.byref(cache), layer,
+                _block_lengths(cache, past, "past"), n,
+                _block_lengths(cache, new_len, "new_len"), C.byref(rk),
+                C.byref(rv), _block_stream(cache, stream))
+
+
+def rq_block_attention_workspace(cache, n_new, max_tokens=None,
+                                 accumulate=False, window=0):
+    """Workspace bytes of an attention call (a call with a window needs no
+    more than one without)."""
+    a = RqBlockQuery(n_new, cache.capacity if max_tokens is None else max_tokens)
+    a.window, a.accumulate = int(window), int(bool(accumulate))
+    v = C.c_uint64()
+    _check(lib().rq_block_attention_workspace(C.byref(cache), C.byref(a),
+                                              C.byref(v)))
+    return v.value
+
+
+def rq_block_attention(cache, layer, past, q, out, ws, new_len=None,
+                       max_tokens=None, scale=None, cap=0.0, window=0,
+                       slopes=None, accumulate=False, stream=None):
+    """q: torch [batch][n_q_heads][n_new][head_dim] in the cache's dtype; out:
+    the same shape in float32, float16 or bfloat16 (both any strides,
+    contiguous rows); past, new_len: device int32 [batch]; slopes: device
+    float32 [n_q_heads]; ws: device byte tensor of at least
+    rq_block_attention_workspace bytes; max_tokens: bound on the sequences'
+    lengths (the capacity by default)."""
+    import torch
+    n = q.shape[2] if q.dim() == 4 else -1
+    types = (torch.float32, torch.float16, torch.bfloat16)
+    if past is None:
+        raise ValueError("past is missing")
+    if slopes is not None and (slopes.device != cache._device
+                               or slopes.dtype != torch.float32
+                               or tuple(slopes.shape) != (cache.n_q_heads,)
+                               or not slopes.is_contiguous()):
+        raise ValueError(f"slopes must be float32 [{cache.n_q_heads}] on the cache's device")
+    if ws.device != cache._device or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous tensor on the cache's device")
+    a = RqBlockQuery(
+        n, cache.capacity if max_tokens is None else max_tokens,
+        _block_lengths(cache, past, "past"),
+        _block_lengths(cache, new_len, "new_len"),
+        _block_rows(cache, q, "q", cache.n_q_heads, n, (_block_dtype(cache),)),
+        _block_rows(cache, out, "out", cache.n_q_heads, n, types),
+        (RQ_F32, RQ_F16, RQ_BF16)[types.index(out.dtype)],
+        cache.head_dim ** -0.5 if scale is None else float(scale), float(cap),
+        int(window), None if slopes is None else C.c_void_p(slopes.data_ptr()),
+        int(bool(accumulate)))
+    _block_call(cache, lib().rq_block_attention, C.byref(cache), layer,
+                C.byref(a), C.c_void_p(ws.data_ptr()),
+                ws.numel() * ws.element_size(), _block_stream(cache, stream))
+
+
+def rq_block_evict_workspace(cache, keep):
+    v = C.c_uint64()
+    _check(lib().rq_block_evict_workspace(C.byref(cache), keep, C.byref(v)))
+    return v.value
+
+
+def rq_block_evict(src, dst, layer, lengths, keep, new_lengths, ws, n_sink=4,
+                   n_recent=32, stream=None):
+    """Shrink one layer of src into dst; lengths, new_lengths: device int32
+    [batch]; ws: device byte tensor of at least rq_block_evict_workspace
+    bytes."""
+    if lengths is None or new_lengths is None:
+        raise ValueError("lengths and new_lengths are needed")
+    if dst._device != src._device:
+        raise ValueError("the caches are on different devices")
+    if ws.device != src._device or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous tensor on the cache's device")
+    _block_call(src, lib().rq_block_evict, C.byref(src), C.byref(dst), layer,
+                _block_lengths(src, lengths, "lengths"), keep, n_sink,
+                n_recent, _block_lengths(src, new_lengths, "new_lengths"),
+                C.c_void_p(ws.data_ptr()), ws.numel() * ws.element_size(),
+                _block_stream(src, stream))
+
+
+class BlockCache:
+    """Device buffers (torch), lengths and the descriptor of one block-scaled
+    8-bit cache.  `lengths` (device int32 [n_layers][batch]) says what each
+    sequence holds, `bound` (host) at most how much any does."""
+
+    def __init__(self, format, dtype, n_layers, batch, n_kv_heads, n_q_heads,
+                 head_dim, capacity, device="cuda", weights=False):
+        import torch
+        self.shape = (format, dtype, n_layers, batch, n_kv_heads, n_q_heads,
+                      head_dim)
+        sizes = rq_block_sizes(make_block_cache(*self.shape, capacity))
+        types = (torch.uint8, torch.float32,
+                 torch.bfloat16 if dtype == RQ_BF16 else torch.float16,
+                 torch.int32, torch.float32)
+        names = ("codes", "scales", "tail", "positions", "weights")
+        for name, size, t in zip(names, sizes, types):
+            new = torch.zeros(size // t.itemsize, dtype=t, device=device)
+            setattr(self, name, new if name != "weights" or weights else None)
+        self.desc = make_block_cache(*self.shape, capacity,
+                                     **{n: getattr(self, n) for n in names})
+        self.lengths = torch.zeros(n_layers, batch, dtype=torch.int32,
+                                   device=device)
+        self.bound = [0] * n_layers
+        self._ws = None
+
+    def _workspace(self, need, stream):
+        import torch
+        if self._ws is None or self._ws.numel() < need:
+            s = torch.cuda.current_stream(self.codes.device) if stream is None else stream
+            with torch.cuda.stream(s):
+                self._ws = torch.empty(max(need, 16), dtype=torch.uint8,
+                                       device=self.codes.device)
+        return self._ws
+
+    def _grow(self, layer, n, new_len, stream):
+        import torch
+        s = torch.cuda.current_stream(self.codes.device) if stream is None else stream
+        with torch.cuda.stream(s):
+            self.lengths[layer] += n if new_len is None else new_len.clamp(0, n)
+        self.bound[layer] += n
+
+    def _room(self, layer, n):
+        if self.bound[layer] + n > self.desc.capacity:
+            raise ValueError(f"tokens {self.bound[layer]} + {n} exceed the "
+                             f"capacity {self.desc.capacity}")
+
+    def append(self, layer, k, v, new_len=None, stream=None):
+        """Append k, v ([batch][n_kv_heads][n][head_dim]); new_len: how many
+        of the n rows each sequence takes."""
+        self._room(layer, k.shape[2])
+        rq_block_append(self.desc, layer, self.lengths[layer], k, v, new_len,
+                        stream)
+        self._grow(layer, k.shape[2], new_len, stream)
+
+    def _attend(self, layer, past, bound, q, out, new_len, stream, kw):
+        import torch
+        need = rq_block_attention_workspace(self.desc, q.shape[2], bound,
+                                            kw.get("accumulate", False),
+                                            kw.get("window", 0))
+        ws = self._workspace(need, stream)
+        s = torch.cuda.current_stream(self.codes.device) if stream is None else stream
+        if out is None:
+            with torch.cuda.stream(s):
+                out = torch.zeros_like(q) if new_len is not None else torch.empty_like(q)
+        rq_block_attention(self.desc, layer, past, q, out, ws, new_len, bound,
+                           stream=stream, **kw)
+        return out
+
+    def attention(self, layer, q, out=None, new_len=None, stream=None, **kw):
+        """Attention of the tokens appended last (q: [batch][n_q_heads][n]
+        [head_dim]; scale, cap, window, slopes, accumulate as
+        rq_block_attention)."""
+        import torch
+        s = torch.cuda.current_stream(self.codes.device) if stream is None else stream
+        with torch.cuda.stream(s):
+            past = self.lengths[layer] - (q.shape[2] if new_len is None
+                                          else new_len.clamp(0, q.shape[2]))
+        return self._attend(layer, past, self.bound[layer], q, out, new_len,
+                            stream, kw)
+
+    def step(self, layer, k, v, q, out=None, new_len=None, stream=None, **kw):
+        """Append k, v and attend with the same tokens' q."""
+        self._room(layer, k.shape[2])
+        past = self.lengths[layer]
+        rq_block_append(self.desc, layer, past, k, v, new_len, stream)
+        out = self._attend(layer, past, self.bound[layer] + k.shape[2], q, out,
+                           new_len, stream, kw)
+        self._grow(layer, k.shape[2], new_len, stream)
+        return out
+
+    def evict(self, keep, n_sink=4, n_recent=32, into=None, stream=None):
+        """Shrink every layer to at most `keep` tokens a sequence: into
+        another BlockCache of this shape, or a new one of the least
+        capacity."""
+        import torch
+        if into is None:
+            s = torch.cuda.current_stream(self.codes.device) if stream is None else stream
+            with torch.cuda.stream(s):
+                into = BlockCache(*self.shape, (keep + 31) // 32 * 32,
+                                  device=self.codes.device, weights=True)
+        ws = self._workspace(rq_block_evict_workspace(self.desc, keep), stream)
+        for layer in range(self.desc.n_layers):
+            rq_block_evict(self.desc, into.desc, layer, self.lengths[layer],
+                           keep, into.lengths[layer], ws, n_sink, n_recent,
+                           stream)
+            into.bound[layer] = min(self.bound[layer], keep)
+        return into

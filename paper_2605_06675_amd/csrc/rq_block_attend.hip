@@ -1,0 +1,390 @@
+// Attention over the block-scaled 8-bit cache, for few query rows a unit: the
+// cache is streamed once per tile of 16 rows.
+//
+//   out = softmax(f(scale q . k^)) v^,  f(x) = cap tanh(x / cap) - slope distance
+//
+// One pass with a running maximum and sum.  The products run on
+// v_mfma_f32_16x16x32_f16 with the tokens as rows and the queries as columns:
+// S^T = K Q^T leaves a lane with 8 tokens of one query, which is the operand
+// that O^T = V^T P^T wants of it, so the probabilities never move between
+// lanes.  Every code is exact in fp16; a block's key scale multiplies the
+// fp32 scores, its value scale the probabilities.  These are split into an
+// fp16 pair hi + lo (22 bits), in units that keep p * scale below 2^15.
+#include "rq_block.h"
+
+namespace rq {
+
+namespace {
+
+template <int D>
+struct ValueBlock {
+  u2 w[8];        // D = 64: one word each
+  float scale;
+};
+
+// Lane (r, g) has, of its 8 tokens 16 (j / 4) + 4 g + j % 4, the channels
+// D / 16 r + 0..D/16-1.
+template <int D>
+__device__ __forceinline__ void load_values(const RQ_GLOBAL uint8_t* v, const RQ_GLOBAL float* scale,
+                                            int blk, ValueBlock<D>* t) {
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int tok = 16 * (j >> 2) + 4 * g + (j & 3);
+    const RQ_GLOBAL uint8_t* p = v + (uint32_t)(blk * kBlockTokens + tok) * D + (D / 16) * r;
+    if constexpr (D == 128)
+      t->w[j] = *(const RQ_GLOBAL u2*)p;
+    else
+      t->w[j].x = *(const RQ_GLOBAL uint32_t*)p;
+  }
+  t->scale = scale[blk];
+}
+
+// The running state of one wave: lane (r, g) holds, of query row r, the
+// channels D / 16 (4 g + i) + e in o[e][i], in units of kValueUnit / unit.
+template <int D>
+struct Running {
+  f4 o[D / 16];
+  float m, l;      // maximum so far (moved lazily: p <= 2^8), this lane's sum
+  float unit;      // a power of two: value scale * unit <= 2^7 (0: no block yet)
+};
+
+template <int D>
+__device__ __forceinline__ void rescale(Running<D>* st, float by) {
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) st->o[e] *= by;
+}
+
+// Probabilities of a block's scores, and the sums' rescaling where a score
+// exceeds the reference by more than 8 (log2).
+template <int D>
+__device__ __forceinline__ void probabilities(Running<D>* st, f4 s[2]) {
+  float top = -3.0e38f;
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = __builtin_fmaxf(top, s[m][i]);
+  if (__any(top > st->m + 8.0f)) {
+    top = __builtin_fmaxf(top, __shfl_xor(top, 16, 64));
+    top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
+    const float mn = __builtin_fmaxf(st->m, top);
+    const float by = exp2_f(st->m - mn);
+    st->m = mn;
+    st->l *= by;
+    rescale<D>(st, by);
+  }
+  float sum = 0.0f;
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[m][i] = exp2_f(s[m][i] - st->m);
+      sum += s[m][i];
+    }
+  st->l += sum;
+}
+
+template <int FMT, int D>
+__device__ __forceinline__ void add_values(const ValueBlock<D>& v, const f4 s[2], Running<D>* st) {
+  if (v.scale * st->unit > 128.0f || st->unit == 0.0f) {      // (the same in every lane)
+    // (a scale of zero has no exponent; 0 serves)
+    int e = v.scale > 0.0f ? __builtin_amdgcn_frexp_expf(v.scale) : 0;
+    e = e < -100 ? -100 : e;
+    const float unit = __builtin_amdgcn_ldexpf(128.0f, -e);
+    rescale<D>(st, st->unit == 0.0f ? 1.0f : unit / st->unit);
+    st->unit = unit;
+  }
+  const float by = v.scale * st->unit;
+  u4 hi, lo;
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float a = s[m][2 * i] * by, b = s[m][2 * i + 1] * by;
+      // (toward zero by its own instruction: a conversion left to the compiler
+      // may be fused with the product above, where hi would not be that of a)
+      const h2 h = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(a, b));
+      hi[2 * m + i] = as_u32(h);
+      lo[2 * m + i] = as_u32((h2){(_Float16)(a - (float)h.x), (_Float16)(b - (float)h.y)});
+    }
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c) {
+    uint32_t op[4][4];        // [token pair][channel]
+#pragma unroll
+    for (int j = 0; j < 4; ++j) value_pairs<FMT>(v.w[2 * j][c], v.w[2 * j + 1][c], op[j]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const h8 f = as_h8((u4){op[0][e], op[1][e], op[2][e], op[3][e]});
+      f4 o = st->o[4 * c + e];
+      o = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, as_h8(hi), o, 0, 0, 0);
+      st->o[4 * c + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, as_h8(lo), o, 0, 0, 0);
+    }
+  }
+}
+
+// The tail's values: bf16 operands, whose range needs no unit.  An fp16 value
+// is a bf16 pair hi + lo, as the probabilities are.  Rows from n_tail on
+// count as zero.
+template <int FMT, int D, bool BF16>
+__device__ __forceinline__ void add_tail(const RQ_GLOBAL uint16_t* vt, int n_tail, const f4 s[2],
+                                         Running<D>* st) {
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  if (st->unit == 0.0f) st->unit = 1.0f;
+  const float by = st->unit * kValueUnit<FMT>;
+  u4 hi, lo;
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float a = s[m][2 * i] * by, b = s[m][2 * i + 1] * by;
+      const uint32_t ha = bf16_rne(a), hb = bf16_rne(b);
+      hi[2 * m + i] = ha | (hb << 16);
+      lo[2 * m + i] = (uint32_t)bf16_rne(a - __uint_as_float(ha << 16)) |
+                      ((uint32_t)bf16_rne(b - __uint_as_float(hb << 16)) << 16);
+    }
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {     // two channels a word
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int tok = 16 * (j >> 2) + 4 * g + (j & 3);
+      w[j] = tok < n_tail ? *(const RQ_GLOBAL uint32_t*)(vt + tok * D + (D / 16) * r + 2 * c) : 0u;
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      u4 f, f2;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        f[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], e ? 0x07060302u : 0x05040100u);
+        if constexpr (!BF16) {
+          const float x = widen_t<false>(f[j] & 0xffffu), y = widen_t<false>(f[j] >> 16);
+          const uint32_t hx = bf16_rne(x), hy = bf16_rne(y);
+          f[j] = hx | (hy << 16);
+          f2[j] = (uint32_t)bf16_rne(x - __uint_as_float(hx << 16)) |
+                  ((uint32_t)bf16_rne(y - __uint_as_float(hy << 16)) << 16);
+        }
+      }
+      f4 o = st->o[2 * c + e];
+      o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_b8(f), as_b8(hi), o, 0, 0, 0);
+      o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_b8(f), as_b8(lo), o, 0, 0, 0);
+      if constexpr (!BF16)
+        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_b8(f2), as_b8(hi), o, 0, 0, 0);
+      st->o[2 * c + e] = o;
+    }
+  }
+}
+
+// One thread's share of an output row: N channels from ch.
+template <int N>
+__device__ __forceinline__ void store_out(const BlockAttendLaunch& a, int b, int head, int token,
+                                          int ch, const float* x) {
+  const int64_t at = b * a.out.sb + head * a.out.sh + token * a.out.st + ch;
+  if (a.out_dtype == RQ_F32) {
+    RQ_GLOBAL float* o = gptr((float*)a.out.p) + at;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i)
+      *(RQ_GLOBAL f4_any*)(o + 4 * i) = (f4){x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+    return;
+  }
+  RQ_GLOBAL uint16_t* o = gptr((uint16_t*)a.out.p) + at;
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    u2 w;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float y = x[4 * i + 2 * j], z = x[4 * i + 2 * j + 1];
+      w[j] = a.out_dtype == RQ_BF16 ? bf16_rne(y) | ((uint32_t)bf16_rne(z) << 16)
+                                    : narrow_t<false>(y) | ((uint32_t)narrow_t<false>(z) << 16);
+    }
+    *(RQ_GLOBAL u2_any*)(o + 4 * i) = w;
+  }
+}
+
+template <int FMT, int D, bool BF16>
+__global__ void __launch_bounds__(256) block_attend_kernel(BlockAttendLaunch a) {
+  constexpr int kStride = D + 4;           // floats of a row in LDS
+  __shared__ float sh_o[4][16 * kStride];
+  __shared__ float sh_ml[4][16][2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const int split = blockIdx.x % a.splits, rt = blockIdx.x / a.splits, unit = blockIdx.y;
+  const int b = unit / a.c.H, h = unit - b * a.c.H;
+  int past, nnew;
+  block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
+  const int first = rt * 16 / a.G;         // the tile's rows belong to tokens first..last
+  if (first >= nnew) return;
+  int last = (rt * 16 + 15) / a.G;
+  last = last < nnew ? last : nnew - 1;
+  const int total = past + nnew, full = total / kBlockTokens;
+  // blocks the rows may see; block `full` is the tail
+  const int hi_all = (past + last) / kBlockTokens + 1;
+  int lo_all = a.window ? past + first - a.window + 1 : 0;
+  lo_all = lo_all > 0 ? lo_all / kBlockTokens : 0;
+  const int64_t nb = hi_all - lo_all;
+  const int lo = lo_all + (int)(nb * split / a.splits);
+  const int hi = lo_all + (int)(nb * (split + 1) / a.splits);
+
+  QueryTile<D> q;
+  load_queries<D, BF16>(a, b, h, rt * 16 + r, past, nnew, &q);
+  Running<D> st;
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) st.o[e] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+  st.m = -1.0e30f;
+  st.l = 0.0f;
+  st.unit = 0.0f;
+
+  const RQ_GLOBAL uint8_t* kc = gptr(a.c.codes) + (size_t)unit * 2 * a.c.cap * D;
+  const RQ_GLOBAL uint8_t* vc = kc + (size_t)a.c.cap * D;
+  const RQ_GLOBAL float* ks = gptr(a.c.scales) + (size_t)unit * 2 * (a.c.cap / kBlockTokens);
+  const RQ_GLOBAL float* vs = ks + a.c.cap / kBlockTokens;
+  const RQ_GLOBAL int32_t* pos = gptr(a.c.positions) + (size_t)unit * a.c.cap;
+  // blocks below all_seen lie wholly before every row of the tile
+  const int all_seen = a.window ? 0 : (past + first + 1) / kBlockTokens;
+
+  const int end = hi < full ? hi : full;
+  auto step = [&](const KeyBlock<D>& k, const ValueBlock<D>& v, int blk) {
+    f4 s[2];
+    key_products<FMT, D>(k, q, s);
+    block_scores<D>(a, q, pos, k.scale * q.qs, blk * kBlockTokens, past, blk >= all_seen, s);
+    probabilities<D>(&st, s);
+    add_values<FMT, D>(v, s, &st);
+  };
+  int blk = lo + wave;
+  if (blk < end) {
+    // the next block's codes are in flight while one is worked on (the last
+    // load repeats the last block)
+    KeyBlock<D> k0, k1;
+    ValueBlock<D> v0, v1;
+    load_keys<D>(kc, ks, blk, &k0);
+    load_values<D>(vc, vs, blk, &v0);
+    for (;;) {
+      const int b1 = blk + 4 < end ? blk + 4 : blk;
+      load_keys<D>(kc, ks, b1, &k1);
+      load_values<D>(vc, vs, b1, &v1);
+      step(k0, v0, blk);
+      if (b1 == blk) break;
+      blk = b1;
+      const int b2 = blk + 4 < end ? blk + 4 : blk;
+      load_keys<D>(kc, ks, b2, &k0);
+      load_values<D>(vc, vs, b2, &v0);
+      step(k1, v1, blk);
+      if (b2 == blk) break;
+      blk = b2;
+    }
+  }
+  if (lo <= full && full < hi && (full - lo) % 4 == wave) {
+    const RQ_GLOBAL uint16_t* kt = gptr(a.c.tail) + (size_t)unit * 2 * kBlockTokens * D;
+    f4 s[2];
+    tail_products<D, BF16>(a, b, h, kt, q, s);
+    block_scores<D>(a, q, pos, a.qscale, full * kBlockTokens, past, true, s);
+    probabilities<D>(&st, s);
+    add_tail<FMT, D, BF16>(kt + kBlockTokens * D, total % kBlockTokens, s, &st);
+  }
+
+  // the four waves' sums
+  st.l += __shfl_xor(st.l, 16, 64);
+  st.l += __shfl_xor(st.l, 32, 64);
+  const float to_value = st.unit == 0.0f ? 0.0f : 1.0f / (st.unit * kValueUnit<FMT>);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int e = 0; e < D / 16; e += 4)
+      *(f4*)&sh_o[wave][r * kStride + (D / 16) * (4 * g + i) + e] =
+          (f4){st.o[e][i], st.o[e + 1][i], st.o[e + 2][i], st.o[e + 3][i]} * to_value;
+  if (g == 0) {
+    sh_ml[wave][r][0] = st.m;
+    sh_ml[wave][r][1] = st.l;
+  }
+  __syncthreads();
+  const int row = threadIdx.x >> 4, ch = (threadIdx.x & 15) * (D / 16);
+  float m = sh_ml[0][row][0];
+  for (int w = 1; w < 4; ++w) m = __builtin_fmaxf(m, sh_ml[w][row][0]);
+  float l = 0.0f, x[D / 16];
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) x[e] = 0.0f;
+  for (int w = 0; w < 4; ++w) {
+    const float by = exp2_f(sh_ml[w][row][0] - m);
+    l = __builtin_fmaf(sh_ml[w][row][1], by, l);
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e)
+      x[e] = __builtin_fmaf(sh_o[w][row * kStride + ch + e], by, x[e]);
+  }
+  if (a.splits > 1) {
+    const size_t at = ((size_t)unit * a.row_tiles + rt) * a.splits + split;
+    RQ_GLOBAL float* o = gptr(a.part) + at * 16 * D + row * D + ch;
+#pragma unroll
+    for (int e = 0; e < D / 16; e += 4) *(RQ_GLOBAL f4*)(o + e) = (f4){x[e], x[e + 1], x[e + 2], x[e + 3]};
+    if (ch == 0) {
+      gptr(a.part_ml)[(at * 16 + row) * 2] = m;
+      gptr(a.part_ml)[(at * 16 + row) * 2 + 1] = l;
+    }
+    return;
+  }
+  const int grow = rt * 16 + row, token = grow / a.G;
+  if (token >= nnew) return;
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) x[e] *= inv;
+  store_out<D / 16>(a, b, h * a.G + grow - token * a.G, token, ch, x);
+  if (a.accumulate && ch == 0) {
+    gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + grow) * 2] = m;
+    gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + grow) * 2 + 1] = inv;
+  }
+}
+
+// Adds the splits' partial results of one row tile.
+template <int D>
+__global__ void __launch_bounds__(256) block_merge_kernel(BlockAttendLaunch a) {
+  const int rt = blockIdx.x, unit = blockIdx.y;
+  const int b = unit / a.c.H, h = unit - b * a.c.H;
+  int past, nnew;
+  block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
+  const int row = threadIdx.x >> 4, ch = (threadIdx.x & 15) * (D / 16);
+  const int grow = rt * 16 + row, token = grow / a.G;
+  if (token >= nnew) return;
+  const size_t base = ((size_t)unit * a.row_tiles + rt) * a.splits;
+  const RQ_GLOBAL float* ml = gptr(a.part_ml) + (base * 16 + row) * 2;
+  const RQ_GLOBAL float* o = gptr(a.part) + base * 16 * D + row * D + ch;
+  float m = -1.0e30f;
+  for (int s = 0; s < a.splits; ++s) m = __builtin_fmaxf(m, ml[s * 32]);
+  float l = 0.0f, x[D / 16];
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) x[e] = 0.0f;
+  for (int s = 0; s < a.splits; ++s) {
+    const float by = exp2_f(ml[s * 32] - m);
+    l = __builtin_fmaf(ml[s * 32 + 1], by, l);
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e)
+      x[e] = __builtin_fmaf(o[(size_t)s * 16 * D + e], by, x[e]);
+  }
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) x[e] *= inv;
+  store_out<D / 16>(a, b, h * a.G + grow - token * a.G, token, ch, x);
+  if (a.accumulate && ch == 0) {
+    gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + grow) * 2] = m;
+    gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + grow) * 2 + 1] = inv;
+  }
+}
+
+template <int FMT, int D>
+hipError_t launch(const BlockAttendLaunch& a, hipStream_t s) {
+  const dim3 grid(a.splits * a.row_tiles, a.c.B * a.c.H);
+  if (a.c.is_bf16)
+    hipLaunchKernelGGL((block_attend_kernel<FMT, D, true>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((block_attend_kernel<FMT, D, false>), grid, dim3(256), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return e;
+  hipLaunchKernelGGL((block_merge_kernel<D>), dim3(a.row_tiles, a.c.B * a.c.H), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_block_attend(const BlockAttendLaunch& a, hipStream_t s) {
+  if (a.c.fmt == RQ_INT8) return a.c.D == 64 ? launch<RQ_INT8, 64>(a, s) : launch<RQ_INT8, 128>(a, s);
+  return a.c.D == 64 ? launch<RQ_E4M3, 64>(a, s) : launch<RQ_E4M3, 128>(a, s);
+}
+
+}  // namespace rq

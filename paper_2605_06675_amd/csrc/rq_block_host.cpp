@@ -1,0 +1,282 @@
+// Entry points of the block-scaled 8-bit cache: validation and launch set-up.
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+
+#include "rq_block.h"
+#include "rq_internal.h"
+
+namespace {
+
+rq_status fail(rq_status code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return rq::set_error(code, buf);
+}
+
+rq_status ok() { return rq::set_error(RQ_OK, ""); }
+
+rq_status launched(hipError_t e, const char* what) {
+  if (e != hipSuccess) return fail(RQ_EDEVICE, "%s: %s", what, hipGetErrorString(e));
+  return ok();
+}
+
+bool unaligned(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 != 0; }
+
+rq_status check_shape(const rq_block_cache* c) {
+  if (!c) return fail(RQ_EINVAL, "cache descriptor is NULL");
+  if (c->format != RQ_INT8 && c->format != RQ_E4M3)
+    return fail(RQ_EINVAL, "unknown code format %d", c->format);
+  if (c->dtype != RQ_F16 && c->dtype != RQ_BF16)
+    return fail(RQ_EINVAL, "unknown dtype %d", c->dtype);
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(RQ_EUNSUPPORTED, "head_dim %d (64 and 128 are supported)", c->head_dim);
+  if (c->n_layers < 1 || c->batch < 1)
+    return fail(RQ_EINVAL, "n_layers and batch must be >= 1");
+  if (c->n_kv_heads < 1 || c->n_kv_heads > RQ_MAX_KV_HEADS)
+    return fail(RQ_EINVAL, "n_kv_heads %d outside 1..%d", c->n_kv_heads, RQ_MAX_KV_HEADS);
+  if ((int64_t)c->batch * c->n_kv_heads > 32767)
+    return fail(RQ_EUNSUPPORTED, "batch * n_kv_heads = %lld exceeds 32767",
+                (long long)c->batch * c->n_kv_heads);
+  if (c->n_q_heads < c->n_kv_heads || c->n_q_heads % c->n_kv_heads)
+    return fail(RQ_EINVAL, "n_q_heads %d is not a multiple of n_kv_heads %d", c->n_q_heads,
+                c->n_kv_heads);
+  if (c->n_q_heads / c->n_kv_heads > 16)
+    return fail(RQ_EUNSUPPORTED, "more than 16 query heads per kv-head");
+  if (c->capacity < rq::kBlockTokens || c->capacity % rq::kBlockTokens ||
+      c->capacity > (1 << 24))
+    return fail(RQ_EINVAL, "capacity %d must be a positive multiple of 32, at most 2^24",
+                c->capacity);
+  const double codes = 2.0 * c->n_layers * c->batch * c->n_kv_heads * c->capacity * c->head_dim;
+  if (codes > 9.0e18) return fail(RQ_EINVAL, "cache too large");
+  return RQ_OK;
+}
+
+rq_status check_buffers(const rq_block_cache* c, int32_t layer) {
+  rq_status st = check_shape(c);
+  if (st != RQ_OK) return st;
+  if (layer < 0 || layer >= c->n_layers) return fail(RQ_EINVAL, "layer %d out of range", layer);
+  if (!c->codes || !c->scales || !c->tail || !c->positions)
+    return fail(RQ_EINVAL, "the cache has a NULL buffer");
+  if (unaligned(c->codes) || unaligned(c->scales) || unaligned(c->tail) ||
+      unaligned(c->positions) || unaligned(c->weights))
+    return fail(RQ_EINVAL, "a cache buffer is not 16-byte aligned");
+  return RQ_OK;
+}
+
+uint64_t units(const rq_block_cache* c) { return (uint64_t)c->batch * c->n_kv_heads; }
+
+rq::BlockLayer layer_of(const rq_block_cache* c, int32_t layer) {
+  const uint64_t u = units(c) * layer, cap = c->capacity, D = c->head_dim;
+  rq::BlockLayer l{};
+  l.codes = static_cast<uint8_t*>(c->codes) + u * 2 * cap * D;
+  l.scales = c->scales + u * 2 * (cap / rq::kBlockTokens);
+  l.tail = static_cast<uint16_t*>(c->tail) + u * 2 * rq::kBlockTokens * D;
+  l.positions = c->positions + u * cap;
+  l.weights = c->weights ? c->weights + u * cap : nullptr;
+  l.B = c->batch;
+  l.H = c->n_kv_heads;
+  l.cap = c->capacity;
+  l.D = c->head_dim;
+  l.fmt = c->format;
+  l.is_bf16 = c->dtype == RQ_BF16;
+  return l;
+}
+
+rq::BlockRows rows_of(const rq_block_rows* r) {
+  return rq::BlockRows{r->data, r->stride_batch, r->stride_head, r->stride_token};
+}
+
+rq_status check_query(const rq_block_cache* c, const rq_block_query* a) {
+  if (!a) return fail(RQ_EINVAL, "query is NULL");
+  if (a->n_new < 1 || a->n_new > c->capacity)
+    return fail(RQ_EINVAL, "n_new %d outside 1..%d", a->n_new, c->capacity);
+  if (a->max_tokens < a->n_new || a->max_tokens > c->capacity)
+    return fail(RQ_EINVAL, "max_tokens %d outside %d..%d", a->max_tokens, a->n_new, c->capacity);
+  if (a->window < 0) return fail(RQ_EINVAL, "window %d must be >= 0", a->window);
+  return RQ_OK;
+}
+
+// How an attention call is split, and what it needs of the workspace.
+struct Plan {
+  int row_tiles, splits;
+  uint64_t part, part_ml, stats;   // bytes
+  uint64_t bytes() const { return part + part_ml + stats; }
+};
+
+// One resident round: three workgroups a CU over the units' row tiles, at
+// least four blocks (one a wave) a workgroup.
+Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
+  Plan p{};
+  const int64_t G = c->n_q_heads / c->n_kv_heads, u = (int64_t)units(c);
+  p.row_tiles = (int)((a->n_new * G + 15) / 16);
+  int64_t blocks = (a->max_tokens + rq::kBlockTokens - 1) / rq::kBlockTokens;
+  if (a->window) {
+    const int64_t seen = ((int64_t)a->window + 16 / G + 1) / rq::kBlockTokens + 2;
+    blocks = seen < blocks ? seen : blocks;
+  }
+  int64_t s = 3 * (int64_t)rq::device_cus() / (u * p.row_tiles);
+  s = std::min(s, (blocks + 3) / 4);
+  p.splits = (int)std::max<int64_t>(s, 1);
+  const uint64_t tiles = (uint64_t)u * p.row_tiles;
+  if (p.splits > 1) {
+    p.part = tiles * p.splits * 16 * c->head_dim * sizeof(float);
+    p.part_ml = tiles * p.splits * 16 * 2 * sizeof(float);
+  }
+  if (a->accumulate) p.stats = tiles * 16 * 2 * sizeof(float);
+  return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+rq_status rq_block_sizes(const rq_block_cache* c, uint64_t* codes_bytes, uint64_t* scales_bytes,
+                         uint64_t* tail_bytes, uint64_t* positions_bytes,
+                         uint64_t* weights_bytes) {
+  rq_status st = check_shape(c);
+  if (st != RQ_OK) return st;
+  const uint64_t u = units(c) * c->n_layers, cap = c->capacity, D = c->head_dim;
+  if (codes_bytes) *codes_bytes = u * 2 * cap * D;
+  if (scales_bytes) *scales_bytes = u * 2 * (cap / rq::kBlockTokens) * sizeof(float);
+  if (tail_bytes) *tail_bytes = u * 2 * rq::kBlockTokens * D * sizeof(uint16_t);
+  if (positions_bytes) *positions_bytes = u * cap * sizeof(int32_t);
+  if (weights_bytes) *weights_bytes = u * cap * sizeof(float);
+  return ok();
+}
+
+rq_status rq_block_append(const rq_block_cache* c, int32_t layer, const int32_t* past,
+                          int32_t n_new, const int32_t* new_len, const rq_block_rows* k,
+                          const rq_block_rows* v, rq_stream stream) {
+  rq_status st = check_buffers(c, layer);
+  if (st != RQ_OK) return st;
+  if (n_new < 1 || n_new > c->capacity)
+    return fail(RQ_EINVAL, "n_new %d outside 1..%d", n_new, c->capacity);
+  if (!past || !k || !v || !k->data || !v->data) return fail(RQ_EINVAL, "NULL device pointer");
+  rq::BlockAppendLaunch a{};
+  a.c = layer_of(c, layer);
+  a.past = past;
+  a.new_len = new_len;
+  a.k = rows_of(k);
+  a.v = rows_of(v);
+  a.n = n_new;
+  return launched(rq::launch_block_append(a, reinterpret_cast<hipStream_t>(stream)),
+                  "append launch");
+}
+
+rq_status rq_block_attention_workspace(const rq_block_cache* c, const rq_block_query* a,
+                                       uint64_t* bytes) {
+  rq_status st = check_shape(c);
+  if (st != RQ_OK) return st;
+  st = check_query(c, a);
+  if (st != RQ_OK) return st;
+  if (!bytes) return fail(RQ_EINVAL, "bytes is NULL");
+  *bytes = plan_attention(c, a).bytes();
+  return ok();
+}
+
+rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_block_query* q,
+                             void* ws, uint64_t ws_bytes, rq_stream stream) {
+  rq_status st = check_buffers(c, layer);
+  if (st != RQ_OK) return st;
+  st = check_query(c, q);
+  if (st != RQ_OK) return st;
+  if (!q->past || !q->q.data || !q->out.data) return fail(RQ_EINVAL, "NULL device pointer");
+  if (q->out_dtype != RQ_F32 && q->out_dtype != RQ_F16 && q->out_dtype != RQ_BF16)
+    return fail(RQ_EINVAL, "unknown output dtype %d", q->out_dtype);
+  if (!std::isfinite(q->scale)) return fail(RQ_EINVAL, "scale is not finite");
+  if (!std::isfinite(q->cap) || q->cap < 0.0f)
+    return fail(RQ_EINVAL, "cap must be finite and >= 0");
+  if (q->accumulate && !c->weights) return fail(RQ_EINVAL, "the cache keeps no weights");
+  const float log2e = 1.4426950408889634f;
+  const float qscale = q->cap > 0.0f ? q->scale / q->cap : q->scale * log2e;
+  if (!std::isfinite(qscale) || !std::isfinite(q->cap * log2e))
+    return fail(RQ_EINVAL, "scale %g and cap %g leave the fp32 range", q->scale, q->cap);
+  const Plan p = plan_attention(c, q);
+  if (ws_bytes < p.bytes())
+    return fail(RQ_ESMALLWS, "workspace %llu bytes < %llu needed", (unsigned long long)ws_bytes,
+                (unsigned long long)p.bytes());
+  if (p.bytes() && (!ws || unaligned(ws)))
+    return fail(RQ_EINVAL, "the workspace is NULL or not 16-byte aligned");
+  rq::BlockAttendLaunch a{};
+  a.c = layer_of(c, layer);
+  a.past = q->past;
+  a.new_len = q->new_len;
+  a.q = rows_of(&q->q);
+  a.out = rows_of(&q->out);
+  a.out_dtype = q->out_dtype;
+  a.G = c->n_q_heads / c->n_kv_heads;
+  a.n = q->n_new;
+  a.max_tokens = q->max_tokens;
+  a.row_tiles = p.row_tiles;
+  a.splits = p.splits;
+  a.qscale = qscale;
+  a.cap = q->cap * log2e;
+  a.window = q->window;
+  a.slopes = q->slopes;
+  a.accumulate = q->accumulate != 0;
+  uint8_t* w = static_cast<uint8_t*>(ws);
+  a.part = reinterpret_cast<float*>(w);
+  a.part_ml = reinterpret_cast<float*>(w + p.part);
+  a.stats = reinterpret_cast<float*>(w + p.part + p.part_ml);
+  const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  hipError_t e = rq::launch_block_attend(a, s);
+  if (e == hipSuccess && a.accumulate) e = rq::launch_block_weigh(a, s);
+  return launched(e, "attention launch");
+}
+
+rq_status rq_block_evict_workspace(const rq_block_cache* src, int32_t keep, uint64_t* bytes) {
+  rq_status st = check_shape(src);
+  if (st != RQ_OK) return st;
+  if (keep < 1) return fail(RQ_EINVAL, "keep %d must be >= 1", keep);
+  if (!bytes) return fail(RQ_EINVAL, "bytes is NULL");
+  *bytes = units(src) * keep * sizeof(int32_t);
+  return ok();
+}
+
+rq_status rq_block_evict(const rq_block_cache* src, const rq_block_cache* dst, int32_t layer,
+                         const int32_t* lengths, int32_t keep, int32_t n_sink, int32_t n_recent,
+                         int32_t* new_lengths, void* ws, uint64_t ws_bytes, rq_stream stream) {
+  rq_status st = check_buffers(src, layer);
+  if (st != RQ_OK) return st;
+  st = check_buffers(dst, layer);
+  if (st != RQ_OK) return st;
+  if (src->format != dst->format || src->dtype != dst->dtype || src->n_layers != dst->n_layers ||
+      src->batch != dst->batch || src->n_kv_heads != dst->n_kv_heads ||
+      src->n_q_heads != dst->n_q_heads || src->head_dim != dst->head_dim)
+    return fail(RQ_EINVAL, "the two caches differ in more than their capacity");
+  if (src->codes == dst->codes || src->scales == dst->scales || src->tail == dst->tail ||
+      src->positions == dst->positions || src->weights == dst->weights)
+    return fail(RQ_EINVAL, "the two caches share a buffer, or the source keeps no weights");
+  if (!src->weights) return fail(RQ_EINVAL, "the source keeps no weights");
+  if (keep < 1 || keep > dst->capacity)
+    return fail(RQ_EINVAL, "keep %d outside 1..%d", keep, dst->capacity);
+  if (n_sink < 0 || n_recent < 1 || (int64_t)n_sink + n_recent > keep)
+    return fail(RQ_EINVAL, "n_sink %d >= 0 and n_recent %d >= 1 must fit keep %d", n_sink,
+                n_recent, keep);
+  if (!lengths || !new_lengths) return fail(RQ_EINVAL, "NULL device pointer");
+  uint64_t need = 0;
+  st = rq_block_evict_workspace(src, keep, &need);
+  if (st != RQ_OK) return st;
+  if (ws_bytes < need)
+    return fail(RQ_ESMALLWS, "workspace %llu bytes < %llu needed", (unsigned long long)ws_bytes,
+                (unsigned long long)need);
+  if (!ws || unaligned(ws)) return fail(RQ_EINVAL, "the workspace is NULL or not 16-byte aligned");
+  rq::BlockEvictLaunch a{};
+  a.src = layer_of(src, layer);
+  a.dst = layer_of(dst, layer);
+  a.lengths = lengths;
+  a.new_lengths = new_lengths;
+  a.keep = keep;
+  a.n_sink = n_sink;
+  a.n_recent = n_recent;
+  a.slots = static_cast<int32_t*>(ws);
+  return launched(rq::launch_block_evict(a, reinterpret_cast<hipStream_t>(stream)),
+                  "eviction launch");
+}
+
+}  // extern "C"

@@ -444,6 +444,8 @@ rq_status decode_attention(const rq_cache* c, int32_t layer, int32_t n_tokens, c
 
 rq_status set_error(rq_status code, const char* msg) { return fail(code, "%s", msg); }
 
+int device_cus() { return cu_count(); }
+
 }  // namespace rq
 
 extern "C" {

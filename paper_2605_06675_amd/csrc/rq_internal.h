@@ -188,7 +188,9 @@ rq_status decode_attention(const rq_cache* c, int32_t layer, int32_t n_tokens, c
                            bool launch = true);
 // Bytes of arrival counters a cache's calls use.
 uint64_t decode_counter_bytes(const rq_cache* c);
-// Record an error message for rq_last_error and return code.
+// Record an error message for rq_last_error and return code (RQ_OK: clear it).
 rq_status set_error(rq_status code, const char* msg);
+// Compute units of the current device (256 where none can be queried).
+int device_cus();
 
 }  // namespace rq

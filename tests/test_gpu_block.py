@@ -1,0 +1,598 @@
+"""The block-scaled 8-bit cache on the GPU against its oracle: cache contents
+bit for bit, attention and weights within bounds that follow from the
+arithmetic.
+
+Bounds.  With A a row's largest sum of |scale log2(e) q_c k_c|, a score (log2
+units) is off by at most D 2^-24 A (fp32 sums of D exact products, any order)
+plus D 2^-25 A' for bf16 queries held as fp16 (A' with |q_c| replaced by the
+row's largest) plus four roundings of the score itself; a softmax ratio by
+twice that times ln 2, plus the exponential's error (2^-22 each) and the sums'
+(fp32, one rounding a term in each of at most T / 4 + 64 steps).  Values add
+2^-21 of the largest one (22-bit products, scale)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_06675_amd as rq
+from oracle import block
+
+pytestmark = pytest.mark.gpu
+FMT = {"int8": (rq.RQ_INT8, block.INT8), "e4m3": (rq.RQ_E4M3, block.E4M3)}
+DT = {"bf16": (rq.RQ_BF16, torch.bfloat16), "fp16": (rq.RQ_F16, torch.float16)}
+
+
+def rounder(dt):
+    return lambda x: torch.from_numpy(np.ascontiguousarray(x, np.float32)).to(dt).float().numpy()
+
+
+class Rig:
+    """A device cache whose unused memory holds NaNs, and its oracle units."""
+
+    def __init__(self, fmt="int8", dtype="bf16", B=2, H=2, G=2, D=128, cap=128, weights=True, seed=0,
+                 layers=1, layer=0):
+        self.fmt, self.B, self.H, self.G, self.D, self.cap = fmt, B, H, G, D, cap
+        self.rdt, self.dt = DT[dtype]
+        self.layer = layer
+        self.g = torch.Generator().manual_seed(seed)
+        self.c = rq.BlockCache(FMT[fmt][0], self.rdt, layers, B, H, H * G, D, cap, weights=weights)
+        self.c.codes.fill_(0x7f)                      # e4m3: NaN
+        self.c.scales.fill_(math.nan)
+        self.c.tail.fill_(math.nan)
+        self.c.positions.fill_(-(1 << 30))
+        if weights:
+            self.c.weights.fill_(math.nan)
+        self.u = [[block.Unit(FMT[fmt][1], D, rounder(self.dt)) for _ in range(H)] for _ in range(B)]
+        self.channel = torch.exp(torch.randn(H, 1, D, generator=self.g))
+
+    def randn(self, *shape):
+        return torch.randn(*shape, generator=self.g)
+
+    def kv(self, n, new=None, size=1.0):
+        k = self.randn(self.B, self.H, n, self.D) * self.channel * size
+        k = k.clamp(-65504, 65504).to(self.dt)        # (keys must be finite in fp16)
+        v = (self.randn(self.B, self.H, n, self.D) * size).to(self.dt)
+        if new is not None:                           # padding rows hold NaNs
+            for b, m in enumerate(new):
+                k[b, :, m:], v[b, :, m:] = math.nan, math.nan
+        return k, v
+
+    def append(self, n, new=None, size=1.0, kv=None):
+        k, v = self.kv(n, new, size) if kv is None else kv
+        self.c.append(self.layer, k.cuda(), v.cuda(), None if new is None else ints(new))
+        self.took(k, v, new)
+
+    def took(self, k, v, new=None):
+        for b in range(self.B):
+            m = k.shape[2] if new is None else new[b]
+            for h in range(self.H):
+                self.u[b][h].append(k[b, h, :m].float().numpy(), v[b, h, :m].float().numpy())
+
+    def lengths(self):
+        return [self.u[b][0].length for b in range(self.B)]
+
+    def check(self, weights=True):
+        """Buffers equal the oracle's; what it does not hold is untouched."""
+        c, L = self.c, self.layer
+        sh = (c.desc.n_layers, self.B, self.H)
+        codes = c.codes.cpu().numpy().reshape(*sh, 2, self.cap, self.D)[L]
+        scales = c.scales.cpu().numpy().reshape(*sh, 2, self.cap // 32)[L]
+        tail = c.tail.cpu().float().numpy().reshape(*sh, 2, 32, self.D)[L]
+        pos = c.positions.cpu().numpy().reshape(*sh, self.cap)[L]
+        assert c.lengths[L].tolist() == self.lengths()
+        for b in range(self.B):
+            for h in range(self.H):
+                u = self.u[b][h]
+                n, full = u.length, u.length // 32 * 32
+                for s in (0, 1):
+                    np.testing.assert_array_equal(codes[b, h, s, :full], u.codes[s])
+                    np.testing.assert_array_equal(scales[b, h, s, :full // 32], u.scales[s])
+                    np.testing.assert_array_equal(tail[b, h, s, :n - full], u.tail[s])
+                    assert (codes[b, h, s, full:] == 0x7f).all()
+                    assert np.isnan(scales[b, h, s, full // 32:]).all()
+                np.testing.assert_array_equal(pos[b, h, :n], u.pos)
+                assert (pos[b, h, n:] == -(1 << 30)).all()
+
+    def weights(self):
+        return self.c.weights.cpu().view(-1, self.B, self.H, self.cap)[self.layer].double().numpy()
+
+    def bounds(self, b, h, q, scale, cap, slopes):
+        """(bound on a softmax ratio, largest |value|) for each row of q
+        [n][G][D]."""
+        u = self.u[b][h]
+        K, V = (u.values(s).astype(np.float64) for s in (0, 1))
+        q = np.abs(q.astype(np.float64))
+        a = scale * 1.4427 * (q @ np.abs(K).T).max(-1)
+        a2 = scale * 1.4427 * (q.max(-1) * np.abs(K).sum(-1).max())
+        far = 0.0 if slopes is None else 1.4427 * float(np.max(slopes)) * float(u.pos.max())
+        s = self.D * 2.0 ** -24 * a + (self.D * 2.0 ** -25 * a2 if self.dt == torch.bfloat16 else 0)
+        # a capped score never errs by more than the uncapped one, and by the tanh's own 2^-21
+        s = s + 4 * 2.0 ** -24 * (a + far) + (1.4427 * cap * 2.0 ** -21 if cap else 0)
+        ratio = 2 * s * math.log(2) + 2.0 ** -21 + (u.length / 4 + 64) * 2.0 ** -24
+        return ratio, (np.abs(V).max() if len(V) else 0.0)
+
+    def attend(self, n, new=None, out=torch.float32, scale=None, cap=0.0, window=0, slopes=None,
+               accumulate=False, q=None, size=1.0, stream=None, max_tokens=None):
+        """One call, checked against the oracle."""
+        q = (self.randn(self.B, self.H * self.G, n, self.D) * size).to(self.dt) if q is None else q
+        if new is not None:
+            for b, m in enumerate(new):
+                q[b, :, m:] = math.nan
+        past = [L - (n if new is None else new[b]) for b, L in enumerate(self.lengths())]
+        bound = max(self.lengths() + [n]) if max_tokens is None else max_tokens
+        before = self.weights() if accumulate else None
+        o = torch.full(q.shape, 7.5, dtype=out, device="cuda")
+        ws = torch.full((max(16, rq.rq_block_attention_workspace(self.c.desc, n, bound, accumulate, window)),),
+                        0xff, dtype=torch.uint8, device="cuda")
+        rq.rq_block_attention(self.c.desc, self.layer, ints(past), q.cuda(), o, ws,
+                              None if new is None else ints(new), bound, scale, cap, window,
+                              None if slopes is None else torch.tensor(slopes).cuda(), accumulate, stream)
+        torch.cuda.synchronize()
+        self.compare(q, o, new, scale, cap, window, slopes, accumulate, before)
+        return o
+
+    def compare(self, q, o, new=None, scale=None, cap=0.0, window=0, slopes=None, accumulate=False,
+                before=None):
+        n, G, out = q.shape[2], self.G, o.dtype
+        scale = self.D ** -0.5 if scale is None else scale
+        half = 0.0 if out == torch.float32 else torch.finfo(out).eps / 2
+        after = self.weights() if accumulate else None
+        o = o.cpu().double().numpy()
+        for b in range(self.B):
+            m = n if new is None else new[b]
+            assert (o[b, :, m:] == 7.5).all()
+            for h in range(self.H):
+                if m == 0:
+                    continue
+                u = self.u[b][h]
+                qq = q[b, h * G:(h + 1) * G, :m].float().numpy().transpose(1, 0, 2)
+                sl = None if slopes is None else np.asarray(slopes[h * G:(h + 1) * G])
+                old = u.weight.copy()
+                want = u.attend(qq, scale, cap, window, sl, accumulate)
+                ratio, big = self.bounds(b, h, qq, scale, cap, sl)
+                got = o[b, h * G:(h + 1) * G, :m].transpose(1, 0, 2)
+                err = np.abs(got - want)
+                tol = (ratio[..., None] + 2.0 ** -21) * big + half * np.abs(want) + 1e-30
+                if out == torch.float16:
+                    tol = tol + 2.0 ** -25
+                assert (err <= tol).all(), (b, h, float((err / tol).max()))
+                if accumulate:
+                    L = u.length
+                    add = u.weight - old
+                    grown = after[b, h, :L] - before[b, h, :L]
+                    tol = ratio.max() * add + 2.0 ** -24 * (np.abs(after[b, h, :L]) + m * G * add)
+                    assert (np.abs(grown - add) <= tol + 1e-30).all(), (b, h)
+                    assert np.isnan(after[b, h, L:]).all()
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+both = pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+types = pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+
+
+# ------------------------------------------------------------------- append
+@both
+@types
+@pytest.mark.parametrize("D", [64, 128])
+def test_append_in_pieces(fmt, dtype, D):
+    r = Rig(fmt, dtype, D=D, cap=192)
+    for n in (1, 30, 1, 1, 31, 64, 33, 3):
+        r.append(n)
+        r.check()
+    assert (r.weights()[:, :, :164] == 0).all() and np.isnan(r.weights()[:, :, 164:]).all()
+
+
+@both
+def test_append_ragged_and_padded(fmt):
+    r = Rig(fmt, "fp16", B=4, D=64, cap=160)
+    for n, new in ((50, [50, 0, 1, 32]), (64, [14, 64, 0, 33]), (9, [9, 0, 1, 2])):
+        r.append(n, new)
+        r.check()
+
+
+@both
+@types
+def test_append_sizes(fmt, dtype):
+    """Zeros, one spike, the dtype's largest and smallest numbers, ties."""
+    r = Rig(fmt, dtype, B=1, H=1, cap=192)
+    n, big = 32, float(torch.finfo(r.dt).max) if dtype == "fp16" else 2.0 ** 55
+    z = torch.zeros(1, 1, n, 128, dtype=r.dt)
+    spike, most, small = z.clone(), z.clone(), z.clone()
+    spike[0, 0, 17, 5] = -3.0
+    most[0, 0] = torch.where(torch.rand(n, 128, generator=r.g) < 0.5, big, -big).to(r.dt)
+    small[0, 0] = (r.randn(n, 128) * float(torch.finfo(r.dt).smallest_normal)).to(r.dt)
+    ties = (torch.arange(n * 128).view(1, 1, n, 128) % 255 - 127).to(r.dt) / 2
+    for x in (z, spike, most, small, ties):
+        r.append(n, kv=(x, -x))
+    r.check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_append_strided_and_unaligned_rows(D):
+    r = Rig("int8", "bf16", B=2, H=3, D=D, cap=128)
+    n = 45
+    k, v = r.kv(n)
+    dk = torch.empty(2, n, 3, D, dtype=r.dt, device="cuda").transpose(1, 2)     # [B][n][H][D]
+    dk.copy_(k)
+    flat = torch.empty(2 * 3 * n * (D + 3) + 1, dtype=r.dt, device="cuda")
+    dv = flat[1:].view(2, 3, n, D + 3)[..., 2:D + 2]                            # any element
+    dv.copy_(v)
+    r.c.append(0, dk, dv)
+    r.took(k, v)
+    r.check()
+    k1, v1 = r.kv(1)                       # one token broadcast over the batch
+    k1[1], v1[1] = k1[0], v1[0]
+    r.c.append(0, k1[:1].cuda().expand(2, -1, -1, -1), v1[:1].cuda().expand(2, -1, -1, -1))
+    r.took(k1, v1)
+    r.check()
+
+
+def test_append_stops_at_the_capacity():
+    r = Rig("int8", B=3, H=1, cap=64)
+    r.append(40, [40, 20, 40])
+    k, v = r.kv(40)
+    rq.rq_block_append(r.c.desc, 0, ints([40, 20, -5]), k.cuda(), v.cuda())
+    r.c.lengths[0] = ints([64, 60, 40])
+    u = r.u
+    u[0][0].append(k[0, 0, :24].float().numpy(), v[0, 0, :24].float().numpy())
+    u[1][0].append(k[1, 0].float().numpy(), v[1, 0].float().numpy())
+    u[2][0] = block.Unit(block.INT8, 128, rounder(r.dt))     # -5 counts as 0
+    u[2][0].append(k[2, 0].float().numpy(), v[2, 0].float().numpy())
+    r.check()
+    rq.rq_block_append(r.c.desc, 0, ints([64, 64, 1000]), k.cuda(), v.cuda(), ints([3, 0, -1]))
+    r.c.lengths[0] = ints([64, 60, 40])
+    r.check()
+
+
+def test_layers_are_apart():
+    r = Rig("e4m3", layers=3, layer=1, cap=64)
+    r.append(40)
+    r.check()
+    c = r.c.codes.view(3, -1)
+    assert (c[0] == 0x7f).all() and (c[2] == 0x7f).all()
+    assert torch.isnan(r.c.tail.view(3, -1)[[0, 2]]).all()
+    r.attend(3, accumulate=True)
+    assert torch.isnan(r.c.weights.view(3, -1)[[0, 2]]).all()
+
+
+# ---------------------------------------------------------------- attention
+@both
+@types
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("L", [1, 31, 32, 33, 100, 1000])
+def test_attend_one_token(fmt, dtype, D, L):
+    r = Rig(fmt, dtype, G=4, D=D, cap=1024)
+    r.append(L)
+    r.attend(1)
+
+
+@pytest.mark.parametrize("G", [1, 3, 6, 16])
+@pytest.mark.parametrize("n", [2, 5, 40])
+def test_attend_several_tokens(G, n):
+    r = Rig("e4m3", "bf16", H=1, G=G, D=64, cap=256)
+    r.append(170)
+    r.attend(n)
+    r.append(n)
+    r.attend(n, out=torch.bfloat16)
+
+
+@both
+@types
+@pytest.mark.parametrize("n", [1, 7, 130])
+@pytest.mark.parametrize("kw", [dict(cap=20.0), dict(window=1), dict(window=50), dict(window=4000),
+                                dict(slopes=[0.5, 0.25, 0.0, 1.0]),
+                                dict(cap=5.0, window=33, slopes=[0.01, 0.02, 0.03, 0.04])])
+def test_attend_masks_and_biases(fmt, dtype, n, kw):
+    r = Rig(fmt, dtype, D=64, cap=512)
+    r.append(333)
+    r.attend(n, accumulate=True, **kw)
+
+
+@both
+def test_attend_ragged(fmt):
+    """Empty sequences, padded rows of NaNs, lengths inside one block."""
+    r = Rig(fmt, "bf16", B=5, G=3, cap=256)
+    r.append(200, [200, 0, 5, 64, 33])
+    new = [9, 0, 1, 4, 9]
+    r.append(9, new)
+    r.attend(9, new, accumulate=True)
+    r.attend(9, new, out=torch.float16, window=3, max_tokens=256)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("size", [1e-4, 1.0, 2000.0])
+def test_attend_value_and_query_sizes(dtype, size):
+    r = Rig("int8", dtype, cap=256)
+    r.append(64, size=size)
+    r.append(32, size=size * 0.01)
+    r.append(32)
+    r.append(9, size=size)
+    r.attend(1, scale=0.05 / size ** 2 if size > 1 else None, size=size)
+    r.attend(6, scale=0.05 / size ** 2 if size > 1 else None, size=size)
+
+
+@both
+def test_attend_equal_scores_give_the_mean(fmt):
+    """Queries of zero: every probability is the same, so the output shows
+    the products' 22 bits and the sums alone."""
+    r = Rig(fmt, "bf16", cap=2048)
+    r.append(1500)
+    q = torch.zeros(2, 4, 1, 128, dtype=r.dt)
+    o = r.attend(1, q=q).cpu().double().numpy()
+    for b in range(2):
+        for h in range(2):
+            mean = r.u[b][h].values(1).astype(np.float64).mean(0)
+            assert np.abs(o[b, 2 * h, 0] - mean).max() <= 4 * 2.0 ** -22 * np.abs(r.u[b][h].values(1)).max()
+
+
+def test_attend_zero_blocks():
+    r = Rig("e4m3", "fp16", cap=128)
+    z = torch.zeros(2, 2, 32, 128, dtype=r.dt)
+    r.append(32, kv=(z, z))
+    r.attend(2)
+    r.append(40)
+    r.append(32, kv=(z, z))
+    r.attend(2)
+
+
+def test_attend_one_dominant_score_far_back():
+    """A late maximum rescales what came before, an early one never moves."""
+    for at in (3, 700):
+        r = Rig("int8", "bf16", B=1, H=1, G=1, cap=1024)
+        k, v = r.kv(800)
+        q = r.randn(1, 1, 1, 128).to(r.dt)
+        k[0, 0, at] = (q[0, 0, 0].float() * 4).to(r.dt)
+        r.append(800, kv=(k, v))
+        r.attend(1, q=q)
+
+
+def test_attend_strided_unaligned_and_long_batch():
+    r = Rig("e4m3", "bf16", B=2, H=2, G=2, D=64, cap=96)
+    r.append(77)
+    n, q = 4, r.randn(2, 4, 4, 64).to(r.dt)
+    dq = torch.empty(2 * n * 4 * 67 + 1, dtype=r.dt, device="cuda")[1:].view(2, n, 4, 67)[..., 1:65].transpose(1, 2)
+    dq.copy_(q)
+    for out in (torch.float32, torch.bfloat16):
+        do = torch.full((2 * n * 4 * 67 + 1,), 7.5, dtype=out, device="cuda")[1:].view(2, n, 4, 67)
+        o = do[..., 2:66].transpose(1, 2)
+        ws = torch.empty(rq.rq_block_attention_workspace(r.c.desc, n, 77) + 16, dtype=torch.uint8, device="cuda")
+        rq.rq_block_attention(r.c.desc, 0, ints([73, 73]), dq, o, ws, max_tokens=77)
+        r.compare(q, o)
+        assert (do[..., :2] == 7.5).all() and (do[..., 66:] == 7.5).all()
+
+
+def test_lengths_out_of_range_are_taken_as_the_nearest():
+    r = Rig("int8", "bf16", B=2, cap=96)
+    r.append(96, [96, 2])
+    q = r.randn(2, 4, 2, 128).to(r.dt).cuda()
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+
+    def call(past, new):
+        o = torch.full(q.shape, 7.5, device="cuda")
+        rq.rq_block_attention(r.c.desc, 0, ints(past), q, o, ws, ints(new))
+        return o
+    torch.testing.assert_close(call([1000, -3], [2, 2]), call([94, 0], [2, 2]), rtol=0, atol=0)
+    torch.testing.assert_close(call([94, 50], [9, -1]), call([94, 50], [2, 0]), rtol=0, atol=0)
+
+
+def test_attend_repeats_bit_for_bit():
+    r = Rig("int8", "bf16", B=1, cap=4096)
+    r.append(4001)
+    q = r.randn(1, 4, 1, 128).to(r.dt)
+    a, w = r.attend(1, q=q), r.c.weights.clone()
+    assert torch.equal(a, r.attend(1, q=q))
+    r.attend(1, q=q, accumulate=True)
+    w1 = r.c.weights.clone()
+    r.c.weights.copy_(w)
+    for u in r.u[0]:
+        u.weight[:] = 0
+    r.attend(1, q=q, accumulate=True)
+    assert torch.equal(w1[~torch.isnan(w1)], r.c.weights[~torch.isnan(w1)])
+
+
+# ----------------------------------------------------------------- eviction
+def evict(r, keep, sink, recent, weight=None):
+    """Evicts r's cache; returns a rig around the new one, checked."""
+    if weight is not None:
+        w = torch.full((r.B, r.H, r.cap), math.nan)
+        for b in range(r.B):
+            for h in range(r.H):
+                w[b, h, :r.u[b][h].length] = weight[b, h, :r.u[b][h].length]
+        r.c.weights.view(r.B, r.H, r.cap).copy_(w)
+    dev_w = r.weights()
+    before = [t.clone() for t in (r.c.codes, r.c.scales, r.c.tail, r.c.positions, r.c.weights)]
+    to = Rig(r.fmt, "bf16" if r.dt == torch.bfloat16 else "fp16", r.B, r.H, r.G, r.D,
+             (keep + 31) // 32 * 32 + 32)
+    r.c.evict(keep, sink, recent, into=to.c)
+    for t, old in zip((r.c.codes, r.c.scales, r.c.tail, r.c.positions, r.c.weights), before):
+        assert torch.equal(t.view(torch.uint8), old.view(torch.uint8))
+    for b in range(r.B):
+        for h in range(r.H):
+            to.u[b][h] = r.u[b][h].evict(keep, sink, recent, dev_w[b, h, :r.u[b][h].length])
+    to.channel = r.channel
+    to.check()
+    got = to.weights()
+    for b in range(r.B):
+        for h in range(r.H):
+            n = to.u[b][h].length
+            np.testing.assert_array_equal(got[b, h, :n], to.u[b][h].weight)
+            assert np.isnan(got[b, h, n:]).all()
+    return to
+
+
+@both
+@types
+@pytest.mark.parametrize("D", [64, 128])
+def test_evict_random_weights(fmt, dtype, D):
+    r = Rig(fmt, dtype, B=3, D=D, cap=512)
+    r.append(500, [500, 37, 200])
+    to = evict(r, 131, 4, 20, torch.rand(3, 2, 512, generator=r.g))
+    to.append(5)
+    to.check()
+    to.attend(5, window=90)
+
+
+@pytest.mark.parametrize("kind", ["zero", "equal", "few", "levels", "tiny", "inf"])
+def test_evict_ties_and_sizes(kind):
+    r = Rig("int8", "bf16", B=1, H=2, D=64, cap=2112)
+    r.append(2100)
+    w = torch.rand(1, 2, 2112, generator=r.g)
+    w = {"zero": w * 0, "equal": w * 0 + 0.37, "few": (w < 0.01).float(), "levels": (w * 7).floor(),
+         "tiny": w * 1e-40, "inf": torch.where(w < 0.1, math.inf, w)}[kind]
+    evict(r, 700, 3, 50, w)
+
+
+@pytest.mark.parametrize("keep,sink,recent", [(1, 0, 1), (32, 31, 1), (33, 0, 33), (64, 4, 8), (99, 10, 20),
+                                              (100, 0, 1), (101, 0, 1), (120, 50, 70)])
+def test_evict_counts(keep, sink, recent):
+    r = Rig("e4m3", "bf16", B=2, H=1, D=64, cap=128)
+    r.append(100, [100, 0])
+    evict(r, keep, sink, recent, torch.rand(2, 1, 128, generator=r.g))
+
+
+def test_evict_long():
+    r = Rig("int8", "fp16", B=1, H=1, D=64, cap=20032)
+    k, v = r.kv(20001)
+    r.c.append(0, k.cuda(), v.cuda())
+    u = r.u[0][0]
+    full = 20000
+    q = [block.quantize(block.INT8, x[0, 0, i:i + 32].float().numpy()) for x in (k, v) for i in range(0, full, 32)]
+    half = len(q) // 2
+    for s in (0, 1):
+        part = q[s * half:(s + 1) * half]
+        u.codes[s] = np.concatenate([c for c, _ in part])
+        u.scales[s] = np.array([x for _, x in part], np.float32)
+        u.tail[s] = (k, v)[s][0, 0, full:].float().numpy()
+    u.pos, u.weight = np.arange(20001), np.zeros(20001)
+    r.check()
+    w = -torch.log(torch.rand(1, 1, 20032, generator=r.g))
+    evict(r, 5000, 4, 64, w)
+
+
+# ----------------------------------------------------------- used together
+@both
+def test_serving_run(fmt):
+    """Padded prompts, decoded tokens that gather weight, an eviction when the
+    cache is full, more tokens over the shrunk cache."""
+    r = Rig(fmt, "bf16", B=3, G=2, D=128, cap=160)
+    new = [120, 47, 90]
+    k, v = r.kv(120, new)
+    q = r.randn(3, 4, 120, 128).to(r.dt)
+    for b, m in enumerate(new):
+        q[b, :, m:] = math.nan
+    before = np.zeros_like(r.weights())
+    o = r.c.step(0, k.cuda(), v.cuda(), q.cuda(), torch.full(q.shape, 7.5, dtype=r.dt, device="cuda"),
+                 ints(new), accumulate=True)
+    r.took(k, v, new)
+    r.compare(q, o, new, accumulate=True, before=before)
+    for turn in range(2):
+        for _ in range(30):
+            k, v = r.kv(1)
+            q = r.randn(3, 4, 1, 128).to(r.dt)
+            before = np.nan_to_num(r.weights())
+            o = r.c.step(0, k.cuda(), v.cuda(), q.cuda(), accumulate=True)
+            r.took(k, v)
+            r.compare(q, o, accumulate=True, before=before)
+            r.check()
+        if turn == 0:
+            r = evict(r, 64, 4, 16)
+    assert r.lengths() == [94, 94, 94]
+    assert [u[0].pos[-1] for u in r.u] == [179, 106, 149]
+
+
+def test_captured_step_follows_the_lengths():
+    """One captured decode step, replayed: lengths, blocks, weights move on."""
+    r = Rig("int8", "bf16", B=2, cap=256)
+    r.append(60, [60, 13])
+    sk, sv = (torch.zeros(2, 2, 1, 128, dtype=r.dt, device="cuda") for _ in range(2))
+    sq = torch.zeros(2, 4, 1, 128, dtype=r.dt, device="cuda")
+    so = torch.zeros(2, 4, 1, 128, device="cuda")
+    ws = torch.empty(rq.rq_block_attention_workspace(r.c.desc, 1, 256, True), dtype=torch.uint8, device="cuda")
+
+    def step():
+        past = r.c.lengths[0]
+        rq.rq_block_append(r.c.desc, 0, past, sk, sv)
+        rq.rq_block_attention(r.c.desc, 0, past, sq, so, ws, accumulate=True)
+        r.c.lengths[0] += 1
+    lengths = r.c.lengths.clone()
+    keep = [t.clone() for t in (r.c.codes, r.c.scales, r.c.tail, r.c.positions, r.c.weights)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    r.c.lengths.copy_(lengths)
+    for t, old in zip((r.c.codes, r.c.scales, r.c.tail, r.c.positions, r.c.weights), keep):
+        t.copy_(old)
+    for turn in range(70):
+        k, v = r.kv(1)
+        q = r.randn(2, 4, 1, 128).to(r.dt)
+        sk.copy_(k)
+        sv.copy_(v)
+        sq.copy_(q)
+        before = np.nan_to_num(r.weights())
+        graph.replay()
+        torch.cuda.synchronize()
+        r.took(k, v)
+        r.compare(q, so, accumulate=True, before=before)
+    r.check()
+
+
+def test_another_stream_and_shared_workspace_in_order():
+    r = Rig("e4m3", "bf16", cap=256)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        k, v = r.kv(200)
+        dk, dv = k.cuda(), v.cuda()
+    r.c.append(0, dk, dv, stream=side)
+    r.took(k, v)
+    q = r.randn(2, 4, 1, 128).to(r.dt)
+    with torch.cuda.stream(side):
+        dq = q.cuda()
+        o = torch.empty(q.shape, device="cuda")
+    o = r.c.attention(0, dq, o, stream=side)
+    side.synchronize()
+    r.compare(q, o)
+    to = r.c.evict(50, stream=side)
+    side.synchronize()
+    assert to.lengths.tolist() == [[50, 50]]
+
+
+def test_python_refusals():
+    r = Rig("int8", "bf16", cap=64)
+    r.append(40)
+    k, v = (x.cuda() for x in r.kv(2))
+    past = ints([40, 40])
+    with pytest.raises(ValueError):
+        r.c.append(0, *(x.cuda() for x in r.kv(25)))              # 40 + 25 > 64
+    for bad in (k.half(), k[:, :1], k[..., :64], k.cpu(), k.transpose(2, 3), k[0]):
+        with pytest.raises(ValueError):
+            rq.rq_block_append(r.c.desc, 0, past, bad, v)
+    for bad in (None, past.long(), past[:1], past.cpu(), torch.stack([past, past], 1)[:, 0]):
+        with pytest.raises(ValueError):
+            rq.rq_block_append(r.c.desc, 0, bad, k, v)
+    q = torch.zeros(2, 4, 1, 128, dtype=r.dt, device="cuda")
+    o = torch.zeros_like(q)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    for kw in (dict(q=q.half()), dict(q=q[:, :2]), dict(out=o.double()), dict(out=o[:1]), dict(ws=ws.cpu()),
+               dict(ws=ws[::2]), dict(slopes=torch.zeros(3, device="cuda")), dict(slopes=torch.zeros(4)),
+               dict(new_len=past.long())):
+        a = dict(q=q, out=o, ws=ws)
+        a.update(kw)
+        with pytest.raises(ValueError):
+            rq.rq_block_attention(r.c.desc, 0, past, **a)
+    for kw in (dict(window=-1), dict(cap=-1.0), dict(scale=math.nan), dict(max_tokens=100), dict(ws=ws[:16])):
+        with pytest.raises(rq.RQError):
+            rq.rq_block_attention(r.c.desc, 0, past, **{**dict(q=q, out=o, ws=ws, accumulate=True), **kw})
+    with pytest.raises(ValueError):
+        rq.make_block_cache(*r.c.shape, 128, codes=r.c.codes)      # too small
+    with pytest.raises(rq.RQError):
+        r.c.evict(10, n_sink=8, n_recent=8)
