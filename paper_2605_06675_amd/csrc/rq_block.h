@@ -58,6 +58,8 @@ struct BlockAttendLaunch {
   float* part;             // [unit][row tile][split][16][D]
   float* part_ml;          // [unit][row tile][split][16][2]: maximum (log2) and sum
   float* stats;            // [unit][row][2]: maximum and 1 / sum, where accumulate
+  float* scores;           // [unit][block][row][32]: log2 scores, where accumulate
+                           // and all rows fit one tile; else NULL
 };
 
 struct BlockEvictLaunch {
@@ -92,6 +94,14 @@ __device__ __forceinline__ void block_lengths(const int32_t* past, const int32_t
   ps = ps < 0 ? 0 : (ps > most - nw ? most - nw : ps);
   *p = __builtin_amdgcn_readfirstlane(ps);
   *w = __builtin_amdgcn_readfirstlane(nw);
+}
+
+// Blocks that rows first..last (tokens of the call) see: [lo, hi).
+__device__ __forceinline__ void seen_blocks(int past, int first, int last, int window, int* lo,
+                                            int* hi) {
+  *hi = (past + last) / kBlockTokens + 1;
+  const int slot = window ? past + first - window + 1 : 0;
+  *lo = slot > 0 ? slot / kBlockTokens : 0;
 }
 
 // ------------------------------------------------------------- quantization

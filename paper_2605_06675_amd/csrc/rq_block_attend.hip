@@ -33,9 +33,9 @@ __device__ __forceinline__ void load_values(const RQ_GLOBAL uint8_t* v, const RQ
     const int tok = 16 * (j >> 2) + 4 * g + (j & 3);
     const RQ_GLOBAL uint8_t* p = v + (uint32_t)(blk * kBlockTokens + tok) * D + (D / 16) * r;
     if constexpr (D == 128)
-      t->w[j] = *(const RQ_GLOBAL u2*)p;
+      t->w[j] = __builtin_nontemporal_load((const RQ_GLOBAL u2*)p);
     else
-      t->w[j].x = *(const RQ_GLOBAL uint32_t*)p;
+      t->w[j].x = __builtin_nontemporal_load((const RQ_GLOBAL uint32_t*)p);
   }
   t->scale = scale[blk];
 }
@@ -201,7 +201,7 @@ __device__ __forceinline__ void store_out(const BlockAttendLaunch& a, int b, int
 }
 
 template <int FMT, int D, bool BF16>
-__global__ void __launch_bounds__(256) block_attend_kernel(BlockAttendLaunch a) {
+__global__ void __launch_bounds__(256, 3) block_attend_kernel(BlockAttendLaunch a) {
   constexpr int kStride = D + 4;           // floats of a row in LDS
   __shared__ float sh_o[4][16 * kStride];
   __shared__ float sh_ml[4][16][2];
@@ -216,10 +216,8 @@ __global__ void __launch_bounds__(256) block_attend_kernel(BlockAttendLaunch a) 
   int last = (rt * 16 + 15) / a.G;
   last = last < nnew ? last : nnew - 1;
   const int total = past + nnew, full = total / kBlockTokens;
-  // blocks the rows may see; block `full` is the tail
-  const int hi_all = (past + last) / kBlockTokens + 1;
-  int lo_all = a.window ? past + first - a.window + 1 : 0;
-  lo_all = lo_all > 0 ? lo_all / kBlockTokens : 0;
+  int lo_all, hi_all;                      // block `full` is the tail
+  seen_blocks(past, first, last, a.window, &lo_all, &hi_all);
   const int64_t nb = hi_all - lo_all;
   const int lo = lo_all + (int)(nb * split / a.splits);
   const int hi = lo_all + (int)(nb * (split + 1) / a.splits);
@@ -241,11 +239,22 @@ __global__ void __launch_bounds__(256) block_attend_kernel(BlockAttendLaunch a) 
   // blocks below all_seen lie wholly before every row of the tile
   const int all_seen = a.window ? 0 : (past + first + 1) / kBlockTokens;
 
+  // scores kept for the weights: this lane's row, 4 tokens of each half block
+  const int rows = a.n * a.G;
+  RQ_GLOBAL float* kept = gptr(a.scores) + ((size_t)unit * ((a.max_tokens + kBlockTokens - 1) / kBlockTokens) * rows + r) * kBlockTokens + 4 * g;
+  auto keep = [&](const f4 s[2], int blk) {
+    if (a.scores && r < rows)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+        *(RQ_GLOBAL f4*)(kept + (size_t)blk * rows * kBlockTokens + 16 * m) = s[m];
+  };
+
   const int end = hi < full ? hi : full;
   auto step = [&](const KeyBlock<D>& k, const ValueBlock<D>& v, int blk) {
     f4 s[2];
     key_products<FMT, D>(k, q, s);
     block_scores<D>(a, q, pos, k.scale * q.qs, blk * kBlockTokens, past, blk >= all_seen, s);
+    keep(s, blk);
     probabilities<D>(&st, s);
     add_values<FMT, D>(v, s, &st);
   };
@@ -277,6 +286,7 @@ __global__ void __launch_bounds__(256) block_attend_kernel(BlockAttendLaunch a) 
     f4 s[2];
     tail_products<D, BF16>(a, b, h, kt, q, s);
     block_scores<D>(a, q, pos, a.qscale, full * kBlockTokens, past, true, s);
+    keep(s, full);
     probabilities<D>(&st, s);
     add_tail<FMT, D, BF16>(kt + kBlockTokens * D, total % kBlockTokens, s, &st);
   }
@@ -326,45 +336,113 @@ __global__ void __launch_bounds__(256) block_attend_kernel(BlockAttendLaunch a) 
 #pragma unroll
   for (int e = 0; e < D / 16; ++e) x[e] *= inv;
   store_out<D / 16>(a, b, h * a.G + grow - token * a.G, token, ch, x);
-  if (a.accumulate && ch == 0) {
+  if (a.stats && ch == 0) {
     gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + grow) * 2] = m;
     gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + grow) * 2 + 1] = inv;
   }
 }
 
-// Adds the splits' partial results of one row tile.
+// Adds the splits' partial results of one row: 256 threads hold four channels
+// each of 1024 / D splits at a time.  (Eight units of 96 splits: 5.0 us; one
+// thread a channel group, a split after the other: 50 us.)
 template <int D>
-__global__ void __launch_bounds__(256) block_merge_kernel(BlockAttendLaunch a) {
-  const int rt = blockIdx.x, unit = blockIdx.y;
-  const int b = unit / a.c.H, h = unit - b * a.c.H;
-  int past, nnew;
-  block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
-  const int row = threadIdx.x >> 4, ch = (threadIdx.x & 15) * (D / 16);
-  const int grow = rt * 16 + row, token = grow / a.G;
+__device__ __forceinline__ void merge_row(const BlockAttendLaunch& a, int grow, int unit, int b,
+                                          int h, int nnew) {
+  constexpr int kCols = D / 4, kGroups = 256 / kCols;
+  __shared__ f4 sum[kGroups][kCols];
+  const int token = grow / a.G, rt = grow >> 4, row = grow & 15;
   if (token >= nnew) return;
+  const int lane = threadIdx.x & 63, col = threadIdx.x % kCols, group = threadIdx.x / kCols;
   const size_t base = ((size_t)unit * a.row_tiles + rt) * a.splits;
   const RQ_GLOBAL float* ml = gptr(a.part_ml) + (base * 16 + row) * 2;
-  const RQ_GLOBAL float* o = gptr(a.part) + base * 16 * D + row * D + ch;
+  const RQ_GLOBAL float* o = gptr(a.part) + (base * 16 + row) * D + col * 4;
   float m = -1.0e30f;
-  for (int s = 0; s < a.splits; ++s) m = __builtin_fmaxf(m, ml[s * 32]);
-  float l = 0.0f, x[D / 16];
-#pragma unroll
-  for (int e = 0; e < D / 16; ++e) x[e] = 0.0f;
-  for (int s = 0; s < a.splits; ++s) {
+  for (int s = lane; s < a.splits; s += 64) m = __builtin_fmaxf(m, ml[s * 32]);
+  for (int d = 32; d >= 1; d >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d, 64));
+  float l = 0.0f;
+  for (int s = lane; s < a.splits; s += 64)
+    l = __builtin_fmaf(ml[s * 32 + 1], exp2_f(ml[s * 32] - m), l);
+  for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+  f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int s = group; s < a.splits; s += kGroups) {
     const float by = exp2_f(ml[s * 32] - m);
-    l = __builtin_fmaf(ml[s * 32 + 1], by, l);
-#pragma unroll
-    for (int e = 0; e < D / 16; ++e)
-      x[e] = __builtin_fmaf(o[(size_t)s * 16 * D + e], by, x[e]);
+    x += *(const RQ_GLOBAL f4*)(o + (size_t)s * 16 * D) * by;
   }
+  sum[group][col] = x;
+  __syncthreads();
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-#pragma unroll
-  for (int e = 0; e < D / 16; ++e) x[e] *= inv;
-  store_out<D / 16>(a, b, h * a.G + grow - token * a.G, token, ch, x);
-  if (a.accumulate && ch == 0) {
+  if (group == 0) {
+    for (int i = 1; i < kGroups; ++i) x += sum[i][col];
+    x *= inv;
+    store_out<4>(a, b, h * a.G + grow - token * a.G, token, col * 4, (const float*)&x);
+  }
+  if (a.stats && threadIdx.x == 0) {
     gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + grow) * 2] = m;
     gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + grow) * 2 + 1] = inv;
   }
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) block_merge_kernel(BlockAttendLaunch a) {
+  const int unit = blockIdx.y, b = unit / a.c.H;
+  int past, nnew;
+  block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
+  merge_row<D>(a, blockIdx.x, unit, b, unit - b * a.c.H, nnew);
+}
+
+// The same, and in the workgroups behind those of the rows the weights of 1024
+// tokens each: the scores that the first kernel kept against the rows' maxima
+// and sums (every workgroup merges those by itself).
+template <int D>
+__global__ void __launch_bounds__(256) block_merge_weigh_kernel(BlockAttendLaunch a) {
+  __shared__ float sh_m[16], sh_inv[16];
+  const int unit = blockIdx.y, b = unit / a.c.H;
+  int past, nnew;
+  block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
+  const int all = a.n * a.G, merges = a.splits > 1 ? all : 0;
+  if ((int)blockIdx.x < merges) {
+    merge_row<D>(a, blockIdx.x, unit, b, unit - b * a.c.H, nnew);
+    return;
+  }
+  const int rows = nnew * a.G;
+  int lo, hi;
+  seen_blocks(past, 0, nnew - 1, a.window, &lo, &hi);
+  const int first = (lo / 32 + blockIdx.x - merges) * 32;    // blocks first..first + 31
+  if (nnew == 0 || first >= hi) return;
+  const int row = threadIdx.x >> 4, lane = threadIdx.x & 15;
+  if (a.splits > 1) {
+    const RQ_GLOBAL float* ml = gptr(a.part_ml) + ((size_t)unit * a.splits * 16 + row) * 2;
+    float m = -1.0e30f, l = 0.0f;
+    for (int s = lane; s < a.splits; s += 16) m = __builtin_fmaxf(m, ml[s * 32]);
+    for (int d = 8; d >= 1; d >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d, 64));
+    for (int s = lane; s < a.splits; s += 16)
+      l = __builtin_fmaf(ml[s * 32 + 1], exp2_f(ml[s * 32] - m), l);
+    for (int d = 8; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+    if (lane == 0) {
+      sh_m[row] = m;
+      sh_inv[row] = l > 0.0f ? 1.0f / l : 0.0f;
+    }
+  } else if (lane == 0 && row < rows) {
+    sh_m[row] = gptr(a.stats)[((size_t)unit * 16 + row) * 2];
+    sh_inv[row] = gptr(a.stats)[((size_t)unit * 16 + row) * 2 + 1];
+  }
+  __syncthreads();
+  const int blk = first + (threadIdx.x >> 3), slot = blk * kBlockTokens + 4 * (threadIdx.x & 7);
+  if (blk < lo || blk >= hi) return;
+  const size_t blocks = (a.max_tokens + kBlockTokens - 1) / kBlockTokens;
+  const RQ_GLOBAL float* x = gptr(a.scores) + (unit * blocks + blk) * all * kBlockTokens + 4 * (threadIdx.x & 7);
+  f4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int i = 0; i < rows; ++i) {
+    const f4 s = *(const RQ_GLOBAL f4*)(x + i * kBlockTokens);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] = __builtin_fmaf(exp2_f(s[j] - sh_m[i]), sh_inv[i], sum[j]);
+  }
+  RQ_GLOBAL float* w = gptr(a.c.weights) + (size_t)unit * a.c.cap + slot;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (slot + j < past + nnew) w[j] += sum[j];
 }
 
 template <int FMT, int D>
@@ -375,8 +453,20 @@ hipError_t launch(const BlockAttendLaunch& a, hipStream_t s) {
   else
     hipLaunchKernelGGL((block_attend_kernel<FMT, D, false>), grid, dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.splits == 1) return e;
-  hipLaunchKernelGGL((block_merge_kernel<D>), dim3(a.row_tiles, a.c.B * a.c.H), dim3(256), 0, s, a);
+  if (e != hipSuccess) return e;
+  const int rows = a.n * a.G;
+  if (a.scores) {
+    // 1024 tokens a workgroup (one more where a window begins inside one)
+    int tokens = a.max_tokens;
+    if (a.window && a.window + a.n < tokens) tokens = a.window + a.n;
+    const int parts = (tokens + 1023) / 1024 + (a.window ? 1 : 0);
+    hipLaunchKernelGGL((block_merge_weigh_kernel<D>), dim3((a.splits > 1 ? rows : 0) + parts, a.c.B * a.c.H),
+                       dim3(256), 0, s, a);
+  } else if (a.splits > 1) {
+    hipLaunchKernelGGL((block_merge_kernel<D>), dim3(rows, a.c.B * a.c.H), dim3(256), 0, s, a);
+  } else {
+    return e;
+  }
   return hipGetLastError();
 }
 

@@ -104,8 +104,8 @@ rq_status check_query(const rq_block_cache* c, const rq_block_query* a) {
 // How an attention call is split, and what it needs of the workspace.
 struct Plan {
   int row_tiles, splits;
-  uint64_t part, part_ml, stats;   // bytes
-  uint64_t bytes() const { return part + part_ml + stats; }
+  uint64_t part, part_ml, stats, scores;   // bytes
+  uint64_t bytes() const { return part + part_ml + stats + scores; }
 };
 
 // One resident round: three workgroups a CU over the units' row tiles, at
@@ -127,7 +127,14 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
     p.part = tiles * p.splits * 16 * c->head_dim * sizeof(float);
     p.part_ml = tiles * p.splits * 16 * 2 * sizeof(float);
   }
-  if (a->accumulate) p.stats = tiles * 16 * 2 * sizeof(float);
+  if (a->accumulate) {
+    p.stats = tiles * 16 * 2 * sizeof(float);
+    // one tile of rows: the scores are kept (4 bytes a row and token) rather
+    // than computed again from the keys (D bytes a token)
+    if (p.row_tiles == 1)
+      p.scores = (uint64_t)u * ((a->max_tokens + rq::kBlockTokens - 1) / rq::kBlockTokens) * a->n_new *
+                 G * rq::kBlockTokens * sizeof(float);
+  }
   return p;
 }
 
@@ -222,10 +229,11 @@ rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_bl
   uint8_t* w = static_cast<uint8_t*>(ws);
   a.part = reinterpret_cast<float*>(w);
   a.part_ml = reinterpret_cast<float*>(w + p.part);
-  a.stats = reinterpret_cast<float*>(w + p.part + p.part_ml);
+  if (p.stats) a.stats = reinterpret_cast<float*>(w + p.part + p.part_ml);
+  if (p.scores) a.scores = reinterpret_cast<float*>(w + p.part + p.part_ml + p.stats);
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = rq::launch_block_attend(a, s);
-  if (e == hipSuccess && a.accumulate) e = rq::launch_block_weigh(a, s);
+  if (e == hipSuccess && a.accumulate && !a.scores) e = rq::launch_block_weigh(a, s);
   return launched(e, "attention launch");
 }
 
