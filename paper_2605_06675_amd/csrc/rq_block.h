@@ -15,6 +15,10 @@
 namespace rq {
 
 constexpr int kBlockTokens = 32;
+// Eviction: units of at most this many slots are selected by one workgroup
+// (16 keys a thread); longer ones in parts of a multiple of kSelectPart, at
+// most kSelectParts of them.
+constexpr int kSelectShort = 16384, kSelectPart = 8192, kSelectParts = 32;
 
 // One layer of a cache, and its shape.
 struct BlockLayer {
@@ -68,6 +72,11 @@ struct BlockEvictLaunch {
   int32_t* new_lengths;
   int keep, n_sink, n_recent;
   int32_t* slots;          // [unit][keep] source slots, ascending
+  // selection of units in several parts (parts > 1) of `part` tokens each
+  int part, parts;
+  uint32_t* state;         // [unit][8]: what each launch found
+  uint32_t* before;        // [unit][parts]: kept keys of the parts before
+  uint32_t* counts;        // [3][unit][parts][2048]
 };
 
 hipError_t launch_block_append(const BlockAppendLaunch& a, hipStream_t s);

@@ -138,6 +138,28 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
   return p;
 }
 
+// How an eviction selects, and what it needs of the workspace (bytes).
+struct EvictPlan {
+  int part, parts;
+  uint64_t slots, state, before, counts;
+  uint64_t bytes() const { return slots + state + before + counts; }
+};
+
+EvictPlan plan_eviction(const rq_block_cache* src, int keep) {
+  EvictPlan p{};
+  const uint64_t u = units(src);
+  p.slots = (u * keep * sizeof(int32_t) + 15) / 16 * 16;
+  p.parts = 1;
+  if (src->capacity <= rq::kSelectShort) return p;
+  const int most = (src->capacity + rq::kSelectParts - 1) / rq::kSelectParts;
+  p.part = (most + rq::kSelectPart - 1) / rq::kSelectPart * rq::kSelectPart;
+  p.parts = (src->capacity + p.part - 1) / p.part;
+  p.state = u * 8 * sizeof(uint32_t);
+  p.before = (u * p.parts * sizeof(uint32_t) + 15) / 16 * 16;
+  p.counts = 3 * u * p.parts * 2048 * sizeof(uint32_t);
+  return p;
+}
+
 }  // namespace
 
 extern "C" {
@@ -242,7 +264,7 @@ rq_status rq_block_evict_workspace(const rq_block_cache* src, int32_t keep, uint
   if (st != RQ_OK) return st;
   if (keep < 1) return fail(RQ_EINVAL, "keep %d must be >= 1", keep);
   if (!bytes) return fail(RQ_EINVAL, "bytes is NULL");
-  *bytes = units(src) * keep * sizeof(int32_t);
+  *bytes = plan_eviction(src, keep).bytes();
   return ok();
 }
 
@@ -267,9 +289,8 @@ rq_status rq_block_evict(const rq_block_cache* src, const rq_block_cache* dst, i
     return fail(RQ_EINVAL, "n_sink %d >= 0 and n_recent %d >= 1 must fit keep %d", n_sink,
                 n_recent, keep);
   if (!lengths || !new_lengths) return fail(RQ_EINVAL, "NULL device pointer");
-  uint64_t need = 0;
-  st = rq_block_evict_workspace(src, keep, &need);
-  if (st != RQ_OK) return st;
+  const EvictPlan p = plan_eviction(src, keep);
+  const uint64_t need = p.bytes();
   if (ws_bytes < need)
     return fail(RQ_ESMALLWS, "workspace %llu bytes < %llu needed", (unsigned long long)ws_bytes,
                 (unsigned long long)need);
@@ -282,7 +303,13 @@ rq_status rq_block_evict(const rq_block_cache* src, const rq_block_cache* dst, i
   a.keep = keep;
   a.n_sink = n_sink;
   a.n_recent = n_recent;
-  a.slots = static_cast<int32_t*>(ws);
+  uint8_t* w = static_cast<uint8_t*>(ws);
+  a.slots = reinterpret_cast<int32_t*>(w);
+  a.part = p.part;
+  a.parts = p.parts;
+  a.state = reinterpret_cast<uint32_t*>(w + p.slots);
+  a.before = reinterpret_cast<uint32_t*>(w + p.slots + p.state);
+  a.counts = reinterpret_cast<uint32_t*>(w + p.slots + p.state + p.before);
   return launched(rq::launch_block_evict(a, reinterpret_cast<hipStream_t>(stream)),
                   "eviction launch");
 }

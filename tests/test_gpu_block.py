@@ -454,7 +454,9 @@ def test_evict_counts(keep, sink, recent):
     evict(r, keep, sink, recent, torch.rand(2, 1, 128, generator=r.g))
 
 
-def test_evict_long():
+@pytest.mark.parametrize("kind", ["random", "zero", "few", "late"])
+def test_evict_long(kind):
+    """A unit selected in several parts; ties across them."""
     r = Rig("int8", "fp16", B=1, H=1, D=64, cap=20032)
     k, v = r.kv(20001)
     r.c.append(0, k.cuda(), v.cuda())
@@ -470,7 +472,28 @@ def test_evict_long():
     u.pos, u.weight = np.arange(20001), np.zeros(20001)
     r.check()
     w = -torch.log(torch.rand(1, 1, 20032, generator=r.g))
+    w = {"random": w, "zero": w * 0, "few": (w < 0.01).float(), "late": (torch.arange(20032) > 17000).float()[None, None]}[kind]
     evict(r, 5000, 4, 64, w)
+
+
+def test_evict_parts_of_uneven_sequences():
+    """Sequences that end in the first, a later and no part, one that keeps
+    everything; more layers than one."""
+    r = Rig("e4m3", "bf16", B=4, H=1, D=64, cap=25024, layers=2, layer=1)
+    new = [25000, 9000, 0, 300]
+    k, v = r.kv(25000)
+    r.c.append(1, k.cuda(), v.cuda(), ints(new))
+    w = torch.rand(4, 1, 25024, generator=r.g)
+    r.c.weights.view(2, 4, 1, -1)[1] = w.cuda()
+    to = rq.BlockCache(*r.c.shape, 512, weights=True)
+    r.c.evict(500, 3, 20, into=to)
+    assert to.lengths.tolist() == [[0] * 4, [500, 500, 0, 300]]
+    pos = to.positions.view(2, 4, 512)[1].cpu()
+    for b, L in enumerate(new):
+        order = w[b, 0, :L].double()
+        order[:3] = order[max(0, L - 20):] = 9.0
+        want = torch.sort(torch.topk(order, min(L, 500))[1])[0]
+        assert torch.equal(pos[b, :min(L, 500)].long(), want)
 
 
 # ----------------------------------------------------------- used together
