@@ -81,6 +81,8 @@ struct BlockEvictLaunch {
 
 hipError_t launch_block_append(const BlockAppendLaunch& a, hipStream_t s);
 hipError_t launch_block_attend(const BlockAttendLaunch& a, hipStream_t s);
+hipError_t launch_block_prompt(const BlockAttendLaunch& a, hipStream_t s);
+hipError_t launch_block_merge(const BlockAttendLaunch& a, hipStream_t s);
 hipError_t launch_block_weigh(const BlockAttendLaunch& a, hipStream_t s);
 hipError_t launch_block_evict(const BlockEvictLaunch& a, hipStream_t s);
 
@@ -233,6 +235,32 @@ __device__ __forceinline__ float tanh_f(float x) {
 }
 
 // ------------------------------------------------------------------ attention
+// One thread's share of an output row: N channels from ch.
+template <int N>
+__device__ __forceinline__ void store_out(const BlockAttendLaunch& a, int b, int head, int token,
+                                          int ch, const float* x) {
+  const int64_t at = b * a.out.sb + head * a.out.sh + token * a.out.st + ch;
+  if (a.out_dtype == RQ_F32) {
+    RQ_GLOBAL float* o = gptr((float*)a.out.p) + at;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i)
+      *(RQ_GLOBAL f4_any*)(o + 4 * i) = (f4){x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+    return;
+  }
+  RQ_GLOBAL uint16_t* o = gptr((uint16_t*)a.out.p) + at;
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    u2 w;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float y = x[4 * i + 2 * j], z = x[4 * i + 2 * j + 1];
+      w[j] = a.out_dtype == RQ_BF16 ? bf16_rne(y) | ((uint32_t)bf16_rne(z) << 16)
+                                    : narrow_t<false>(y) | ((uint32_t)narrow_t<false>(z) << 16);
+    }
+    *(RQ_GLOBAL u2_any*)(o + 4 * i) = w;
+  }
+}
+
 // A tile of 16 query rows as one wave holds it: lane (r = lane & 15,
 // g = lane >> 4) has, of row r, the channels 64 c + 16 g + 8 f + 0..7 in
 // operand 2 c + f.

@@ -174,32 +174,6 @@ __device__ __forceinline__ void add_tail(const RQ_GLOBAL uint16_t* vt, int n_tai
   }
 }
 
-// One thread's share of an output row: N channels from ch.
-template <int N>
-__device__ __forceinline__ void store_out(const BlockAttendLaunch& a, int b, int head, int token,
-                                          int ch, const float* x) {
-  const int64_t at = b * a.out.sb + head * a.out.sh + token * a.out.st + ch;
-  if (a.out_dtype == RQ_F32) {
-    RQ_GLOBAL float* o = gptr((float*)a.out.p) + at;
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i)
-      *(RQ_GLOBAL f4_any*)(o + 4 * i) = (f4){x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
-    return;
-  }
-  RQ_GLOBAL uint16_t* o = gptr((uint16_t*)a.out.p) + at;
-#pragma unroll
-  for (int i = 0; i < N / 4; ++i) {
-    u2 w;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float y = x[4 * i + 2 * j], z = x[4 * i + 2 * j + 1];
-      w[j] = a.out_dtype == RQ_BF16 ? bf16_rne(y) | ((uint32_t)bf16_rne(z) << 16)
-                                    : narrow_t<false>(y) | ((uint32_t)narrow_t<false>(z) << 16);
-    }
-    *(RQ_GLOBAL u2_any*)(o + 4 * i) = w;
-  }
-}
-
 template <int FMT, int D, bool BF16>
 __global__ void __launch_bounds__(256, 3) block_attend_kernel(BlockAttendLaunch a) {
   constexpr int kStride = D + 4;           // floats of a row in LDS
@@ -462,15 +436,22 @@ hipError_t launch(const BlockAttendLaunch& a, hipStream_t s) {
     const int parts = (tokens + 1023) / 1024 + (a.window ? 1 : 0);
     hipLaunchKernelGGL((block_merge_weigh_kernel<D>), dim3((a.splits > 1 ? rows : 0) + parts, a.c.B * a.c.H),
                        dim3(256), 0, s, a);
-  } else if (a.splits > 1) {
-    hipLaunchKernelGGL((block_merge_kernel<D>), dim3(rows, a.c.B * a.c.H), dim3(256), 0, s, a);
-  } else {
-    return e;
+    return hipGetLastError();
   }
-  return hipGetLastError();
+  return launch_block_merge(a, s);
 }
 
 }  // namespace
+
+hipError_t launch_block_merge(const BlockAttendLaunch& a, hipStream_t s) {
+  if (a.splits == 1) return hipSuccess;
+  const dim3 grid(a.n * a.G, a.c.B * a.c.H);
+  if (a.c.D == 64)
+    hipLaunchKernelGGL((block_merge_kernel<64>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((block_merge_kernel<128>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
 
 hipError_t launch_block_attend(const BlockAttendLaunch& a, hipStream_t s) {
   if (a.c.fmt == RQ_INT8) return a.c.D == 64 ? launch<RQ_INT8, 64>(a, s) : launch<RQ_INT8, 128>(a, s);

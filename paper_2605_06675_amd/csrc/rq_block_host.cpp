@@ -103,6 +103,7 @@ rq_status check_query(const rq_block_cache* c, const rq_block_query* a) {
 
 // How an attention call is split, and what it needs of the workspace.
 struct Plan {
+  int prompt;                      // tiles of 256 rows (rq_block_prompt.hip)
   int row_tiles, splits;
   uint64_t part, part_ml, stats, scores;   // bytes
   uint64_t bytes() const { return part + part_ml + stats + scores; }
@@ -119,8 +120,15 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
     const int64_t seen = ((int64_t)a->window + 16 / G + 1) / rq::kBlockTokens + 2;
     blocks = seen < blocks ? seen : blocks;
   }
-  int64_t s = 3 * (int64_t)rq::device_cus() / (u * p.row_tiles);
-  s = std::min(s, (blocks + 3) / 4);
+  p.prompt = p.row_tiles > 2;
+  int64_t s;
+  if (p.prompt) {
+    s = (int64_t)rq::device_cus() / (u * ((a->n_new * G + 255) / 256));
+    s = std::min(s, (blocks + 7) / 8);
+  } else {
+    s = 3 * (int64_t)rq::device_cus() / (u * p.row_tiles);
+    s = std::min(s, (blocks + 3) / 4);
+  }
   p.splits = (int)std::max<int64_t>(s, 1);
   const uint64_t tiles = (uint64_t)u * p.row_tiles;
   if (p.splits > 1) {
@@ -254,7 +262,8 @@ rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_bl
   if (p.stats) a.stats = reinterpret_cast<float*>(w + p.part + p.part_ml);
   if (p.scores) a.scores = reinterpret_cast<float*>(w + p.part + p.part_ml + p.stats);
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  hipError_t e = rq::launch_block_attend(a, s);
+  hipError_t e = p.prompt ? rq::launch_block_prompt(a, s) : rq::launch_block_attend(a, s);
+  if (e == hipSuccess && p.prompt) e = rq::launch_block_merge(a, s);
   if (e == hipSuccess && a.accumulate && !a.scores) e = rq::launch_block_weigh(a, s);
   return launched(e, "attention launch");
 }

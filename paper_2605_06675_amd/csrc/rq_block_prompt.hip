@@ -1,0 +1,484 @@
+// Attention over the block-scaled 8-bit cache for many query rows a unit
+// (prompts and their chunks): matrix products of tiles.
+//
+// A workgroup of eight waves owns 256 rows of a unit (token-major, the heads of
+// a group together), 32 a wave, and walks its tokens in tiles of 64.  Codes are
+// converted to fp16 once a workgroup on their way into LDS (two buffers, one
+// barrier a tile), keys as [token][channel], values as [channel][token].  On
+// v_mfma_f32_32x32x16_f16 S^T = K Q^T leaves a lane with 16 tokens of one row,
+// the operand that O^T = V^T P^T wants of it (the values' tokens are stored in
+// that order), so probabilities never move between lanes.
+//
+// A block's value scale goes into the exponent: P' = 2^(x - m + log2(by)),
+// by = value scale * unit, and the row's sum takes the block's sum of P' / by.
+// P' is rounded to fp16 (2^-12, less than the rounding of a bf16 output and as
+// much as that of an fp16 one); for fp32 outputs (EXACT) it is a pair hi + lo.
+#include "rq_block.h"
+
+namespace rq {
+
+namespace {
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+constexpr int kRows = 256, kTile = 64, kThreads = 512;
+
+// 16-byte pieces of an LDS row are permuted by a key of the row, so that lanes
+// that read the same piece of consecutive rows, or write pieces of every
+// fourth, meet different banks.
+template <int D>
+__device__ __forceinline__ int key_at(int token, int piece) {
+  return token * D * 2 + ((piece ^ (token & (D / 8 - 1))) << 4);
+}
+__device__ __forceinline__ int value_at(int ch, int piece) {
+  return ch * kTile * 2 + ((piece ^ ((ch >> 2) & 7) ^ ((ch & 2) << 1)) << 4);
+}
+
+// One thread's share of a tile: D / 8 key codes of a token, and 4 channels of 4
+// tokens of the values (with D = 64 the first four waves').
+template <int D>
+struct TileLoad {
+  u4 k;
+  uint32_t v[4];
+};
+
+template <int D>
+__device__ __forceinline__ void load_tile(const RQ_GLOBAL uint8_t* kc, const RQ_GLOBAL uint8_t* vc,
+                                          int slot0, int slots, TileLoad<D>* t) {
+  const int tid = threadIdx.x;
+  const int tok = slot0 + tid / 8;
+  if (tok < slots) {
+    if constexpr (D == 128) {
+      t->k = *(const RQ_GLOBAL u4*)(kc + (uint32_t)tok * D + 16 * (tid % 8));
+    } else {
+      const u2 w = *(const RQ_GLOBAL u2*)(kc + (uint32_t)tok * D + 8 * (tid % 8));
+      t->k.x = w.x;
+      t->k.y = w.y;
+    }
+  }
+  const int quad = tid / (D / 4), ch = 4 * (tid % (D / 4)), first = slot0 + 4 * quad;
+  if (quad < kTile / 4 && first < slots)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      t->v[i] = *(const RQ_GLOBAL uint32_t*)(vc + (uint32_t)(first + i) * D + ch);
+}
+
+template <int FMT, int D>
+__device__ __forceinline__ void store_tile(const TileLoad<D>& t, int slot0, int slots, uint8_t* sk,
+                                           uint8_t* sv) {
+  const int tid = threadIdx.x, tok = tid / 8;
+  if (slot0 + tok < slots) {
+#pragma unroll
+    for (int p = 0; p < D / 64; ++p) {
+      const u4 w = {key_pair<FMT>(t.k[2 * p], false), key_pair<FMT>(t.k[2 * p], true),
+                    key_pair<FMT>(t.k[2 * p + 1], false), key_pair<FMT>(t.k[2 * p + 1], true)};
+      *(u4*)(sk + key_at<D>(tok, D / 64 * (tid % 8) + p)) = w;
+    }
+  }
+  const int quad = tid / (D / 4), ch = 4 * (tid % (D / 4));
+  if (quad < kTile / 4) {
+    uint32_t a[4] = {0u, 0u, 0u, 0u}, b[4] = {0u, 0u, 0u, 0u};
+    if (slot0 + 4 * quad < slots) {
+      value_pairs<FMT>(t.v[0], t.v[1], a);
+      value_pairs<FMT>(t.v[2], t.v[3], b);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *(u2*)(sv + value_at(ch + e, 2 * (quad / 4) + (quad & 1)) + 8 * ((quad >> 1) & 1)) = (u2){a[e], b[e]};
+  }
+}
+
+// The tail's rows as the block of 32 tokens at `at` of the tile: fp16 numbers
+// of their own, bf16 ones divided by a power of two that brings the largest of
+// the side below 1 (returned as the block's scales).  Rows from n_tail on count
+// as zero.  The whole workgroup calls it.
+template <int FMT, int D, bool BF16>
+__device__ __forceinline__ void store_tail(const RQ_GLOBAL uint16_t* kt, int n_tail, int at, uint8_t* sk,
+                                           uint8_t* sv, float* red, float* ks, float* vs) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const RQ_GLOBAL uint16_t* vt = kt + kBlockTokens * D;
+  // 8 keys of one token, and 2 channels of 4 tokens of the values
+  constexpr int kPieces = D / 8;
+  const int ktok = tid / kPieces, piece = tid % kPieces;
+  const int quad = tid / (D / 2), ch = 2 * (tid % (D / 2));
+  u4 k = {0u, 0u, 0u, 0u};
+  uint32_t v[4] = {0u, 0u, 0u, 0u};
+  if (ktok < n_tail) k = *(const RQ_GLOBAL u4*)(kt + ktok * D + 8 * piece);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (quad < 8 && 4 * quad + i < n_tail) v[i] = *(const RQ_GLOBAL uint32_t*)(vt + (4 * quad + i) * D + ch);
+  int ke = 0, ve = 0;
+  if constexpr (BF16) {
+    float km = 0.0f, vm = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      km = __builtin_fmaxf(km, __builtin_fmaxf(__builtin_fabsf(widen_t<true>(k[i] & 0xffffu)), __builtin_fabsf(widen_t<true>(k[i] >> 16))));
+      vm = __builtin_fmaxf(vm, __builtin_fmaxf(__builtin_fabsf(widen_t<true>(v[i] & 0xffffu)), __builtin_fabsf(widen_t<true>(v[i] >> 16))));
+    }
+    for (int d = 32; d >= 1; d >>= 1) {
+      km = __builtin_fmaxf(km, __shfl_xor(km, d, 64));
+      vm = __builtin_fmaxf(vm, __shfl_xor(vm, d, 64));
+    }
+    if (lane == 0) {
+      red[wave] = km;
+      red[8 + wave] = vm;
+    }
+    __syncthreads();
+    for (int i = 0; i < 8; ++i) {
+      km = __builtin_fmaxf(km, red[i]);
+      vm = __builtin_fmaxf(vm, red[8 + i]);
+    }
+    ke = km > 0.0f ? __builtin_amdgcn_frexp_expf(km) : 0;
+    ve = vm > 0.0f ? __builtin_amdgcn_frexp_expf(vm) : 0;
+    auto pair = [](uint32_t x, int e) {
+      const h2 y = {(_Float16)__builtin_amdgcn_ldexpf(widen_t<true>(x & 0xffffu), -e),
+                    (_Float16)__builtin_amdgcn_ldexpf(widen_t<true>(x >> 16), -e)};
+      return as_u32(y);
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      k[i] = pair(k[i], ke);
+      v[i] = pair(v[i], ve);
+    }
+  }
+  *ks = __builtin_amdgcn_ldexpf(1.0f, ke);
+  *vs = __builtin_amdgcn_ldexpf(kValueUnit<FMT>, ve);
+  if (ktok < kBlockTokens) *(u4*)(sk + key_at<D>(at + ktok, piece)) = k;
+  if (quad < 8) {
+    const int q = at / 4 + quad;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t sel = e ? 0x07060302u : 0x05040100u;
+      *(u2*)(sv + value_at(ch + e, 2 * (q / 4) + (q & 1)) + 8 * ((q >> 1) & 1)) =
+          (u2){__builtin_amdgcn_perm(v[1], v[0], sel), __builtin_amdgcn_perm(v[3], v[2], sel)};
+    }
+  }
+}
+
+template <int FMT, int D, bool BF16, bool EXACT>
+__global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLaunch a) {
+  __shared__ __align__(16) uint8_t sh_k[2][kTile * D * 2];
+  __shared__ __align__(16) uint8_t sh_v[2][kTile * D * 2];
+  __shared__ int32_t sh_pos[2][kTile];
+  __shared__ float red[16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, hl = lane >> 5;
+  // workgroups go round the XCDs: where the units are a multiple of eight, a
+  // unit's tiles share an L2; the tiles that see most tokens go first
+  const int units = a.c.B * a.c.H, tiles = (a.n * a.G + kRows - 1) / kRows, each = tiles * a.splits;
+  int unit, w;
+  if (units % 8 == 0) {
+    unit = (int)(blockIdx.x / 8 / each) * 8 + blockIdx.x % 8;
+    w = blockIdx.x / 8 % each;
+  } else {
+    unit = blockIdx.x / each;
+    w = blockIdx.x % each;
+  }
+  const int rt = tiles - 1 - w / a.splits, split = w % a.splits;
+  const int b = unit / a.c.H, h = unit - b * a.c.H;
+  int past, nnew;
+  block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
+  const int first = rt * kRows / a.G;
+  if (first >= nnew) return;
+  int last = (rt * kRows + kRows - 1) / a.G;
+  last = last < nnew ? last : nnew - 1;
+  const int total = past + nnew, full = total / kBlockTokens;
+  int lo, hi;
+  seen_blocks(past, first, last, a.window, &lo, &hi);
+  {
+    // splits begin at whole tiles
+    const int64_t nt = (hi - lo + 1) / 2;
+    const int t0 = (int)(nt * split / a.splits), t1 = (int)(nt * (split + 1) / a.splits);
+    hi = lo + 2 * t1 < hi ? lo + 2 * t1 : hi;
+    lo += 2 * t0;
+  }
+
+  // this lane's row, as BlockAttendLaunch has it: 16 k + 8 hl + 0..7 in f[k]
+  const int row = rt * kRows + wave * 32 + col;
+  int token = row / a.G;
+  const int head = row - token * a.G;
+  const bool valid = token < nnew;
+  if (!valid) token = nnew - 1;
+  const int wave_first = (rt * kRows + wave * 32) / a.G;      // tokens of the wave's rows
+  int wave_last = (rt * kRows + wave * 32 + 31) / a.G;
+  wave_last = wave_last < nnew ? wave_last : nnew - 1;
+  const bool idle = wave_first >= nnew;
+  h8 q[D / 16];
+  float qs = __builtin_fabsf(a.qscale), slope = 0.0f;
+  int qpos = 0;
+  {
+    const RQ_GLOBAL uint16_t* p = gptr(static_cast<const uint16_t*>(a.q.p)) + b * a.q.sb +
+                                  (int64_t)(h * a.G + head) * a.q.sh + token * a.q.st;
+    u4 raw[D / 16];
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+      raw[k] = valid ? *(const RQ_GLOBAL u4_any*)(p + 16 * k + 8 * hl) : (u4){0u, 0u, 0u, 0u};
+    // (a negative scale turns the queries, so that scores grow with products)
+    const uint32_t turn = a.qscale < 0.0f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) raw[k] ^= turn;
+    if constexpr (BF16) {
+      float most = 0.0f;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          most = __builtin_fmaxf(most, __builtin_fabsf(widen_t<true>(raw[k][i] & 0xffffu)));
+          most = __builtin_fmaxf(most, __builtin_fabsf(widen_t<true>(raw[k][i] >> 16)));
+        }
+      most = __builtin_fmaxf(most, __shfl_xor(most, 32, 64));
+      const int e = most > 0.0f ? __builtin_amdgcn_frexp_expf(most) : 0;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          q[k][2 * i] = (_Float16)__builtin_amdgcn_ldexpf(widen_t<true>(raw[k][i] & 0xffffu), -e);
+          q[k][2 * i + 1] = (_Float16)__builtin_amdgcn_ldexpf(widen_t<true>(raw[k][i] >> 16), -e);
+        }
+      qs = __builtin_amdgcn_ldexpf(qs, e);
+    } else {
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) q[k] = as_h8(raw[k]);
+    }
+    if (a.slopes) slope = gptr(a.slopes)[h * a.G + head] * 1.4426950408889634f;
+    if (a.slopes || a.window)
+      qpos = gptr(a.c.positions)[(size_t)unit * a.c.cap + past + token];
+  }
+
+  const RQ_GLOBAL uint8_t* kc = gptr(a.c.codes) + (size_t)unit * 2 * a.c.cap * D;
+  const RQ_GLOBAL uint8_t* vc = kc + (size_t)a.c.cap * D;
+  const RQ_GLOBAL float* kscale = gptr(a.c.scales) + (size_t)unit * 2 * (a.c.cap / kBlockTokens);
+  const RQ_GLOBAL float* vscale = kscale + a.c.cap / kBlockTokens;
+  const RQ_GLOBAL int32_t* pos = gptr(a.c.positions) + (size_t)unit * a.c.cap;
+  const RQ_GLOBAL uint16_t* tail = gptr(a.c.tail) + (size_t)unit * 2 * kBlockTokens * D;
+  const int coded = (hi < full ? hi : full) * kBlockTokens;     // slots of the split's coded blocks
+
+  f16v o[D / 32];
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[c][i] = 0.0f;
+  float m = -1.0e30f, l = 0.0f, unit2 = 0.0f;
+  const bool far = a.slopes || a.window;
+
+  float ks[2][2], vs[2][2];           // scales of the two buffers' blocks
+  TileLoad<D> next;
+  auto fetch = [&](int blk) {
+    load_tile<D>(kc, vc, blk * kBlockTokens, coded, &next);
+  };
+  auto put = [&](int blk, int buf) {
+    store_tile<FMT, D>(next, blk * kBlockTokens, coded, sh_k[buf], sh_v[buf]);
+    if (far && threadIdx.x < kTile) {
+      const int slot = blk * kBlockTokens + threadIdx.x;
+      sh_pos[buf][threadIdx.x] = slot < total ? pos[slot] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      ks[buf][i] = blk + i < full ? kscale[blk + i] : 0.0f;
+      vs[buf][i] = blk + i < full ? vscale[blk + i] : 0.0f;
+    }
+    if (full < hi && (blk == full || blk + 1 == full)) {
+      // (the zeros that store_tile left for the tail's values come first)
+      __syncthreads();
+      store_tail<FMT, D, BF16>(tail, total - full * kBlockTokens, (full - blk) * kBlockTokens, sh_k[buf],
+                               sh_v[buf], red, &ks[buf][full - blk], &vs[buf][full - blk]);
+    }
+  };
+
+  auto work = [&](int blk, int buf, const float tks[2], const float tvs[2]) {
+    const int slot0 = blk * kBlockTokens;
+    if (idle || slot0 > past + wave_last) return;
+    f16v s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        const h8 f = *(const h8*)(sh_k[buf] + key_at<D>(32 * t + col, 2 * k + hl));
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[k], s[t], 0, 0, 0);
+      }
+    }
+    const bool masked = a.window || slot0 + kTile - 1 > past + wave_first;
+    float f[2] = {tks[0] * qs, tks[1] * qs};
+    if (a.cap != 0.0f || far || masked) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (a.cap != 0.0f) {
+          if constexpr (EXACT) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[t][i] = a.cap * tanh_f(s[t][i] * f[t]);
+          } else {
+            // cap tanh(x) = cap - 2 cap / (1 + e^(2x)): off by 2^-23 cap, which
+            // the rounding of P' hides
+            const float e2 = f[t] * 2.8853900817779268f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              s[t][i] = __builtin_fmaf(__builtin_amdgcn_rcpf(1.0f + exp2_f(s[t][i] * e2)), -2.0f * a.cap, a.cap);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[t][i] *= f[t];
+        }
+        f[t] = 1.0f;
+        if (far) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int away = qpos - sh_pos[buf][32 * t + 8 * (i >> 2) + 4 * hl + (i & 3)];
+            s[t][i] = __builtin_fmaf(-slope, (float)away, s[t][i]);
+            if (a.window && away >= a.window) s[t][i] = -__builtin_inff();
+          }
+        }
+        if (masked) {
+          const int end = past + token - slot0 - 32 * t - 4 * hl;
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (8 * (i >> 2) + (i & 3) > end) s[t][i] = -__builtin_inff();
+        }
+      }
+    }
+    // the running maximum (moved when a score exceeds it by 8) and unit
+    float top = -3.0e38f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      float x = s[t][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) x = __builtin_fmaxf(x, s[t][i]);
+      top = __builtin_fmaxf(top, x * f[t]);
+    }
+    const float sv = __builtin_fmaxf(tvs[0], tvs[1]);
+    const bool grow = unit2 == 0.0f || sv * unit2 > 128.0f;      // (the same in every lane)
+    if (grow || __any(top > m + 8.0f)) {
+      top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
+      const float mn = __builtin_fmaxf(m, top);
+      float by = exp2_f(m - mn);
+      m = mn;
+      l *= by;
+      if (grow) {
+        int e = sv > 0.0f ? __builtin_amdgcn_frexp_expf(sv) : 0;
+        e = e < -100 ? -100 : e;
+        const float u = __builtin_amdgcn_ldexpf(128.0f, -e);
+        by *= unit2 == 0.0f ? 1.0f : u / unit2;
+        unit2 = u;
+      }
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) o[c] *= by;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      // (codes under a scale of zero are zero: any factor serves)
+      const float by = tvs[t] > 0.0f ? __builtin_fmaxf(tvs[t] * unit2, 0x1p-80f) : 1.0f;
+      const float c = m - __builtin_amdgcn_logf(by);
+      uint32_t hi2[8], lo2[8];
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = exp2_f(__builtin_fmaf(s[t][2 * i], f[t], -c));
+        const float y = exp2_f(__builtin_fmaf(s[t][2 * i + 1], f[t], -c));
+        if constexpr (EXACT) {
+          const h2 p = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x, y));
+          hi2[i] = as_u32(p);
+          lo2[i] = as_u32((h2){(_Float16)(x - (float)p.x), (_Float16)(y - (float)p.y)});
+        } else {
+          hi2[i] = as_u32((h2){(_Float16)x, (_Float16)y});
+        }
+        // (of the fp32 numbers: where by is small, fp16 loses P' but the sum
+        // must not)
+        sum += x;
+        sum += y;
+      }
+      l = __builtin_fmaf(sum, 1.0f / by, l);
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const h8 ph = as_h8((u4){hi2[4 * g], hi2[4 * g + 1], hi2[4 * g + 2], hi2[4 * g + 3]});
+#pragma unroll
+        for (int c2 = 0; c2 < D / 32; ++c2) {
+          const h8 vf = *(const h8*)(sh_v[buf] + value_at(32 * c2 + col, 2 * (2 * t + g) + hl));
+          o[c2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph, o[c2], 0, 0, 0);
+          if constexpr (EXACT) {
+            const h8 pl = as_h8((u4){lo2[4 * g], lo2[4 * g + 1], lo2[4 * g + 2], lo2[4 * g + 3]});
+            o[c2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl, o[c2], 0, 0, 0);
+          }
+        }
+      }
+    }
+  };
+
+  if (lo < hi) {
+    fetch(lo);
+    put(lo, 0);
+    __syncthreads();
+    for (int blk = lo;;) {
+      const bool more = blk + 2 < hi;
+      if (more) fetch(blk + 2);
+      work(blk, 0, ks[0], vs[0]);
+      if (!more) break;
+      put(blk + 2, 1);
+      __syncthreads();
+      blk += 2;
+      const bool more2 = blk + 2 < hi;
+      if (more2) fetch(blk + 2);
+      work(blk, 1, ks[1], vs[1]);
+      if (!more2) break;
+      put(blk + 2, 0);
+      __syncthreads();
+      blk += 2;
+    }
+  }
+
+  l += __shfl_xor(l, 32, 64);
+  const float to_value = unit2 == 0.0f ? 0.0f : 1.0f / (unit2 * kValueUnit<FMT>);
+  if (a.splits > 1) {
+    if (row >= a.row_tiles * 16) return;
+    const size_t at = ((size_t)unit * a.row_tiles + (row >> 4)) * a.splits + split;
+    RQ_GLOBAL float* p = gptr(a.part) + (at * 16 + (row & 15)) * D + 4 * hl;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(RQ_GLOBAL f4*)(p + 32 * c + 8 * i) =
+            (f4){o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]} * to_value;
+    if (hl == 0) {
+      gptr(a.part_ml)[(at * 16 + (row & 15)) * 2] = m;
+      gptr(a.part_ml)[(at * 16 + (row & 15)) * 2 + 1] = l;
+    }
+    return;
+  }
+  if (!valid) return;
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f, by = inv * to_value;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x[4] = {o[c][4 * i] * by, o[c][4 * i + 1] * by, o[c][4 * i + 2] * by, o[c][4 * i + 3] * by};
+      store_out<4>(a, b, h * a.G + head, token, 32 * c + 8 * i + 4 * hl, x);
+    }
+  if (a.stats && hl == 0) {
+    gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + row) * 2] = m;
+    gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + row) * 2 + 1] = inv;
+  }
+}
+
+template <int FMT, int D, bool BF16>
+hipError_t launch(const BlockAttendLaunch& a, hipStream_t s) {
+  const dim3 grid((unsigned)((a.n * a.G + kRows - 1) / kRows * a.splits) * a.c.B * a.c.H);
+  if (a.out_dtype == RQ_F32)
+    hipLaunchKernelGGL((block_prompt_kernel<FMT, D, BF16, true>), grid, dim3(kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((block_prompt_kernel<FMT, D, BF16, false>), grid, dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+template <int FMT, int D>
+hipError_t launch(const BlockAttendLaunch& a, hipStream_t s) {
+  return a.c.is_bf16 ? launch<FMT, D, true>(a, s) : launch<FMT, D, false>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_block_prompt(const BlockAttendLaunch& a, hipStream_t s) {
+  if (a.c.fmt == RQ_INT8) return a.c.D == 64 ? launch<RQ_INT8, 64>(a, s) : launch<RQ_INT8, 128>(a, s);
+  return a.c.D == 64 ? launch<RQ_E4M3, 64>(a, s) : launch<RQ_E4M3, 128>(a, s);
+}
+
+}  // namespace rq
