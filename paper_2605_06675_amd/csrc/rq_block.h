@@ -94,6 +94,14 @@ typedef u4 u4_any __attribute__((aligned(2)));
 typedef u2 u2_any __attribute__((aligned(2)));
 typedef f4 f4_any __attribute__((aligned(4)));
 
+// Memory that no kernel writes while this one runs: uniform addresses are
+// scalar loads.
+#define RQ_CONSTANT __attribute__((address_space(4)))
+template <class T>
+__device__ __forceinline__ const RQ_CONSTANT T* cptr(const T* p) {
+  return (const RQ_CONSTANT T*)p;
+}
+
 // Cached and new tokens of batch entry b, whatever the device arrays hold:
 // 0 <= past, new <= n, past + new <= most.
 __device__ __forceinline__ void block_lengths(const int32_t* past, const int32_t* new_len, int b,

@@ -123,7 +123,7 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
   p.prompt = p.row_tiles > 2;
   int64_t s;
   if (p.prompt) {
-    s = (int64_t)rq::device_cus() / (u * ((a->n_new * G + 255) / 256));
+    s = 2 * (int64_t)rq::device_cus() / (u * ((a->n_new * G + 127) / 128));
     s = std::min(s, (blocks + 7) / 8);
   } else {
     s = 3 * (int64_t)rq::device_cus() / (u * p.row_tiles);

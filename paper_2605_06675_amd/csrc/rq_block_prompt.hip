@@ -21,7 +21,8 @@ namespace {
 
 typedef float f16v __attribute__((ext_vector_type(16)));
 
-constexpr int kRows = 256, kTile = 64, kThreads = 512;
+constexpr int kWaves = 4, kRows = 32 * kWaves, kTile = 64, kThreads = 64 * kWaves;
+constexpr int kPasses = 512 / kThreads;     // a tile's conversion is 512 shares
 
 // 16-byte pieces of an LDS row are permuted by a key of the row, so that lanes
 // that read the same piece of consecutive rows, or write pieces of every
@@ -34,57 +35,62 @@ __device__ __forceinline__ int value_at(int ch, int piece) {
   return ch * kTile * 2 + ((piece ^ ((ch >> 2) & 7) ^ ((ch & 2) << 1)) << 4);
 }
 
-// One thread's share of a tile: D / 8 key codes of a token, and 4 channels of 4
-// tokens of the values (with D = 64 the first four waves').
-template <int D>
+// A share of a tile: D / 8 key codes of a token, and 4 channels of 4 tokens of
+// the values (with D = 64 the first half of the shares).
 struct TileLoad {
-  u4 k;
-  uint32_t v[4];
+  u4 k[kPasses];
+  uint32_t v[kPasses][4];
 };
 
 template <int D>
 __device__ __forceinline__ void load_tile(const RQ_GLOBAL uint8_t* kc, const RQ_GLOBAL uint8_t* vc,
-                                          int slot0, int slots, TileLoad<D>* t) {
-  const int tid = threadIdx.x;
-  const int tok = slot0 + tid / 8;
-  if (tok < slots) {
-    if constexpr (D == 128) {
-      t->k = *(const RQ_GLOBAL u4*)(kc + (uint32_t)tok * D + 16 * (tid % 8));
-    } else {
-      const u2 w = *(const RQ_GLOBAL u2*)(kc + (uint32_t)tok * D + 8 * (tid % 8));
-      t->k.x = w.x;
-      t->k.y = w.y;
-    }
-  }
-  const int quad = tid / (D / 4), ch = 4 * (tid % (D / 4)), first = slot0 + 4 * quad;
-  if (quad < kTile / 4 && first < slots)
+                                          int slot0, int slots, TileLoad* t) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      t->v[i] = *(const RQ_GLOBAL uint32_t*)(vc + (uint32_t)(first + i) * D + ch);
+  for (int p = 0; p < kPasses; ++p) {
+    const int id = threadIdx.x + p * kThreads;
+    const int tok = slot0 + id / 8;
+    if (tok < slots) {
+      if constexpr (D == 128) {
+        t->k[p] = *(const RQ_GLOBAL u4*)(kc + (uint32_t)tok * D + 16 * (id % 8));
+      } else {
+        const u2 w = *(const RQ_GLOBAL u2*)(kc + (uint32_t)tok * D + 8 * (id % 8));
+        t->k[p].x = w.x;
+        t->k[p].y = w.y;
+      }
+    }
+    const int quad = id / (D / 4), ch = 4 * (id % (D / 4)), first = slot0 + 4 * quad;
+    if (quad < kTile / 4 && first < slots)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        t->v[p][i] = *(const RQ_GLOBAL uint32_t*)(vc + (uint32_t)(first + i) * D + ch);
+  }
 }
 
 template <int FMT, int D>
-__device__ __forceinline__ void store_tile(const TileLoad<D>& t, int slot0, int slots, uint8_t* sk,
+__device__ __forceinline__ void store_tile(const TileLoad& t, int slot0, int slots, uint8_t* sk,
                                            uint8_t* sv) {
-  const int tid = threadIdx.x, tok = tid / 8;
-  if (slot0 + tok < slots) {
 #pragma unroll
-    for (int p = 0; p < D / 64; ++p) {
-      const u4 w = {key_pair<FMT>(t.k[2 * p], false), key_pair<FMT>(t.k[2 * p], true),
-                    key_pair<FMT>(t.k[2 * p + 1], false), key_pair<FMT>(t.k[2 * p + 1], true)};
-      *(u4*)(sk + key_at<D>(tok, D / 64 * (tid % 8) + p)) = w;
-    }
-  }
-  const int quad = tid / (D / 4), ch = 4 * (tid % (D / 4));
-  if (quad < kTile / 4) {
-    uint32_t a[4] = {0u, 0u, 0u, 0u}, b[4] = {0u, 0u, 0u, 0u};
-    if (slot0 + 4 * quad < slots) {
-      value_pairs<FMT>(t.v[0], t.v[1], a);
-      value_pairs<FMT>(t.v[2], t.v[3], b);
-    }
+  for (int p = 0; p < kPasses; ++p) {
+    const int id = threadIdx.x + p * kThreads, tok = id / 8;
+    if (slot0 + tok < slots) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      *(u2*)(sv + value_at(ch + e, 2 * (quad / 4) + (quad & 1)) + 8 * ((quad >> 1) & 1)) = (u2){a[e], b[e]};
+      for (int i = 0; i < D / 64; ++i) {
+        const u4 w = {key_pair<FMT>(t.k[p][2 * i], false), key_pair<FMT>(t.k[p][2 * i], true),
+                      key_pair<FMT>(t.k[p][2 * i + 1], false), key_pair<FMT>(t.k[p][2 * i + 1], true)};
+        *(u4*)(sk + key_at<D>(tok, D / 64 * (id % 8) + i)) = w;
+      }
+    }
+    const int quad = id / (D / 4), ch = 4 * (id % (D / 4));
+    if (quad < kTile / 4) {
+      uint32_t a[4] = {0u, 0u, 0u, 0u}, b[4] = {0u, 0u, 0u, 0u};
+      if (slot0 + 4 * quad < slots) {
+        value_pairs<FMT>(t.v[p][0], t.v[p][1], a);
+        value_pairs<FMT>(t.v[p][2], t.v[p][3], b);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *(u2*)(sv + value_at(ch + e, 2 * (quad / 4) + (quad & 1)) + 8 * ((quad >> 1) & 1)) = (u2){a[e], b[e]};
+    }
   }
 }
 
@@ -95,26 +101,31 @@ __device__ __forceinline__ void store_tile(const TileLoad<D>& t, int slot0, int 
 template <int FMT, int D, bool BF16>
 __device__ __forceinline__ void store_tail(const RQ_GLOBAL uint16_t* kt, int n_tail, int at, uint8_t* sk,
                                            uint8_t* sv, float* red, float* ks, float* vs) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const RQ_GLOBAL uint16_t* vt = kt + kBlockTokens * D;
-  // 8 keys of one token, and 2 channels of 4 tokens of the values
+  // shares of 8 keys of one token, and 2 channels of 4 tokens of the values
   constexpr int kPieces = D / 8;
-  const int ktok = tid / kPieces, piece = tid % kPieces;
-  const int quad = tid / (D / 2), ch = 2 * (tid % (D / 2));
-  u4 k = {0u, 0u, 0u, 0u};
-  uint32_t v[4] = {0u, 0u, 0u, 0u};
-  if (ktok < n_tail) k = *(const RQ_GLOBAL u4*)(kt + ktok * D + 8 * piece);
+  u4 k[kPasses];
+  uint32_t v[kPasses][4];
+  float km = 0.0f, vm = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (quad < 8 && 4 * quad + i < n_tail) v[i] = *(const RQ_GLOBAL uint32_t*)(vt + (4 * quad + i) * D + ch);
-  int ke = 0, ve = 0;
-  if constexpr (BF16) {
-    float km = 0.0f, vm = 0.0f;
+  for (int p = 0; p < kPasses; ++p) {
+    const int id = threadIdx.x + p * kThreads, tok = id / kPieces, quad = id / (D / 2);
+    k[p] = (u4){0u, 0u, 0u, 0u};
+    if (tok < n_tail) k[p] = *(const RQ_GLOBAL u4*)(kt + tok * D + 8 * (id % kPieces));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      km = __builtin_fmaxf(km, __builtin_fmaxf(__builtin_fabsf(widen_t<true>(k[i] & 0xffffu)), __builtin_fabsf(widen_t<true>(k[i] >> 16))));
-      vm = __builtin_fmaxf(vm, __builtin_fmaxf(__builtin_fabsf(widen_t<true>(v[i] & 0xffffu)), __builtin_fabsf(widen_t<true>(v[i] >> 16))));
+      v[p][i] = 0u;
+      if (quad < 8 && 4 * quad + i < n_tail)
+        v[p][i] = *(const RQ_GLOBAL uint32_t*)(vt + (4 * quad + i) * D + 2 * (id % (D / 2)));
+      km = __builtin_fmaxf(km, __builtin_fmaxf(__builtin_fabsf(widen_t<true>(k[p][i] & 0xffffu)),
+                                               __builtin_fabsf(widen_t<true>(k[p][i] >> 16))));
+      vm = __builtin_fmaxf(vm, __builtin_fmaxf(__builtin_fabsf(widen_t<true>(v[p][i] & 0xffffu)),
+                                               __builtin_fabsf(widen_t<true>(v[p][i] >> 16))));
     }
+  }
+  int ke = 0, ve = 0;
+  if constexpr (BF16) {
     for (int d = 32; d >= 1; d >>= 1) {
       km = __builtin_fmaxf(km, __shfl_xor(km, d, 64));
       vm = __builtin_fmaxf(vm, __shfl_xor(vm, d, 64));
@@ -124,7 +135,7 @@ __device__ __forceinline__ void store_tail(const RQ_GLOBAL uint16_t* kt, int n_t
       red[8 + wave] = vm;
     }
     __syncthreads();
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < kWaves; ++i) {
       km = __builtin_fmaxf(km, red[i]);
       vm = __builtin_fmaxf(vm, red[8 + i]);
     }
@@ -136,21 +147,28 @@ __device__ __forceinline__ void store_tail(const RQ_GLOBAL uint16_t* kt, int n_t
       return as_u32(y);
     };
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      k[i] = pair(k[i], ke);
-      v[i] = pair(v[i], ve);
-    }
+    for (int p = 0; p < kPasses; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        k[p][i] = pair(k[p][i], ke);
+        v[p][i] = pair(v[p][i], ve);
+      }
   }
   *ks = __builtin_amdgcn_ldexpf(1.0f, ke);
   *vs = __builtin_amdgcn_ldexpf(kValueUnit<FMT>, ve);
-  if (ktok < kBlockTokens) *(u4*)(sk + key_at<D>(at + ktok, piece)) = k;
-  if (quad < 8) {
-    const int q = at / 4 + quad;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const uint32_t sel = e ? 0x07060302u : 0x05040100u;
-      *(u2*)(sv + value_at(ch + e, 2 * (q / 4) + (q & 1)) + 8 * ((q >> 1) & 1)) =
-          (u2){__builtin_amdgcn_perm(v[1], v[0], sel), __builtin_amdgcn_perm(v[3], v[2], sel)};
+  for (int p = 0; p < kPasses; ++p) {
+    const int id = threadIdx.x + p * kThreads, tok = id / kPieces, quad = id / (D / 2);
+    const int ch = 2 * (id % (D / 2));
+    if (tok < kBlockTokens) *(u4*)(sk + key_at<D>(at + tok, id % kPieces)) = k[p];
+    if (quad < 8) {
+      const int q = at / 4 + quad;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t sel = e ? 0x07060302u : 0x05040100u;
+        *(u2*)(sv + value_at(ch + e, 2 * (q / 4) + (q & 1)) + 8 * ((q >> 1) & 1)) =
+            (u2){__builtin_amdgcn_perm(v[p][1], v[p][0], sel), __builtin_amdgcn_perm(v[p][3], v[p][2], sel)};
+      }
     }
   }
 }
@@ -247,8 +265,10 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
 
   const RQ_GLOBAL uint8_t* kc = gptr(a.c.codes) + (size_t)unit * 2 * a.c.cap * D;
   const RQ_GLOBAL uint8_t* vc = kc + (size_t)a.c.cap * D;
-  const RQ_GLOBAL float* kscale = gptr(a.c.scales) + (size_t)unit * 2 * (a.c.cap / kBlockTokens);
-  const RQ_GLOBAL float* vscale = kscale + a.c.cap / kBlockTokens;
+  // (scales by scalar loads: a vector load's wait would be one for the next
+  // tile's codes in flight)
+  const RQ_CONSTANT float* kscale = cptr(a.c.scales) + (size_t)unit * 2 * (a.c.cap / kBlockTokens);
+  const RQ_CONSTANT float* vscale = kscale + a.c.cap / kBlockTokens;
   const RQ_GLOBAL int32_t* pos = gptr(a.c.positions) + (size_t)unit * a.c.cap;
   const RQ_GLOBAL uint16_t* tail = gptr(a.c.tail) + (size_t)unit * 2 * kBlockTokens * D;
   const int coded = (hi < full ? hi : full) * kBlockTokens;     // slots of the split's coded blocks
@@ -262,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
   const bool far = a.slopes || a.window;
 
   float ks[2][2], vs[2][2];           // scales of the two buffers' blocks
-  TileLoad<D> next;
+  TileLoad next;
   auto fetch = [&](int blk) {
     load_tile<D>(kc, vc, blk * kBlockTokens, coded, &next);
   };
@@ -300,25 +320,28 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
       }
     }
     const bool masked = a.window || slot0 + kTile - 1 > past + wave_first;
-    float f[2] = {tks[0] * qs, tks[1] * qs};
-    if (a.cap != 0.0f || far || masked) {
+    // scores are s f + off; a mask needs them formed (f may be 0)
+    float f[2] = {tks[0] * qs, tks[1] * qs}, off = 0.0f;
+    if (a.cap != 0.0f && !EXACT) {
+      // cap tanh(x) = cap - 2 cap / (1 + e^(2x)): off by 2^-23 cap, which the
+      // rounding of P' hides
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        if (a.cap != 0.0f) {
-          if constexpr (EXACT) {
+        const float e2 = f[t] * 2.8853900817779268f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[t][i] = a.cap * tanh_f(s[t][i] * f[t]);
-          } else {
-            // cap tanh(x) = cap - 2 cap / (1 + e^(2x)): off by 2^-23 cap, which
-            // the rounding of P' hides
-            const float e2 = f[t] * 2.8853900817779268f;
+        for (int i = 0; i < 16; ++i) s[t][i] = __builtin_amdgcn_rcpf(-1.0f - exp2_f(s[t][i] * e2));
+        f[t] = 2.0f * a.cap;
+      }
+      off = a.cap;
+    }
+    if (far || masked || (EXACT && a.cap != 0.0f)) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              s[t][i] = __builtin_fmaf(__builtin_amdgcn_rcpf(1.0f + exp2_f(s[t][i] * e2)), -2.0f * a.cap, a.cap);
-          }
-        } else {
+      for (int t = 0; t < 2; ++t) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[t][i] *= f[t];
+        for (int i = 0; i < 16; ++i) s[t][i] = __builtin_fmaf(s[t][i], f[t], off);
+        if (EXACT && a.cap != 0.0f) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[t][i] = a.cap * tanh_f(s[t][i]);
         }
         f[t] = 1.0f;
         if (far) {
@@ -336,6 +359,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
             if (8 * (i >> 2) + (i & 3) > end) s[t][i] = -__builtin_inff();
         }
       }
+      off = 0.0f;
     }
     // the running maximum (moved when a score exceeds it by 8) and unit
     float top = -3.0e38f;
@@ -344,7 +368,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
       float x = s[t][0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) x = __builtin_fmaxf(x, s[t][i]);
-      top = __builtin_fmaxf(top, x * f[t]);
+      top = __builtin_fmaxf(top, __builtin_fmaf(x, f[t], off));
     }
     const float sv = __builtin_fmaxf(tvs[0], tvs[1]);
     const bool grow = unit2 == 0.0f || sv * unit2 > 128.0f;      // (the same in every lane)
@@ -368,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
     for (int t = 0; t < 2; ++t) {
       // (codes under a scale of zero are zero: any factor serves)
       const float by = tvs[t] > 0.0f ? __builtin_fmaxf(tvs[t] * unit2, 0x1p-80f) : 1.0f;
-      const float c = m - __builtin_amdgcn_logf(by);
+      const float c = m - __builtin_amdgcn_logf(by) - off;
       uint32_t hi2[8], lo2[8];
       float sum = 0.0f;
 #pragma unroll

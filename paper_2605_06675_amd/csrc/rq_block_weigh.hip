@@ -1,74 +1,282 @@
-// Accumulated attention weight of every cached token: after an attention call
-// has left each row's maximum and sum, the scores are computed again and each
-// token's probabilities added over the call's rows.  One wave owns 32 tokens
-// and adds its rows in order, so the result does not depend on scheduling.
+// Accumulated attention weight of every cached token, for calls of many query
+// rows: after an attention launch has left each row's maximum and sum, the
+// scores are computed again and each token's probabilities added over the rows.
+//
+// A wave holds the keys of 64 tokens as fp16 operands and walks the rows in
+// tiles of 32, which the workgroup's four waves share through LDS (two buffers,
+// one barrier a tile).  With the tokens as the products' rows every lane adds
+// up 32 tokens' weights over its query rows; the lanes' sums meet at the end.
+// A token's rows are added by one wave in order, so the result does not depend
+// on scheduling.
 #include "rq_block.h"
 
 namespace rq {
 
 namespace {
 
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+constexpr int kWaveTokens = 64, kTokens = 4 * kWaveTokens, kTileRows = 32;
+
+template <int D>
+__device__ __forceinline__ int query_at(int row, int piece) {
+  return row * D * 2 + ((piece ^ (row & (D / 8 - 1))) << 4);
+}
+
+// Keys of 32 tokens: lane (r = lane & 31, hl = lane >> 5) gets, of token r, the
+// channels 16 k + 8 hl + 0..7 in f[k]; returns the block's scale.
+template <int FMT, int D>
+__device__ __forceinline__ float coded_keys(const RQ_GLOBAL uint8_t* kc, const RQ_CONSTANT float* scales,
+                                            int blk, h8 f[D / 16]) {
+  const int lane = threadIdx.x & 63;
+  const RQ_GLOBAL uint8_t* p = kc + (uint32_t)(blk * kBlockTokens + (lane & 31)) * D + 8 * (lane >> 5);
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) {
+    const u2 w = *(const RQ_GLOBAL u2*)(p + 16 * k);
+    f[k] = as_h8((u4){key_pair<FMT>(w.x, false), key_pair<FMT>(w.x, true), key_pair<FMT>(w.y, false),
+                      key_pair<FMT>(w.y, true)});
+  }
+  return scales[blk];
+}
+
+// Largest magnitude of packed bf16 numbers.
+__device__ __forceinline__ float bf16_top(u4 x) {
+  float m = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    m = __builtin_fmaxf(m, __builtin_fmaxf(__builtin_fabsf(widen_t<true>(x[i] & 0xffffu)),
+                                           __builtin_fabsf(widen_t<true>(x[i] >> 16))));
+  return m;
+}
+// bf16 numbers times 2^-e as fp16.
+__device__ __forceinline__ h8 bf16_scaled(u4 x, int e) {
+  h8 f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = (_Float16)__builtin_amdgcn_ldexpf(widen_t<true>(x[i] & 0xffffu), -e);
+    f[2 * i + 1] = (_Float16)__builtin_amdgcn_ldexpf(widen_t<true>(x[i] >> 16), -e);
+  }
+  return f;
+}
+
+// The same of the tail's first n_tail rows (bf16 keys over a power of two, which
+// is returned).
+template <int D, bool BF16>
+__device__ __forceinline__ float tail_keys(const RQ_GLOBAL uint16_t* kt, int n_tail, h8 f[D / 16]) {
+  const int lane = threadIdx.x & 63, row = lane & 31;
+  u4 raw[D / 16];
+  float most = 0.0f;
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) {
+    raw[k] = row < n_tail ? *(const RQ_GLOBAL u4*)(kt + row * D + 16 * k + 8 * (lane >> 5))
+                          : (u4){0u, 0u, 0u, 0u};
+    most = __builtin_fmaxf(most, bf16_top(raw[k]));
+  }
+  if constexpr (!BF16) {
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) f[k] = as_h8(raw[k]);
+    return 1.0f;
+  }
+  for (int d = 32; d >= 1; d >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d, 64));
+  const int e = most > 0.0f ? __builtin_amdgcn_frexp_expf(most) : 0;
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) f[k] = bf16_scaled(raw[k], e);
+  return __builtin_amdgcn_ldexpf(1.0f, e);
+}
+
+// What a score needs of its row.
+struct RowInfo {
+  float qs, m, inv, slope;
+  int token, pos;
+};
+
 template <int FMT, int D, bool BF16>
-__global__ void __launch_bounds__(256) block_weigh_kernel(BlockAttendLaunch a) {
+__global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a) {
+  constexpr int kShare = kTileRows * D / 256;       // channels of a row that a thread loads
+  constexpr int kLanes = D / kShare;                // threads of a row: 8
+  __shared__ __align__(16) uint8_t sh_q[2][kTileRows * D * 2];
+  __shared__ RowInfo sh_row[2][kTileRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = lane & 15, g = lane >> 4;
+  const int col = lane & 31, hl = lane >> 5;
   const int unit = blockIdx.y, b = unit / a.c.H, h = unit - b * a.c.H;
   int past, nnew;
   block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
   const int total = past + nnew, full = total / kBlockTokens;
-  const int blk = blockIdx.x * 4 + wave, slot0 = blk * kBlockTokens;
-  if (slot0 >= total) return;
-  KeyBlock<D> k;
-  const RQ_GLOBAL uint16_t* kt = gptr(a.c.tail) + (size_t)unit * 2 * kBlockTokens * D;
-  if (blk < full)
-    load_keys<D>(gptr(a.c.codes) + (size_t)unit * 2 * a.c.cap * D,
-                 gptr(a.c.scales) + (size_t)unit * 2 * (a.c.cap / kBlockTokens), blk, &k);
-  const RQ_GLOBAL int32_t* pos = gptr(a.c.positions) + (size_t)unit * a.c.cap;
-  const RQ_GLOBAL float* stats = gptr(a.stats) + (size_t)unit * a.row_tiles * 32;
-  // the first token that sees the block, and the tiles from its row on
-  const int sees = slot0 - past > 0 ? slot0 - past : 0;
-  const int tiles = (nnew * a.G + 15) / 16;
-  f4 sum[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
-  for (int rt = sees * a.G / 16; rt < tiles; ++rt) {
-    const int row = rt * 16 + r;
-    QueryTile<D> q;
-    load_queries<D, BF16>(a, b, h, row, past, nnew, &q);
-    f4 s[2];
-    float factor = a.qscale;
-    if (blk < full) {
-      key_products<FMT, D>(k, q, s);
-      factor = k.scale * q.qs;
-    } else {
-      tail_products<D, BF16>(a, b, h, kt, q, s);
+  const int wg_slot = blockIdx.x * kTokens;
+  if (wg_slot >= total) return;
+  const int slot0 = wg_slot + wave * kWaveTokens, blk = slot0 / kBlockTokens;
+
+  h8 key[2][D / 16];
+  float ks[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    ks[t] = 0.0f;
+    if (blk + t < full)
+      ks[t] = coded_keys<FMT, D>(gptr(a.c.codes) + (size_t)unit * 2 * a.c.cap * D,
+                                 cptr(a.c.scales) + (size_t)unit * 2 * (a.c.cap / kBlockTokens), blk + t, key[t]);
+    else if (blk + t == full)
+      ks[t] = tail_keys<D, BF16>(gptr(a.c.tail) + (size_t)unit * 2 * kBlockTokens * D, total - full * kBlockTokens, key[t]);
+    else
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) key[t][k] = as_h8((u4){0u, 0u, 0u, 0u});
+  }
+  const bool far = a.slopes || a.window;
+  int pos[2][16];
+  if (far) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int slot = slot0 + 32 * t + 8 * (i >> 2) + 4 * hl + (i & 3);
+        pos[t][i] = slot < total ? gptr(a.c.positions)[(size_t)unit * a.c.cap + slot] : 0;
+      }
+  }
+
+  // tiles of rows that see some of the workgroup's tokens
+  const int rows = nnew * a.G;
+  int from = wg_slot - past, to = nnew;              // tokens of the call
+  from = from > 0 ? from : 0;
+  if (a.window) {
+    const int64_t seen = (int64_t)wg_slot + kTokens - 1 + a.window - past;
+    to = seen < to ? (int)seen : to;
+  }
+  if (from >= to) return;
+  const int tile0 = from * a.G / kTileRows, tile1 = (to * a.G + kTileRows - 1) / kTileRows;
+
+  // this thread's share of a tile
+  const int row_in = threadIdx.x / kLanes, ch = (threadIdx.x % kLanes) * kShare;
+  u4 raw[kShare / 8];
+  float2 stat;
+  auto fetch = [&](int tile) {
+    const int row = tile * kTileRows + row_in;
+    const int token = row / a.G, head = row - token * a.G;
+    stat = make_float2(3.0e38f, 0.0f);       // a row behind the last adds exp2(-3e38) * 0
+#pragma unroll
+    for (int i = 0; i < kShare / 8; ++i) raw[i] = (u4){0u, 0u, 0u, 0u};
+    if (row < rows) {
+      const RQ_GLOBAL uint16_t* p = gptr(static_cast<const uint16_t*>(a.q.p)) + b * a.q.sb +
+                                    (int64_t)(h * a.G + head) * a.q.sh + token * a.q.st + ch;
+#pragma unroll
+      for (int i = 0; i < kShare / 8; ++i) raw[i] = *(const RQ_GLOBAL u4_any*)(p + 8 * i);
+      const RQ_GLOBAL float* st = gptr(a.stats) + ((size_t)unit * a.row_tiles * 16 + row) * 2;
+      stat = make_float2(st[0], st[1]);
     }
-    block_scores<D>(a, q, pos, factor, slot0, past, true, s);
-    if (q.valid) {
-      const float m = stats[row * 2], inv = stats[row * 2 + 1];
+  };
+  auto put = [&](int tile, int buf) {
+    const int row = tile * kTileRows + row_in;
+    int e = 0;
+    if constexpr (BF16) {
+      float most = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kShare / 8; ++i) most = __builtin_fmaxf(most, bf16_top(raw[i]));
+      for (int d = kLanes / 2; d >= 1; d >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d, 64));
+      e = most > 0.0f ? __builtin_amdgcn_frexp_expf(most) : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kShare / 8; ++i)
+      *(h8*)(sh_q[buf] + query_at<D>(row_in, ch / 8 + i)) = BF16 ? bf16_scaled(raw[i], e) : as_h8(raw[i]);
+    if (ch == 0) {
+      RowInfo r;
+      r.qs = __builtin_amdgcn_ldexpf(a.qscale, e);
+      r.m = stat.x;
+      r.inv = stat.y;
+      r.token = row / a.G;
+      const int head = row - r.token * a.G;
+      r.slope = a.slopes ? gptr(a.slopes)[h * a.G + head] * 1.4426950408889634f : 0.0f;
+      r.pos = far && row < rows ? gptr(a.c.positions)[(size_t)unit * a.c.cap + past + r.token] : 0;
+      sh_row[buf][row_in] = r;
+    }
+  };
+
+  f16v sum[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[t][i] = 0.0f;
+  auto work = [&](int tile, int buf) {
+    const int lastrow = tile * kTileRows + kTileRows - 1;
+    if (past + lastrow / a.G < slot0) return;
+    const RowInfo r = sh_row[buf][col];
+    f16v s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      const h8 q = *(const h8*)(sh_q[buf] + query_at<D>(col, 2 * k + hl));
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          sum[t][i] = __builtin_fmaf(exp2_f(s[t][i] - m), inv, sum[t][i]);
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key[t][k], q, s[t], 0, 0, 0);
     }
+    const bool masked = a.window || slot0 + kWaveTokens - 1 > past + tile * kTileRows / a.G;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      float f = ks[t] * r.qs;
+      if (a.cap != 0.0f || far || masked) {
+        if (a.cap != 0.0f) {
+          // cap tanh(x) = cap - 2 cap / (1 + e^(2x)), off by 2^-23 cap
+          const float e2 = f * 2.8853900817779268f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            s[t][i] = __builtin_fmaf(__builtin_amdgcn_rcpf(1.0f + exp2_f(s[t][i] * e2)), -2.0f * a.cap, a.cap);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[t][i] *= f;
+        }
+        f = 1.0f;
+        if (far) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int away = r.pos - pos[t][i];
+            s[t][i] = __builtin_fmaf(-r.slope, (float)away, s[t][i]);
+            if (a.window && away >= a.window) s[t][i] = -__builtin_inff();
+          }
+        }
+        if (masked) {
+          const int end = past + r.token - slot0 - 32 * t - 4 * hl;
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (8 * (i >> 2) + (i & 3) > end) s[t][i] = -__builtin_inff();
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        sum[t][i] = __builtin_fmaf(exp2_f(__builtin_fmaf(s[t][i], f, -r.m)), r.inv, sum[t][i]);
+    }
+  };
+
+  fetch(tile0);
+  put(tile0, 0);
+  __syncthreads();
+  for (int tile = tile0;; ++tile) {
+    const int buf = (tile - tile0) & 1;
+    const bool more = tile + 1 < tile1;
+    if (more) fetch(tile + 1);
+    work(tile, buf);
+    if (!more) break;
+    put(tile + 1, buf ^ 1);
+    __syncthreads();
   }
+
+  // add the 32 rows' lanes; lane (col, hl) with col < 16 writes register col
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+  for (int t = 0; t < 2; ++t) {
+    float add = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      for (int d = 1; d < 16; d <<= 1) sum[t][i] += __shfl_xor(sum[t][i], d, 64);
-  // lane (r, g) with r < 8 writes token 16 (r / 4) + 4 g + r % 4
-  float add = 0.0f;
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) add = r == 4 * t + i ? sum[t][i] : add;
-  const int slot = slot0 + 16 * (r >> 2) + 4 * g + (r & 3);
-  if (r < 8 && slot < total) gptr(a.c.weights)[(size_t)unit * a.c.cap + slot] += add;
+    for (int i = 0; i < 16; ++i) {
+      float x = sum[t][i];
+      for (int d = 1; d < 32; d <<= 1) x += __shfl_xor(x, d, 64);
+      add = col == i ? x : add;
+    }
+    const int slot = slot0 + 32 * t + 8 * (col >> 2) + 4 * hl + (col & 3);
+    if (col < 16 && slot < total) gptr(a.c.weights)[(size_t)unit * a.c.cap + slot] += add;
+  }
 }
 
 template <int FMT, int D>
 hipError_t launch(const BlockAttendLaunch& a, hipStream_t s) {
-  const dim3 grid((a.max_tokens + 4 * kBlockTokens - 1) / (4 * kBlockTokens), a.c.B * a.c.H);
+  const dim3 grid((a.max_tokens + kTokens - 1) / kTokens, a.c.B * a.c.H);
   if (a.c.is_bf16)
     hipLaunchKernelGGL((block_weigh_kernel<FMT, D, true>), grid, dim3(256), 0, s, a);
   else
