@@ -64,6 +64,8 @@ struct BlockAttendLaunch {
   float* stats;            // [unit][row][2]: maximum and 1 / sum, where accumulate
   float* scores;           // [unit][block][row][32]: log2 scores, where accumulate
                            // and all rows fit one tile; else NULL
+  int row_parts;           // else: workgroups that share a token's rows,
+  float* sums;             // and, of more than one, [part][unit][token] sums
 };
 
 struct BlockEvictLaunch {
@@ -87,6 +89,7 @@ hipError_t launch_block_weigh(const BlockAttendLaunch& a, hipStream_t s);
 hipError_t launch_block_evict(const BlockEvictLaunch& a, hipStream_t s);
 
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 // callers' rows may begin at any element

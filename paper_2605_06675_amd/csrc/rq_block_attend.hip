@@ -357,6 +357,40 @@ __device__ __forceinline__ void merge_row(const BlockAttendLaunch& a, int grow, 
   }
 }
 
+// Few splits of many rows: 1024 / D rows a workgroup, each thread four channels
+// of one.
+template <int D>
+__global__ void __launch_bounds__(256) block_merge_rows_kernel(BlockAttendLaunch a) {
+  constexpr int kCols = D / 4;
+  const int unit = blockIdx.y, b = unit / a.c.H, h = unit - b * a.c.H;
+  int past, nnew;
+  block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
+  const int grow = blockIdx.x * (256 / kCols) + threadIdx.x / kCols, col = threadIdx.x % kCols;
+  const int token = grow / a.G, row = grow & 15;
+  if (token >= nnew) return;
+  const size_t base = ((size_t)unit * a.row_tiles + (grow >> 4)) * a.splits;
+  const RQ_GLOBAL f2* ml = (const RQ_GLOBAL f2*)(gptr(a.part_ml) + (base * 16 + row) * 2);
+  const RQ_GLOBAL float* o = gptr(a.part) + (base * 16 + row) * D + col * 4;
+  float m = -1.0e30f, l = 0.0f;
+  f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int s = 0; s < a.splits; ++s) m = __builtin_fmaxf(m, ml[s * 16].x);
+#pragma unroll 4
+  for (int s = 0; s < a.splits; ++s) {
+    const f2 p = ml[s * 16];
+    const float by = exp2_f(p.x - m);
+    l = __builtin_fmaf(p.y, by, l);
+    x += *(const RQ_GLOBAL f4*)(o + (size_t)s * 16 * D) * by;
+  }
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  x *= inv;
+  store_out<4>(a, b, h * a.G + grow - token * a.G, token, col * 4, (const float*)&x);
+  if (a.stats && col == 0) {
+    gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + grow) * 2] = m;
+    gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + grow) * 2 + 1] = inv;
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttendLaunch a) {
   const int unit = blockIdx.y, b = unit / a.c.H;
@@ -443,14 +477,19 @@ hipError_t launch(const BlockAttendLaunch& a, hipStream_t s) {
 
 }  // namespace
 
+template <int D>
+static hipError_t merge(const BlockAttendLaunch& a, hipStream_t s) {
+  const int rows = a.n * a.G, units = a.c.B * a.c.H, per = 1024 / D;
+  if (a.splits <= 8 || (int64_t)rows * units >= 4096)
+    hipLaunchKernelGGL((block_merge_rows_kernel<D>), dim3((rows + per - 1) / per, units), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((block_merge_kernel<D>), dim3(rows, units), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
 hipError_t launch_block_merge(const BlockAttendLaunch& a, hipStream_t s) {
   if (a.splits == 1) return hipSuccess;
-  const dim3 grid(a.n * a.G, a.c.B * a.c.H);
-  if (a.c.D == 64)
-    hipLaunchKernelGGL((block_merge_kernel<64>), grid, dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((block_merge_kernel<128>), grid, dim3(256), 0, s, a);
-  return hipGetLastError();
+  return a.c.D == 64 ? merge<64>(a, s) : merge<128>(a, s);
 }
 
 hipError_t launch_block_attend(const BlockAttendLaunch& a, hipStream_t s) {

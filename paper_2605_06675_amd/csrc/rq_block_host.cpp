@@ -104,13 +104,18 @@ rq_status check_query(const rq_block_cache* c, const rq_block_query* a) {
 // How an attention call is split, and what it needs of the workspace.
 struct Plan {
   int prompt;                      // tiles of 256 rows (rq_block_prompt.hip)
-  int row_tiles, splits;
-  uint64_t part, part_ml, stats, scores;   // bytes
-  uint64_t bytes() const { return part + part_ml + stats + scores; }
+  int row_tiles, splits, row_parts;
+  uint64_t part, part_ml, stats, scores, sums;   // bytes
+  uint64_t bytes() const { return part + part_ml + stats + scores + sums; }
 };
 
-// One resident round: three workgroups a CU over the units' row tiles, at
-// least four blocks (one a wave) a workgroup.
+// Few rows: one resident round, three workgroups a CU over the units' row tiles,
+// at least four blocks (one a wave) a workgroup.
+// More than two tiles of 16 rows: tiles of 128 rows, two workgroups a CU, at
+// least eight blocks each.  Where the new tokens are few beside the cached ones,
+// sequences may differ in length and a round's workgroups with them: one split
+// more (4 sequences, 8 kv-heads of 4 heads, 512 tokens over 8192: 358 us
+// unsplit, 366 in two; lengths from 2048 to 8192: 289 and 250).
 Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
   Plan p{};
   const int64_t G = c->n_q_heads / c->n_kv_heads, u = (int64_t)units(c);
@@ -125,6 +130,7 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
   if (p.prompt) {
     s = 2 * (int64_t)rq::device_cus() / (u * ((a->n_new * G + 127) / 128));
     s = std::min(s, (blocks + 7) / 8);
+    if (s <= 1 && a->max_tokens >= 4 * (int64_t)a->n_new && blocks >= 128) s = 2;
   } else {
     s = 3 * (int64_t)rq::device_cus() / (u * p.row_tiles);
     s = std::min(s, (blocks + 3) / 4);
@@ -142,6 +148,14 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
     if (p.row_tiles == 1)
       p.scores = (uint64_t)u * ((a->max_tokens + rq::kBlockTokens - 1) / rq::kBlockTokens) * a->n_new *
                  G * rq::kBlockTokens * sizeof(float);
+    // else workgroups of 256 tokens, and parts of the rows to fill four rounds
+    // (two a CU), 512 rows or more in each
+    const int64_t wgs = u * ((a->max_tokens + 255) / 256);
+    int64_t parts = 8 * (int64_t)rq::device_cus() / wgs;
+    parts = std::min(parts, (a->n_new * G + 511) / 512);
+    p.row_parts = (int)std::max<int64_t>(parts, 1);
+    if (p.row_tiles > 1 && p.row_parts > 1)
+      p.sums = (uint64_t)p.row_parts * u * a->max_tokens * sizeof(float);
   }
   return p;
 }
@@ -261,6 +275,8 @@ rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_bl
   a.part_ml = reinterpret_cast<float*>(w + p.part);
   if (p.stats) a.stats = reinterpret_cast<float*>(w + p.part + p.part_ml);
   if (p.scores) a.scores = reinterpret_cast<float*>(w + p.part + p.part_ml + p.stats);
+  a.row_parts = p.row_parts;
+  if (p.sums) a.sums = reinterpret_cast<float*>(w + p.part + p.part_ml + p.stats + p.scores);
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = p.prompt ? rq::launch_block_prompt(a, s) : rq::launch_block_attend(a, s);
   if (e == hipSuccess && p.prompt) e = rq::launch_block_merge(a, s);

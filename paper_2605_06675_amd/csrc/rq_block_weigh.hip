@@ -3,11 +3,11 @@
 // scores are computed again and each token's probabilities added over the rows.
 //
 // A wave holds the keys of 64 tokens as fp16 operands and walks the rows in
-// tiles of 32, which the workgroup's four waves share through LDS (two buffers,
+// tiles of 64, which the workgroup's four waves share through LDS (two buffers,
 // one barrier a tile).  With the tokens as the products' rows every lane adds
 // up 32 tokens' weights over its query rows; the lanes' sums meet at the end.
-// A token's rows are added by one wave in order, so the result does not depend
-// on scheduling.
+// Where the tokens' workgroups are few, several share the rows, and a small
+// launch adds their sums in order: the result does not depend on scheduling.
 #include "rq_block.h"
 
 namespace rq {
@@ -16,7 +16,7 @@ namespace {
 
 typedef float f16v __attribute__((ext_vector_type(16)));
 
-constexpr int kWaveTokens = 64, kTokens = 4 * kWaveTokens, kTileRows = 32;
+constexpr int kWaveTokens = 64, kTokens = 4 * kWaveTokens, kTileRows = 64;
 
 template <int D>
 __device__ __forceinline__ int query_at(int row, int piece) {
@@ -93,7 +93,7 @@ struct RowInfo {
 template <int FMT, int D, bool BF16>
 __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a) {
   constexpr int kShare = kTileRows * D / 256;       // channels of a row that a thread loads
-  constexpr int kLanes = D / kShare;                // threads of a row: 8
+  constexpr int kLanes = D / kShare;                // threads of a row: 4
   __shared__ __align__(16) uint8_t sh_q[2][kTileRows * D * 2];
   __shared__ RowInfo sh_row[2][kTileRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
   int past, nnew;
   block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
   const int total = past + nnew, full = total / kBlockTokens;
-  const int wg_slot = blockIdx.x * kTokens;
+  const int part = blockIdx.x % a.row_parts, wg_slot = blockIdx.x / a.row_parts * kTokens;
   if (wg_slot >= total) return;
   const int slot0 = wg_slot + wave * kWaveTokens, blk = slot0 / kBlockTokens;
 
@@ -140,8 +140,14 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
     const int64_t seen = (int64_t)wg_slot + kTokens - 1 + a.window - past;
     to = seen < to ? (int)seen : to;
   }
-  if (from >= to) return;
-  const int tile0 = from * a.G / kTileRows, tile1 = (to * a.G + kTileRows - 1) / kTileRows;
+  int tile0 = from * a.G / kTileRows, tile1 = (to * a.G + kTileRows - 1) / kTileRows;
+  {
+    // this workgroup's part of all tiles
+    const int64_t all = (a.n * a.G + kTileRows - 1) / kTileRows;
+    const int p0 = (int)(all * part / a.row_parts), p1 = (int)(all * (part + 1) / a.row_parts);
+    tile0 = tile0 > p0 ? tile0 : p0;
+    tile1 = tile1 < p1 ? tile1 : p1;
+  }
 
   // this thread's share of a tile
   const int row_in = threadIdx.x / kLanes, ch = (threadIdx.x % kLanes) * kShare;
@@ -193,10 +199,10 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum[t][i] = 0.0f;
-  auto work = [&](int tile, int buf) {
-    const int lastrow = tile * kTileRows + kTileRows - 1;
-    if (past + lastrow / a.G < slot0) return;
-    const RowInfo r = sh_row[buf][col];
+  auto work = [&](int tile, int buf, int half) {          // 32 rows of a tile
+    const int row0 = tile * kTileRows + 32 * half;
+    if (past + (row0 + 31) / a.G < slot0) return;
+    const RowInfo r = sh_row[buf][32 * half + col];
     f16v s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -204,12 +210,12 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
       for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
-      const h8 q = *(const h8*)(sh_q[buf] + query_at<D>(col, 2 * k + hl));
+      const h8 q = *(const h8*)(sh_q[buf] + query_at<D>(32 * half + col, 2 * k + hl));
 #pragma unroll
       for (int t = 0; t < 2; ++t)
         s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key[t][k], q, s[t], 0, 0, 0);
     }
-    const bool masked = a.window || slot0 + kWaveTokens - 1 > past + tile * kTileRows / a.G;
+    const bool masked = a.window || slot0 + kWaveTokens - 1 > past + row0 / a.G;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       float f = ks[t] * r.qs;
@@ -246,17 +252,20 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
     }
   };
 
-  fetch(tile0);
-  put(tile0, 0);
-  __syncthreads();
-  for (int tile = tile0;; ++tile) {
-    const int buf = (tile - tile0) & 1;
-    const bool more = tile + 1 < tile1;
-    if (more) fetch(tile + 1);
-    work(tile, buf);
-    if (!more) break;
-    put(tile + 1, buf ^ 1);
+  if (from < to && tile0 < tile1) {
+    fetch(tile0);
+    put(tile0, 0);
     __syncthreads();
+    for (int tile = tile0;; ++tile) {
+      const int buf = (tile - tile0) & 1;
+      const bool more = tile + 1 < tile1;
+      if (more) fetch(tile + 1);
+      work(tile, buf, 0);
+      work(tile, buf, 1);
+      if (!more) break;
+      put(tile + 1, buf ^ 1);
+      __syncthreads();
+    }
   }
 
   // add the 32 rows' lanes; lane (col, hl) with col < 16 writes register col
@@ -270,17 +279,37 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
       add = col == i ? x : add;
     }
     const int slot = slot0 + 32 * t + 8 * (col >> 2) + 4 * hl + (col & 3);
-    if (col < 16 && slot < total) gptr(a.c.weights)[(size_t)unit * a.c.cap + slot] += add;
+    if (col < 16 && slot < total) {
+      if (a.row_parts > 1)
+        gptr(a.sums)[((size_t)part * gridDim.y + unit) * a.max_tokens + slot] = add;
+      else
+        gptr(a.c.weights)[(size_t)unit * a.c.cap + slot] += add;
+    }
   }
+}
+
+__global__ void __launch_bounds__(256) block_add_kernel(BlockAttendLaunch a) {
+  const int unit = blockIdx.y, slot = blockIdx.x * 256 + threadIdx.x;
+  int past, nnew;
+  block_lengths(a.past, a.new_len, unit / a.c.H, a.n, a.max_tokens, &past, &nnew);
+  if (slot >= past + nnew) return;
+  float sum = 0.0f;
+#pragma unroll 4
+  for (int p = 0; p < a.row_parts; ++p)
+    sum += gptr(a.sums)[((size_t)p * gridDim.y + unit) * a.max_tokens + slot];
+  gptr(a.c.weights)[(size_t)unit * a.c.cap + slot] += sum;
 }
 
 template <int FMT, int D>
 hipError_t launch(const BlockAttendLaunch& a, hipStream_t s) {
-  const dim3 grid((a.max_tokens + kTokens - 1) / kTokens, a.c.B * a.c.H);
+  const dim3 grid((a.max_tokens + kTokens - 1) / kTokens * a.row_parts, a.c.B * a.c.H);
   if (a.c.is_bf16)
     hipLaunchKernelGGL((block_weigh_kernel<FMT, D, true>), grid, dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((block_weigh_kernel<FMT, D, false>), grid, dim3(256), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.row_parts == 1) return e;
+  hipLaunchKernelGGL(block_add_kernel, dim3((a.max_tokens + 255) / 256, a.c.B * a.c.H), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
