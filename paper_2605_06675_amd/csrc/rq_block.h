@@ -64,7 +64,9 @@ struct BlockAttendLaunch {
   float* stats;            // [unit][row][2]: maximum and 1 / sum, where accumulate
   float* scores;           // [unit][block][row][32]: log2 scores, where accumulate
                            // and all rows fit one tile; else NULL
-  int row_parts;           // else: workgroups that share a token's rows,
+  uint16_t* queries;       // else: [unit][row][D] queries as fp16 operands,
+  float* factors;          // [unit][row] and the factor of their scores;
+  int row_parts;           // workgroups that share a token's rows,
   float* sums;             // and, of more than one, [part][unit][token] sums
 };
 

@@ -105,8 +105,8 @@ rq_status check_query(const rq_block_cache* c, const rq_block_query* a) {
 struct Plan {
   int prompt;                      // tiles of 256 rows (rq_block_prompt.hip)
   int row_tiles, splits, row_parts;
-  uint64_t part, part_ml, stats, scores, sums;   // bytes
-  uint64_t bytes() const { return part + part_ml + stats + scores + sums; }
+  uint64_t part, part_ml, stats, scores, queries, factors, sums;   // bytes
+  uint64_t bytes() const { return part + part_ml + stats + scores + queries + factors + sums; }
 };
 
 // Few rows: one resident round, three workgroups a CU over the units' row tiles,
@@ -125,7 +125,7 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
     const int64_t seen = ((int64_t)a->window + 16 / G + 1) / rq::kBlockTokens + 2;
     blocks = seen < blocks ? seen : blocks;
   }
-  p.prompt = p.row_tiles > 2;
+  p.prompt = p.row_tiles > 2 || (p.row_tiles > 1 && a->accumulate);
   int64_t s;
   if (p.prompt) {
     s = 2 * (int64_t)rq::device_cus() / (u * ((a->n_new * G + 127) / 128));
@@ -145,17 +145,20 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
     p.stats = tiles * 16 * 2 * sizeof(float);
     // one tile of rows: the scores are kept (4 bytes a row and token) rather
     // than computed again from the keys (D bytes a token)
-    if (p.row_tiles == 1)
-      p.scores = (uint64_t)u * ((a->max_tokens + rq::kBlockTokens - 1) / rq::kBlockTokens) * a->n_new *
-                 G * rq::kBlockTokens * sizeof(float);
+    const int64_t rows = a->n_new * G;
+    if (p.row_tiles == 1) {
+      p.scores = (uint64_t)u * ((a->max_tokens + rq::kBlockTokens - 1) / rq::kBlockTokens) * rows *
+                 rq::kBlockTokens * sizeof(float);
+      return p;
+    }
     // else workgroups of 256 tokens, and parts of the rows to fill four rounds
     // (two a CU), 512 rows or more in each
-    const int64_t wgs = u * ((a->max_tokens + 255) / 256);
-    int64_t parts = 8 * (int64_t)rq::device_cus() / wgs;
-    parts = std::min(parts, (a->n_new * G + 511) / 512);
+    int64_t parts = 8 * (int64_t)rq::device_cus() / (u * ((a->max_tokens + 255) / 256));
+    parts = std::min(parts, (rows + 511) / 512);
     p.row_parts = (int)std::max<int64_t>(parts, 1);
-    if (p.row_tiles > 1 && p.row_parts > 1)
-      p.sums = (uint64_t)p.row_parts * u * a->max_tokens * sizeof(float);
+    p.queries = tiles * 16 * c->head_dim * sizeof(uint16_t);
+    p.factors = tiles * 16 * sizeof(float);
+    if (p.row_parts > 1) p.sums = (uint64_t)p.row_parts * u * a->max_tokens * sizeof(float);
   }
   return p;
 }
@@ -271,12 +274,19 @@ rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_bl
   a.slopes = q->slopes;
   a.accumulate = q->accumulate != 0;
   uint8_t* w = static_cast<uint8_t*>(ws);
-  a.part = reinterpret_cast<float*>(w);
-  a.part_ml = reinterpret_cast<float*>(w + p.part);
-  if (p.stats) a.stats = reinterpret_cast<float*>(w + p.part + p.part_ml);
-  if (p.scores) a.scores = reinterpret_cast<float*>(w + p.part + p.part_ml + p.stats);
+  auto take = [&w](uint64_t bytes) {
+    uint8_t* p = bytes ? w : nullptr;
+    w += bytes;
+    return p;
+  };
+  a.part = reinterpret_cast<float*>(take(p.part));
+  a.part_ml = reinterpret_cast<float*>(take(p.part_ml));
+  a.stats = reinterpret_cast<float*>(take(p.stats));
+  a.scores = reinterpret_cast<float*>(take(p.scores));
+  a.queries = reinterpret_cast<uint16_t*>(take(p.queries));
+  a.factors = reinterpret_cast<float*>(take(p.factors));
+  a.sums = reinterpret_cast<float*>(take(p.sums));
   a.row_parts = p.row_parts;
-  if (p.sums) a.sums = reinterpret_cast<float*>(w + p.part + p.part_ml + p.stats + p.scores);
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = p.prompt ? rq::launch_block_prompt(a, s) : rq::launch_block_attend(a, s);
   if (e == hipSuccess && p.prompt) e = rq::launch_block_merge(a, s);

@@ -258,6 +258,13 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) q[k] = as_h8(raw[k]);
     }
+    if (a.queries && split == 0 && valid) {       // for the weights' launch
+      const size_t at = (size_t)unit * a.row_tiles * 16 + row;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+        *(RQ_GLOBAL h8*)(gptr(a.queries) + at * D + 16 * k + 8 * hl) = q[k];
+      if (hl == 0) gptr(a.factors)[at] = qs;
+    }
     if (a.slopes) slope = gptr(a.slopes)[h * a.G + head] * 1.4426950408889634f;
     if (a.slopes || a.window)
       qpos = gptr(a.c.positions)[(size_t)unit * a.c.cap + past + token];

@@ -3,8 +3,8 @@
 // scores are computed again and each token's probabilities added over the rows.
 //
 // A wave holds the keys of 64 tokens as fp16 operands and walks the rows in
-// tiles of 64, which the workgroup's four waves share through LDS (two buffers,
-// one barrier a tile).  With the tokens as the products' rows every lane adds
+// tiles of 64 (their fp16 copies that the attention launch left), which the
+// workgroup's four waves share through LDS (two buffers, one barrier a tile).  With the tokens as the products' rows every lane adds
 // up 32 tokens' weights over its query rows; the lanes' sums meet at the end.
 // Where the tokens' workgroups are few, several share the rows, and a small
 // launch adds their sums in order: the result does not depend on scheduling.
@@ -151,47 +151,37 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
 
   // this thread's share of a tile
   const int row_in = threadIdx.x / kLanes, ch = (threadIdx.x % kLanes) * kShare;
+  const RQ_GLOBAL uint16_t* queries = gptr(a.queries) + ((size_t)unit * a.row_tiles * 16 + row_in) * D + ch;
+  const RQ_GLOBAL float* stats = gptr(a.stats) + ((size_t)unit * a.row_tiles * 16 + row_in) * 2;
+  const RQ_GLOBAL float* factors = gptr(a.factors) + (size_t)unit * a.row_tiles * 16 + row_in;
   u4 raw[kShare / 8];
-  float2 stat;
+  RowInfo info;
   auto fetch = [&](int tile) {
     const int row = tile * kTileRows + row_in;
-    const int token = row / a.G, head = row - token * a.G;
-    stat = make_float2(3.0e38f, 0.0f);       // a row behind the last adds exp2(-3e38) * 0
 #pragma unroll
     for (int i = 0; i < kShare / 8; ++i) raw[i] = (u4){0u, 0u, 0u, 0u};
-    if (row < rows) {
-      const RQ_GLOBAL uint16_t* p = gptr(static_cast<const uint16_t*>(a.q.p)) + b * a.q.sb +
-                                    (int64_t)(h * a.G + head) * a.q.sh + token * a.q.st + ch;
-#pragma unroll
-      for (int i = 0; i < kShare / 8; ++i) raw[i] = *(const RQ_GLOBAL u4_any*)(p + 8 * i);
-      const RQ_GLOBAL float* st = gptr(a.stats) + ((size_t)unit * a.row_tiles * 16 + row) * 2;
-      stat = make_float2(st[0], st[1]);
-    }
-  };
-  auto put = [&](int tile, int buf) {
-    const int row = tile * kTileRows + row_in;
-    int e = 0;
-    if constexpr (BF16) {
-      float most = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kShare / 8; ++i) most = __builtin_fmaxf(most, bf16_top(raw[i]));
-      for (int d = kLanes / 2; d >= 1; d >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d, 64));
-      e = most > 0.0f ? __builtin_amdgcn_frexp_expf(most) : 0;
-    }
+    // (a row behind the last adds exp2(-3e38) * 0)
+    info.m = 3.0e38f;
+    info.qs = info.inv = info.slope = 0.0f;
+    info.token = info.pos = 0;
+    if (row >= rows) return;
 #pragma unroll
     for (int i = 0; i < kShare / 8; ++i)
-      *(h8*)(sh_q[buf] + query_at<D>(row_in, ch / 8 + i)) = BF16 ? bf16_scaled(raw[i], e) : as_h8(raw[i]);
+      raw[i] = *(const RQ_GLOBAL u4*)(queries + (size_t)tile * kTileRows * D + 8 * i);
     if (ch == 0) {
-      RowInfo r;
-      r.qs = __builtin_amdgcn_ldexpf(a.qscale, e);
-      r.m = stat.x;
-      r.inv = stat.y;
-      r.token = row / a.G;
-      const int head = row - r.token * a.G;
-      r.slope = a.slopes ? gptr(a.slopes)[h * a.G + head] * 1.4426950408889634f : 0.0f;
-      r.pos = far && row < rows ? gptr(a.c.positions)[(size_t)unit * a.c.cap + past + r.token] : 0;
-      sh_row[buf][row_in] = r;
+      info.qs = factors[tile * kTileRows];
+      info.m = stats[tile * kTileRows * 2];
+      info.inv = stats[tile * kTileRows * 2 + 1];
+      info.token = row / a.G;
+      if (a.slopes) info.slope = gptr(a.slopes)[h * a.G + row - info.token * a.G] * 1.4426950408889634f;
+      if (far) info.pos = gptr(a.c.positions)[(size_t)unit * a.c.cap + past + info.token];
     }
+  };
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < kShare / 8; ++i)
+      *(u4*)(sh_q[buf] + query_at<D>(row_in, ch / 8 + i)) = raw[i];
+    if (ch == 0) sh_row[buf][row_in] = info;
   };
 
   f16v sum[2];
@@ -218,19 +208,20 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
     const bool masked = a.window || slot0 + kWaveTokens - 1 > past + row0 / a.G;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      float f = ks[t] * r.qs;
-      if (a.cap != 0.0f || far || masked) {
-        if (a.cap != 0.0f) {
-          // cap tanh(x) = cap - 2 cap / (1 + e^(2x)), off by 2^-23 cap
-          const float e2 = f * 2.8853900817779268f;
+      float f = ks[t] * r.qs, off = 0.0f;      // scores are s f + off
+      if (a.cap != 0.0f) {
+        // cap tanh(x) = cap - 2 cap / (1 + e^(2x)), off by 2^-23 cap
+        const float e2 = f * 2.8853900817779268f;
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            s[t][i] = __builtin_fmaf(__builtin_amdgcn_rcpf(1.0f + exp2_f(s[t][i] * e2)), -2.0f * a.cap, a.cap);
-        } else {
+        for (int i = 0; i < 16; ++i) s[t][i] = __builtin_amdgcn_rcpf(-1.0f - exp2_f(s[t][i] * e2));
+        f = 2.0f * a.cap;
+        off = a.cap;
+      }
+      if (far || masked) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[t][i] *= f;
-        }
+        for (int i = 0; i < 16; ++i) s[t][i] = __builtin_fmaf(s[t][i], f, off);
         f = 1.0f;
+        off = 0.0f;
         if (far) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
@@ -246,15 +237,16 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
             if (8 * (i >> 2) + (i & 3) > end) s[t][i] = -__builtin_inff();
         }
       }
+      const float c = off - r.m;
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        sum[t][i] = __builtin_fmaf(exp2_f(__builtin_fmaf(s[t][i], f, -r.m)), r.inv, sum[t][i]);
+        sum[t][i] = __builtin_fmaf(exp2_f(__builtin_fmaf(s[t][i], f, c)), r.inv, sum[t][i]);
     }
   };
 
   if (from < to && tile0 < tile1) {
     fetch(tile0);
-    put(tile0, 0);
+    put(0);
     __syncthreads();
     for (int tile = tile0;; ++tile) {
       const int buf = (tile - tile0) & 1;
@@ -263,7 +255,7 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
       work(tile, buf, 0);
       work(tile, buf, 1);
       if (!more) break;
-      put(tile + 1, buf ^ 1);
+      put(buf ^ 1);
       __syncthreads();
     }
   }
