@@ -380,7 +380,8 @@ rq_status rq_fallback_beta(int32_t n, double* beta, const double* r2,
  * floor(L / 32) * 32 are coded, the rest lie in the tail.
  *
  * Buffers (the caller allocates the sizes reported by rq_block_sizes, each
- * aligned to 16 bytes; contents of a new cache do not matter):
+ * aligned to 16 bytes; but for the counters, contents of a new cache do not
+ * matter):
  *  codes      8-bit [n_layers][batch][n_kv_heads][2][capacity][head_dim]
  *  scales     fp32  [n_layers][batch][n_kv_heads][2][capacity / 32]
  *  tail       16-bit, in dtype [n_layers][batch][n_kv_heads][2][32][head_dim]
@@ -389,6 +390,10 @@ rq_status rq_fallback_beta(int32_t n, double* beta, const double* r2,
  *             position in its sequence, ascending
  *  weights    fp32  [n_layers][batch][n_kv_heads][capacity]: accumulated
  *             attention weight of each slot; NULL if none is kept
+ *  counters   uint32 [n_layers][batch][n_kv_heads][2]: zeroed by the caller
+ *             before the first call, and zero again after every one; NULL:
+ *             attention that splits a sequence takes a launch more.  Calls
+ *             that attend to one layer must not overlap where it is given.
  * (2: K, then V).  Entries behind a sequence's last token are neither read
  * for a result nor written.
  *
@@ -411,6 +416,7 @@ typedef struct rq_block_cache {
   void* tail;
   int32_t* positions;
   float* weights;
+  uint32_t* counters;
 } rq_block_cache;
 
 /* A device tensor [batch][heads][tokens][head_dim] whose rows are contiguous
@@ -424,7 +430,8 @@ typedef struct rq_block_rows {
  * buffer sizes in bytes.  Any output pointer may be NULL.  Host only. */
 rq_status rq_block_sizes(const rq_block_cache* c, uint64_t* codes_bytes,
                          uint64_t* scales_bytes, uint64_t* tail_bytes,
-                         uint64_t* positions_bytes, uint64_t* weights_bytes);
+                         uint64_t* positions_bytes, uint64_t* weights_bytes,
+                         uint64_t* counters_bytes);
 
 /* Append tokens to one layer.  past: device int32 [batch], tokens each
  * sequence holds (0..capacity).  k, v: [batch][n_kv_heads][n_new][head_dim]

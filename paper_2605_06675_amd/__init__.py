@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -58,7 +59,7 @@ class RqBlockCache(C.Structure):
                 ("head_dim", C.c_int32), ("capacity", C.c_int32),
                 ("codes", C.c_void_p), ("scales", C.c_void_p),
                 ("tail", C.c_void_p), ("positions", C.c_void_p),
-                ("weights", C.c_void_p)]
+                ("weights", C.c_void_p), ("counters", C.c_void_p)]
 
 
 class RqBlockRows(C.Structure):
@@ -120,13 +121,12 @@ def lib():
             "rq_decode_step": (i32, [pc, i32, i32, vp, vp, vp, vp, C.c_float,
                                      vp, u64, vp]),
         }
-        pb, pr, pq = (C.POINTER(t) for t in (RqBlockCache, RqBlockRows,
-                                             RqBlockQuery))
+        pb, pq = C.POINTER(RqBlockCache), C.POINTER(RqBlockQuery)
         sig.update({
-            "rq_block_sizes": (i32, [pb, pu64, pu64, pu64, pu64, pu64]),
-            "rq_block_append": (i32, [pb, i32, vp, i32, vp, pr, pr, vp]),
+            "rq_block_sizes": (i32, [pb] + [pu64] * 6),
+            "rq_block_append": (i32, [pb, i32, vp, i32, vp, vp, vp, vp]),
             "rq_block_attention_workspace": (i32, [pb, pq, pu64]),
-            "rq_block_attention": (i32, [pb, i32, pq, vp, u64, vp]),
+            "rq_block_attention": (i32, [pb, i32, vp, vp, u64, vp]),
             "rq_block_evict_workspace": (i32, [pb, i32, pu64]),
             "rq_block_evict": (i32, [pb, pb, i32, vp, i32, i32, i32, vp, vp,
                                      u64, vp]),
@@ -491,8 +491,8 @@ def make_block_cache(format, dtype, n_layers, batch, n_kv_heads, n_q_heads,
                      head_dim, capacity, codes=None, scales=None, tail=None,
                      positions=None, weights=None):
     """Fill an RqBlockCache descriptor.  The device tensors must have the
-    sizes rq_block_sizes reports; they are kept alive on the returned
-    object."""
+    sizes rq_block_sizes reports; they are kept alive on the returned object,
+    as are its counters, which are made here."""
     c = RqBlockCache(format, dtype, n_layers, batch, n_kv_heads, n_q_heads,
                      head_dim, capacity)
     buffers = (codes, scales, tail, positions, weights)
@@ -509,43 +509,61 @@ def make_block_cache(format, dtype, n_layers, batch, n_kv_heads, n_q_heads,
                 raise ValueError(f"{name} has {t.numel() * t.element_size()} "
                                  f"bytes, needs {size}")
             setattr(c, name, _tptr(t))
+        import torch
         c._device = given[0].device
+        c._lengths = torch.int32
+        # (the inputs' type, then the outputs')
+        c._types = (torch.bfloat16 if dtype == RQ_BF16 else torch.float16,
+                    torch.float32, torch.float16, torch.bfloat16)
+        counters = torch.zeros(sizes[5] // 4, dtype=torch.int32, device=c._device)
+        # calls may come on any stream
+        torch.cuda.current_stream(c._device).synchronize()
+        c.counters = counters.data_ptr()
+        buffers += (counters,)
     c._buffers = buffers
     return c
 
 
 def rq_block_sizes(cache):
-    """Bytes of (codes, scales, tail, positions, weights)."""
-    v = [C.c_uint64() for _ in range(5)]
+    """Bytes of (codes, scales, tail, positions, weights, counters)."""
+    v = [C.c_uint64() for _ in range(6)]
     _check(lib().rq_block_sizes(C.byref(cache), *(C.byref(x) for x in v)))
     return tuple(x.value for x in v)
 
 
-def _block_stream(cache, stream):
-    """The stream of a call: the given one, or the current one of the cache's
-    device."""
-    import torch
-    s = torch.cuda.current_stream(cache._device) if stream is None else stream
-    if s.device != cache._device:
-        raise ValueError(f"the stream is on {s.device}, the cache on {cache._device}")
-    return C.c_void_p(s.cuda_stream)
+# rq_block_rows and rq_block_query as packed bytes (a tenth of the time that
+# filling ctypes structures takes, where a call takes ten microseconds)
+_ROWS = struct.Struct("@Pqqq")
+_QUERY = struct.Struct("@iiPPPqqqPqqqiffiPi4x")
+assert _ROWS.size == C.sizeof(RqBlockRows)
+assert _QUERY.size == C.sizeof(RqBlockQuery)
 
 
-def _block_call(cache, f, *args):
-    """Launch with the cache's device current."""
+def _block_call(cache, stream, f, *args):
+    """Launch on the given stream, or the current one of the cache's device,
+    with that device current."""
     import torch
-    if torch.cuda.current_device() == cache._device.index:
-        _check(f(*args))
+    device = cache._device
+    if stream is None:
+        s = torch._C._cuda_getCurrentRawStream(device.index)
+    elif stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the cache on {device}")
     else:
-        with torch.cuda.device(cache._device):
-            _check(f(*args))
+        s = stream.cuda_stream
+    if torch.cuda.current_device() == device.index:
+        status = f(*args, s)
+    else:
+        with torch.cuda.device(device):
+            status = f(*args, s)
+    if status != RQ_OK:
+        _check(status)
 
 
 def _block_rows(cache, t, what, heads, n, dtypes):
-    """RqBlockRows of t [batch][heads][n][head_dim] (any strides, contiguous
-    rows)."""
+    """Pointer and strides of t [batch][heads][n][head_dim] (any strides,
+    contiguous rows)."""
     shape = (cache.batch, heads, n, cache.head_dim)
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {shape}")
     if t.device != cache._device:
         raise ValueError(f"{what} is on {t.device}, the cache on {cache._device}")
@@ -554,37 +572,37 @@ def _block_rows(cache, t, what, heads, n, dtypes):
     sb, sh, st, sd = t.stride()
     if sd != 1:
         raise ValueError(f"the rows of {what} must be contiguous")
-    return RqBlockRows(t.data_ptr(), sb, sh, st)
+    return t.data_ptr(), sb, sh, st
 
 
 def _block_lengths(cache, t, what):
-    import torch
+    """Pointer of an int32 [batch] tensor (0 for None)."""
     if t is None:
-        return None
-    if t.device != cache._device or t.dtype != torch.int32 \
-            or tuple(t.shape) != (cache.batch,) or not t.is_contiguous():
+        return 0
+    if t.dtype is not cache._lengths or t.device != cache._device \
+            or t.shape != (cache.batch,) or not t.is_contiguous():
         raise ValueError(f"{what} must be int32 [{cache.batch}] on the cache's device")
-    return C.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
-def _block_dtype(cache):
-    import torch
-    return torch.bfloat16 if cache.dtype == RQ_BF16 else torch.float16
+def _block_ws(cache, ws):
+    if ws.device != cache._device or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous tensor on the cache's device")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def rq_block_append(cache, layer, past, k, v, new_len=None, stream=None):
     """k, v: torch [batch][n_kv_heads][n_new][head_dim] in the cache's dtype
     (any strides, contiguous rows); past, new_len: device int32 [batch]."""
     n = k.shape[2] if k.dim() == 4 else -1
-    dt = (_block_dtype(cache),)
-    rk = _block_rows(cache, k, "k", cache.n_kv_heads, n, dt)
-    rv = _block_rows(cache, v, "v", cache.n_kv_heads, n, dt)
+    rk = _block_rows(cache, k, "k", cache.n_kv_heads, n, cache._types[:1])
+    rv = _block_rows(cache, v, "v", cache.n_kv_heads, n, cache._types[:1])
     if past is None:
         raise ValueError("past is missing")
-    _block_call(cache, lib().rq_block_append, C.byref(cache), layer,
+    _block_call(cache, stream, lib().rq_block_append, C.byref(cache), layer,
                 _block_lengths(cache, past, "past"), n,
-                _block_lengths(cache, new_len, "new_len"), C.byref(rk),
-                C.byref(rv), _block_stream(cache, stream))
+                _block_lengths(cache, new_len, "new_len"), _ROWS.pack(*rk),
+                _ROWS.pack(*rv))
 
 
 def rq_block_attention_workspace(cache, n_new, max_tokens=None,
@@ -608,31 +626,25 @@ def rq_block_attention(cache, layer, past, q, out, ws, new_len=None,
     float32 [n_q_heads]; ws: device byte tensor of at least
     rq_block_attention_workspace bytes; max_tokens: bound on the sequences'
     lengths (the capacity by default)."""
-    import torch
     n = q.shape[2] if q.dim() == 4 else -1
-    types = (torch.float32, torch.float16, torch.bfloat16)
     if past is None:
         raise ValueError("past is missing")
     if slopes is not None and (slopes.device != cache._device
-                               or slopes.dtype != torch.float32
-                               or tuple(slopes.shape) != (cache.n_q_heads,)
+                               or slopes.dtype != cache._types[1]
+                               or slopes.shape != (cache.n_q_heads,)
                                or not slopes.is_contiguous()):
         raise ValueError(f"slopes must be float32 [{cache.n_q_heads}] on the cache's device")
-    if ws.device != cache._device or not ws.is_contiguous():
-        raise ValueError("ws must be a contiguous tensor on the cache's device")
-    a = RqBlockQuery(
+    rq_ = _block_rows(cache, q, "q", cache.n_q_heads, n, cache._types[:1])
+    ro = _block_rows(cache, out, "out", cache.n_q_heads, n, cache._types[1:])
+    a = _QUERY.pack(
         n, cache.capacity if max_tokens is None else max_tokens,
         _block_lengths(cache, past, "past"),
-        _block_lengths(cache, new_len, "new_len"),
-        _block_rows(cache, q, "q", cache.n_q_heads, n, (_block_dtype(cache),)),
-        _block_rows(cache, out, "out", cache.n_q_heads, n, types),
-        (RQ_F32, RQ_F16, RQ_BF16)[types.index(out.dtype)],
-        cache.head_dim ** -0.5 if scale is None else float(scale), float(cap),
-        int(window), None if slopes is None else C.c_void_p(slopes.data_ptr()),
-        int(bool(accumulate)))
-    _block_call(cache, lib().rq_block_attention, C.byref(cache), layer,
-                C.byref(a), C.c_void_p(ws.data_ptr()),
-                ws.numel() * ws.element_size(), _block_stream(cache, stream))
+        _block_lengths(cache, new_len, "new_len"), *rq_, *ro,
+        (RQ_F32, RQ_F16, RQ_BF16)[cache._types.index(out.dtype, 1) - 1],
+        cache.head_dim ** -0.5 if scale is None else scale, cap, window,
+        0 if slopes is None else slopes.data_ptr(), 1 if accumulate else 0)
+    _block_call(cache, stream, lib().rq_block_attention, C.byref(cache), layer,
+                a, *_block_ws(cache, ws))
 
 
 def rq_block_evict_workspace(cache, keep):
@@ -650,13 +662,10 @@ def rq_block_evict(src, dst, layer, lengths, keep, new_lengths, ws, n_sink=4,
         raise ValueError("lengths and new_lengths are needed")
     if dst._device != src._device:
         raise ValueError("the caches are on different devices")
-    if ws.device != src._device or not ws.is_contiguous():
-        raise ValueError("ws must be a contiguous tensor on the cache's device")
-    _block_call(src, lib().rq_block_evict, C.byref(src), C.byref(dst), layer,
-                _block_lengths(src, lengths, "lengths"), keep, n_sink,
+    _block_call(src, stream, lib().rq_block_evict, C.byref(src), C.byref(dst),
+                layer, _block_lengths(src, lengths, "lengths"), keep, n_sink,
                 n_recent, _block_lengths(src, new_lengths, "new_lengths"),
-                C.c_void_p(ws.data_ptr()), ws.numel() * ws.element_size(),
-                _block_stream(src, stream))
+                *_block_ws(src, ws))
 
 
 class BlockCache:

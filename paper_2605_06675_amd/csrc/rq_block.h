@@ -15,6 +15,8 @@
 namespace rq {
 
 constexpr int kBlockTokens = 32;
+// Splits of an attention tile that its last workgroup may add.
+constexpr int kTicketSplits = 32;
 // Eviction: units of at most this many slots are selected by one workgroup
 // (16 keys a thread); longer ones in parts of a multiple of kSelectPart, at
 // most kSelectParts of them.
@@ -27,6 +29,7 @@ struct BlockLayer {
   uint16_t* tail;       // [B][H][2][32][D]
   int32_t* positions;   // [B][H][cap]
   float* weights;       // [B][H][cap] or NULL
+  uint32_t* counters;   // [B][H][2] or NULL
   int B, H, cap;
   int D, fmt, is_bf16;  // select the kernels
 };
@@ -59,6 +62,7 @@ struct BlockAttendLaunch {
   int window;
   const float* slopes;     // [H * G] or NULL
   int accumulate;
+  int tickets;             // the last of a row tile's splits adds them all
   float* part;             // [unit][row tile][split][16][D]
   float* part_ml;          // [unit][row tile][split][16][2]: maximum (log2) and sum
   float* stats;            // [unit][row][2]: maximum and 1 / sum, where accumulate

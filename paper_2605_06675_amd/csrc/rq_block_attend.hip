@@ -174,6 +174,96 @@ __device__ __forceinline__ void add_tail(const RQ_GLOBAL uint16_t* vt, int n_tai
   }
 }
 
+// Partial results of one row tile: [split][16][D] sums and [split][16][2]
+// maxima (log2) and sums of probabilities.  Stored and loaded with the sc1 bit
+// (agent scope): coherent across the XCDs' L2 caches without a flush.
+struct Parts {
+  __amdgpu_buffer_rsrc_t o, ml;
+  __device__ __forceinline__ Parts(const BlockAttendLaunch& a, size_t tile) {
+    const int D = a.c.D;
+    o = __builtin_amdgcn_make_buffer_rsrc(a.part + tile * a.splits * 16 * D, 0,
+                                          a.splits * 16 * D * (int)sizeof(float), 0x00027000);
+    ml = __builtin_amdgcn_make_buffer_rsrc(a.part_ml + tile * a.splits * 32, 0,
+                                           a.splits * 32 * (int)sizeof(float), 0x00027000);
+  }
+  template <int D>
+  __device__ __forceinline__ void store_o(int split, int row, int ch, f4 x) const {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, x), o, ((split * 16 + row) * D + ch) * 4, 0, 16);
+  }
+  __device__ __forceinline__ void store_ml(int split, int row, f2 x) const {
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, x), ml, (split * 16 + row) * 8, 0, 16);
+  }
+  template <int D>
+  __device__ __forceinline__ f4 load_o(int split, int row, int ch) const {
+    return __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(o, ((split * 16 + row) * D + ch) * 4, 0, 16));
+  }
+  __device__ __forceinline__ f2 load_ml(int split, int row) const {
+    return __builtin_bit_cast(f2, __builtin_amdgcn_raw_buffer_load_b64(ml, (split * 16 + row) * 8, 0, 16));
+  }
+};
+
+// A tile's splits (at most kTicketSplits) added and written by one workgroup.  D / 4 lanes
+// form a group, four channels a lane; a row has `share` groups (a power of two),
+// each with every share-th split, so that all loads go out at once.
+template <int D>
+__device__ __forceinline__ void merge_tile(const BlockAttendLaunch& a, const Parts& parts, int b, int h,
+                                           int rt, int rows, f4* lds) {
+  constexpr int kCols = D / 4, kGroups = 256 / kCols, kEach = kTicketSplits / kCols;
+  const int group = threadIdx.x / kCols, col = threadIdx.x % kCols;
+  int share = kGroups;
+  while (share > 1 && share * rows > kGroups) share >>= 1;
+  for (int row0 = 0; row0 < rows; row0 += kGroups / share) {
+    const int row = row0 + group / share, first = group % share;
+    const bool on = row < rows;
+    // this lane has the maxima and sums of splits col, col + kCols, ..
+    f2 ml[kEach];
+    float m = -1.0e30f, l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      ml[i] = (f2){-1.0e30f, 0.0f};
+      if (on && col + i * kCols < a.splits) ml[i] = parts.load_ml(col + i * kCols, row);
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) m = __builtin_fmaxf(m, ml[i].x);
+    for (int d = kCols / 2; d >= 1; d >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d, 64));
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      ml[i].x = exp2_f(ml[i].x - m);
+      l = __builtin_fmaf(ml[i].y, ml[i].x, l);
+    }
+    for (int d = kCols / 2; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+    f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    // eight loads at a time; those behind the last split return zeros
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int n = a.splits - i * kCols < kCols ? a.splits - i * kCols : kCols;
+      for (int s0 = first; s0 < n; s0 += 8 * share) {
+        f4 o[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = parts.load_o<D>(s0 + j * share + i * kCols, row, col * 4);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int s = s0 + j * share;            // (from kCols on: not of this i)
+          const float w = __shfl(ml[i].x, s & (kCols - 1), kCols);
+          x += o[j] * (s < kCols ? w : 0.0f);
+        }
+      }
+    }
+    if (share > 1) {
+      lds[threadIdx.x] = x;
+      __syncthreads();
+      if (first == 0)
+        for (int i = 1; i < share; ++i) x += lds[threadIdx.x + i * kCols];
+      __syncthreads();
+    }
+    if (on && first == 0) {
+      x *= l > 0.0f ? 1.0f / l : 0.0f;
+      const int grow = rt * 16 + row, token = grow / a.G;
+      store_out<4>(a, b, h * a.G + grow - token * a.G, token, col * 4, (const float*)&x);
+    }
+  }
+}
+
 template <int FMT, int D, bool BF16>
 __global__ void __launch_bounds__(256, 3) block_attend_kernel(BlockAttendLaunch a) {
   constexpr int kStride = D + 4;           // floats of a row in LDS
@@ -294,14 +384,28 @@ __global__ void __launch_bounds__(256, 3) block_attend_kernel(BlockAttendLaunch 
       x[e] = __builtin_fmaf(sh_o[w][row * kStride + ch + e], by, x[e]);
   }
   if (a.splits > 1) {
-    const size_t at = ((size_t)unit * a.row_tiles + rt) * a.splits + split;
-    RQ_GLOBAL float* o = gptr(a.part) + at * 16 * D + row * D + ch;
+    const size_t tile = (size_t)unit * a.row_tiles + rt;
+    const Parts parts(a, tile);
+    const int seen = nnew * a.G - rt * 16;           // rows with a query
+    if (row < seen) {
 #pragma unroll
-    for (int e = 0; e < D / 16; e += 4) *(RQ_GLOBAL f4*)(o + e) = (f4){x[e], x[e + 1], x[e + 2], x[e + 3]};
-    if (ch == 0) {
-      gptr(a.part_ml)[(at * 16 + row) * 2] = m;
-      gptr(a.part_ml)[(at * 16 + row) * 2 + 1] = l;
+      for (int e = 0; e < D / 16; e += 4)
+        parts.store_o<D>(split, row, ch + e, (f4){x[e], x[e + 1], x[e + 2], x[e + 3]});
+      if (ch == 0) parts.store_ml(split, row, (f2){m, l});
     }
+    // the tile's last workgroup adds its parts
+    if (!a.tickets) return;
+    __shared__ uint32_t ticket;
+    RQ_GLOBAL uint32_t* counter = gptr(a.c.counters) + (size_t)unit * 2 + rt;
+    __builtin_amdgcn_s_waitcnt(0);                   // this wave's parts are out
+    __syncthreads();
+    if (threadIdx.x == 0)
+      ticket = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (ticket != (uint32_t)a.splits - 1) return;
+    if (threadIdx.x == 0)
+      __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    merge_tile<D>(a, parts, b, h, rt, seen < 16 ? seen : 16, reinterpret_cast<f4*>(sh_o));
     return;
   }
   const int grow = rt * 16 + row, token = grow / a.G;
@@ -472,7 +576,7 @@ hipError_t launch(const BlockAttendLaunch& a, hipStream_t s) {
                        dim3(256), 0, s, a);
     return hipGetLastError();
   }
-  return launch_block_merge(a, s);
+  return a.tickets ? hipSuccess : launch_block_merge(a, s);
 }
 
 }  // namespace

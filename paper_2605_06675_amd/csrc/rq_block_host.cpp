@@ -63,7 +63,7 @@ rq_status check_buffers(const rq_block_cache* c, int32_t layer) {
   if (!c->codes || !c->scales || !c->tail || !c->positions)
     return fail(RQ_EINVAL, "the cache has a NULL buffer");
   if (unaligned(c->codes) || unaligned(c->scales) || unaligned(c->tail) ||
-      unaligned(c->positions) || unaligned(c->weights))
+      unaligned(c->positions) || unaligned(c->weights) || unaligned(c->counters))
     return fail(RQ_EINVAL, "a cache buffer is not 16-byte aligned");
   return RQ_OK;
 }
@@ -78,6 +78,7 @@ rq::BlockLayer layer_of(const rq_block_cache* c, int32_t layer) {
   l.tail = static_cast<uint16_t*>(c->tail) + u * 2 * rq::kBlockTokens * D;
   l.positions = c->positions + u * cap;
   l.weights = c->weights ? c->weights + u * cap : nullptr;
+  l.counters = c->counters ? c->counters + u * 2 : nullptr;
   l.B = c->batch;
   l.H = c->n_kv_heads;
   l.cap = c->capacity;
@@ -191,7 +192,7 @@ extern "C" {
 
 rq_status rq_block_sizes(const rq_block_cache* c, uint64_t* codes_bytes, uint64_t* scales_bytes,
                          uint64_t* tail_bytes, uint64_t* positions_bytes,
-                         uint64_t* weights_bytes) {
+                         uint64_t* weights_bytes, uint64_t* counters_bytes) {
   rq_status st = check_shape(c);
   if (st != RQ_OK) return st;
   const uint64_t u = units(c) * c->n_layers, cap = c->capacity, D = c->head_dim;
@@ -200,6 +201,7 @@ rq_status rq_block_sizes(const rq_block_cache* c, uint64_t* codes_bytes, uint64_
   if (tail_bytes) *tail_bytes = u * 2 * rq::kBlockTokens * D * sizeof(uint16_t);
   if (positions_bytes) *positions_bytes = u * cap * sizeof(int32_t);
   if (weights_bytes) *weights_bytes = u * cap * sizeof(float);
+  if (counters_bytes) *counters_bytes = u * 2 * sizeof(uint32_t);
   return ok();
 }
 
@@ -287,6 +289,13 @@ rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_bl
   a.factors = reinterpret_cast<float*>(take(p.factors));
   a.sums = reinterpret_cast<float*>(take(p.sums));
   a.row_parts = p.row_parts;
+  // The last workgroup of a tile adds its splits where they are few: a launch
+  // less, but one workgroup's loads.  us with / without, one sequence of 8
+  // kv-heads: 4 heads 1000 tokens (8 splits) 10.5 / 13, 4000 (32) 11.1 / 13.1,
+  // 8000 (63) 15.9 / 13.1; 8 heads 2000 (16) 10.1 / 12.7, 4000 (32) 12.0 / 13.0;
+  // 32 units of 8 heads 32768 (24) 49.8 / 48.5, of 4 heads 4000 (24) 14.7 / 15.1.
+  a.tickets = !p.prompt && p.splits > 1 && p.splits <= rq::kTicketSplits &&
+              p.splits * std::min(a.n * a.G, 16) <= 160 && a.c.counters && !a.accumulate;
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = p.prompt ? rq::launch_block_prompt(a, s) : rq::launch_block_attend(a, s);
   if (e == hipSuccess && p.prompt) e = rq::launch_block_merge(a, s);

@@ -16,7 +16,7 @@ def desc(**kw):
     a = dict(format=rq.RQ_INT8, dtype=rq.RQ_BF16, n_layers=2, batch=3,
              n_kv_heads=4, n_q_heads=8, head_dim=128, capacity=96)
     ptrs = {n: P * (i + 1) for i, n in enumerate(
-        ("codes", "scales", "tail", "positions", "weights"))}
+        ("codes", "scales", "tail", "positions", "weights", "counters"))}
     for n in list(kw):
         if n in ptrs:
             ptrs[n] = kw.pop(n)
@@ -43,7 +43,7 @@ def query(**kw):
 def test_sizes(D):
     u = 2 * 3 * 4
     assert rq.rq_block_sizes(desc(head_dim=D)) == (
-        u * 2 * 96 * D, u * 2 * 3 * 4, u * 2 * 32 * D * 2, u * 96 * 4, u * 96 * 4)
+        u * 2 * 96 * D, u * 2 * 3 * 4, u * 2 * 32 * D * 2, u * 96 * 4, u * 96 * 4, u * 2 * 4)
 
 
 BAD_SHAPES = [
@@ -71,7 +71,8 @@ def test_shape_refusals(kw, status):
 
 @pytest.mark.parametrize("kw", [dict(codes=None), dict(scales=None), dict(tail=None),
                                 dict(positions=None), dict(codes=P + 8), dict(scales=P + 4),
-                                dict(tail=P + 2), dict(positions=P + 4), dict(weights=P + 4)])
+                                dict(tail=P + 2), dict(positions=P + 4), dict(weights=P + 4),
+                                dict(counters=P + 4)])
 def test_buffer_refusals(kw):
     c, L = desc(**kw), rq.lib()
     assert L.rq_block_append(C.byref(c), 0, P, 1, None, C.byref(rows()), C.byref(rows()),

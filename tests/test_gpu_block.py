@@ -381,6 +381,33 @@ def test_lengths_out_of_range_are_taken_as_the_nearest():
     torch.testing.assert_close(call([94, 50], [9, -1]), call([94, 50], [2, 0]), rtol=0, atol=0)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,H,G,L", [(1, 1, 1, 500), (1, 1, 1, 4000), (1, 1, 2, 9000), (1, 2, 3, 2000),
+                                     (2, 4, 8, 1500), (1, 8, 4, 4000), (1, 4, 16, 1100), (3, 5, 4, 3001)])
+def test_attend_split_sequences(D, B, H, G, L):
+    """Splits merged by the last workgroup and by a launch of their own."""
+    r = Rig("int8", "bf16", B=B, H=H, G=G, D=D, cap=(L + 63) // 32 * 32)
+    k, v = r.kv(L)
+    r.c.append(0, k.cuda(), v.cuda())
+    for b in range(B):
+        for h in range(H):
+            u, full = r.u[b][h], L // 32 * 32
+            for s, x in ((0, k), (1, v)):
+                part = [block.quantize(block.INT8, x[b, h, i:i + 32].float().numpy()) for i in range(0, full, 32)]
+                u.codes[s] = np.concatenate([c for c, _ in part])
+                u.scales[s] = np.array([y for _, y in part], np.float32)
+                u.tail[s] = x[b, h, full:].float().numpy()
+            u.pos, u.weight = np.arange(L), np.zeros(L)
+    r.attend(1)
+    q = r.randn(B, H * G, 1, D).to(r.dt)
+    first = r.attend(1, q=q)
+    r.c.desc.counters, counters = None, r.c.desc.counters
+    other = r.attend(1, q=q)
+    r.c.desc.counters = counters
+    torch.testing.assert_close(first, other, rtol=1e-5, atol=1e-6)
+    assert (r.c.desc._buffers[-1] == 0).all()
+
+
 def test_attend_repeats_bit_for_bit():
     r = Rig("int8", "bf16", B=1, cap=4096)
     r.append(4001)
