@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(256) block_append_kernel(BlockAppendLaunch a) 
     for (int i = 0; i < kLoads; ++i) {
       const int row = row0 + kRows * i, slot = blk * kBlockTokens + row;
       x[i] = slot < past ? *(const RQ_GLOBAL u4*)(tail + row * D + ch)
-                         : *(const RQ_GLOBAL u4_any*)(in + (int64_t)(slot - past) * src.st + ch);
+                         : __builtin_nontemporal_load((const RQ_GLOBAL u4_any*)(in + (int64_t)(slot - past) * src.st + ch));
     }
     float most = 0.0f;
 #pragma unroll
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(256) block_append_kernel(BlockAppendLaunch a) 
       for (int p = 0; p < 2; ++p)
         w[p] = block_codes<FMT>(widen_t<BF16>(x[i][2 * p] & 0xffffu), widen_t<BF16>(x[i][2 * p] >> 16),
                                 widen_t<BF16>(x[i][2 * p + 1] & 0xffffu), widen_t<BF16>(x[i][2 * p + 1] >> 16), inv);
-      *(RQ_GLOBAL u2*)(out + (row0 + kRows * i) * D + ch) = w;
+      __builtin_nontemporal_store(w, (RQ_GLOBAL u2*)(out + (row0 + kRows * i) * D + ch));
     }
     if (lane == 0) gptr(a.c.scales)[(size_t)(unit * 2 + kind) * (a.c.cap / kBlockTokens) + blk] = scale;
   }

@@ -265,7 +265,7 @@ __device__ __forceinline__ void merge_tile(const BlockAttendLaunch& a, const Par
 }
 
 template <int FMT, int D, bool BF16>
-__global__ void __launch_bounds__(256, 3) block_attend_kernel(BlockAttendLaunch a) {
+__global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch a) {
   constexpr int kStride = D + 4;           // floats of a row in LDS
   __shared__ float sh_o[4][16 * kStride];
   __shared__ float sh_ml[4][16][2];

@@ -110,8 +110,14 @@ struct Plan {
   uint64_t bytes() const { return part + part_ml + stats + scores + queries + factors + sums; }
 };
 
-// Few rows: one resident round, three workgroups a CU over the units' row tiles,
-// at least four blocks (one a wave) a workgroup.
+// Few rows: one workgroup a CU over the units' row tiles, at least four blocks
+// (one a wave) each.  Four waves with a block in flight each keep a CU's share
+// of the memory busy; more workgroups are set-ups and parts to merge, but even
+// out sequences of unlike lengths where the scores are kept too.  us with one /
+// two / three a CU: 128 full units of 8192 tokens 44.7 / 47 / 47, 32 of 32768 (8
+// heads, capped) 43.7 / 48.5 / 50, 8 of 131072 46.8 / 48 / 49.4, 64 of 4000 15.6 /
+// 17 / 18, 192 of 4000 31.3 / 39 / 36.5; uneven lengths: 128 units to 8192 35 /
+// 33.8 / 34, with weights 42.5 / 37.8 / 39.
 // More than two tiles of 16 rows: tiles of 128 rows, two workgroups a CU, at
 // least eight blocks each.  Where the new tokens are few beside the cached ones,
 // sequences may differ in length and a round's workgroups with them: one split
@@ -133,7 +139,7 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
     s = std::min(s, (blocks + 7) / 8);
     if (s <= 1 && a->max_tokens >= 4 * (int64_t)a->n_new && blocks >= 128) s = 2;
   } else {
-    s = 3 * (int64_t)rq::device_cus() / (u * p.row_tiles);
+    s = (a->accumulate && c->batch > 1 ? 2 : 1) * (int64_t)rq::device_cus() / (u * p.row_tiles);
     s = std::min(s, (blocks + 3) / 4);
   }
   p.splits = (int)std::max<int64_t>(s, 1);
@@ -290,12 +296,11 @@ rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_bl
   a.sums = reinterpret_cast<float*>(take(p.sums));
   a.row_parts = p.row_parts;
   // The last workgroup of a tile adds its splits where they are few: a launch
-  // less, but one workgroup's loads.  us with / without, one sequence of 8
-  // kv-heads: 4 heads 1000 tokens (8 splits) 10.5 / 13, 4000 (32) 11.1 / 13.1,
-  // 8000 (63) 15.9 / 13.1; 8 heads 2000 (16) 10.1 / 12.7, 4000 (32) 12.0 / 13.0;
-  // 32 units of 8 heads 32768 (24) 49.8 / 48.5, of 4 heads 4000 (24) 14.7 / 15.1.
+  // less, but one workgroup's loads.  us with / without, splits x rows: 8 x 4
+  // 8.5 / 9.4, 8 x 8 44.2 / 45.4 (32 units of 32768 tokens), 2 x 4 15.4 / 16.5,
+  // 32 x 4 10.8 / 9.3, 16 x 16 18.7 / 18.1, 32 x 8 15.0 / 12.5.
   a.tickets = !p.prompt && p.splits > 1 && p.splits <= rq::kTicketSplits &&
-              p.splits * std::min(a.n * a.G, 16) <= 160 && a.c.counters && !a.accumulate;
+              p.splits * std::min(a.n * a.G, 16) <= 100 && a.c.counters && !a.accumulate;
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = p.prompt ? rq::launch_block_prompt(a, s) : rq::launch_block_attend(a, s);
   if (e == hipSuccess && p.prompt) e = rq::launch_block_merge(a, s);
