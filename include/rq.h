@@ -379,9 +379,9 @@ rq_status rq_fallback_beta(int32_t n, double* beta, const double* r2,
  * stay in 16 bits until the block is full: with L tokens cached, the first
  * floor(L / 32) * 32 are coded, the rest lie in the tail.
  *
- * Buffers (the caller allocates the sizes reported by rq_block_sizes, each
- * aligned to 16 bytes; but for the counters, contents of a new cache do not
- * matter):
+ * Buffers (the caller allocates the sizes reported by rq_block_sizes, aligned
+ * to 16 bytes, the counters to 4; but for these, contents of a new cache do
+ * not matter):
  *  codes      8-bit [n_layers][batch][n_kv_heads][2][capacity][head_dim]
  *  scales     fp32  [n_layers][batch][n_kv_heads][2][capacity / 32]
  *  tail       16-bit, in dtype [n_layers][batch][n_kv_heads][2][32][head_dim]
@@ -390,7 +390,7 @@ rq_status rq_fallback_beta(int32_t n, double* beta, const double* r2,
  *             position in its sequence, ascending
  *  weights    fp32  [n_layers][batch][n_kv_heads][capacity]: accumulated
  *             attention weight of each slot; NULL if none is kept
- *  counters   uint32 [n_layers][batch][n_kv_heads][2]: zeroed by the caller
+ *  counters   uint32 [n_layers][batch][n_kv_heads]: zeroed by the caller
  *             before the first call, and zero again after every one; NULL:
  *             attention that splits a sequence takes a launch more.  Calls
  *             that attend to one layer must not overlap where it is given.

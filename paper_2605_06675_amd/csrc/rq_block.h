@@ -18,9 +18,9 @@ constexpr int kBlockTokens = 32;
 // Splits of an attention tile that its last workgroup may add.
 constexpr int kTicketSplits = 32;
 // Eviction: units of at most this many slots are selected by one workgroup
-// (16 keys a thread); longer ones in parts of a multiple of kSelectPart, at
+// (up to 32 keys a thread); longer ones in parts of a multiple of kSelectPart, at
 // most kSelectParts of them.
-constexpr int kSelectShort = 16384, kSelectPart = 8192, kSelectParts = 32;
+constexpr int kSelectShort = 32768, kSelectPart = 8192, kSelectParts = 32;
 
 // One layer of a cache, and its shape.
 struct BlockLayer {
@@ -29,7 +29,7 @@ struct BlockLayer {
   uint16_t* tail;       // [B][H][2][32][D]
   int32_t* positions;   // [B][H][cap]
   float* weights;       // [B][H][cap] or NULL
-  uint32_t* counters;   // [B][H][2] or NULL
+  uint32_t* counters;   // [B][H] or NULL
   int B, H, cap;
   int D, fmt, is_bf16;  // select the kernels
 };
@@ -67,7 +67,7 @@ struct BlockAttendLaunch {
   float* part_ml;          // [unit][row tile][split][16][2]: maximum (log2) and sum
   float* stats;            // [unit][row][2]: maximum and 1 / sum, where accumulate
   float* scores;           // [unit][block][row][32]: log2 scores, where accumulate
-                           // and all rows fit one tile; else NULL
+                           // and there are at most 32 rows; else NULL
   uint16_t* queries;       // else: [unit][row][D] queries as fp16 operands,
   float* factors;          // [unit][row] and the factor of their scores;
   int row_parts;           // workgroups that share a token's rows,
@@ -366,19 +366,23 @@ __device__ __forceinline__ void load_keys(const RQ_GLOBAL uint8_t* k, const RQ_G
   t->scale = scale[blk];
 }
 
-// Products of a block's keys with a query tile: lane (r, g) gets, for query
-// row r, tokens 16 m + 4 g + i in s[m][i].
-template <int FMT, int D>
-__device__ __forceinline__ void key_products(const KeyBlock<D>& t, const QueryTile<D>& q, f4 s[2]) {
+// Products of a block's keys with QT query tiles: lane (r, g) gets, for query
+// row r of tile n, tokens 16 m + 4 g + i in s[n][m][i].
+template <int FMT, int D, int QT>
+__device__ __forceinline__ void key_products(const KeyBlock<D>& t, const QueryTile<D> q[QT],
+                                             f4 s[QT][2]) {
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
-    s[m] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int n = 0; n < QT; ++n) s[n][m] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < D / 32; ++k) {
       const uint32_t x = t.w[m][k >> 1][2 * (k & 1)], y = t.w[m][k >> 1][2 * (k & 1) + 1];
       const u4 op = {key_pair<FMT>(x, false), key_pair<FMT>(x, true), key_pair<FMT>(y, false),
                      key_pair<FMT>(y, true)};
-      s[m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(op), q.f[k], s[m], 0, 0, 0);
+#pragma unroll
+      for (int n = 0; n < QT; ++n)
+        s[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(op), q[n].f[k], s[n][m], 0, 0, 0);
     }
   }
 }

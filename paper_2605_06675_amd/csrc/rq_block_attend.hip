@@ -1,5 +1,5 @@
-// Attention over the block-scaled 8-bit cache, for few query rows a unit: the
-// cache is streamed once per tile of 16 rows.
+// Attention over the block-scaled 8-bit cache, for up to 32 query rows a unit:
+// the cache is streamed once, for one or two tiles of 16 rows.
 //
 //   out = softmax(f(scale q . k^)) v^,  f(x) = cap tanh(x / cap) - slope distance
 //
@@ -84,29 +84,37 @@ __device__ __forceinline__ void probabilities(Running<D>* st, f4 s[2]) {
   st->l += sum;
 }
 
-template <int FMT, int D>
-__device__ __forceinline__ void add_values(const ValueBlock<D>& v, const f4 s[2], Running<D>* st) {
-  if (v.scale * st->unit > 128.0f || st->unit == 0.0f) {      // (the same in every lane)
+// Adds a block's values to the states of QT query tiles (whose units are the
+// same).
+template <int FMT, int D, int QT>
+__device__ __forceinline__ void add_values(const ValueBlock<D>& v, const f4 s[QT][2],
+                                           Running<D> st[QT]) {
+  if (v.scale * st[0].unit > 128.0f || st[0].unit == 0.0f) {  // (the same in every lane)
     // (a scale of zero has no exponent; 0 serves)
     int e = v.scale > 0.0f ? __builtin_amdgcn_frexp_expf(v.scale) : 0;
     e = e < -100 ? -100 : e;
     const float unit = __builtin_amdgcn_ldexpf(128.0f, -e);
-    rescale<D>(st, st->unit == 0.0f ? 1.0f : unit / st->unit);
-    st->unit = unit;
-  }
-  const float by = v.scale * st->unit;
-  u4 hi, lo;
 #pragma unroll
-  for (int m = 0; m < 2; ++m)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float a = s[m][2 * i] * by, b = s[m][2 * i + 1] * by;
-      // (toward zero by its own instruction: a conversion left to the compiler
-      // may be fused with the product above, where hi would not be that of a)
-      const h2 h = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(a, b));
-      hi[2 * m + i] = as_u32(h);
-      lo[2 * m + i] = as_u32((h2){(_Float16)(a - (float)h.x), (_Float16)(b - (float)h.y)});
+    for (int n = 0; n < QT; ++n) {
+      rescale<D>(&st[n], st[n].unit == 0.0f ? 1.0f : unit / st[n].unit);
+      st[n].unit = unit;
     }
+  }
+  const float by = v.scale * st[0].unit;
+  u4 hi[QT], lo[QT];
+#pragma unroll
+  for (int n = 0; n < QT; ++n)
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float a = s[n][m][2 * i] * by, b = s[n][m][2 * i + 1] * by;
+        // (toward zero by its own instruction: a conversion left to the compiler
+        // may be fused with the product above, where hi would not be that of a)
+        const h2 h = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(a, b));
+        hi[n][2 * m + i] = as_u32(h);
+        lo[n][2 * m + i] = as_u32((h2){(_Float16)(a - (float)h.x), (_Float16)(b - (float)h.y)});
+      }
 #pragma unroll
   for (int c = 0; c < D / 64; ++c) {
     uint32_t op[4][4];        // [token pair][channel]
@@ -115,9 +123,12 @@ __device__ __forceinline__ void add_values(const ValueBlock<D>& v, const f4 s[2]
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const h8 f = as_h8((u4){op[0][e], op[1][e], op[2][e], op[3][e]});
-      f4 o = st->o[4 * c + e];
-      o = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, as_h8(hi), o, 0, 0, 0);
-      st->o[4 * c + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, as_h8(lo), o, 0, 0, 0);
+#pragma unroll
+      for (int n = 0; n < QT; ++n) {
+        f4 o = st[n].o[4 * c + e];
+        o = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, as_h8(hi[n]), o, 0, 0, 0);
+        st[n].o[4 * c + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, as_h8(lo[n]), o, 0, 0, 0);
+      }
     }
   }
 }
@@ -264,63 +275,67 @@ __device__ __forceinline__ void merge_tile(const BlockAttendLaunch& a, const Par
   }
 }
 
-template <int FMT, int D, bool BF16>
+// QT tiles of 16 rows hold all rows of a unit.
+template <int FMT, int D, bool BF16, int QT>
 __global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch a) {
   constexpr int kStride = D + 4;           // floats of a row in LDS
   __shared__ float sh_o[4][16 * kStride];
   __shared__ float sh_ml[4][16][2];
+  __shared__ uint32_t ticket;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const int split = blockIdx.x % a.splits, rt = blockIdx.x / a.splits, unit = blockIdx.y;
+  const int split = blockIdx.x, unit = blockIdx.y;
   const int b = unit / a.c.H, h = unit - b * a.c.H;
   int past, nnew;
   block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
-  const int first = rt * 16 / a.G;         // the tile's rows belong to tokens first..last
-  if (first >= nnew) return;
-  int last = (rt * 16 + 15) / a.G;
-  last = last < nnew ? last : nnew - 1;
+  if (nnew == 0) return;
   const int total = past + nnew, full = total / kBlockTokens;
   int lo_all, hi_all;                      // block `full` is the tail
-  seen_blocks(past, first, last, a.window, &lo_all, &hi_all);
+  seen_blocks(past, 0, nnew - 1, a.window, &lo_all, &hi_all);
   const int64_t nb = hi_all - lo_all;
   const int lo = lo_all + (int)(nb * split / a.splits);
   const int hi = lo_all + (int)(nb * (split + 1) / a.splits);
 
-  QueryTile<D> q;
-  load_queries<D, BF16>(a, b, h, rt * 16 + r, past, nnew, &q);
-  Running<D> st;
+  QueryTile<D> q[QT];
+  Running<D> st[QT];
 #pragma unroll
-  for (int e = 0; e < D / 16; ++e) st.o[e] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
-  st.m = -1.0e30f;
-  st.l = 0.0f;
-  st.unit = 0.0f;
+  for (int n = 0; n < QT; ++n) {
+    load_queries<D, BF16>(a, b, h, 16 * n + r, past, nnew, &q[n]);
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) st[n].o[e] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+    st[n].m = -1.0e30f;
+    st[n].l = 0.0f;
+    st[n].unit = 0.0f;
+  }
 
   const RQ_GLOBAL uint8_t* kc = gptr(a.c.codes) + (size_t)unit * 2 * a.c.cap * D;
   const RQ_GLOBAL uint8_t* vc = kc + (size_t)a.c.cap * D;
   const RQ_GLOBAL float* ks = gptr(a.c.scales) + (size_t)unit * 2 * (a.c.cap / kBlockTokens);
   const RQ_GLOBAL float* vs = ks + a.c.cap / kBlockTokens;
   const RQ_GLOBAL int32_t* pos = gptr(a.c.positions) + (size_t)unit * a.c.cap;
-  // blocks below all_seen lie wholly before every row of the tile
-  const int all_seen = a.window ? 0 : (past + first + 1) / kBlockTokens;
-
+  // blocks below all_seen lie wholly before every row
+  const int all_seen = a.window ? 0 : (past + 1) / kBlockTokens;
   // scores kept for the weights: this lane's row, 4 tokens of each half block
   const int rows = a.n * a.G;
   RQ_GLOBAL float* kept = gptr(a.scores) + ((size_t)unit * ((a.max_tokens + kBlockTokens - 1) / kBlockTokens) * rows + r) * kBlockTokens + 4 * g;
-  auto keep = [&](const f4 s[2], int blk) {
-    if (a.scores && r < rows)
+  auto keep = [&](const f4 s[2], int n, int blk) {
+    if (a.scores && 16 * n + r < rows)
 #pragma unroll
       for (int m = 0; m < 2; ++m)
-        *(RQ_GLOBAL f4*)(kept + (size_t)blk * rows * kBlockTokens + 16 * m) = s[m];
+        *(RQ_GLOBAL f4*)(kept + ((size_t)blk * rows + 16 * n) * kBlockTokens + 16 * m) = s[m];
   };
 
   const int end = hi < full ? hi : full;
   auto step = [&](const KeyBlock<D>& k, const ValueBlock<D>& v, int blk) {
-    f4 s[2];
-    key_products<FMT, D>(k, q, s);
-    block_scores<D>(a, q, pos, k.scale * q.qs, blk * kBlockTokens, past, blk >= all_seen, s);
-    keep(s, blk);
-    probabilities<D>(&st, s);
-    add_values<FMT, D>(v, s, &st);
+    f4 s[QT][2];
+    key_products<FMT, D, QT>(k, q, s);
+#pragma unroll
+    for (int n = 0; n < QT; ++n) {
+      block_scores<D>(a, q[n], pos, k.scale * q[n].qs, blk * kBlockTokens, past, blk >= all_seen, s[n]);
+      keep(s[n], n, blk);
+      probabilities<D>(&st[n], s[n]);
+    }
+    add_values<FMT, D, QT>(v, s, st);
   };
   int blk = lo + wave;
   if (blk < end) {
@@ -347,76 +362,84 @@ __global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch 
   }
   if (lo <= full && full < hi && (full - lo) % 4 == wave) {
     const RQ_GLOBAL uint16_t* kt = gptr(a.c.tail) + (size_t)unit * 2 * kBlockTokens * D;
-    f4 s[2];
-    tail_products<D, BF16>(a, b, h, kt, q, s);
-    block_scores<D>(a, q, pos, a.qscale, full * kBlockTokens, past, true, s);
-    keep(s, full);
-    probabilities<D>(&st, s);
-    add_tail<FMT, D, BF16>(kt + kBlockTokens * D, total % kBlockTokens, s, &st);
+#pragma unroll
+    for (int n = 0; n < QT; ++n) {
+      f4 s[2];
+      tail_products<D, BF16>(a, b, h, kt, q[n], s);
+      block_scores<D>(a, q[n], pos, a.qscale, full * kBlockTokens, past, true, s);
+      keep(s, n, full);
+      probabilities<D>(&st[n], s);
+      add_tail<FMT, D, BF16>(kt + kBlockTokens * D, total % kBlockTokens, s, &st[n]);
+    }
   }
 
-  // the four waves' sums
-  st.l += __shfl_xor(st.l, 16, 64);
-  st.l += __shfl_xor(st.l, 32, 64);
-  const float to_value = st.unit == 0.0f ? 0.0f : 1.0f / (st.unit * kValueUnit<FMT>);
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int n = 0; n < QT; ++n) {
+    if (16 * n >= nnew * a.G) break;
+    // the four waves' sums
+    float lsum = st[n].l + __shfl_xor(st[n].l, 16, 64);
+    lsum += __shfl_xor(lsum, 32, 64);
+    const float to_value = st[n].unit == 0.0f ? 0.0f : 1.0f / (st[n].unit * kValueUnit<FMT>);
+    if (n > 0) __syncthreads();
 #pragma unroll
-    for (int e = 0; e < D / 16; e += 4)
-      *(f4*)&sh_o[wave][r * kStride + (D / 16) * (4 * g + i) + e] =
-          (f4){st.o[e][i], st.o[e + 1][i], st.o[e + 2][i], st.o[e + 3][i]} * to_value;
-  if (g == 0) {
-    sh_ml[wave][r][0] = st.m;
-    sh_ml[wave][r][1] = st.l;
-  }
-  __syncthreads();
-  const int row = threadIdx.x >> 4, ch = (threadIdx.x & 15) * (D / 16);
-  float m = sh_ml[0][row][0];
-  for (int w = 1; w < 4; ++w) m = __builtin_fmaxf(m, sh_ml[w][row][0]);
-  float l = 0.0f, x[D / 16];
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-  for (int e = 0; e < D / 16; ++e) x[e] = 0.0f;
-  for (int w = 0; w < 4; ++w) {
-    const float by = exp2_f(sh_ml[w][row][0] - m);
-    l = __builtin_fmaf(sh_ml[w][row][1], by, l);
+      for (int e = 0; e < D / 16; e += 4)
+        *(f4*)&sh_o[wave][r * kStride + (D / 16) * (4 * g + i) + e] =
+            (f4){st[n].o[e][i], st[n].o[e + 1][i], st[n].o[e + 2][i], st[n].o[e + 3][i]} * to_value;
+    if (g == 0) {
+      sh_ml[wave][r][0] = st[n].m;
+      sh_ml[wave][r][1] = lsum;
+    }
+    __syncthreads();
+    const int row = threadIdx.x >> 4, ch = (threadIdx.x & 15) * (D / 16);
+    float m = sh_ml[0][row][0];
+    for (int w = 1; w < 4; ++w) m = __builtin_fmaxf(m, sh_ml[w][row][0]);
+    float l = 0.0f, x[D / 16];
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e)
-      x[e] = __builtin_fmaf(sh_o[w][row * kStride + ch + e], by, x[e]);
-  }
-  if (a.splits > 1) {
-    const size_t tile = (size_t)unit * a.row_tiles + rt;
-    const Parts parts(a, tile);
-    const int seen = nnew * a.G - rt * 16;           // rows with a query
-    if (row < seen) {
+    for (int e = 0; e < D / 16; ++e) x[e] = 0.0f;
+    for (int w = 0; w < 4; ++w) {
+      const float by = exp2_f(sh_ml[w][row][0] - m);
+      l = __builtin_fmaf(sh_ml[w][row][1], by, l);
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e)
+        x[e] = __builtin_fmaf(sh_o[w][row * kStride + ch + e], by, x[e]);
+    }
+    const int grow = 16 * n + row, token = grow / a.G;
+    if (token >= nnew) continue;
+    if (a.splits > 1) {
+      const Parts parts(a, (size_t)unit * QT + n);
 #pragma unroll
       for (int e = 0; e < D / 16; e += 4)
         parts.store_o<D>(split, row, ch + e, (f4){x[e], x[e + 1], x[e + 2], x[e + 3]});
       if (ch == 0) parts.store_ml(split, row, (f2){m, l});
+      continue;
     }
-    // the tile's last workgroup adds its parts
-    if (!a.tickets) return;
-    __shared__ uint32_t ticket;
-    RQ_GLOBAL uint32_t* counter = gptr(a.c.counters) + (size_t)unit * 2 + rt;
-    __builtin_amdgcn_s_waitcnt(0);                   // this wave's parts are out
-    __syncthreads();
-    if (threadIdx.x == 0)
-      ticket = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if (ticket != (uint32_t)a.splits - 1) return;
-    if (threadIdx.x == 0)
-      __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    merge_tile<D>(a, parts, b, h, rt, seen < 16 ? seen : 16, reinterpret_cast<f4*>(sh_o));
-    return;
-  }
-  const int grow = rt * 16 + row, token = grow / a.G;
-  if (token >= nnew) return;
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
-  for (int e = 0; e < D / 16; ++e) x[e] *= inv;
-  store_out<D / 16>(a, b, h * a.G + grow - token * a.G, token, ch, x);
-  if (a.stats && ch == 0) {
-    gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + grow) * 2] = m;
-    gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + grow) * 2 + 1] = inv;
+    for (int e = 0; e < D / 16; ++e) x[e] *= inv;
+    store_out<D / 16>(a, b, h * a.G + grow - token * a.G, token, ch, x);
+    if (a.stats && ch == 0) {
+      gptr(a.stats)[((size_t)unit * QT * 16 + grow) * 2] = m;
+      gptr(a.stats)[((size_t)unit * QT * 16 + grow) * 2 + 1] = inv;
+    }
+  }
+  // the unit's last workgroup adds its parts
+  if (!a.tickets) return;
+  RQ_GLOBAL uint32_t* counter = gptr(a.c.counters) + unit;
+  __builtin_amdgcn_s_waitcnt(0);                     // this wave's parts are out
+  __syncthreads();
+  if (threadIdx.x == 0)
+    ticket = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (ticket != (uint32_t)a.splits - 1) return;
+  if (threadIdx.x == 0)
+    __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+  for (int n = 0; n < QT; ++n) {
+    const int seen = nnew * a.G - 16 * n;            // rows with a query
+    merge_tile<D>(a, Parts(a, (size_t)unit * QT + n), b, h, n, seen < 16 ? seen : 16,
+                  reinterpret_cast<f4*>(sh_o));
   }
 }
 
@@ -508,7 +531,7 @@ __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttendLaunch a) {
 // and sums (every workgroup merges those by itself).
 template <int D>
 __global__ void __launch_bounds__(256) block_merge_weigh_kernel(BlockAttendLaunch a) {
-  __shared__ float sh_m[16], sh_inv[16];
+  __shared__ float sh_m[32], sh_inv[32];
   const int unit = blockIdx.y, b = unit / a.c.H;
   int past, nnew;
   block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
@@ -522,22 +545,24 @@ __global__ void __launch_bounds__(256) block_merge_weigh_kernel(BlockAttendLaunc
   seen_blocks(past, 0, nnew - 1, a.window, &lo, &hi);
   const int first = (lo / 32 + blockIdx.x - merges) * 32;    // blocks first..first + 31
   if (nnew == 0 || first >= hi) return;
-  const int row = threadIdx.x >> 4, lane = threadIdx.x & 15;
-  if (a.splits > 1) {
-    const RQ_GLOBAL float* ml = gptr(a.part_ml) + ((size_t)unit * a.splits * 16 + row) * 2;
-    float m = -1.0e30f, l = 0.0f;
-    for (int s = lane; s < a.splits; s += 16) m = __builtin_fmaxf(m, ml[s * 32]);
-    for (int d = 8; d >= 1; d >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d, 64));
-    for (int s = lane; s < a.splits; s += 16)
-      l = __builtin_fmaf(ml[s * 32 + 1], exp2_f(ml[s * 32] - m), l);
-    for (int d = 8; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
-    if (lane == 0) {
-      sh_m[row] = m;
-      sh_inv[row] = l > 0.0f ? 1.0f / l : 0.0f;
+  const int lane = threadIdx.x & 15;
+  for (int row = threadIdx.x >> 4; row < rows; row += 16) {
+    if (a.splits > 1) {
+      const RQ_GLOBAL float* ml = gptr(a.part_ml) + (((size_t)unit * a.row_tiles + (row >> 4)) * a.splits * 16 + (row & 15)) * 2;
+      float m = -1.0e30f, l = 0.0f;
+      for (int s = lane; s < a.splits; s += 16) m = __builtin_fmaxf(m, ml[s * 32]);
+      for (int d = 8; d >= 1; d >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d, 64));
+      for (int s = lane; s < a.splits; s += 16)
+        l = __builtin_fmaf(ml[s * 32 + 1], exp2_f(ml[s * 32] - m), l);
+      for (int d = 8; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+      if (lane == 0) {
+        sh_m[row] = m;
+        sh_inv[row] = l > 0.0f ? 1.0f / l : 0.0f;
+      }
+    } else if (lane == 0) {
+      sh_m[row] = gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + row) * 2];
+      sh_inv[row] = gptr(a.stats)[((size_t)unit * a.row_tiles * 16 + row) * 2 + 1];
     }
-  } else if (lane == 0 && row < rows) {
-    sh_m[row] = gptr(a.stats)[((size_t)unit * 16 + row) * 2];
-    sh_inv[row] = gptr(a.stats)[((size_t)unit * 16 + row) * 2 + 1];
   }
   __syncthreads();
   const int blk = first + (threadIdx.x >> 3), slot = blk * kBlockTokens + 4 * (threadIdx.x & 7);
@@ -557,13 +582,21 @@ __global__ void __launch_bounds__(256) block_merge_weigh_kernel(BlockAttendLaunc
     if (slot + j < past + nnew) w[j] += sum[j];
 }
 
+template <int FMT, int D, bool BF16>
+void launch(const BlockAttendLaunch& a, hipStream_t s) {
+  const dim3 grid(a.splits, a.c.B * a.c.H);
+  if (a.row_tiles == 1)
+    hipLaunchKernelGGL((block_attend_kernel<FMT, D, BF16, 1>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((block_attend_kernel<FMT, D, BF16, 2>), grid, dim3(256), 0, s, a);
+}
+
 template <int FMT, int D>
 hipError_t launch(const BlockAttendLaunch& a, hipStream_t s) {
-  const dim3 grid(a.splits * a.row_tiles, a.c.B * a.c.H);
   if (a.c.is_bf16)
-    hipLaunchKernelGGL((block_attend_kernel<FMT, D, true>), grid, dim3(256), 0, s, a);
+    launch<FMT, D, true>(a, s);
   else
-    hipLaunchKernelGGL((block_attend_kernel<FMT, D, false>), grid, dim3(256), 0, s, a);
+    launch<FMT, D, false>(a, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int rows = a.n * a.G;

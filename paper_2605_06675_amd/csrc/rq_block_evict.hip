@@ -23,13 +23,14 @@ constexpr int kCopies = 4;
 struct SelectShared {
   uint32_t hist[kBins * kCopies];
   uint32_t sum[kSelWaves], tie[kSelWaves];
-  uint32_t pick[2];
+  uint32_t pick[3];
 };
 
 // Where the search stands: the leading digits of the k-th largest key, and how
 // many of the keys with these digits stay.
 struct Found {
   uint32_t prefix, need;
+  uint32_t all;             // all of them do
 };
 
 // A weight's place in the order, as an unsigned number above 0; the tokens that
@@ -113,11 +114,13 @@ __device__ __forceinline__ uint32_t pick_digit(SelectShared& sh, uint32_t c1, ui
     const bool first = f->need <= above + c1;
     sh.pick[0] = top_digit() - (first ? 0 : 1);
     sh.pick[1] = first ? above : above + c1;
+    sh.pick[2] = f->need - sh.pick[1] == (first ? c1 : c2);
   }
   __syncthreads();
   const uint32_t d = sh.pick[0];
   f->prefix = level == 0 ? d : (f->prefix << (level == 1 ? 11 : 10)) | d;
   f->need -= sh.pick[1];
+  f->all = sh.pick[2];
   __syncthreads();
   return d;
 }
@@ -191,9 +194,9 @@ __device__ __forceinline__ int kept_length(const BlockEvictLaunch& a, int b, int
   return L;
 }
 
-// A unit by one workgroup, its keys in registers.
+// A unit by one workgroup, its keys in registers, N x 4 a thread.
+template <int N>
 __global__ void __launch_bounds__(kSelThreads) block_select_kernel(BlockEvictLaunch a) {
-  constexpr int N = kSelectShort / (4 * kSelThreads);
   __shared__ SelectShared sh;
   const int unit = blockIdx.x, b = unit / a.src.H, tid = threadIdx.x;
   int k;
@@ -207,7 +210,7 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(BlockEvictLau
   uint32_t key[4 * N];
   const int base = (tid >> 6) * N * 256;
   load_ranks<N>(a, gptr(a.src.weights) + (size_t)unit * a.src.cap, base, L, key);
-  Found f = {0, (uint32_t)k};
+  Found f = {0, (uint32_t)k, 0};
   for (int level = 0; level < 3; ++level) {
     clear_digits(sh);
     count_digits<N>(sh, key, level, f.prefix);
@@ -215,6 +218,13 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(BlockEvictLau
     uint32_t c1, c2;
     read_digits(sh, &c1, &c2);
     pick_digit(sh, c1, c2, level, &f);
+    if (f.all && level < 2) {
+      // every key from these digits on stays: no need to look closer
+      const uint32_t from = f.prefix << digit_shift(level);
+      f.prefix = from > 0 ? from - 1 : 0;
+      f.need = 0;
+      break;
+    }
   }
   uint32_t kept = 0, ties = 0;
   write_slots<N>(sh, key, base, f, out, &kept, &ties);
@@ -244,7 +254,7 @@ __global__ void __launch_bounds__(kSelThreads) block_select_part_kernel(BlockEvi
   RQ_GLOBAL uint32_t* count = gptr(a.counts) + (size_t)unit * a.parts * kBins;
   RQ_GLOBAL uint32_t* state = gptr(a.state) + (size_t)unit * 8;
   RQ_GLOBAL uint32_t* before = gptr(a.before) + (size_t)unit * a.parts;
-  Found f = {0, (uint32_t)k};
+  Found f = {0, (uint32_t)k, 0};
   uint32_t kept = 0, ties = 0;
   const int in_use = (L + a.part - 1) / a.part;
   if (level > 0) {
@@ -441,7 +451,13 @@ hipError_t launch_gather(const BlockEvictLaunch& a, hipStream_t s) {
 hipError_t launch_block_evict(const BlockEvictLaunch& a, hipStream_t s) {
   const int units = a.src.B * a.src.H;
   if (a.parts == 1) {
-    hipLaunchKernelGGL(block_select_kernel, dim3(units), dim3(kSelThreads), 0, s, a);
+    static_assert(kSelectShort == 32 * kSelThreads, "keys of a unit in one workgroup");
+    if (a.src.cap <= 4 * kSelThreads)
+      hipLaunchKernelGGL((block_select_kernel<1>), dim3(units), dim3(kSelThreads), 0, s, a);
+    else if (a.src.cap <= 16 * kSelThreads)
+      hipLaunchKernelGGL((block_select_kernel<4>), dim3(units), dim3(kSelThreads), 0, s, a);
+    else
+      hipLaunchKernelGGL((block_select_kernel<8>), dim3(units), dim3(kSelThreads), 0, s, a);
   } else {
     for (int level = 0; level < 4; ++level)
       hipLaunchKernelGGL(block_select_part_kernel, dim3(a.parts, units), dim3(kSelThreads), 0, s, a, level);

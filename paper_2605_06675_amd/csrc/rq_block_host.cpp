@@ -63,7 +63,8 @@ rq_status check_buffers(const rq_block_cache* c, int32_t layer) {
   if (!c->codes || !c->scales || !c->tail || !c->positions)
     return fail(RQ_EINVAL, "the cache has a NULL buffer");
   if (unaligned(c->codes) || unaligned(c->scales) || unaligned(c->tail) ||
-      unaligned(c->positions) || unaligned(c->weights) || unaligned(c->counters))
+      unaligned(c->positions) || unaligned(c->weights) ||
+      reinterpret_cast<uintptr_t>(c->counters) % 4)
     return fail(RQ_EINVAL, "a cache buffer is not 16-byte aligned");
   return RQ_OK;
 }
@@ -78,7 +79,7 @@ rq::BlockLayer layer_of(const rq_block_cache* c, int32_t layer) {
   l.tail = static_cast<uint16_t*>(c->tail) + u * 2 * rq::kBlockTokens * D;
   l.positions = c->positions + u * cap;
   l.weights = c->weights ? c->weights + u * cap : nullptr;
-  l.counters = c->counters ? c->counters + u * 2 : nullptr;
+  l.counters = c->counters ? c->counters + u : nullptr;
   l.B = c->batch;
   l.H = c->n_kv_heads;
   l.cap = c->capacity;
@@ -110,7 +111,7 @@ struct Plan {
   uint64_t bytes() const { return part + part_ml + stats + scores + queries + factors + sums; }
 };
 
-// Few rows: one workgroup a CU over the units' row tiles, at least four blocks
+// Up to 32 rows: one workgroup a CU over the units, at least four blocks
 // (one a wave) each.  Four waves with a block in flight each keep a CU's share
 // of the memory busy; more workgroups are set-ups and parts to merge, but even
 // out sequences of unlike lengths where the scores are kept too.  us with one /
@@ -119,7 +120,7 @@ struct Plan {
 // 17 / 18, 192 of 4000 31.3 / 39 / 36.5; uneven lengths: 128 units to 8192 35 /
 // 33.8 / 34, with weights 42.5 / 37.8 / 39.
 // More than two tiles of 16 rows: tiles of 128 rows, two workgroups a CU, at
-// least eight blocks each.  Where the new tokens are few beside the cached ones,
+// least four blocks each.  Where the new tokens are few beside the cached ones,
 // sequences may differ in length and a round's workgroups with them: one split
 // more (4 sequences, 8 kv-heads of 4 heads, 512 tokens over 8192: 358 us
 // unsplit, 366 in two; lengths from 2048 to 8192: 289 and 250).
@@ -132,14 +133,14 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
     const int64_t seen = ((int64_t)a->window + 16 / G + 1) / rq::kBlockTokens + 2;
     blocks = seen < blocks ? seen : blocks;
   }
-  p.prompt = p.row_tiles > 2 || (p.row_tiles > 1 && a->accumulate);
+  p.prompt = p.row_tiles > 2;
   int64_t s;
   if (p.prompt) {
     s = 2 * (int64_t)rq::device_cus() / (u * ((a->n_new * G + 127) / 128));
-    s = std::min(s, (blocks + 7) / 8);
+    s = std::min(s, (blocks + 3) / 4);
     if (s <= 1 && a->max_tokens >= 4 * (int64_t)a->n_new && blocks >= 128) s = 2;
   } else {
-    s = (a->accumulate && c->batch > 1 ? 2 : 1) * (int64_t)rq::device_cus() / (u * p.row_tiles);
+    s = (a->accumulate && c->batch > 1 ? 2 : 1) * (int64_t)rq::device_cus() / u;
     s = std::min(s, (blocks + 3) / 4);
   }
   p.splits = (int)std::max<int64_t>(s, 1);
@@ -150,18 +151,18 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
   }
   if (a->accumulate) {
     p.stats = tiles * 16 * 2 * sizeof(float);
-    // one tile of rows: the scores are kept (4 bytes a row and token) rather
+    // one or two tiles of rows: the scores are kept (4 bytes a row and token) rather
     // than computed again from the keys (D bytes a token)
     const int64_t rows = a->n_new * G;
-    if (p.row_tiles == 1) {
+    if (!p.prompt) {
       p.scores = (uint64_t)u * ((a->max_tokens + rq::kBlockTokens - 1) / rq::kBlockTokens) * rows *
                  rq::kBlockTokens * sizeof(float);
       return p;
     }
     // else workgroups of 256 tokens, and parts of the rows to fill four rounds
-    // (two a CU), 512 rows or more in each
+    // (two a CU), 128 rows or more in each
     int64_t parts = 8 * (int64_t)rq::device_cus() / (u * ((a->max_tokens + 255) / 256));
-    parts = std::min(parts, (rows + 511) / 512);
+    parts = std::min(parts, (rows + 127) / 128);
     p.row_parts = (int)std::max<int64_t>(parts, 1);
     p.queries = tiles * 16 * c->head_dim * sizeof(uint16_t);
     p.factors = tiles * 16 * sizeof(float);
@@ -207,7 +208,7 @@ rq_status rq_block_sizes(const rq_block_cache* c, uint64_t* codes_bytes, uint64_
   if (tail_bytes) *tail_bytes = u * 2 * rq::kBlockTokens * D * sizeof(uint16_t);
   if (positions_bytes) *positions_bytes = u * cap * sizeof(int32_t);
   if (weights_bytes) *weights_bytes = u * cap * sizeof(float);
-  if (counters_bytes) *counters_bytes = u * 2 * sizeof(uint32_t);
+  if (counters_bytes) *counters_bytes = u * sizeof(uint32_t);
   return ok();
 }
 
@@ -300,7 +301,7 @@ rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_bl
   // 8.5 / 9.4, 8 x 8 44.2 / 45.4 (32 units of 32768 tokens), 2 x 4 15.4 / 16.5,
   // 32 x 4 10.8 / 9.3, 16 x 16 18.7 / 18.1, 32 x 8 15.0 / 12.5.
   a.tickets = !p.prompt && p.splits > 1 && p.splits <= rq::kTicketSplits &&
-              p.splits * std::min(a.n * a.G, 16) <= 100 && a.c.counters && !a.accumulate;
+              p.splits * a.n * a.G <= 100 && a.c.counters && !a.accumulate;
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = p.prompt ? rq::launch_block_prompt(a, s) : rq::launch_block_attend(a, s);
   if (e == hipSuccess && p.prompt) e = rq::launch_block_merge(a, s);

@@ -43,7 +43,7 @@ def query(**kw):
 def test_sizes(D):
     u = 2 * 3 * 4
     assert rq.rq_block_sizes(desc(head_dim=D)) == (
-        u * 2 * 96 * D, u * 2 * 3 * 4, u * 2 * 32 * D * 2, u * 96 * 4, u * 96 * 4, u * 2 * 4)
+        u * 2 * 96 * D, u * 2 * 3 * 4, u * 2 * 32 * D * 2, u * 96 * 4, u * 96 * 4, u * 4)
 
 
 BAD_SHAPES = [
@@ -72,7 +72,7 @@ def test_shape_refusals(kw, status):
 @pytest.mark.parametrize("kw", [dict(codes=None), dict(scales=None), dict(tail=None),
                                 dict(positions=None), dict(codes=P + 8), dict(scales=P + 4),
                                 dict(tail=P + 2), dict(positions=P + 4), dict(weights=P + 4),
-                                dict(counters=P + 4)])
+                                dict(counters=P + 2)])
 def test_buffer_refusals(kw):
     c, L = desc(**kw), rq.lib()
     assert L.rq_block_append(C.byref(c), 0, P, 1, None, C.byref(rows()), C.byref(rows()),

@@ -486,11 +486,11 @@ def test_evict_counts(keep, sink, recent):
 @pytest.mark.parametrize("kind", ["random", "zero", "few", "late"])
 def test_evict_long(kind):
     """A unit selected in several parts; ties across them."""
-    r = Rig("int8", "fp16", B=1, H=1, D=64, cap=20032)
-    k, v = r.kv(20001)
+    r = Rig("int8", "fp16", B=1, H=1, D=64, cap=40032)
+    k, v = r.kv(40001)
     r.c.append(0, k.cuda(), v.cuda())
     u = r.u[0][0]
-    full = 20000
+    full = 40000
     q = [block.quantize(block.INT8, x[0, 0, i:i + 32].float().numpy()) for x in (k, v) for i in range(0, full, 32)]
     half = len(q) // 2
     for s in (0, 1):
@@ -498,21 +498,40 @@ def test_evict_long(kind):
         u.codes[s] = np.concatenate([c for c, _ in part])
         u.scales[s] = np.array([x for _, x in part], np.float32)
         u.tail[s] = (k, v)[s][0, 0, full:].float().numpy()
-    u.pos, u.weight = np.arange(20001), np.zeros(20001)
+    u.pos, u.weight = np.arange(40001), np.zeros(40001)
     r.check()
-    w = -torch.log(torch.rand(1, 1, 20032, generator=r.g))
-    w = {"random": w, "zero": w * 0, "few": (w < 0.01).float(), "late": (torch.arange(20032) > 17000).float()[None, None]}[kind]
+    w = -torch.log(torch.rand(1, 1, 40032, generator=r.g))
+    w = {"random": w, "zero": w * 0, "few": (w < 0.01).float(), "late": (torch.arange(40032) > 37000).float()[None, None]}[kind]
     evict(r, 5000, 4, 64, w)
+
+
+@pytest.mark.parametrize("L,cap", [(4000, 4096), (9001, 9024), (20001, 20032), (32768, 32768)])
+@pytest.mark.parametrize("kind", ["random", "zero", "few"])
+def test_evict_selection(L, cap, kind):
+    """The kept slots alone, for units selected by one workgroup."""
+    r = Rig("int8", "bf16", B=2, H=1, D=64, cap=cap)
+    k, v = r.kv(L)
+    r.c.append(0, k.cuda(), v.cuda())
+    w = torch.rand(2, 1, cap, generator=r.g)
+    w = {"random": w, "zero": w * 0, "few": (w < 0.01).float()}[kind]
+    r.c.weights.view(2, 1, cap).copy_(w)
+    keep = L // 3
+    pos = r.c.evict(keep, 4, 30).positions.view(2, -1).cpu()
+    for b in range(2):
+        order = w[b, 0, :L].double()
+        order[:4] = order[L - 30:] = 9.0
+        rank = torch.sort(order, stable=True, descending=True)[1][:keep]
+        assert torch.equal(pos[b, :keep].long(), torch.sort(rank)[0])
 
 
 def test_evict_parts_of_uneven_sequences():
     """Sequences that end in the first, a later and no part, one that keeps
     everything; more layers than one."""
-    r = Rig("e4m3", "bf16", B=4, H=1, D=64, cap=25024, layers=2, layer=1)
-    new = [25000, 9000, 0, 300]
-    k, v = r.kv(25000)
+    r = Rig("e4m3", "bf16", B=4, H=1, D=64, cap=50016, layers=2, layer=1)
+    new = [50000, 9000, 0, 300]
+    k, v = r.kv(50000)
     r.c.append(1, k.cuda(), v.cuda(), ints(new))
-    w = torch.rand(4, 1, 25024, generator=r.g)
+    w = torch.rand(4, 1, 50016, generator=r.g)
     r.c.weights.view(2, 4, 1, -1)[1] = w.cuda()
     to = rq.BlockCache(*r.c.shape, 512, weights=True)
     r.c.evict(500, 3, 20, into=to)
