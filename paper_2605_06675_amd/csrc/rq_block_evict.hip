@@ -125,6 +125,16 @@ __device__ __forceinline__ uint32_t pick_digit(SelectShared& sh, uint32_t c1, ui
   return d;
 }
 
+// Where every key from f's digits on stays there is no need to look closer: f
+// becomes a bound below them all.
+__device__ __forceinline__ bool settle(int level, Found* f) {
+  if (!f->all) return false;
+  const uint32_t from = f->prefix << digit_shift(level);
+  f->prefix = from > 0 ? from - 1 : 0;
+  f->need = 0;
+  return true;
+}
+
 __device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
   for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
   return x;
@@ -218,13 +228,7 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(BlockEvictLau
     uint32_t c1, c2;
     read_digits(sh, &c1, &c2);
     pick_digit(sh, c1, c2, level, &f);
-    if (f.all && level < 2) {
-      // every key from these digits on stays: no need to look closer
-      const uint32_t from = f.prefix << digit_shift(level);
-      f.prefix = from > 0 ? from - 1 : 0;
-      f.need = 0;
-      break;
-    }
+    if (level < 2 && settle(level, &f)) break;
   }
   uint32_t kept = 0, ties = 0;
   write_slots<N>(sh, key, base, f, out, &kept, &ties);
@@ -232,9 +236,10 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(BlockEvictLau
 
 // Longer units: a workgroup for every part of a.part tokens, and a launch for
 // each digit.  Launch `level` finds the digit before from the parts' counters
-// of the launch before, and counts its own (level 3: writes the slots instead).
-// A part's place in the output, the keys above the k-th in the parts before,
-// is added up on the way.
+// of the launch before, and counts its own; once the digits settle the choice
+// (or at level 3) it writes the slots instead, and later launches have nothing
+// to do.  A part's place in the output, the keys above the k-th in the parts
+// before, is added up on the way.
 __global__ void __launch_bounds__(kSelThreads) block_select_part_kernel(BlockEvictLaunch a, int level) {
   constexpr int N = 2, kTile = 4 * N * kSelThreads;
   __shared__ SelectShared sh;
@@ -257,10 +262,15 @@ __global__ void __launch_bounds__(kSelThreads) block_select_part_kernel(BlockEvi
   Found f = {0, (uint32_t)k, 0};
   uint32_t kept = 0, ties = 0;
   const int in_use = (L + a.part - 1) / a.part;
+  bool write = level == 3;
   if (level > 0) {
     if (level > 1) {
       f.prefix = state[2 * (level - 2)];
       f.need = state[2 * (level - 2) + 1];
+      if (f.need == 0) {                    // settled: the launch before wrote
+        if (level == 2 && part == 0 && tid == 0) state[2 * (level - 1) + 1] = 0;
+        return;
+      }
       kept = before[part];
     }
     // (counters lie in falling order of their digits, a thread's two together)
@@ -274,8 +284,15 @@ __global__ void __launch_bounds__(kSelThreads) block_select_part_kernel(BlockEvi
     }
     const uint32_t d = pick_digit(sh, all.x, all.y, level - 1, &f);
     const uint32_t hi = top_digit();
-    const uint32_t g = wave_sum((hi > d ? ahead.x : 0u) + (hi - 1 > d ? ahead.y : 0u));
-    const uint32_t e = wave_sum((hi == d ? ahead.x : 0u) + (hi - 1 == d ? ahead.y : 0u));
+    uint32_t g = (hi > d ? ahead.x : 0u) + (hi - 1 > d ? ahead.y : 0u);
+    uint32_t e = (hi == d ? ahead.x : 0u) + (hi - 1 == d ? ahead.y : 0u);
+    if (!write && settle(level - 1, &f)) {
+      write = true;
+      g += e;                               // (none is a tie any more)
+      e = 0;
+    }
+    g = wave_sum(g);
+    e = wave_sum(e);
     if ((tid & 63) == 0) {
       sh.sum[tid >> 6] = g;
       sh.tie[tid >> 6] = e;
@@ -298,17 +315,17 @@ __global__ void __launch_bounds__(kSelThreads) block_select_part_kernel(BlockEvi
   }
   if (first >= L) return;
   const RQ_GLOBAL float* w = gptr(a.src.weights) + (size_t)unit * a.src.cap;
-  if (level < 3) clear_digits(sh);
+  if (!write) clear_digits(sh);
   for (int at = first; at < last; at += kTile) {
     uint32_t key[4 * N];
     const int base = at + (tid >> 6) * N * 256;
     load_ranks<N>(a, w, base, L, key);
-    if (level < 3)
-      count_digits<N>(sh, key, level, f.prefix);
-    else
+    if (write)
       write_slots<N>(sh, key, base, f, out, &kept, &ties);
+    else
+      count_digits<N>(sh, key, level, f.prefix);
   }
-  if (level == 3) return;
+  if (write) return;
   __syncthreads();
   u2 c;
   uint32_t c1, c2;

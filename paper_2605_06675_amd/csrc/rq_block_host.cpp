@@ -118,7 +118,10 @@ struct Plan {
 // two / three a CU: 128 full units of 8192 tokens 44.7 / 47 / 47, 32 of 32768 (8
 // heads, capped) 43.7 / 48.5 / 50, 8 of 131072 46.8 / 48 / 49.4, 64 of 4000 15.6 /
 // 17 / 18, 192 of 4000 31.3 / 39 / 36.5; uneven lengths: 128 units to 8192 35 /
-// 33.8 / 34, with weights 42.5 / 37.8 / 39.
+// 33.8 / 34, with weights 42.5 / 37.8 / 39.  Two tiles of rows are more work a
+// block, and units that leave a workgroup alone with a long one wait for it: 104
+// units of 24 rows to 9029 even 60.1 / 54.5 / 57.7, uneven 54.2 / 39.3 / 39.3, but
+// 64 units of 32 rows to 8192 31.2 / 33.1 / 40, 8 of 65536 30.5 / 34.5 / 39.
 // More than two tiles of 16 rows: tiles of 128 rows, two workgroups a CU, at
 // least four blocks each.  Where the new tokens are few beside the cached ones,
 // sequences may differ in length and a round's workgroups with them: one split
@@ -140,7 +143,8 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
     s = std::min(s, (blocks + 3) / 4);
     if (s <= 1 && a->max_tokens >= 4 * (int64_t)a->n_new && blocks >= 128) s = 2;
   } else {
-    s = (a->accumulate && c->batch > 1 ? 2 : 1) * (int64_t)rq::device_cus() / u;
+    const bool two = (a->accumulate && c->batch > 1) || (p.row_tiles > 1 && u > 64);
+    s = (two ? 2 : 1) * (int64_t)rq::device_cus() / u;
     s = std::min(s, (blocks + 3) / 4);
   }
   p.splits = (int)std::max<int64_t>(s, 1);

@@ -211,6 +211,12 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
     lo += 2 * t0;
   }
 
+  const RQ_GLOBAL uint8_t* kc = gptr(a.c.codes) + (size_t)unit * 2 * a.c.cap * D;
+  const RQ_GLOBAL uint8_t* vc = kc + (size_t)a.c.cap * D;
+  const int coded = (hi < full ? hi : full) * kBlockTokens;     // slots of the split's coded blocks
+  TileLoad next;
+  if (lo < hi) load_tile<D>(kc, vc, lo * kBlockTokens, coded, &next);
+
   // this lane's row, as BlockAttendLaunch has it: 16 k + 8 hl + 0..7 in f[k]
   const int row = rt * kRows + wave * 32 + col;
   int token = row / a.G;
@@ -270,15 +276,12 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
       qpos = gptr(a.c.positions)[(size_t)unit * a.c.cap + past + token];
   }
 
-  const RQ_GLOBAL uint8_t* kc = gptr(a.c.codes) + (size_t)unit * 2 * a.c.cap * D;
-  const RQ_GLOBAL uint8_t* vc = kc + (size_t)a.c.cap * D;
   // (scales by scalar loads: a vector load's wait would be one for the next
   // tile's codes in flight)
   const RQ_CONSTANT float* kscale = cptr(a.c.scales) + (size_t)unit * 2 * (a.c.cap / kBlockTokens);
   const RQ_CONSTANT float* vscale = kscale + a.c.cap / kBlockTokens;
   const RQ_GLOBAL int32_t* pos = gptr(a.c.positions) + (size_t)unit * a.c.cap;
   const RQ_GLOBAL uint16_t* tail = gptr(a.c.tail) + (size_t)unit * 2 * kBlockTokens * D;
-  const int coded = (hi < full ? hi : full) * kBlockTokens;     // slots of the split's coded blocks
 
   f16v o[D / 32];
 #pragma unroll
@@ -288,11 +291,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
   float m = -1.0e30f, l = 0.0f, unit2 = 0.0f;
   const bool far = a.slopes || a.window;
 
-  float ks[2][2], vs[2][2];           // scales of the two buffers' blocks
-  TileLoad next;
-  auto fetch = [&](int blk) {
-    load_tile<D>(kc, vc, blk * kBlockTokens, coded, &next);
-  };
+  float tks[2], tvs[2];               // scales of a tile's blocks
   auto put = [&](int blk, int buf) {
     store_tile<FMT, D>(next, blk * kBlockTokens, coded, sh_k[buf], sh_v[buf]);
     if (far && threadIdx.x < kTile) {
@@ -301,18 +300,26 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      ks[buf][i] = blk + i < full ? kscale[blk + i] : 0.0f;
-      vs[buf][i] = blk + i < full ? vscale[blk + i] : 0.0f;
+      tks[i] = blk + i < full ? kscale[blk + i] : 0.0f;
+      tvs[i] = blk + i < full ? vscale[blk + i] : 0.0f;
     }
     if (full < hi && (blk == full || blk + 1 == full)) {
       // (the zeros that store_tile left for the tail's values come first)
       __syncthreads();
+      float k, v;
       store_tail<FMT, D, BF16>(tail, total - full * kBlockTokens, (full - blk) * kBlockTokens, sh_k[buf],
-                               sh_v[buf], red, &ks[buf][full - blk], &vs[buf][full - blk]);
+                               sh_v[buf], red, &k, &v);
+      if (blk == full) {
+        tks[0] = k;
+        tvs[0] = v;
+      } else {
+        tks[1] = k;
+        tvs[1] = v;
+      }
     }
   };
 
-  auto work = [&](int blk, int buf, const float tks[2], const float tvs[2]) {
+  auto work = [&](int blk, int buf) {
     const int slot0 = blk * kBlockTokens;
     if (idle || slot0 > past + wave_last) return;
     f16v s[2];
@@ -435,26 +442,12 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
     }
   };
 
-  if (lo < hi) {
-    fetch(lo);
-    put(lo, 0);
+  // a wave may be a tile behind the others, never more: one barrier a tile
+  for (int blk = lo, buf = 0; blk < hi; blk += 2, buf ^= 1) {
+    put(blk, buf);
     __syncthreads();
-    for (int blk = lo;;) {
-      const bool more = blk + 2 < hi;
-      if (more) fetch(blk + 2);
-      work(blk, 0, ks[0], vs[0]);
-      if (!more) break;
-      put(blk + 2, 1);
-      __syncthreads();
-      blk += 2;
-      const bool more2 = blk + 2 < hi;
-      if (more2) fetch(blk + 2);
-      work(blk, 1, ks[1], vs[1]);
-      if (!more2) break;
-      put(blk + 2, 0);
-      __syncthreads();
-      blk += 2;
-    }
+    if (blk + 2 < hi) load_tile<D>(kc, vc, (blk + 2) * kBlockTokens, coded, &next);
+    work(blk, buf);
   }
 
   l += __shfl_xor(l, 32, 64);

@@ -246,17 +246,12 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
 
   if (from < to && tile0 < tile1) {
     fetch(tile0);
-    put(0);
-    __syncthreads();
-    for (int tile = tile0;; ++tile) {
-      const int buf = (tile - tile0) & 1;
-      const bool more = tile + 1 < tile1;
-      if (more) fetch(tile + 1);
-      work(tile, buf, 0);
-      work(tile, buf, 1);
-      if (!more) break;
-      put(buf ^ 1);
+    for (int tile = tile0, buf = 0; tile < tile1; ++tile, buf ^= 1) {
+      put(buf);
       __syncthreads();
+      if (tile + 1 < tile1) fetch(tile + 1);
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) work(tile, buf, half);
     }
   }
 
