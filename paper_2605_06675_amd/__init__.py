@@ -572,6 +572,9 @@ def _block_rows(cache, t, what, heads, n, dtypes):
     sb, sh, st, sd = t.stride()
     if sd != 1:
         raise ValueError(f"the rows of {what} must be contiguous")
+    if what == "out" and (not sb and shape[0] > 1 or not sh and heads > 1
+                          or not st and n > 1):
+        raise ValueError("rows of out share memory")
     return t.data_ptr(), sb, sh, st
 
 

@@ -84,14 +84,14 @@ __device__ __forceinline__ void probabilities(Running<D>* st, f4 s[2]) {
   st->l += sum;
 }
 
-// Adds a block's values to the states of QT query tiles (whose units are the
-// same).
-template <int FMT, int D, int QT>
-__device__ __forceinline__ void add_values(const ValueBlock<D>& v, const f4 s[QT][2],
-                                           Running<D> st[QT]) {
-  if (v.scale * st[0].unit > 128.0f || st[0].unit == 0.0f) {  // (the same in every lane)
-    // (a scale of zero has no exponent; 0 serves)
-    int e = v.scale > 0.0f ? __builtin_amdgcn_frexp_expf(v.scale) : 0;
+// The probabilities of QT tiles times a block's value scale, in the tiles'
+// common unit, as fp16 pairs hi + lo.  The unit follows the largest scale; a
+// scale of zero has none to follow, and its products are zero.
+template <int D, int QT>
+__device__ __forceinline__ void split_products(const f4 s[QT][2], float scale, Running<D> st[QT],
+                                               u4 hi[QT], u4 lo[QT]) {
+  if (scale > 0.0f && (scale * st[0].unit > 128.0f || st[0].unit == 0.0f)) {   // (the same in every lane)
+    int e = __builtin_amdgcn_frexp_expf(scale);
     e = e < -100 ? -100 : e;
     const float unit = __builtin_amdgcn_ldexpf(128.0f, -e);
 #pragma unroll
@@ -100,8 +100,7 @@ __device__ __forceinline__ void add_values(const ValueBlock<D>& v, const f4 s[QT
       st[n].unit = unit;
     }
   }
-  const float by = v.scale * st[0].unit;
-  u4 hi[QT], lo[QT];
+  const float by = scale * st[0].unit;
 #pragma unroll
   for (int n = 0; n < QT; ++n)
 #pragma unroll
@@ -115,73 +114,71 @@ __device__ __forceinline__ void add_values(const ValueBlock<D>& v, const f4 s[QT
         hi[n][2 * m + i] = as_u32(h);
         lo[n][2 * m + i] = as_u32((h2){(_Float16)(a - (float)h.x), (_Float16)(b - (float)h.y)});
       }
+}
+
+// Adds one operand of values (channels e of every D / 16) to QT tiles.
+template <int D, int QT>
+__device__ __forceinline__ void add_operand(u4 f, int e, const u4 hi[QT], const u4 lo[QT],
+                                            Running<D> st[QT]) {
+#pragma unroll
+  for (int n = 0; n < QT; ++n) {
+    const f4 o = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(f), as_h8(hi[n]), st[n].o[e], 0, 0, 0);
+    st[n].o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(f), as_h8(lo[n]), o, 0, 0, 0);
+  }
+}
+
+template <int FMT, int D, int QT>
+__device__ __forceinline__ void add_values(const ValueBlock<D>& v, const f4 s[QT][2],
+                                           Running<D> st[QT]) {
+  u4 hi[QT], lo[QT];
+  split_products<D, QT>(s, v.scale, st, hi, lo);
 #pragma unroll
   for (int c = 0; c < D / 64; ++c) {
     uint32_t op[4][4];        // [token pair][channel]
 #pragma unroll
     for (int j = 0; j < 4; ++j) value_pairs<FMT>(v.w[2 * j][c], v.w[2 * j + 1][c], op[j]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const h8 f = as_h8((u4){op[0][e], op[1][e], op[2][e], op[3][e]});
-#pragma unroll
-      for (int n = 0; n < QT; ++n) {
-        f4 o = st[n].o[4 * c + e];
-        o = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, as_h8(hi[n]), o, 0, 0, 0);
-        st[n].o[4 * c + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, as_h8(lo[n]), o, 0, 0, 0);
-      }
-    }
+    for (int e = 0; e < 4; ++e)
+      add_operand<D, QT>((u4){op[0][e], op[1][e], op[2][e], op[3][e]}, 4 * c + e, hi, lo, st);
   }
 }
 
-// The tail's values: bf16 operands, whose range needs no unit.  An fp16 value
-// is a bf16 pair hi + lo, as the probabilities are.  Rows from n_tail on
-// count as zero.
-template <int FMT, int D, bool BF16>
-__device__ __forceinline__ void add_tail(const RQ_GLOBAL uint16_t* vt, int n_tail, const f4 s[2],
-                                         Running<D>* st) {
+// The tail's values, divided by a power of two that brings the largest below 1
+// (fp16 holds the others to 2^-25 of it), as a block of that scale.  Rows from
+// n_tail on count as zero.
+template <int FMT, int D, bool BF16, int QT>
+__device__ __forceinline__ void add_tail(const RQ_GLOBAL uint16_t* vt, int n_tail, const f4 s[QT][2],
+                                         Running<D> st[QT]) {
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  if (st->unit == 0.0f) st->unit = 1.0f;
-  const float by = st->unit * kValueUnit<FMT>;
-  u4 hi, lo;
+  uint32_t w[D / 32][8];      // [two channels][token]
+  float most = 0.0f;
 #pragma unroll
-  for (int m = 0; m < 2; ++m)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float a = s[m][2 * i] * by, b = s[m][2 * i + 1] * by;
-      const uint32_t ha = bf16_rne(a), hb = bf16_rne(b);
-      hi[2 * m + i] = ha | (hb << 16);
-      lo[2 * m + i] = (uint32_t)bf16_rne(a - __uint_as_float(ha << 16)) |
-                      ((uint32_t)bf16_rne(b - __uint_as_float(hb << 16)) << 16);
-    }
-#pragma unroll
-  for (int c = 0; c < D / 32; ++c) {     // two channels a word
-    uint32_t w[8];
+  for (int c = 0; c < D / 32; ++c)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int tok = 16 * (j >> 2) + 4 * g + (j & 3);
-      w[j] = tok < n_tail ? *(const RQ_GLOBAL uint32_t*)(vt + tok * D + (D / 16) * r + 2 * c) : 0u;
+      w[c][j] = tok < n_tail ? *(const RQ_GLOBAL uint32_t*)(vt + tok * D + (D / 16) * r + 2 * c) : 0u;
+      most = __builtin_fmaxf(most, __builtin_fmaxf(__builtin_fabsf(widen_t<BF16>(w[c][j] & 0xffffu)),
+                                                   __builtin_fabsf(widen_t<BF16>(w[c][j] >> 16))));
     }
+  for (int d = 32; d >= 1; d >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d, 64));
+  if (most == 0.0f) return;
+  const int e = __builtin_amdgcn_frexp_expf(most);
+  u4 hi[QT], lo[QT];
+  split_products<D, QT>(s, __builtin_amdgcn_ldexpf(kValueUnit<FMT>, e), st, hi, lo);
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      u4 f, f2;
+  for (int c = 0; c < D / 32; ++c) {
+    u4 f[2];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        f[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], e ? 0x07060302u : 0x05040100u);
-        if constexpr (!BF16) {
-          const float x = widen_t<false>(f[j] & 0xffffu), y = widen_t<false>(f[j] >> 16);
-          const uint32_t hx = bf16_rne(x), hy = bf16_rne(y);
-          f[j] = hx | (hy << 16);
-          f2[j] = (uint32_t)bf16_rne(x - __uint_as_float(hx << 16)) |
-                  ((uint32_t)bf16_rne(y - __uint_as_float(hy << 16)) << 16);
-        }
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const h2 p = {(_Float16)__builtin_amdgcn_ldexpf(widen_t<BF16>((w[c][2 * j] >> (16 * i)) & 0xffffu), -e),
+                      (_Float16)__builtin_amdgcn_ldexpf(widen_t<BF16>((w[c][2 * j + 1] >> (16 * i)) & 0xffffu), -e)};
+        f[i][j] = as_u32(p);
       }
-      f4 o = st->o[2 * c + e];
-      o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_b8(f), as_b8(hi), o, 0, 0, 0);
-      o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_b8(f), as_b8(lo), o, 0, 0, 0);
-      if constexpr (!BF16)
-        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_b8(f2), as_b8(hi), o, 0, 0, 0);
-      st->o[2 * c + e] = o;
-    }
+    add_operand<D, QT>(f[0], 2 * c, hi, lo, st);
+    add_operand<D, QT>(f[1], 2 * c + 1, hi, lo, st);
   }
 }
 
@@ -362,15 +359,15 @@ __global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch 
   }
   if (lo <= full && full < hi && (full - lo) % 4 == wave) {
     const RQ_GLOBAL uint16_t* kt = gptr(a.c.tail) + (size_t)unit * 2 * kBlockTokens * D;
+    f4 s[QT][2];
 #pragma unroll
     for (int n = 0; n < QT; ++n) {
-      f4 s[2];
-      tail_products<D, BF16>(a, b, h, kt, q[n], s);
-      block_scores<D>(a, q[n], pos, a.qscale, full * kBlockTokens, past, true, s);
-      keep(s, n, full);
-      probabilities<D>(&st[n], s);
-      add_tail<FMT, D, BF16>(kt + kBlockTokens * D, total % kBlockTokens, s, &st[n]);
+      tail_products<D, BF16>(a, b, h, kt, q[n], s[n]);
+      block_scores<D>(a, q[n], pos, a.qscale, full * kBlockTokens, past, true, s[n]);
+      keep(s[n], n, full);
+      probabilities<D>(&st[n], s[n]);
     }
+    add_tail<FMT, D, BF16, QT>(kt + kBlockTokens * D, total % kBlockTokens, s, st);
   }
 
 #pragma unroll

@@ -131,12 +131,12 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
   Plan p{};
   const int64_t G = c->n_q_heads / c->n_kv_heads, u = (int64_t)units(c);
   p.row_tiles = (int)((a->n_new * G + 15) / 16);
+  p.prompt = p.row_tiles > 2;
   int64_t blocks = (a->max_tokens + rq::kBlockTokens - 1) / rq::kBlockTokens;
   if (a->window) {
-    const int64_t seen = ((int64_t)a->window + 16 / G + 1) / rq::kBlockTokens + 2;
+    const int64_t seen = ((int64_t)a->window + (p.prompt ? 128 / G + 1 : a->n_new)) / rq::kBlockTokens + 2;
     blocks = seen < blocks ? seen : blocks;
   }
-  p.prompt = p.row_tiles > 2;
   int64_t s;
   if (p.prompt) {
     s = 2 * (int64_t)rq::device_cus() / (u * ((a->n_new * G + 127) / 128));
@@ -264,6 +264,8 @@ rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_bl
   if (!std::isfinite(qscale) || !std::isfinite(q->cap * log2e))
     return fail(RQ_EINVAL, "scale %g and cap %g leave the fp32 range", q->scale, q->cap);
   const Plan p = plan_attention(c, q);
+  if ((double)p.row_tiles * p.splits * units(c) > 2.0e9)
+    return fail(RQ_EUNSUPPORTED, "more than 2e9 tiles of 16 query rows");
   if (ws_bytes < p.bytes())
     return fail(RQ_ESMALLWS, "workspace %llu bytes < %llu needed", (unsigned long long)ws_bytes,
                 (unsigned long long)p.bytes());

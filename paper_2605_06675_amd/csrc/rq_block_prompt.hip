@@ -94,10 +94,10 @@ __device__ __forceinline__ void store_tile(const TileLoad& t, int slot0, int slo
   }
 }
 
-// The tail's rows as the block of 32 tokens at `at` of the tile: fp16 numbers
-// of their own, bf16 ones divided by a power of two that brings the largest of
-// the side below 1 (returned as the block's scales).  Rows from n_tail on count
-// as zero.  The whole workgroup calls it.
+// The tail's rows as the block of 32 tokens at `at` of the tile, divided by a
+// power of two that brings the largest of the side below 1 (returned as the
+// block's scales; fp16 holds the others to 2^-25 of it).  Rows from n_tail on
+// count as zero.  The whole workgroup calls it.
 template <int FMT, int D, bool BF16>
 __device__ __forceinline__ void store_tail(const RQ_GLOBAL uint16_t* kt, int n_tail, int at, uint8_t* sk,
                                            uint8_t* sv, float* red, float* ks, float* vs) {
@@ -118,44 +118,41 @@ __device__ __forceinline__ void store_tail(const RQ_GLOBAL uint16_t* kt, int n_t
       v[p][i] = 0u;
       if (quad < 8 && 4 * quad + i < n_tail)
         v[p][i] = *(const RQ_GLOBAL uint32_t*)(vt + (4 * quad + i) * D + 2 * (id % (D / 2)));
-      km = __builtin_fmaxf(km, __builtin_fmaxf(__builtin_fabsf(widen_t<true>(k[p][i] & 0xffffu)),
-                                               __builtin_fabsf(widen_t<true>(k[p][i] >> 16))));
-      vm = __builtin_fmaxf(vm, __builtin_fmaxf(__builtin_fabsf(widen_t<true>(v[p][i] & 0xffffu)),
-                                               __builtin_fabsf(widen_t<true>(v[p][i] >> 16))));
+      km = __builtin_fmaxf(km, __builtin_fmaxf(__builtin_fabsf(widen_t<BF16>(k[p][i] & 0xffffu)),
+                                               __builtin_fabsf(widen_t<BF16>(k[p][i] >> 16))));
+      vm = __builtin_fmaxf(vm, __builtin_fmaxf(__builtin_fabsf(widen_t<BF16>(v[p][i] & 0xffffu)),
+                                               __builtin_fabsf(widen_t<BF16>(v[p][i] >> 16))));
     }
   }
-  int ke = 0, ve = 0;
-  if constexpr (BF16) {
-    for (int d = 32; d >= 1; d >>= 1) {
-      km = __builtin_fmaxf(km, __shfl_xor(km, d, 64));
-      vm = __builtin_fmaxf(vm, __shfl_xor(vm, d, 64));
-    }
-    if (lane == 0) {
-      red[wave] = km;
-      red[8 + wave] = vm;
-    }
-    __syncthreads();
-    for (int i = 0; i < kWaves; ++i) {
-      km = __builtin_fmaxf(km, red[i]);
-      vm = __builtin_fmaxf(vm, red[8 + i]);
-    }
-    ke = km > 0.0f ? __builtin_amdgcn_frexp_expf(km) : 0;
-    ve = vm > 0.0f ? __builtin_amdgcn_frexp_expf(vm) : 0;
-    auto pair = [](uint32_t x, int e) {
-      const h2 y = {(_Float16)__builtin_amdgcn_ldexpf(widen_t<true>(x & 0xffffu), -e),
-                    (_Float16)__builtin_amdgcn_ldexpf(widen_t<true>(x >> 16), -e)};
-      return as_u32(y);
-    };
-#pragma unroll
-    for (int p = 0; p < kPasses; ++p)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        k[p][i] = pair(k[p][i], ke);
-        v[p][i] = pair(v[p][i], ve);
-      }
+  for (int d = 32; d >= 1; d >>= 1) {
+    km = __builtin_fmaxf(km, __shfl_xor(km, d, 64));
+    vm = __builtin_fmaxf(vm, __shfl_xor(vm, d, 64));
   }
+  if (lane == 0) {
+    red[wave] = km;
+    red[8 + wave] = vm;
+  }
+  __syncthreads();
+  for (int i = 0; i < kWaves; ++i) {
+    km = __builtin_fmaxf(km, red[i]);
+    vm = __builtin_fmaxf(vm, red[8 + i]);
+  }
+  const int ke = km > 0.0f ? __builtin_amdgcn_frexp_expf(km) : 0;
+  const int ve = vm > 0.0f ? __builtin_amdgcn_frexp_expf(vm) : 0;
+  auto pair = [](uint32_t x, int e) {
+    const h2 y = {(_Float16)__builtin_amdgcn_ldexpf(widen_t<BF16>(x & 0xffffu), -e),
+                  (_Float16)__builtin_amdgcn_ldexpf(widen_t<BF16>(x >> 16), -e)};
+    return as_u32(y);
+  };
+#pragma unroll
+  for (int p = 0; p < kPasses; ++p)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      k[p][i] = pair(k[p][i], ke);
+      v[p][i] = pair(v[p][i], ve);
+    }
   *ks = __builtin_amdgcn_ldexpf(1.0f, ke);
-  *vs = __builtin_amdgcn_ldexpf(kValueUnit<FMT>, ve);
+  *vs = vm > 0.0f ? __builtin_amdgcn_ldexpf(kValueUnit<FMT>, ve) : 0.0f;
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) {
     const int id = threadIdx.x + p * kThreads, tok = id / kPieces, quad = id / (D / 2);
@@ -385,7 +382,8 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
       top = __builtin_fmaxf(top, __builtin_fmaf(x, f[t], off));
     }
     const float sv = __builtin_fmaxf(tvs[0], tvs[1]);
-    const bool grow = unit2 == 0.0f || sv * unit2 > 128.0f;      // (the same in every lane)
+    // (the same in every lane; scales of zero have no unit to follow)
+    const bool grow = sv > 0.0f && (unit2 == 0.0f || sv * unit2 > 128.0f);
     if (grow || __any(top > m + 8.0f)) {
       top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
       const float mn = __builtin_fmaxf(m, top);
@@ -393,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
       m = mn;
       l *= by;
       if (grow) {
-        int e = sv > 0.0f ? __builtin_amdgcn_frexp_expf(sv) : 0;
+        int e = __builtin_amdgcn_frexp_expf(sv);
         e = e < -100 ? -100 : e;
         const float u = __builtin_amdgcn_ldexpf(128.0f, -e);
         by *= unit2 == 0.0f ? 1.0f : u / unit2;

@@ -102,7 +102,7 @@ class Rig:
         [n][G][D]."""
         u = self.u[b][h]
         K, V = (u.values(s).astype(np.float64) for s in (0, 1))
-        q = np.abs(q.astype(np.float64))
+        q, scale = np.abs(q.astype(np.float64)), abs(scale)
         a = scale * 1.4427 * (q @ np.abs(K).T).max(-1)
         a2 = scale * 1.4427 * (q.max(-1) * np.abs(K).sum(-1).max())
         far = 0.0 if slopes is None else 1.4427 * float(np.max(slopes)) * float(u.pos.max())
@@ -329,6 +329,40 @@ def test_attend_equal_scores_give_the_mean(fmt):
         for h in range(2):
             mean = r.u[b][h].values(1).astype(np.float64).mean(0)
             assert np.abs(o[b, 2 * h, 0] - mean).max() <= 4 * 2.0 ** -22 * np.abs(r.u[b][h].values(1)).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("kw", [dict(), dict(cap=7.0), dict(slopes=[0.1, 0.2, 0.3, 0.4])])
+@pytest.mark.parametrize("n", [1, 6, 70])
+def test_attend_negative_and_zero_scale(dtype, kw, n):
+    r = Rig("int8", dtype, D=64, cap=256)
+    r.append(201)
+    for scale in (-0.2, 0.0):
+        r.attend(n, scale=scale, accumulate=True, **kw)
+
+
+@both
+@pytest.mark.parametrize("dtype,size", [("fp16", 2.0 ** -10), ("bf16", 2.0 ** -60), ("fp16", 2.0 ** 12),
+                                        ("bf16", 2.0 ** 40)])
+@pytest.mark.parametrize("zeros", [0, 32, 64])
+@pytest.mark.parametrize("L", [7, 64, 100])
+@pytest.mark.parametrize("n", [1, 40])
+def test_attend_precision_of_small_and_large_values(fmt, dtype, size, zeros, L, n):
+    """Queries of zero: the output is the values' mean, to 22 bits of their
+    largest, wherever their magnitude lies, behind blocks of zeros, in the
+    tail, and to 2^-25 in each of its 32 numbers' fp16 forms."""
+    r = Rig(fmt, dtype, cap=256)
+    if zeros:
+        z = torch.zeros(2, 2, zeros, 128, dtype=r.dt)
+        r.append(zeros, kv=(z, z))
+    k, v = r.kv(max(L, n))
+    r.append(max(L, n), kv=(k, (v.float() * size).to(r.dt)))
+    o = r.attend(n, q=torch.zeros(2, 4, n, 128, dtype=r.dt)).cpu().double().numpy()
+    for b in range(2):
+        for h in range(2):
+            V = r.u[b][h].values(1).astype(np.float64)
+            mean = V[:len(V) - n + 1].mean(0)
+            assert np.abs(o[b, 2 * h, 0] - mean).max() <= 6 * 2.0 ** -22 * np.abs(V).max()
 
 
 def test_attend_zero_blocks():
@@ -653,7 +687,7 @@ def test_python_refusals():
     q = torch.zeros(2, 4, 1, 128, dtype=r.dt, device="cuda")
     o = torch.zeros_like(q)
     ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
-    for kw in (dict(q=q.half()), dict(q=q[:, :2]), dict(out=o.double()), dict(out=o[:1]), dict(ws=ws.cpu()),
+    for kw in (dict(q=q.half()), dict(q=q[:, :2]), dict(out=o[:1].expand(2, -1, -1, -1)), dict(out=o.double()), dict(out=o[:1]), dict(ws=ws.cpu()),
                dict(ws=ws[::2]), dict(slopes=torch.zeros(3, device="cuda")), dict(slopes=torch.zeros(4)),
                dict(new_len=past.long())):
         a = dict(q=q, out=o, ws=ws)
