@@ -482,9 +482,12 @@ rq_status rq_block_attention_workspace(const rq_block_cache* c,
  * Rows i >= new_len of out are left as they were.  With accumulate, each
  * slot's weight grows by its softmax probabilities summed over the call's
  * query tokens and the kv-head's query heads.
- * Accuracy: scores, softmax and sums are fp32 on exact operands (queries as
- * fp16 relative to their row's largest element); probabilities times the
- * value scale are rounded to 22 bits relative to the largest.
+ * Accuracy: scores, softmax and sums are fp32 on exact operands (queries, and
+ * the tail's numbers, as fp16 relative to the largest of their row or block);
+ * probabilities times the value scale are rounded to 22 bits relative to the
+ * largest.  Calls of more than 32 query rows a kv-head (n_new times the heads
+ * of a group) round them to 11 bits where the output is bf16, and take a cap's
+ * tanh to 2^-22 of the cap unless the output is fp32, and for the weights.
  * ws: device scratch, 16-byte aligned, contents arbitrary; calls that share
  * it must not overlap.  Asynchronous. */
 rq_status rq_block_attention(const rq_block_cache* c, int32_t layer,

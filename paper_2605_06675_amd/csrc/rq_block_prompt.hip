@@ -11,8 +11,9 @@
 //
 // A block's value scale goes into the exponent: P' = 2^(x - m + log2(by)),
 // by = value scale * unit, and the row's sum takes the block's sum of P' / by.
-// P' is rounded to fp16 (2^-12, less than the rounding of a bf16 output and as
-// much as that of an fp16 one); for fp32 outputs (EXACT) it is a pair hi + lo.
+// P' is rounded to fp16 (2^-11, an eighth of a bf16 output's own rounding); for
+// fp16 and fp32 outputs (EXACT) it is a pair hi + lo, a third more time (4 x 512
+// tokens over 8192: 342 and 449 us).
 #include "rq_block.h"
 
 namespace rq {
@@ -333,9 +334,10 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
     const bool masked = a.window || slot0 + kTile - 1 > past + wave_first;
     // scores are s f + off; a mask needs them formed (f may be 0)
     float f[2] = {tks[0] * qs, tks[1] * qs}, off = 0.0f;
-    if (a.cap != 0.0f && !EXACT) {
-      // cap tanh(x) = cap - 2 cap / (1 + e^(2x)): off by 2^-23 cap, which the
-      // rounding of P' hides
+    const bool fine = EXACT && a.out_dtype == RQ_F32;      // tanh to fp32
+    if (a.cap != 0.0f && !fine) {
+      // cap tanh(x) = cap - 2 cap / (1 + e^(2x)): off by 2^-22 cap, which the
+      // output's rounding hides
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const float e2 = f[t] * 2.8853900817779268f;
@@ -345,12 +347,12 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
       }
       off = a.cap;
     }
-    if (far || masked || (EXACT && a.cap != 0.0f)) {
+    if (far || masked || (fine && a.cap != 0.0f)) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[t][i] = __builtin_fmaf(s[t][i], f[t], off);
-        if (EXACT && a.cap != 0.0f) {
+        if (fine && a.cap != 0.0f) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[t][i] = a.cap * tanh_f(s[t][i]);
         }
@@ -484,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
 template <int FMT, int D, bool BF16>
 hipError_t launch(const BlockAttendLaunch& a, hipStream_t s) {
   const dim3 grid((unsigned)((a.n * a.G + kRows - 1) / kRows * a.splits) * a.c.B * a.c.H);
-  if (a.out_dtype == RQ_F32)
+  if (a.out_dtype != RQ_BF16)
     hipLaunchKernelGGL((block_prompt_kernel<FMT, D, BF16, true>), grid, dim3(kThreads), 0, s, a);
   else
     hipLaunchKernelGGL((block_prompt_kernel<FMT, D, BF16, false>), grid, dim3(kThreads), 0, s, a);

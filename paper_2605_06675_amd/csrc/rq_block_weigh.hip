@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
     for (int t = 0; t < 2; ++t) {
       float f = ks[t] * r.qs, off = 0.0f;      // scores are s f + off
       if (a.cap != 0.0f) {
-        // cap tanh(x) = cap - 2 cap / (1 + e^(2x)), off by 2^-23 cap
+        // cap tanh(x) = cap - 2 cap / (1 + e^(2x)), off by 2^-22 cap
         const float e2 = f * 2.8853900817779268f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[t][i] = __builtin_amdgcn_rcpf(-1.0f - exp2_f(s[t][i] * e2));
