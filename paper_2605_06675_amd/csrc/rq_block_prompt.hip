@@ -322,15 +322,17 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
     if (idle || slot0 > past + wave_last) return;
     f16v s[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+    // (the two blocks' sums in turn: neither waits for its last product)
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
+    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
         const h8 f = *(const h8*)(sh_k[buf] + key_at<D>(32 * t + col, 2 * k + hl));
         s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[k], s[t], 0, 0, 0);
       }
-    }
     const bool masked = a.window || slot0 + kTile - 1 > past + wave_first;
     // scores are s f + off; a mask needs them formed (f may be 0)
     float f[2] = {tks[0] * qs, tks[1] * qs}, off = 0.0f;
