@@ -674,7 +674,14 @@ def rq_block_evict(src, dst, layer, lengths, keep, new_lengths, ws, n_sink=4,
 class BlockCache:
     """Device buffers (torch), lengths and the descriptor of one block-scaled
     8-bit cache.  `lengths` (device int32 [n_layers][batch]) says what each
-    sequence holds, `bound` (host) at most how much any does."""
+    sequence holds, `bound` (host) at most how much any does.
+
+    The calls of one cache share a workspace: they go to one stream, or follow
+    each other by the caller's events.  All can be captured into a graph
+    (evict with a given `into`).  A captured call is planned for the whole
+    capacity; its replays move the lengths on, and drop tokens that do not
+    fit.  From then on the layer's `bound` is the capacity, and a call that
+    appends to it outside a graph may wait to read the lengths."""
 
     def __init__(self, format, dtype, n_layers, batch, n_kv_heads, n_q_heads,
                  head_dim, capacity, device="cuda", weights=False):
@@ -694,33 +701,66 @@ class BlockCache:
         self.lengths = torch.zeros(n_layers, batch, dtype=torch.int32,
                                    device=device)
         self.bound = [0] * n_layers
+        self._replayed = set()      # layers that a graph appends to
         self._ws = None
+        self._held = []             # workspaces that a graph writes to
+
+    def _on(self, stream):
+        """The call's stream, and whether it is being captured."""
+        import torch
+        if stream is None:
+            stream = torch.cuda.current_stream(self.codes.device)
+        with torch.cuda.stream(stream):
+            return stream, torch.cuda.is_current_stream_capturing()
 
     def _workspace(self, need, stream):
         import torch
+        s, capturing = self._on(stream)
         if self._ws is None or self._ws.numel() < need:
-            s = torch.cuda.current_stream(self.codes.device) if stream is None else stream
+            if self._ws is not None:
+                self._ws.record_stream(s)
             with torch.cuda.stream(s):
                 self._ws = torch.empty(max(need, 16), dtype=torch.uint8,
                                        device=self.codes.device)
+        if capturing and not any(w is self._ws for w in self._held):
+            self._held.append(self._ws)
         return self._ws
 
     def _grow(self, layer, n, new_len, stream):
         import torch
-        s = torch.cuda.current_stream(self.codes.device) if stream is None else stream
+        s, capturing = self._on(stream)
         with torch.cuda.stream(s):
-            self.lengths[layer] += n if new_len is None else new_len.clamp(0, n)
-        self.bound[layer] += n
+            row = self.lengths[layer]
+            row += n if new_len is None else new_len.clamp(0, n)
+            if capturing:
+                row.clamp_(max=self.desc.capacity)
+        if layer not in self._replayed:
+            self.bound[layer] += n
 
-    def _room(self, layer, n):
-        if self.bound[layer] + n > self.desc.capacity:
-            raise ValueError(f"tokens {self.bound[layer]} + {n} exceed the "
-                             f"capacity {self.desc.capacity}")
+    def _room(self, layer, n, stream):
+        """Bound on the tokens after n more."""
+        import torch
+        capacity = self.desc.capacity
+        s, capturing = self._on(stream)
+        if capturing:
+            self._replayed.add(layer)
+            self.bound[layer] = capacity
+            return capacity
+        held = self.bound[layer]
+        if held + n > capacity:          # (an upper bound: padding counts)
+            with torch.cuda.stream(s):
+                held = int(self.lengths[layer].max())
+            if held + n > capacity:
+                raise ValueError(f"tokens {held} + {n} exceed the capacity "
+                                 f"{capacity}")
+            if layer not in self._replayed:
+                self.bound[layer] = held
+        return min(self.bound[layer] + n, capacity)
 
     def append(self, layer, k, v, new_len=None, stream=None):
         """Append k, v ([batch][n_kv_heads][n][head_dim]); new_len: how many
         of the n rows each sequence takes."""
-        self._room(layer, k.shape[2])
+        self._room(layer, k.shape[2], stream)
         rq_block_append(self.desc, layer, self.lengths[layer], k, v, new_len,
                         stream)
         self._grow(layer, k.shape[2], new_len, stream)
@@ -731,7 +771,7 @@ class BlockCache:
                                             kw.get("accumulate", False),
                                             kw.get("window", 0))
         ws = self._workspace(need, stream)
-        s = torch.cuda.current_stream(self.codes.device) if stream is None else stream
+        s = self._on(stream)[0]
         if out is None:
             with torch.cuda.stream(s):
                 out = torch.zeros_like(q) if new_len is not None else torch.empty_like(q)
@@ -744,30 +784,31 @@ class BlockCache:
         [head_dim]; scale, cap, window, slopes, accumulate as
         rq_block_attention)."""
         import torch
-        s = torch.cuda.current_stream(self.codes.device) if stream is None else stream
+        s, capturing = self._on(stream)
         with torch.cuda.stream(s):
             past = self.lengths[layer] - (q.shape[2] if new_len is None
                                           else new_len.clamp(0, q.shape[2]))
-        return self._attend(layer, past, self.bound[layer], q, out, new_len,
-                            stream, kw)
+        bound = self.desc.capacity if capturing else self.bound[layer]
+        return self._attend(layer, past, bound, q, out, new_len, stream, kw)
 
     def step(self, layer, k, v, q, out=None, new_len=None, stream=None, **kw):
-        """Append k, v and attend with the same tokens' q."""
-        self._room(layer, k.shape[2])
+        """Append k, v and attend with the same tokens' q.  Where the
+        attention is refused, the tokens are appended all the same."""
+        bound = self._room(layer, k.shape[2], stream)
         past = self.lengths[layer]
         rq_block_append(self.desc, layer, past, k, v, new_len, stream)
-        out = self._attend(layer, past, self.bound[layer] + k.shape[2], q, out,
-                           new_len, stream, kw)
-        self._grow(layer, k.shape[2], new_len, stream)
-        return out
+        try:
+            return self._attend(layer, past, bound, q, out, new_len, stream, kw)
+        finally:
+            self._grow(layer, k.shape[2], new_len, stream)
 
     def evict(self, keep, n_sink=4, n_recent=32, into=None, stream=None):
         """Shrink every layer to at most `keep` tokens a sequence: into
         another BlockCache of this shape, or a new one of the least
         capacity."""
         import torch
+        s, capturing = self._on(stream)
         if into is None:
-            s = torch.cuda.current_stream(self.codes.device) if stream is None else stream
             with torch.cuda.stream(s):
                 into = BlockCache(*self.shape, (keep + 31) // 32 * 32,
                                   device=self.codes.device, weights=True)
@@ -776,5 +817,8 @@ class BlockCache:
             rq_block_evict(self.desc, into.desc, layer, self.lengths[layer],
                            keep, into.lengths[layer], ws, n_sink, n_recent,
                            stream)
-            into.bound[layer] = min(self.bound[layer], keep)
+            if capturing:
+                into._replayed.add(layer)
+            into.bound[layer] = (into.desc.capacity if layer in into._replayed
+                                 else min(self.bound[layer], keep))
         return into

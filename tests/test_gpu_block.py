@@ -650,6 +650,108 @@ def test_captured_step_follows_the_lengths():
     r.check()
 
 
+def graph_of(call):
+    """call(), captured after nothing has run but what it needs."""
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    return graph, out
+
+
+def test_captured_steps_share_the_cache_with_eager_ones():
+    """Two captured steps (one token, three tokens) and eager calls take turns
+    on one BlockCache: its workspace grows between the replays, its host bound
+    is that of the first captures."""
+    r = Rig("e4m3", "bf16", B=2, cap=512)
+    r.append(70, [70, 33])
+    runs = {}
+    for n in (1, 3):
+        k, v = (torch.zeros(2, 2, n, 128, dtype=r.dt, device="cuda") for _ in range(2))
+        q = torch.zeros(2, 4, n, 128, dtype=r.dt, device="cuda")
+        runs[n] = (k, v, q) + graph_of(lambda: r.c.step(0, k, v, q, accumulate=True))
+    assert r.c.lengths.tolist() == [[70, 33]]
+    held = []                                   # memory that the allocator hands out again
+    for turn in range(12):
+        for n in (1, 3, 40 if turn % 3 == 2 else 2):
+            k, v = r.kv(n)
+            q = r.randn(2, 4, n, 128).to(r.dt)
+            before = np.nan_to_num(r.weights())
+            if n in runs:
+                sk, sv, sq, graph, o = runs[n]
+                sk.copy_(k)
+                sv.copy_(v)
+                sq.copy_(q)
+                graph.replay()
+            else:
+                o = r.c.step(0, k.cuda(), v.cuda(), q.cuda(), accumulate=True)
+                held.append(torch.full((1 << 20,), math.nan, device="cuda"))
+            torch.cuda.synchronize()
+            r.took(k, v)
+            r.compare(q, o, accumulate=True, before=before)
+    assert not any((~h.isnan()).any() for h in held)
+    assert r.c.lengths.tolist() == [r.lengths()] and r.c.bound == [512]
+    r.check()
+    q = r.randn(2, 4, 1, 128).to(r.dt)
+    r.compare(q, r.c.attention(0, q.cuda()))
+    with pytest.raises(ValueError):
+        r.c.append(0, *(x.cuda() for x in r.kv(512 - r.lengths()[0] + 1)))
+    r.append(512 - r.lengths()[0])
+    r.check()
+
+
+def test_captured_attention_and_eviction():
+    """A graph that attends, weighs and evicts, replayed over a cache that
+    grows by eager calls in between."""
+    r = Rig("int8", "fp16", B=2, cap=512)
+    to = Rig("int8", "fp16", B=2, cap=96)
+    r.append(50)
+    q = torch.zeros(2, 4, 1, 128, dtype=r.dt, device="cuda")
+    r.c.attention(0, q, accumulate=True)
+
+    def call():
+        o = r.c.attention(0, q, accumulate=True)
+        r.c.evict(90, into=to.c)
+        return o
+    graph, o = graph_of(call)
+    r.c.weights.view(2, 2, 512)[:, :, :50] = 0.0
+    for turn in range(5):
+        x = r.randn(2, 4, 1, 128).to(r.dt)
+        q.copy_(x)
+        before = np.nan_to_num(r.weights())
+        graph.replay()
+        torch.cuda.synchronize()
+        r.compare(x, o, accumulate=True, before=before)
+        want = r.c.evict(90)
+        kept = min(r.lengths()[0], 90)
+        assert to.c.lengths.tolist() == want.lengths.tolist() == [[kept] * 2] and to.c.bound == [96]
+        assert torch.equal(to.c.positions.view(4, 96)[:, :kept], want.positions.view(4, 96)[:, :kept])
+        assert torch.equal(to.c.codes.view(8, 96, 128)[:, :kept // 32 * 32], want.codes.view(8, 96, 128)[:, :kept // 32 * 32])
+        r.append(60)
+
+
+def test_padding_does_not_use_up_the_capacity():
+    r = Rig("int8", "bf16", cap=96)
+    for new in ([20, 3], [1, 20], [0, 17], [10, 9], [12, 0]):
+        r.append(20, new)
+    r.check()
+    assert r.c.lengths.tolist() == [[43, 49]]
+    with pytest.raises(ValueError):
+        r.append(60, [1, 1])          # 49 + 60 rows, whatever they hold
+
+
+def test_refused_attention_leaves_the_step_s_tokens():
+    r = Rig("int8", "bf16", cap=64, weights=False)
+    r.append(40)
+    k, v = r.kv(20)
+    q = torch.zeros(2, 4, 20, 128, dtype=r.dt, device="cuda")
+    with pytest.raises(rq.RQError):
+        r.c.step(0, k.cuda(), v.cuda(), q, accumulate=True)       # it keeps no weights
+    r.took(k, v)
+    assert r.c.lengths.tolist() == [[60, 60]] and r.c.bound == [60]
+    q = r.randn(2, 4, 1, 128).to(r.dt)
+    r.compare(q, r.c.attention(0, q.cuda()))
+
+
 def test_another_stream_and_shared_workspace_in_order():
     r = Rig("e4m3", "bf16", cap=256)
     side = torch.cuda.Stream()
