@@ -21,6 +21,7 @@ constexpr int kTicketSplits = 32;
 // (up to 32 keys a thread); longer ones in parts of a multiple of kSelectPart, at
 // most kSelectParts of them.
 constexpr int kSelectShort = 32768, kSelectPart = 8192, kSelectParts = 32;
+constexpr int kSelectState = 12;     // words a unit (three a launch)
 
 // One layer of a cache, and its shape.
 struct BlockLayer {
@@ -82,7 +83,7 @@ struct BlockEvictLaunch {
   int32_t* slots;          // [unit][keep] source slots, ascending
   // selection of units in several parts (parts > 1) of `part` tokens each
   int part, parts;
-  uint32_t* state;         // [unit][8]: what each launch found
+  uint32_t* state;         // [unit][kSelectState]: what each launch found
   uint32_t* before;        // [unit][parts]: kept keys of the parts before
   uint32_t* counts;        // [3][unit][parts][2048]
 };

@@ -3,9 +3,8 @@
 // the rest stay (ties: the lowest slot), in order, and are quantized again in
 // blocks of the new cache.
 //
-// Selection: the k-th largest weight by radix, digits of 11, 11 and 10 bits;
-// then one ordered pass writes the kept slots.  The copy reads 2 D bytes a kept token
-// and side and writes as many.
+// Selection: the last weight that stays, by radix; then one ordered pass writes
+// the kept slots.  The copy reads 2 D bytes a kept token and side and writes as many.
 #include "rq_block.h"
 
 namespace rq {
@@ -16,22 +15,55 @@ constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 constexpr int kBins = 2048;
 // A wave's lanes would add to one counter one after the other where the
 // weights share their leading digits: each counter is held four times, a lane's
-// by its number (128 units of 8192 tokens 15.7 us; sixteen times, with more to
-// clear and to add up, 18.3).
+// by its number (128 units of 8192 tokens with sixteen copies 2.6 us more, to
+// clear and to add up).
 constexpr int kCopies = 4;
 
+constexpr int kFew = 256;     // keys that are ranked one against the other
+
 struct SelectShared {
-  uint32_t hist[kBins * kCopies];
+  __align__(16) uint32_t hist[kBins * kCopies];
+  __align__(16) uint32_t few[kFew];
   uint32_t sum[kSelWaves], tie[kSelWaves];
-  uint32_t pick[3];
+  uint32_t pick[3], n_few;
 };
 
-// Where the search stands: the leading digits of the k-th largest key, and how
-// many of the keys with these digits stay.
+// Where the search stands: the last key that stays is among the `span` keys
+// from `lo` on, the need-th largest of the `in` of them that occur.
 struct Found {
-  uint32_t prefix, need;
-  uint32_t all;             // all of them do
+  uint32_t lo, span, need, in;
 };
+
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint32_t lane_move(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+
+// Sums over the lanes up to this one (moves within rows of 16 lanes, then of
+// the rows' last lanes).
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  x += lane_move<0x111>(x);
+  x += lane_move<0x112>(x);
+  x += lane_move<0x114>(x);
+  x += lane_move<0x118>(x);
+  x += lane_move<0x142, 0xa>(x);
+  return x + lane_move<0x143, 0xc>(x);
+}
+__device__ __forceinline__ uint32_t last_lane(uint32_t x) { return __builtin_amdgcn_readlane(x, 63); }
+
+// Of one number a wave: the sum over the waves before `end`.
+__device__ __forceinline__ uint32_t sum_before(const uint32_t x[kSelWaves], int end) {
+  static_assert(kSelWaves == 16, "a row of lanes");
+  const int i = threadIdx.x & 15;
+  uint32_t v = x[i];
+  v = i < end ? v : 0u;
+  v += lane_move<0x128>(v);
+  v += lane_move<0x124>(v);
+  v += lane_move<0x122>(v);
+  v += lane_move<0x121>(v);
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 
 // A weight's place in the order, as an unsigned number above 0; the tokens that
 // stay in any case are above all others.
@@ -43,150 +75,208 @@ __device__ __forceinline__ uint32_t rank_key(float w, int slot, int L, int sink,
   return key < 1u ? 1u : (key > 0xfffffffeu ? 0xfffffffeu : key);
 }
 
-// Keys of N x 4 tokens a lane.  A wave's tokens follow each other from `base`
+// Weights of N x 4 tokens a lane.  A wave's tokens follow each other from `base`
 // on: group i of a lane is base + 256 i + 4 lane.  (w is 16-byte aligned, and
 // its rows hold a multiple of 32.)
 template <int N>
-__device__ __forceinline__ void load_ranks(const BlockEvictLaunch& a, const RQ_GLOBAL float* w,
-                                           int base, int L, uint32_t key[4 * N]) {
+__device__ __forceinline__ void load_weights(const RQ_GLOBAL float* w, int base, int end, f4 x[N]) {
   const int lane = threadIdx.x & 63;
-  f4 x[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int t = base + 256 * i + 4 * lane;
-    x[i] = t < L ? *(const RQ_GLOBAL f4*)(w + t) : (f4){0.0f, 0.0f, 0.0f, 0.0f};
+    x[i] = t < end ? *(const RQ_GLOBAL f4*)(w + t) : (f4){0.0f, 0.0f, 0.0f, 0.0f};
   }
+}
+
+template <int N>
+__device__ __forceinline__ void rank_keys(const BlockEvictLaunch& a, const f4 x[N], int base, int L,
+                                          uint32_t key[4 * N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      key[4 * i + j] = rank_key(x[i][j], base + 256 * i + 4 * lane + j, L, a.n_sink, a.n_recent);
+      key[4 * i + j] = rank_key(x[i][j], base + 256 * i + 4 * ((int)threadIdx.x & 63) + j, L, a.n_sink, a.n_recent);
 }
 
-// Digits of 11, 11 and 10 bits.
-__device__ __forceinline__ int digit_shift(int level) { return level == 0 ? 21 : (level == 1 ? 10 : 0); }
+// The first digit: weights from 2^-24 to 2^8 in 32 steps an octave (2^18 keys),
+// all others in steps of 2^22 keys.  Two digits of 11 bits then end the search.
+constexpr uint32_t kFineFrom = 0xb3800000u, kFineTo = 0xc3800000u;
+constexpr uint32_t kFineAt = kFineFrom >> 22, kHighAt = kFineAt + ((kFineTo - kFineFrom) >> 18);
+static_assert(kHighAt + ((0xffffffffu - kFineTo) >> 22) < kBins, "first digits");
+
+__device__ __forceinline__ uint32_t first_digit(uint32_t key) {
+  if (key < kFineFrom) return key >> 22;
+  return key < kFineTo ? kFineAt + ((key - kFineFrom) >> 18) : kHighAt + ((key - kFineTo) >> 22);
+}
+
+// The keys of a first digit (without 0 and those that stay in any case).
+__device__ __forceinline__ void first_range(uint32_t d, uint32_t* lo, uint32_t* span) {
+  const bool fine = d >= kFineAt && d < kHighAt;
+  *lo = d < kFineAt ? d << 22 : (fine ? kFineFrom + ((d - kFineAt) << 18) : kFineTo + ((d - kHighAt) << 22));
+  *span = 1u << (fine ? 18 : 22);
+  if (d == 0) {
+    *lo += 1;
+    *span -= 1;
+  }
+  if (*span > 0xffffffffu - *lo) *span = 0xffffffffu - *lo;
+}
+
+// Later digits: the distance from f.lo, its 11 leading bits.
+__device__ __forceinline__ int digit_shift(const Found& f) {
+  const int bits = 32 - __builtin_clz((f.span - 1) | 1u);
+  return bits > 11 ? bits - 11 : 0;
+}
 
 template <int N>
 __device__ __forceinline__ void count_digits(SelectShared& sh, const uint32_t key[4 * N], int level,
-                                             uint32_t prefix) {
-  const int shift = digit_shift(level), copy = threadIdx.x & (kCopies - 1);
-  const uint32_t mask = level == 2 ? 1023u : 2047u;
+                                             const Found& f) {
+  const int shift = level == 0 ? 0 : digit_shift(f), copy = threadIdx.x & (kCopies - 1);
 #pragma unroll
   for (int i = 0; i < 4 * N; ++i) {
-    const bool in = level == 0 || (level == 1 ? key[i] >> 21 : key[i] >> 10) == prefix;
-    if (in && key[i]) atomicAdd(&sh.hist[((key[i] >> shift) & mask) * kCopies + copy], 1u);
+    const uint32_t from = key[i] - f.lo;
+    if (from < f.span)
+      atomicAdd(&sh.hist[(level == 0 ? first_digit(key[i]) : from >> shift) * kCopies + copy], 1u);
   }
 }
 
 __device__ __forceinline__ void clear_digits(SelectShared& sh) {
-  for (int i = threadIdx.x; i < kBins * kCopies; i += kSelThreads) sh.hist[i] = 0;
+#pragma unroll
+  for (int i = 0; i < kBins * kCopies; i += 4 * kSelThreads) *(u4*)&sh.hist[i + 4 * threadIdx.x] = (u4){0u, 0u, 0u, 0u};
+  if (threadIdx.x < kFew) sh.few[threadIdx.x] = 0;
+  if (threadIdx.x == 0) sh.n_few = 0;
   __syncthreads();
 }
 
 // This thread's two counters: those of digits top_digit() and the one below.
 __device__ __forceinline__ int top_digit() { return kBins - 1 - 2 * (int)threadIdx.x; }
 __device__ __forceinline__ void read_digits(const SelectShared& sh, uint32_t* c1, uint32_t* c2) {
-  *c1 = *c2 = 0;
-#pragma unroll
-  for (int i = 0; i < kCopies; ++i) {
-    const int at = (i + threadIdx.x) & (kCopies - 1);
-    *c1 += sh.hist[top_digit() * kCopies + at];
-    *c2 += sh.hist[(top_digit() - 1) * kCopies + at];
-  }
+  static_assert(kCopies == 4, "one load a digit");
+  const u4 x = *(const u4*)&sh.hist[top_digit() * kCopies], y = *(const u4*)&sh.hist[(top_digit() - 1) * kCopies];
+  *c1 = (x.x + x.y) + (x.z + x.w);
+  *c2 = (y.x + y.y) + (y.z + y.w);
 }
 
-// Extends f by the digit d with (keys above d) < need <= (keys from d on);
+// Narrows f to the digit d with (keys above d) < need <= (keys from d on);
 // returns d.
 __device__ __forceinline__ uint32_t pick_digit(SelectShared& sh, uint32_t c1, uint32_t c2, int level,
                                                Found* f) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t mine = c1 + c2;
-  uint32_t x = mine;
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t y = __shfl_up(x, d, 64);
-    if (lane >= d) x += y;
-  }
+  const int lane = threadIdx.x & 63, wave = wave_index();
+  const uint32_t mine = c1 + c2, x = wave_scan(mine);
   if (lane == 63) sh.sum[wave] = x;
   __syncthreads();
-  uint32_t above = x - mine;
-  for (int i = 0; i < wave; ++i) above += sh.sum[i];
+  const uint32_t above = x - mine + sum_before(sh.sum, wave);
   if (above < f->need && f->need <= above + mine) {
     const bool first = f->need <= above + c1;
     sh.pick[0] = top_digit() - (first ? 0 : 1);
     sh.pick[1] = first ? above : above + c1;
-    sh.pick[2] = f->need - sh.pick[1] == (first ? c1 : c2);
+    sh.pick[2] = first ? c1 : c2;
   }
   __syncthreads();
-  const uint32_t d = sh.pick[0];
-  f->prefix = level == 0 ? d : (f->prefix << (level == 1 ? 11 : 10)) | d;
-  f->need -= sh.pick[1];
-  f->all = sh.pick[2];
+  const uint32_t d = __builtin_amdgcn_readfirstlane(sh.pick[0]);
+  f->need -= __builtin_amdgcn_readfirstlane(sh.pick[1]);
+  f->in = __builtin_amdgcn_readfirstlane(sh.pick[2]);
+  if (level == 0) {
+    first_range(d, &f->lo, &f->span);
+  } else {
+    const int shift = digit_shift(*f);
+    f->lo += d << shift;
+    f->span -= d << shift;
+    if (f->span > 1u << shift) f->span = 1u << shift;
+  }
   __syncthreads();
   return d;
 }
 
-// Where every key from f's digits on stays there is no need to look closer: f
-// becomes a bound below them all.
-__device__ __forceinline__ bool settle(int level, Found* f) {
-  if (!f->all) return false;
-  const uint32_t from = f->prefix << digit_shift(level);
-  f->prefix = from > 0 ? from - 1 : 0;
+// Where every key of f stays there is no need to look closer: f becomes the
+// key below them all, of which none does.
+__device__ __forceinline__ bool settle(Found* f) {
+  if (f->need != f->in) return false;
+  f->lo -= 1;
+  f->span = 1;
   f->need = 0;
   return true;
 }
 
-__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
-  for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
-  return x;
+// Few keys left: each is ranked among them.
+template <int N>
+__device__ __forceinline__ void rank_few(SelectShared& sh, const uint32_t key[4 * N], Found* f) {
+#pragma unroll
+  for (int i = 0; i < 4 * N; ++i)
+    if (key[i] - f->lo < f->span) sh.few[atomicAdd(&sh.n_few, 1u)] = key[i];
+  __syncthreads();
+  // four threads a key, each with every fourth four of the list (0: no key)
+  static_assert(4 * kFew == kSelThreads, "four threads a key");
+  if (wave_index() * 16u < f->in) {
+    const uint32_t mine = sh.few[threadIdx.x >> 2];
+    uint32_t rank = 0;                      // keys above; equal ones 16 bits higher
+    for (uint32_t i = 0; i < f->in; i += 16) {
+      const u4 x = *(const u4*)&sh.few[i + 4 * (threadIdx.x & 3)];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) rank += x[j] > mine ? 1u : (x[j] == mine ? 0x10000u : 0u);
+    }
+    rank += lane_move<0xb1>(rank);          // (the other pair's, then of the other two)
+    rank += lane_move<0x4e>(rank);
+    const uint32_t above = rank & 0xffffu, equal = rank >> 16;
+    if (mine && above < f->need && f->need <= above + equal) {      // (equal keys write the same)
+      sh.pick[0] = mine;
+      sh.pick[1] = above;
+      sh.pick[2] = equal;
+    }
+  }
+  __syncthreads();
+  f->lo = __builtin_amdgcn_readfirstlane(sh.pick[0]);
+  f->span = 1;
+  f->need -= __builtin_amdgcn_readfirstlane(sh.pick[1]);
+  f->in = __builtin_amdgcn_readfirstlane(sh.pick[2]);
+  __syncthreads();
+  settle(f);
 }
 
-// Writes the slots that stay: keys above f.prefix, and of those equal to it the
+// Writes the slots that stay: keys above f.lo, and of those equal to it the
 // first f.need.  *kept, *ties: such keys before this workgroup's tokens; then
 // before the next one's.
 template <int N>
 __device__ __forceinline__ void write_slots(SelectShared& sh, const uint32_t key[4 * N], int base,
                                             const Found& f, RQ_GLOBAL int32_t* out, uint32_t* kept,
                                             uint32_t* ties) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t g = 0, e = 0;
-#pragma unroll
-  for (int i = 0; i < 4 * N; ++i) {
-    g += key[i] > f.prefix;
-    e += key[i] == f.prefix;
-  }
-  g = wave_sum(g);
-  e = wave_sum(e);
-  if (lane == 0) {
-    sh.sum[wave] = g;
-    sh.tie[wave] = e;
-  }
-  __syncthreads();
-  g = *kept;
-  e = *ties;
-  for (int i = 0; i < kSelWaves; ++i) {
-    if (i < wave) {
-      g += sh.sum[i];
-      e += sh.tie[i];
-    }
-    *kept += sh.sum[i];
-    *ties += sh.tie[i];
-  }
-  const uint64_t below = (1ull << lane) - 1;
+  const int lane = threadIdx.x & 63, wave = wave_index();
+  // keys above, and equal ones 16 bits higher: of this lane's four of a group,
+  // then of all lanes up to it
+  uint32_t mine[N], upto[N], all = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    uint32_t gl = g, el = e;               // before this lane's first token
+    mine[i] = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint64_t mg = __ballot(key[4 * i + j] > f.prefix);
-      const uint64_t me = __ballot(key[4 * i + j] == f.prefix);
-      gl += __popcll(mg & below);
-      el += __popcll(me & below);
-      g += __popcll(mg);
-      e += __popcll(me);
+    for (int j = 0; j < 4; ++j) mine[i] += key[4 * i + j] > f.lo;
+    if (f.need > 0)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) mine[i] += key[4 * i + j] == f.lo ? 0x10000u : 0u;
+    upto[i] = wave_scan(mine[i]);
+    all += last_lane(upto[i]);
+  }
+  if (lane == 0) {
+    sh.sum[wave] = all & 0xffffu;
+    sh.tie[wave] = all >> 16;
+  }
+  __syncthreads();
+  uint32_t g = *kept + sum_before(sh.sum, wave), e = *ties + sum_before(sh.tie, wave);
+  *kept += sum_before(sh.sum, kSelWaves);
+  *ties += sum_before(sh.tie, kSelWaves);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t ahead = upto[i] - mine[i], group = last_lane(upto[i]);
+    uint32_t gl = g + (ahead & 0xffffu), el = e + (ahead >> 16);
+    g += group & 0xffffu;
+    e += group >> 16;
+    if (f.need == 0) {                    // no ties
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (key[4 * i + j] > f.lo) out[gl++] = base + 256 * i + 4 * lane + j;
+      continue;
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool gt = key[4 * i + j] > f.prefix, eq = key[4 * i + j] == f.prefix;
+      const bool gt = key[4 * i + j] > f.lo, eq = key[4 * i + j] == f.lo;
       if (gt || (eq && el < f.need))
         out[gl + (el < f.need ? el : f.need)] = base + 256 * i + 4 * lane + j;
       gl += gt;
@@ -204,11 +294,22 @@ __device__ __forceinline__ int kept_length(const BlockEvictLaunch& a, int b, int
   return L;
 }
 
-// A unit by one workgroup, its keys in registers, N x 4 a thread.
+// The search's start: all keys but 0 and those that stay in any case.
+__device__ __forceinline__ Found all_keys(const BlockEvictLaunch& a) {
+  return {1u, 0xfffffffeu, (uint32_t)(a.keep - a.n_sink - a.n_recent), 0u};
+}
+
+// A unit by one workgroup, its keys in registers, N x 4 a thread.  (128 units of
+// 8192 tokens: 7.8 us a workgroup, of which 1.6 wait for the weights, 2 count
+// and find the first digit, 1.6 rank what is left, 1.5 write; with digits of
+// the number itself, three rounds, 13.)
 template <int N>
 __global__ void __launch_bounds__(kSelThreads) block_select_kernel(BlockEvictLaunch a) {
   __shared__ SelectShared sh;
   const int unit = blockIdx.x, b = unit / a.src.H, tid = threadIdx.x;
+  const int base = (tid >> 6) * N * 256;
+  f4 x[N];                // (on their way while the length is)
+  load_weights<N>(gptr(a.src.weights) + (size_t)unit * a.src.cap, base, a.src.cap, x);
   int k;
   const int L = kept_length(a, b, &k);
   if (tid == 0 && unit % a.src.H == 0) gptr(a.new_lengths)[b] = k;
@@ -218,17 +319,24 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(BlockEvictLau
     return;
   }
   uint32_t key[4 * N];
-  const int base = (tid >> 6) * N * 256;
-  load_ranks<N>(a, gptr(a.src.weights) + (size_t)unit * a.src.cap, base, L, key);
-  Found f = {0, (uint32_t)k, 0};
-  for (int level = 0; level < 3; ++level) {
+  Found f = all_keys(a);
+  if (f.need == 0) {
+    rank_keys<N>(a, x, base, L, key);
+    f.lo = 0xfffffffeu;
+  }
+  for (int level = 0; f.need > 0 && level < 3; ++level) {
     clear_digits(sh);
-    count_digits<N>(sh, key, level, f.prefix);
+    if (level == 0) rank_keys<N>(a, x, base, L, key);
+    count_digits<N>(sh, key, level, f);
     __syncthreads();
     uint32_t c1, c2;
     read_digits(sh, &c1, &c2);
     pick_digit(sh, c1, c2, level, &f);
-    if (level < 2 && settle(level, &f)) break;
+    if (f.span == 1 || settle(&f)) break;
+    if (f.in <= kFew) {
+      rank_few<N>(sh, key, &f);
+      break;
+    }
   }
   uint32_t kept = 0, ties = 0;
   write_slots<N>(sh, key, base, f, out, &kept, &ties);
@@ -239,14 +347,19 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(BlockEvictLau
 // of the launch before, and counts its own; once the digits settle the choice
 // (or at level 3) it writes the slots instead, and later launches have nothing
 // to do.  A part's place in the output, the keys above the k-th in the parts
-// before, is added up on the way.
+// before, is added up on the way.  (Eight units of 131072 tokens in sixteen
+// parts: 23 us from the first launch to the fourth.)
 __global__ void __launch_bounds__(kSelThreads) block_select_part_kernel(BlockEvictLaunch a, int level) {
   constexpr int N = 2, kTile = 4 * N * kSelThreads;
   __shared__ SelectShared sh;
   const int part = blockIdx.x, unit = blockIdx.y, b = unit / a.src.H, tid = threadIdx.x;
+  const int first = part * a.part, base = (tid >> 6) * N * 256;
+  const RQ_GLOBAL float* w = gptr(a.src.weights) + (size_t)unit * a.src.cap;
+  f4 x[N];                // (on their way while the counters are)
+  load_weights<N>(w, first + base, a.src.cap, x);
   int k;
   const int L = kept_length(a, b, &k);
-  const int first = part * a.part, last = first + a.part < L ? first + a.part : L;
+  const int last = first + a.part < L ? first + a.part : L;
   RQ_GLOBAL int32_t* out = gptr(a.slots) + (size_t)unit * a.keep;
   if (L <= a.keep) {
     if (level == 0) {
@@ -257,56 +370,71 @@ __global__ void __launch_bounds__(kSelThreads) block_select_part_kernel(BlockEvi
   }
   const size_t side = (size_t)a.src.B * a.src.H * a.parts * kBins;     // one level's counters
   RQ_GLOBAL uint32_t* count = gptr(a.counts) + (size_t)unit * a.parts * kBins;
-  RQ_GLOBAL uint32_t* state = gptr(a.state) + (size_t)unit * 8;
+  RQ_GLOBAL uint32_t* state = gptr(a.state) + (size_t)unit * kSelectState;
   RQ_GLOBAL uint32_t* before = gptr(a.before) + (size_t)unit * a.parts;
-  Found f = {0, (uint32_t)k, 0};
+  Found f = all_keys(a);
   uint32_t kept = 0, ties = 0;
-  const int in_use = (L + a.part - 1) / a.part;
   bool write = level == 3;
   if (level > 0) {
     if (level > 1) {
-      f.prefix = state[2 * (level - 2)];
-      f.need = state[2 * (level - 2) + 1];
+      f.lo = state[3 * (level - 2)];
+      f.span = state[3 * (level - 2) + 1];
+      f.need = state[3 * (level - 2) + 2];
       if (f.need == 0) {                    // settled: the launch before wrote
-        if (level == 2 && part == 0 && tid == 0) state[2 * (level - 1) + 1] = 0;
+        if (level == 2 && part == 0 && tid == 0) state[3 * (level - 1) + 2] = 0;
         return;
       }
       kept = before[part];
+    } else {
+      // the first and last tokens stay in any case
+      const int from = L - a.n_recent;
+      kept = (first < a.n_sink ? first : a.n_sink) + (first > from ? first - from : 0);
     }
     // (counters lie in falling order of their digits, a thread's two together)
+    const int in_use = (L + a.part - 1) / a.part;
     const RQ_GLOBAL u2* c = (const RQ_GLOBAL u2*)(count + side * (level - 1)) + tid;
     u2 all = {0u, 0u}, ahead = {0u, 0u};
-#pragma unroll 8
-    for (int i = 0; i < in_use; ++i) {
-      const u2 x = c[(size_t)i * (kBins / 2)];
-      all += x;
-      if (i < part) ahead += x;
+    for (int i0 = 0; i0 < in_use; i0 += 16) {
+      u2 x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        x[i] = i0 + i < in_use ? c[(size_t)(i0 + i) * (kBins / 2)] : (u2){0u, 0u};
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        all += x[i];
+        if (i0 + i < part) ahead += x[i];
+      }
     }
-    const uint32_t d = pick_digit(sh, all.x, all.y, level - 1, &f);
-    const uint32_t hi = top_digit();
-    uint32_t g = (hi > d ? ahead.x : 0u) + (hi - 1 > d ? ahead.y : 0u);
-    uint32_t e = (hi == d ? ahead.x : 0u) + (hi - 1 == d ? ahead.y : 0u);
-    if (!write && settle(level - 1, &f)) {
+    uint32_t g = 0, e = 0;
+    if (f.need == 0) {                      // (level 1: nothing to choose)
+      f.lo = 0xfffffffeu;
+      write = true;
+    } else {
+      const uint32_t d = pick_digit(sh, all.x, all.y, level - 1, &f);
+      const uint32_t hi = top_digit();
+      g = (hi > d ? ahead.x : 0u) + (hi - 1 > d ? ahead.y : 0u);
+      e = (hi == d ? ahead.x : 0u) + (hi - 1 == d ? ahead.y : 0u);
+    }
+    if (!write && settle(&f)) {
       write = true;
       g += e;                               // (none is a tie any more)
       e = 0;
     }
-    g = wave_sum(g);
-    e = wave_sum(e);
+    g = last_lane(wave_scan(g));
+    e = last_lane(wave_scan(e));
     if ((tid & 63) == 0) {
-      sh.sum[tid >> 6] = g;
-      sh.tie[tid >> 6] = e;
+      sh.sum[wave_index()] = g;
+      sh.tie[wave_index()] = e;
     }
     __syncthreads();
-    for (int i = 0; i < kSelWaves; ++i) {
-      kept += sh.sum[i];
-      ties += sh.tie[i];
-    }
+    kept += sum_before(sh.sum, kSelWaves);
+    ties += sum_before(sh.tie, kSelWaves);
     __syncthreads();
     if (tid == 0) {
       if (part == 0) {
-        state[2 * (level - 1)] = f.prefix;
-        state[2 * (level - 1) + 1] = f.need;
+        state[3 * (level - 1)] = f.lo;
+        state[3 * (level - 1) + 1] = f.span;
+        state[3 * (level - 1) + 2] = f.need;
       }
       before[part] = kept;
     }
@@ -314,16 +442,15 @@ __global__ void __launch_bounds__(kSelThreads) block_select_part_kernel(BlockEvi
     gptr(a.new_lengths)[b] = k;
   }
   if (first >= L) return;
-  const RQ_GLOBAL float* w = gptr(a.src.weights) + (size_t)unit * a.src.cap;
   if (!write) clear_digits(sh);
   for (int at = first; at < last; at += kTile) {
     uint32_t key[4 * N];
-    const int base = at + (tid >> 6) * N * 256;
-    load_ranks<N>(a, w, base, L, key);
+    rank_keys<N>(a, x, at + base, L, key);
+    if (at + kTile < last) load_weights<N>(w, at + kTile + base, L, x);
     if (write)
-      write_slots<N>(sh, key, base, f, out, &kept, &ties);
+      write_slots<N>(sh, key, at + base, f, out, &kept, &ties);
     else
-      count_digits<N>(sh, key, level, f.prefix);
+      count_digits<N>(sh, key, level, f);
   }
   if (write) return;
   __syncthreads();
@@ -471,6 +598,8 @@ hipError_t launch_block_evict(const BlockEvictLaunch& a, hipStream_t s) {
     static_assert(kSelectShort == 32 * kSelThreads, "keys of a unit in one workgroup");
     if (a.src.cap <= 4 * kSelThreads)
       hipLaunchKernelGGL((block_select_kernel<1>), dim3(units), dim3(kSelThreads), 0, s, a);
+    else if (a.src.cap <= 8 * kSelThreads)
+      hipLaunchKernelGGL((block_select_kernel<2>), dim3(units), dim3(kSelThreads), 0, s, a);
     else if (a.src.cap <= 16 * kSelThreads)
       hipLaunchKernelGGL((block_select_kernel<4>), dim3(units), dim3(kSelThreads), 0, s, a);
     else

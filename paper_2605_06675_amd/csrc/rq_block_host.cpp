@@ -191,7 +191,7 @@ EvictPlan plan_eviction(const rq_block_cache* src, int keep) {
   const int most = (src->capacity + rq::kSelectParts - 1) / rq::kSelectParts;
   p.part = (most + rq::kSelectPart - 1) / rq::kSelectPart * rq::kSelectPart;
   p.parts = (src->capacity + p.part - 1) / p.part;
-  p.state = u * 8 * sizeof(uint32_t);
+  p.state = u * rq::kSelectState * sizeof(uint32_t);
   p.before = (u * p.parts * sizeof(uint32_t) + 15) / 16 * 16;
   p.counts = 3 * u * p.parts * 2048 * sizeof(uint32_t);
   return p;

@@ -558,6 +558,27 @@ def test_evict_selection(L, cap, kind):
         assert torch.equal(pos[b, :keep].long(), torch.sort(rank)[0])
 
 
+@pytest.mark.parametrize("L,cap", [(2100, 2112), (33001, 33024), (70001, 70016)])
+@pytest.mark.parametrize("kind", ["wide", "near", "below", "above", "forced"])
+def test_evict_selection_of_unusual_weights(L, cap, kind):
+    """Weights of every size and sign, many within 2^-18 of each other, all
+    below 2^-24 or above 2^8; and no choice at all."""
+    r = Rig("e4m3", "bf16", B=1, H=2, D=64, cap=cap)
+    k, v = r.kv(L)
+    r.c.append(0, k.cuda(), v.cuda())
+    x = torch.rand(2, cap, generator=r.g)
+    w = {"wide": torch.randn(2, cap, generator=r.g) * torch.exp2(x * 250 - 140), "near": 1 + x * 2.0 ** -15,
+         "below": x * 2.0 ** -30 - 2.0 ** -32, "above": 300 + x * 1e30, "forced": x}[kind]
+    r.c.weights.view(2, cap).copy_(w)
+    keep, sink, recent = (L // 5, L // 5 - 40, 40) if kind == "forced" else (L // 3, 4, 30)
+    pos = r.c.evict(keep, sink, recent).positions.view(2, -1).cpu()
+    for h in range(2):
+        order = w[h, :L].double()
+        order[:sink] = order[L - recent:] = math.inf
+        rank = torch.sort(order, stable=True, descending=True)[1][:keep]
+        assert torch.equal(pos[h, :keep].long(), torch.sort(rank)[0])
+
+
 def test_evict_parts_of_uneven_sequences():
     """Sequences that end in the first, a later and no part, one that keeps
     everything; more layers than one."""
