@@ -24,6 +24,15 @@ constexpr int kSelectShort = 32768, kSelectPart = 8192, kSelectParts = 32;
 constexpr int kSelectState = 12;     // words a unit (three a launch)
 
 // One layer of a cache, and its shape.
+// A divisor d, for x / d with x (d - 1) < 2^32 by one product (the compiler's own
+// division is a chain of some twenty instructions).
+struct Divider {
+  uint32_t mul, one;
+};
+inline Divider divider(uint32_t d) {
+  return d == 1 ? Divider{0u, ~0u} : Divider{(uint32_t)(((1ull << 32) + d - 1) / d), 0u};
+}
+
 struct BlockLayer {
   uint8_t* codes;       // [B][H][2][cap][D]
   float* scales;        // [B][H][2][cap / 32]
@@ -32,6 +41,7 @@ struct BlockLayer {
   float* weights;       // [B][H][cap] or NULL
   uint32_t* counters;   // [B][H] or NULL
   int B, H, cap;
+  Divider by_H;
   int D, fmt, is_bf16;  // select the kernels
 };
 
@@ -58,6 +68,7 @@ struct BlockAttendLaunch {
   int G, n, max_tokens;
   int row_tiles;           // tiles of 16 rows (token-major, heads of a group together)
   int splits;              // workgroups that share a row tile's tokens
+  Divider by_G, by_splits;
   float qscale;            // scale * log2(e); scale / cap where scores are capped
   float cap;               // cap * log2(e), or 0
   int window;
@@ -72,6 +83,7 @@ struct BlockAttendLaunch {
   uint16_t* queries;       // else: [unit][row][D] queries as fp16 operands,
   float* factors;          // [unit][row] and the factor of their scores;
   int row_parts;           // workgroups that share a token's rows,
+  Divider by_parts;
   float* sums;             // and, of more than one, [part][unit][token] sums
 };
 
@@ -123,6 +135,16 @@ __device__ __forceinline__ void block_lengths(const int32_t* past, const int32_t
   ps = ps < 0 ? 0 : (ps > most - nw ? most - nw : ps);
   *p = __builtin_amdgcn_readfirstlane(ps);
   *w = __builtin_amdgcn_readfirstlane(nw);
+}
+
+__device__ __forceinline__ int over(int x, Divider d) {
+  return (int)(__umulhi((uint32_t)x, d.mul) + ((uint32_t)x & d.one));
+}
+
+// Where part i of n things begins, in `parts` parts.
+__device__ __forceinline__ int part_from(int n, int i, int parts, Divider by_parts) {
+  const int each = over(n, by_parts), more = n - each * parts;
+  return each * i + (i < more ? i : more);
 }
 
 // Blocks that rows first..last (tokens of the call) see: [lo, hi).
@@ -300,7 +322,7 @@ template <int D, bool BF16>
 __device__ __forceinline__ void load_queries(const BlockAttendLaunch& a, int b, int h, int row,
                                              int past, int nnew, QueryTile<D>* t) {
   const int g = (threadIdx.x & 63) >> 4;
-  t->token = row / a.G;
+  t->token = over(row, a.by_G);
   t->head = row - t->token * a.G;
   t->valid = t->token < nnew;
   if (!t->valid) t->token = nnew > 0 ? nnew - 1 : 0;

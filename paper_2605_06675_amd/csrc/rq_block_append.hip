@@ -21,7 +21,7 @@ __global__ void __launch_bounds__(256) block_append_kernel(BlockAppendLaunch a) 
   const int j = blockIdx.x * 4 + wave;
   if (j >= waves) return;
   const int unit = blockIdx.y >> 1, kind = blockIdx.y & 1;
-  const int b = unit / a.c.H, h = unit - b * a.c.H;
+  const int b = over(unit, a.c.by_H), h = unit - b * a.c.H;
   int past, nnew;
   block_lengths(a.past, nullptr, b, 0, a.c.cap, &past, &nnew);
   nnew = a.new_len ? __builtin_amdgcn_readfirstlane(gptr(a.new_len)[b]) : a.n;

@@ -266,7 +266,7 @@ __device__ __forceinline__ void merge_tile(const BlockAttendLaunch& a, const Par
     }
     if (on && first == 0) {
       x *= l > 0.0f ? 1.0f / l : 0.0f;
-      const int grow = rt * 16 + row, token = grow / a.G;
+      const int grow = rt * 16 + row, token = over(grow, a.by_G);
       store_out<4>(a, b, h * a.G + grow - token * a.G, token, col * 4, (const float*)&x);
     }
   }
@@ -282,16 +282,15 @@ __global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int split = blockIdx.x, unit = blockIdx.y;
-  const int b = unit / a.c.H, h = unit - b * a.c.H;
+  const int b = over(unit, a.c.by_H), h = unit - b * a.c.H;
   int past, nnew;
   block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
   if (nnew == 0) return;
   const int total = past + nnew, full = total / kBlockTokens;
   int lo_all, hi_all;                      // block `full` is the tail
   seen_blocks(past, 0, nnew - 1, a.window, &lo_all, &hi_all);
-  const int64_t nb = hi_all - lo_all;
-  const int lo = lo_all + (int)(nb * split / a.splits);
-  const int hi = lo_all + (int)(nb * (split + 1) / a.splits);
+  const int lo = lo_all + part_from(hi_all - lo_all, split, a.splits, a.by_splits);
+  const int hi = lo_all + part_from(hi_all - lo_all, split + 1, a.splits, a.by_splits);
 
   QueryTile<D> q[QT];
   Running<D> st[QT];
@@ -402,7 +401,7 @@ __global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch 
       for (int e = 0; e < D / 16; ++e)
         x[e] = __builtin_fmaf(sh_o[w][row * kStride + ch + e], by, x[e]);
     }
-    const int grow = 16 * n + row, token = grow / a.G;
+    const int grow = 16 * n + row, token = over(grow, a.by_G);
     if (token >= nnew) continue;
     if (a.splits > 1) {
       const Parts parts(a, (size_t)unit * QT + n);
@@ -448,7 +447,7 @@ __device__ __forceinline__ void merge_row(const BlockAttendLaunch& a, int grow, 
                                           int h, int nnew) {
   constexpr int kCols = D / 4, kGroups = 256 / kCols;
   __shared__ f4 sum[kGroups][kCols];
-  const int token = grow / a.G, rt = grow >> 4, row = grow & 15;
+  const int token = over(grow, a.by_G), rt = grow >> 4, row = grow & 15;
   if (token >= nnew) return;
   const int lane = threadIdx.x & 63, col = threadIdx.x % kCols, group = threadIdx.x / kCols;
   const size_t base = ((size_t)unit * a.row_tiles + rt) * a.splits;
@@ -486,11 +485,11 @@ __device__ __forceinline__ void merge_row(const BlockAttendLaunch& a, int grow, 
 template <int D>
 __global__ void __launch_bounds__(256) block_merge_rows_kernel(BlockAttendLaunch a) {
   constexpr int kCols = D / 4;
-  const int unit = blockIdx.y, b = unit / a.c.H, h = unit - b * a.c.H;
+  const int unit = blockIdx.y, b = over(unit, a.c.by_H), h = unit - b * a.c.H;
   int past, nnew;
   block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
   const int grow = blockIdx.x * (256 / kCols) + threadIdx.x / kCols, col = threadIdx.x % kCols;
-  const int token = grow / a.G, row = grow & 15;
+  const int token = over(grow, a.by_G), row = grow & 15;
   if (token >= nnew) return;
   const size_t base = ((size_t)unit * a.row_tiles + (grow >> 4)) * a.splits;
   const RQ_GLOBAL f2* ml = (const RQ_GLOBAL f2*)(gptr(a.part_ml) + (base * 16 + row) * 2);
@@ -517,7 +516,7 @@ __global__ void __launch_bounds__(256) block_merge_rows_kernel(BlockAttendLaunch
 
 template <int D>
 __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttendLaunch a) {
-  const int unit = blockIdx.y, b = unit / a.c.H;
+  const int unit = blockIdx.y, b = over(unit, a.c.by_H);
   int past, nnew;
   block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
   merge_row<D>(a, blockIdx.x, unit, b, unit - b * a.c.H, nnew);
@@ -529,7 +528,7 @@ __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttendLaunch a) {
 template <int D>
 __global__ void __launch_bounds__(256) block_merge_weigh_kernel(BlockAttendLaunch a) {
   __shared__ float sh_m[32], sh_inv[32];
-  const int unit = blockIdx.y, b = unit / a.c.H;
+  const int unit = blockIdx.y, b = over(unit, a.c.by_H);
   int past, nnew;
   block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
   const int all = a.n * a.G, merges = a.splits > 1 ? all : 0;

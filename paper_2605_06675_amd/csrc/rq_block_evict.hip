@@ -306,13 +306,13 @@ __device__ __forceinline__ Found all_keys(const BlockEvictLaunch& a) {
 template <int N>
 __global__ void __launch_bounds__(kSelThreads) block_select_kernel(BlockEvictLaunch a) {
   __shared__ SelectShared sh;
-  const int unit = blockIdx.x, b = unit / a.src.H, tid = threadIdx.x;
+  const int unit = blockIdx.x, b = over(unit, a.src.by_H), tid = threadIdx.x;
   const int base = (tid >> 6) * N * 256;
   f4 x[N];                // (on their way while the length is)
   load_weights<N>(gptr(a.src.weights) + (size_t)unit * a.src.cap, base, a.src.cap, x);
   int k;
   const int L = kept_length(a, b, &k);
-  if (tid == 0 && unit % a.src.H == 0) gptr(a.new_lengths)[b] = k;
+  if (tid == 0 && unit == b * a.src.H) gptr(a.new_lengths)[b] = k;
   RQ_GLOBAL int32_t* out = gptr(a.slots) + (size_t)unit * a.keep;
   if (L <= a.keep) {
     for (int t = tid; t < L; t += kSelThreads) out[t] = t;
@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(BlockEvictLau
 __global__ void __launch_bounds__(kSelThreads) block_select_part_kernel(BlockEvictLaunch a, int level) {
   constexpr int N = 2, kTile = 4 * N * kSelThreads;
   __shared__ SelectShared sh;
-  const int part = blockIdx.x, unit = blockIdx.y, b = unit / a.src.H, tid = threadIdx.x;
+  const int part = blockIdx.x, unit = blockIdx.y, b = over(unit, a.src.by_H), tid = threadIdx.x;
   const int first = part * a.part, base = (tid >> 6) * N * 256;
   const RQ_GLOBAL float* w = gptr(a.src.weights) + (size_t)unit * a.src.cap;
   f4 x[N];                // (on their way while the counters are)
@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(kSelThreads) block_select_part_kernel(BlockEvi
   if (L <= a.keep) {
     if (level == 0) {
       for (int t = first + tid; t < last; t += kSelThreads) out[t] = t;
-      if (part == 0 && tid == 0 && unit % a.src.H == 0) gptr(a.new_lengths)[b] = k;
+      if (part == 0 && tid == 0 && unit == b * a.src.H) gptr(a.new_lengths)[b] = k;
     }
     return;
   }
@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(kSelThreads) block_select_part_kernel(BlockEvi
       }
       before[part] = kept;
     }
-  } else if (part == 0 && tid == 0 && unit % a.src.H == 0) {
+  } else if (part == 0 && tid == 0 && unit == b * a.src.H) {
     gptr(a.new_lengths)[b] = k;
   }
   if (first >= L) return;
@@ -467,7 +467,7 @@ template <int FMT, int D, bool BF16>
 __global__ void __launch_bounds__(256) block_gather_kernel(BlockEvictLaunch a) {
   constexpr int kChunks = D / 8, kRows = 64 / kChunks, kLoads = kBlockTokens / kRows;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int unit = blockIdx.y >> 1, kind = blockIdx.y & 1, b = unit / a.src.H;
+  const int unit = blockIdx.y >> 1, kind = blockIdx.y & 1, b = over(unit, a.src.by_H);
   int L = gptr(a.lengths)[b];
   L = L < 0 ? 0 : (L > a.src.cap ? a.src.cap : L);
   const int k = L < a.keep ? L : a.keep;

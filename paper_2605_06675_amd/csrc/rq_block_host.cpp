@@ -82,6 +82,7 @@ rq::BlockLayer layer_of(const rq_block_cache* c, int32_t layer) {
   l.counters = c->counters ? c->counters + u : nullptr;
   l.B = c->batch;
   l.H = c->n_kv_heads;
+  l.by_H = rq::divider(c->n_kv_heads);
   l.cap = c->capacity;
   l.D = c->head_dim;
   l.fmt = c->format;
@@ -105,7 +106,7 @@ rq_status check_query(const rq_block_cache* c, const rq_block_query* a) {
 
 // How an attention call is split, and what it needs of the workspace.
 struct Plan {
-  int prompt;                      // tiles of 256 rows (rq_block_prompt.hip)
+  int prompt;                      // tiles of 128 rows (rq_block_prompt.hip)
   int row_tiles, splits, row_parts;
   uint64_t part, part_ml, stats, scores, queries, factors, sums;   // bytes
   uint64_t bytes() const { return part + part_ml + stats + scores + queries + factors + sums; }
@@ -283,6 +284,8 @@ rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_bl
   a.max_tokens = q->max_tokens;
   a.row_tiles = p.row_tiles;
   a.splits = p.splits;
+  a.by_G = rq::divider(a.G);
+  a.by_splits = rq::divider(p.splits);
   a.qscale = qscale;
   a.cap = q->cap * log2e;
   a.window = q->window;
@@ -302,6 +305,7 @@ rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_bl
   a.factors = reinterpret_cast<float*>(take(p.factors));
   a.sums = reinterpret_cast<float*>(take(p.sums));
   a.row_parts = p.row_parts;
+  a.by_parts = rq::divider(std::max(p.row_parts, 1));
   // The last workgroup of a tile adds its splits where they are few: a launch
   // less, but one workgroup's loads.  us with / without, splits x rows: 8 x 4
   // 8.5 / 9.4, 8 x 8 44.2 / 45.4 (32 units of 32768 tokens), 2 x 4 15.4 / 16.5,

@@ -1,19 +1,25 @@
 // Attention over the block-scaled 8-bit cache for many query rows a unit
 // (prompts and their chunks): matrix products of tiles.
 //
-// A workgroup of eight waves owns 256 rows of a unit (token-major, the heads of
-// a group together), 32 a wave, and walks its tokens in tiles of 64.  Codes are
-// converted to fp16 once a workgroup on their way into LDS (two buffers, one
-// barrier a tile), keys as [token][channel], values as [channel][token].  On
-// v_mfma_f32_32x32x16_f16 S^T = K Q^T leaves a lane with 16 tokens of one row,
-// the operand that O^T = V^T P^T wants of it (the values' tokens are stored in
-// that order), so probabilities never move between lanes.
+// A workgroup of four waves owns 128 rows of a unit (token-major, the heads of
+// a group together), 32 a wave, and walks its tokens in tiles of 64; two are on
+// a CU.  Codes are converted to fp16 once a workgroup on their way into LDS (two
+// buffers, one barrier a tile), keys as [token][channel], values as
+// [channel][token].  On v_mfma_f32_32x32x16_f16 S^T = K Q^T leaves a lane with
+// 16 tokens of one row, the operand that O^T = V^T P^T wants of it (the values'
+// tokens are stored in that order), so probabilities never move between lanes.
 //
 // A block's value scale goes into the exponent: P' = 2^(x - m + log2(by)),
 // by = value scale * unit, and the row's sum takes the block's sum of P' / by.
 // P' is rounded to fp16 (2^-11, an eighth of a bf16 output's own rounding); for
-// fp16 and fp32 outputs (EXACT) it is a pair hi + lo, a third more time (4 x 512
-// tokens over 8192: 342 and 449 us).
+// fp16 and fp32 outputs (EXACT) it is a pair hi + lo, a quarter more time.
+//
+// Two prompts of 4096 tokens (8 kv-heads of 4 heads, 128 channels, e4m3): 335 us,
+// 820 TFLOP/s; capped 390; fp16 430.  The vector unit bounds it: 460 instructions
+// a wave and tile, 96 of them (capped) exponentials and reciprocals, take 2400
+// cycles beside 1024 of the matrix unit.  Workgroups of 256 rows (half the
+// conversions) took 513 us where this one took 501; the conversion between the
+// products of the tile before does not fit the registers.
 #include "rq_block.h"
 
 namespace rq {
@@ -184,27 +190,27 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
   const int units = a.c.B * a.c.H, tiles = (a.n * a.G + kRows - 1) / kRows, each = tiles * a.splits;
   int unit, w;
   if (units % 8 == 0) {
-    unit = (int)(blockIdx.x / 8 / each) * 8 + blockIdx.x % 8;
-    w = blockIdx.x / 8 % each;
+    const uint32_t eight = blockIdx.x / 8, u = eight / (uint32_t)each;
+    unit = (int)u * 8 + blockIdx.x % 8;
+    w = eight - u * each;
   } else {
-    unit = blockIdx.x / each;
-    w = blockIdx.x % each;
+    unit = blockIdx.x / (uint32_t)each;
+    w = blockIdx.x - unit * each;
   }
-  const int rt = tiles - 1 - w / a.splits, split = w % a.splits;
-  const int b = unit / a.c.H, h = unit - b * a.c.H;
+  const int t = over(w, a.by_splits), rt = tiles - 1 - t, split = w - t * a.splits;
+  const int b = over(unit, a.c.by_H), h = unit - b * a.c.H;
   int past, nnew;
   block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
-  const int first = rt * kRows / a.G;
+  const int first = over(rt * kRows, a.by_G);
   if (first >= nnew) return;
-  int last = (rt * kRows + kRows - 1) / a.G;
+  int last = over(rt * kRows + kRows - 1, a.by_G);
   last = last < nnew ? last : nnew - 1;
   const int total = past + nnew, full = total / kBlockTokens;
   int lo, hi;
   seen_blocks(past, first, last, a.window, &lo, &hi);
   {
     // splits begin at whole tiles
-    const int64_t nt = (hi - lo + 1) / 2;
-    const int t0 = (int)(nt * split / a.splits), t1 = (int)(nt * (split + 1) / a.splits);
+    const int nt = (hi - lo + 1) / 2, t0 = part_from(nt, split, a.splits, a.by_splits), t1 = part_from(nt, split + 1, a.splits, a.by_splits);
     hi = lo + 2 * t1 < hi ? lo + 2 * t1 : hi;
     lo += 2 * t0;
   }
@@ -217,12 +223,12 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
 
   // this lane's row, as BlockAttendLaunch has it: 16 k + 8 hl + 0..7 in f[k]
   const int row = rt * kRows + wave * 32 + col;
-  int token = row / a.G;
+  int token = over(row, a.by_G);
   const int head = row - token * a.G;
   const bool valid = token < nnew;
   if (!valid) token = nnew - 1;
-  const int wave_first = (rt * kRows + wave * 32) / a.G;      // tokens of the wave's rows
-  int wave_last = (rt * kRows + wave * 32 + 31) / a.G;
+  const int wave_first = over(rt * kRows + wave * 32, a.by_G);      // tokens of the wave's rows
+  int wave_last = over(rt * kRows + wave * 32 + 31, a.by_G);
   wave_last = wave_last < nnew ? wave_last : nnew - 1;
   const bool idle = wave_first >= nnew;
   h8 q[D / 16];
@@ -398,50 +404,67 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
         int e = __builtin_amdgcn_frexp_expf(sv);
         e = e < -100 ? -100 : e;
         const float u = __builtin_amdgcn_ldexpf(128.0f, -e);
-        by *= unit2 == 0.0f ? 1.0f : u / unit2;
+        by *= unit2 == 0.0f ? 1.0f : u * __builtin_amdgcn_rcpf(unit2);     // (powers of two)
         unit2 = u;
       }
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) o[c] *= by;
     }
+    // Probabilities of the second block are formed between the first one's
+    // products.
+    float by[2], c[2], sum[2] = {0.0f, 0.0f};
+    uint32_t hi2[2][8], lo2[2][8];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       // (codes under a scale of zero are zero: any factor serves)
-      const float by = tvs[t] > 0.0f ? __builtin_fmaxf(tvs[t] * unit2, 0x1p-80f) : 1.0f;
-      const float c = m - __builtin_amdgcn_logf(by) - off;
-      uint32_t hi2[8], lo2[8];
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = exp2_f(__builtin_fmaf(s[t][2 * i], f[t], -c));
-        const float y = exp2_f(__builtin_fmaf(s[t][2 * i + 1], f[t], -c));
-        if constexpr (EXACT) {
-          const h2 p = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x, y));
-          hi2[i] = as_u32(p);
-          lo2[i] = as_u32((h2){(_Float16)(x - (float)p.x), (_Float16)(y - (float)p.y)});
-        } else {
-          hi2[i] = as_u32((h2){(_Float16)x, (_Float16)y});
-        }
-        // (of the fp32 numbers: where by is small, fp16 loses P' but the sum
-        // must not)
-        sum += x;
-        sum += y;
-      }
-      l = __builtin_fmaf(sum, 1.0f / by, l);
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const h8 ph = as_h8((u4){hi2[4 * g], hi2[4 * g + 1], hi2[4 * g + 2], hi2[4 * g + 3]});
-#pragma unroll
-        for (int c2 = 0; c2 < D / 32; ++c2) {
-          const h8 vf = *(const h8*)(sh_v[buf] + value_at(32 * c2 + col, 2 * (2 * t + g) + hl));
-          o[c2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph, o[c2], 0, 0, 0);
-          if constexpr (EXACT) {
-            const h8 pl = as_h8((u4){lo2[4 * g], lo2[4 * g + 1], lo2[4 * g + 2], lo2[4 * g + 3]});
-            o[c2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl, o[c2], 0, 0, 0);
-          }
-        }
-      }
+      by[t] = tvs[t] > 0.0f ? __builtin_fmaxf(tvs[t] * unit2, 0x1p-80f) : 1.0f;
+      c[t] = m - __builtin_amdgcn_logf(by[t]) - off;
     }
+    auto form = [&](int t, int i) {
+      const float x = exp2_f(__builtin_fmaf(s[t][2 * i], f[t], -c[t]));
+      const float y = exp2_f(__builtin_fmaf(s[t][2 * i + 1], f[t], -c[t]));
+      if constexpr (EXACT) {
+        const h2 p = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x, y));
+        hi2[t][i] = as_u32(p);
+        lo2[t][i] = as_u32((h2){(_Float16)(x - (float)p.x), (_Float16)(y - (float)p.y)});
+      } else {
+        hi2[t][i] = as_u32((h2){(_Float16)x, (_Float16)y});
+      }
+      // (of the fp32 numbers: where by is small, fp16 loses P' but the sum
+      // must not)
+      sum[t] += x;
+      sum[t] += y;
+    };
+    auto value = [&](int t, int j) {
+      return *(const h8*)(sh_v[buf] + value_at(32 * (j % (D / 32)) + col, 2 * (2 * t + j / (D / 32)) + hl));
+    };
+    auto add = [&](int t, int j, h8 vf) {
+      const int g = j / (D / 32), c2 = j % (D / 32);
+      const h8 ph = as_h8((u4){hi2[t][4 * g], hi2[t][4 * g + 1], hi2[t][4 * g + 2], hi2[t][4 * g + 3]});
+      o[c2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph, o[c2], 0, 0, 0);
+      if constexpr (EXACT) {
+        const h8 pl = as_h8((u4){lo2[t][4 * g], lo2[t][4 * g + 1], lo2[t][4 * g + 2], lo2[t][4 * g + 3]});
+        o[c2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl, o[c2], 0, 0, 0);
+      }
+    };
+    constexpr int kSteps = D / 16;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) form(0, i);
+    h8 v0 = value(0, 0), v1 = value(0, 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < 2 * kSteps; ++j) {
+      const h8 v2 = j + 2 < 2 * kSteps ? value((j + 2) / kSteps, (j + 2) % kSteps) : v0;
+      add(j / kSteps, j % kSteps, v0);
+      if (j < kSteps)
+#pragma unroll
+        for (int i = 0; i < 8 / kSteps; ++i) form(1, 8 / kSteps * j + i);
+      v0 = v1;
+      v1 = v2;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) l = __builtin_fmaf(sum[t], __builtin_amdgcn_rcpf(by[t]), l);
   };
 
   // a wave may be a tile behind the others, never more: one barrier a tile

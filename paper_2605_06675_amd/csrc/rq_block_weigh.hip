@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
   __shared__ RowInfo sh_row[2][kTileRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, hl = lane >> 5;
-  const int unit = blockIdx.y, b = unit / a.c.H, h = unit - b * a.c.H;
+  const int unit = blockIdx.y, b = over(unit, a.c.by_H), h = unit - b * a.c.H;
   int past, nnew;
   block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
   const int total = past + nnew, full = total / kBlockTokens;
@@ -143,8 +143,9 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
   int tile0 = from * a.G / kTileRows, tile1 = (to * a.G + kTileRows - 1) / kTileRows;
   {
     // this workgroup's part of all tiles
-    const int64_t all = (a.n * a.G + kTileRows - 1) / kTileRows;
-    const int p0 = (int)(all * part / a.row_parts), p1 = (int)(all * (part + 1) / a.row_parts);
+    const int all = (a.n * a.G + kTileRows - 1) / kTileRows;
+    const int p0 = part_from(all, part, a.row_parts, a.by_parts);
+    const int p1 = part_from(all, part + 1, a.row_parts, a.by_parts);
     tile0 = tile0 > p0 ? tile0 : p0;
     tile1 = tile1 < p1 ? tile1 : p1;
   }
@@ -172,7 +173,7 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
       info.qs = factors[tile * kTileRows];
       info.m = stats[tile * kTileRows * 2];
       info.inv = stats[tile * kTileRows * 2 + 1];
-      info.token = row / a.G;
+      info.token = over(row, a.by_G);
       if (a.slopes) info.slope = gptr(a.slopes)[h * a.G + row - info.token * a.G] * 1.4426950408889634f;
       if (far) info.pos = gptr(a.c.positions)[(size_t)unit * a.c.cap + past + info.token];
     }
@@ -191,7 +192,7 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
     for (int i = 0; i < 16; ++i) sum[t][i] = 0.0f;
   auto work = [&](int tile, int buf, int half) {          // 32 rows of a tile
     const int row0 = tile * kTileRows + 32 * half;
-    if (past + (row0 + 31) / a.G < slot0) return;
+    if (past + over(row0 + 31, a.by_G) < slot0) return;
     const RowInfo r = sh_row[buf][32 * half + col];
     f16v s[2];
 #pragma unroll
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
       for (int t = 0; t < 2; ++t)
         s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key[t][k], q, s[t], 0, 0, 0);
     }
-    const bool masked = a.window || slot0 + kWaveTokens - 1 > past + row0 / a.G;
+    const bool masked = a.window || slot0 + kWaveTokens - 1 > past + over(row0, a.by_G);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       float f = ks[t] * r.qs, off = 0.0f;      // scores are s f + off
@@ -255,30 +256,32 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
     }
   }
 
-  // add the 32 rows' lanes; lane (col, hl) with col < 16 writes register col
+  // The 32 numbers of each lane are added over the 32 rows' lanes, halved in every
+  // step: a lane keeps the half that its own bit names and hands on the other.
+  // Lane (col, hl) ends with number col.
+  float x[32];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    float add = 0.0f;
+  for (int i = 0; i < 32; ++i) x[i] = sum[i >> 4][i & 15];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float x = sum[t][i];
-      for (int d = 1; d < 32; d <<= 1) x += __shfl_xor(x, d, 64);
-      add = col == i ? x : add;
-    }
-    const int slot = slot0 + 32 * t + 8 * (col >> 2) + 4 * hl + (col & 3);
-    if (col < 16 && slot < total) {
-      if (a.row_parts > 1)
-        gptr(a.sums)[((size_t)part * gridDim.y + unit) * a.max_tokens + slot] = add;
-      else
-        gptr(a.c.weights)[(size_t)unit * a.c.cap + slot] += add;
-    }
+  for (int d = 16; d >= 1; d >>= 1) {
+    const bool upper = col & d;
+#pragma unroll
+    for (int i = 0; i < d; ++i)
+      x[i] = (upper ? x[i + d] : x[i]) + __shfl_xor(upper ? x[i] : x[i + d], d, 64);
+  }
+  const int slot = slot0 + (col & 16) * 2 + 8 * ((col & 15) >> 2) + 4 * hl + (col & 3);
+  if (slot < total) {
+    if (a.row_parts > 1)
+      gptr(a.sums)[((size_t)part * gridDim.y + unit) * a.max_tokens + slot] = x[0];
+    else
+      gptr(a.c.weights)[(size_t)unit * a.c.cap + slot] += x[0];
   }
 }
 
 __global__ void __launch_bounds__(256) block_add_kernel(BlockAttendLaunch a) {
   const int unit = blockIdx.y, slot = blockIdx.x * 256 + threadIdx.x;
   int past, nnew;
-  block_lengths(a.past, a.new_len, unit / a.c.H, a.n, a.max_tokens, &past, &nnew);
+  block_lengths(a.past, a.new_len, over(unit, a.c.by_H), a.n, a.max_tokens, &past, &nnew);
   if (slot >= past + nnew) return;
   float sum = 0.0f;
 #pragma unroll 4
