@@ -164,10 +164,13 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
                  rq::kBlockTokens * sizeof(float);
       return p;
     }
-    // else workgroups of 256 tokens, and parts of the rows to fill four rounds
-    // (two a CU), 128 rows or more in each
-    int64_t parts = 8 * (int64_t)rq::device_cus() / (u * ((a->max_tokens + 255) / 256));
-    parts = std::min(parts, (rows + 127) / 128);
+    // else workgroups of 256 tokens, and parts of the rows to fill two rounds (two
+    // a CU; windows leave some without rows: four), about 128 rows or more in
+    // each.  us with four / two rounds: 32 units of 2000 tokens, 1000 rows 103 / 95,
+    // 8 of 32000 and 400 rows 147 / 136, 2 of 8000 and 400 rows 39 / 41; 32 of 8192
+    // and 2036 rows, window of 2000: 278 / 305.
+    int64_t parts = (a->window ? 8 : 4) * (int64_t)rq::device_cus() / (u * ((a->max_tokens + 255) / 256));
+    parts = std::min(parts, (rows + 63) / 128);
     p.row_parts = (int)std::max<int64_t>(parts, 1);
     p.queries = tiles * 16 * c->head_dim * sizeof(uint16_t);
     p.factors = tiles * 16 * sizeof(float);
