@@ -15,11 +15,12 @@
 // fp16 and fp32 outputs (EXACT) it is a pair hi + lo, a quarter more time.
 //
 // Two prompts of 4096 tokens (8 kv-heads of 4 heads, 128 channels, e4m3): 335 us,
-// 820 TFLOP/s; capped 390; fp16 430.  The vector unit bounds it: 460 instructions
-// a wave and tile, 96 of them (capped) exponentials and reciprocals, take 2400
-// cycles beside 1024 of the matrix unit.  Workgroups of 256 rows (half the
-// conversions) took 513 us where this one took 501; the conversion between the
-// products of the tile before does not fit the registers.
+// 820 TFLOP/s; capped 390; fp16 430.  Neither unit bounds it alone: a wave's tile
+// is 440 vector instructions (96 of them, capped, exponentials and reciprocals)
+// and 1024 cycles of the matrix unit, with two waves a SIMD; capped the units are
+// 64 and 29 % busy.  Workgroups of 256 rows (half the conversions) took 513 us
+// where this one took 501; the conversion between the products of the tile
+// before does not fit the registers.
 #include "rq_block.h"
 
 namespace rq {
