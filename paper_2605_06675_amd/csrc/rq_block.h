@@ -155,6 +155,41 @@ __device__ __forceinline__ void seen_blocks(int past, int first, int last, int w
   *lo = slot > 0 ? slot / kBlockTokens : 0;
 }
 
+// A float's maximum or sum over lanes, in all of them: of a row of 16 lanes, of a
+// lane and the one 16 or 32 further.  Register moves, a few cycles each where an
+// exchange through LDS takes a hundred.
+struct Max {
+  __device__ __forceinline__ float operator()(float a, float b) const { return __builtin_fmaxf(a, b); }
+};
+struct Sum {
+  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+template <class F>
+__device__ __forceinline__ float row_all(float x) {
+  x = F()(x, moved<0xb1>(x));           // lanes 1 and 2 further in a quad,
+  x = F()(x, moved<0x4e>(x));
+  x = F()(x, moved<0x141>(x));          // the other quad of eight,
+  return F()(x, moved<0x140>(x));       // the other eight
+}
+template <class F>
+__device__ __forceinline__ float pair_all(float x) {
+  const u2 p = __builtin_bit_cast(u2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  return F()(__uint_as_float(p.x), __uint_as_float(p.y));
+}
+template <class F>
+__device__ __forceinline__ float half_all(float x) {
+  const u2 p = __builtin_bit_cast(u2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  return F()(__uint_as_float(p.x), __uint_as_float(p.y));
+}
+template <class F>
+__device__ __forceinline__ float wave_all(float x) {
+  return half_all<F>(pair_all<F>(row_all<F>(x)));
+}
+
 // ------------------------------------------------------------- quantization
 // The scale of a block whose largest magnitude is amax, and its reciprocal.
 // Scales below the smallest normal number become 0 (their reciprocal would
@@ -346,8 +381,7 @@ __device__ __forceinline__ void load_queries(const BlockAttendLaunch& a, int b, 
         most = __builtin_fmaxf(most, __builtin_fabsf(__uint_as_float(raw[k][i] << 16)));
         most = __builtin_fmaxf(most, __builtin_fabsf(__uint_as_float(raw[k][i] & 0xffff0000u)));
       }
-    most = __builtin_fmaxf(most, __shfl_xor(most, 16, 64));
-    most = __builtin_fmaxf(most, __shfl_xor(most, 32, 64));
+    most = half_all<Max>(pair_all<Max>(most));
     const int e = most > 0.0f ? __builtin_amdgcn_frexp_expf(most) : 0;
 #pragma unroll
     for (int k = 0; k < D / 32; ++k) {

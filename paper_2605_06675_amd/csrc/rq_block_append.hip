@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(256) block_append_kernel(BlockAppendLaunch a) 
         most = __builtin_fmaxf(most, __builtin_fabsf(widen_t<BF16>(x[i][w] & 0xffffu)));
         most = __builtin_fmaxf(most, __builtin_fabsf(widen_t<BF16>(x[i][w] >> 16)));
       }
-    for (int d = 32; d >= 1; d >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d, 64));
+    most = wave_all<Max>(most);
     float inv;
     const float scale = block_scale<FMT>(most, &inv);
     RQ_GLOBAL uint8_t* out = gptr(a.c.codes) + ((size_t)(unit * 2 + kind) * a.c.cap + (size_t)blk * kBlockTokens) * D;

@@ -65,8 +65,7 @@ __device__ __forceinline__ void probabilities(Running<D>* st, f4 s[2]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) top = __builtin_fmaxf(top, s[m][i]);
   if (__any(top > st->m + 8.0f)) {
-    top = __builtin_fmaxf(top, __shfl_xor(top, 16, 64));
-    top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
+    top = half_all<Max>(pair_all<Max>(top));
     const float mn = __builtin_fmaxf(st->m, top);
     const float by = exp2_f(st->m - mn);
     st->m = mn;
@@ -161,7 +160,7 @@ __device__ __forceinline__ void add_tail(const RQ_GLOBAL uint16_t* vt, int n_tai
       most = __builtin_fmaxf(most, __builtin_fmaxf(__builtin_fabsf(widen_t<BF16>(w[c][j] & 0xffffu)),
                                                    __builtin_fabsf(widen_t<BF16>(w[c][j] >> 16))));
     }
-  for (int d = 32; d >= 1; d >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d, 64));
+  most = wave_all<Max>(most);
   if (most == 0.0f) return;
   const int e = __builtin_amdgcn_frexp_expf(most);
   u4 hi[QT], lo[QT];
@@ -233,13 +232,15 @@ __device__ __forceinline__ void merge_tile(const BlockAttendLaunch& a, const Par
     }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) m = __builtin_fmaxf(m, ml[i].x);
-    for (int d = kCols / 2; d >= 1; d >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d, 64));
+    m = row_all<Max>(m);
+    if constexpr (kCols == 32) m = pair_all<Max>(m);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       ml[i].x = exp2_f(ml[i].x - m);
       l = __builtin_fmaf(ml[i].y, ml[i].x, l);
     }
-    for (int d = kCols / 2; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+    l = row_all<Sum>(l);
+    if constexpr (kCols == 32) l = pair_all<Sum>(l);
     f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
     // eight loads at a time; those behind the last split return zeros
 #pragma unroll
@@ -373,8 +374,7 @@ __global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch 
   for (int n = 0; n < QT; ++n) {
     if (16 * n >= nnew * a.G) break;
     // the four waves' sums
-    float lsum = st[n].l + __shfl_xor(st[n].l, 16, 64);
-    lsum += __shfl_xor(lsum, 32, 64);
+    const float lsum = half_all<Sum>(pair_all<Sum>(st[n].l));
     const float to_value = st[n].unit == 0.0f ? 0.0f : 1.0f / (st[n].unit * kValueUnit<FMT>);
     if (n > 0) __syncthreads();
 #pragma unroll
@@ -455,11 +455,11 @@ __device__ __forceinline__ void merge_row(const BlockAttendLaunch& a, int grow, 
   const RQ_GLOBAL float* o = gptr(a.part) + (base * 16 + row) * D + col * 4;
   float m = -1.0e30f;
   for (int s = lane; s < a.splits; s += 64) m = __builtin_fmaxf(m, ml[s * 32]);
-  for (int d = 32; d >= 1; d >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d, 64));
+  m = wave_all<Max>(m);
   float l = 0.0f;
   for (int s = lane; s < a.splits; s += 64)
     l = __builtin_fmaf(ml[s * 32 + 1], exp2_f(ml[s * 32] - m), l);
-  for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+  l = wave_all<Sum>(l);
   f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
   for (int s = group; s < a.splits; s += kGroups) {
@@ -547,10 +547,10 @@ __global__ void __launch_bounds__(256) block_merge_weigh_kernel(BlockAttendLaunc
       const RQ_GLOBAL float* ml = gptr(a.part_ml) + (((size_t)unit * a.row_tiles + (row >> 4)) * a.splits * 16 + (row & 15)) * 2;
       float m = -1.0e30f, l = 0.0f;
       for (int s = lane; s < a.splits; s += 16) m = __builtin_fmaxf(m, ml[s * 32]);
-      for (int d = 8; d >= 1; d >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d, 64));
+      m = row_all<Max>(m);
       for (int s = lane; s < a.splits; s += 16)
         l = __builtin_fmaf(ml[s * 32 + 1], exp2_f(ml[s * 32] - m), l);
-      for (int d = 8; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+      l = row_all<Sum>(l);
       if (lane == 0) {
         sh_m[row] = m;
         sh_inv[row] = l > 0.0f ? 1.0f / l : 0.0f;

@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(256) block_gather_kernel(BlockEvictLaunch a) {
       most = __builtin_fmaxf(most, top * by[i]);
       asm volatile("" : "+v"(raw[i]));      // not the same values for both uses
     }
-    for (int d = 32; d >= 1; d >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d, 64));
+    most = wave_all<Max>(most);
     float inv;
     const float scale = block_scale<FMT>(most, &inv);
     RQ_GLOBAL uint8_t* out = gptr(a.dst.codes) + (side * a.dst.cap + (size_t)blk * kBlockTokens) * D;
@@ -545,7 +545,7 @@ __global__ void __launch_bounds__(256) block_gather_kernel(BlockEvictLaunch a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) most = __builtin_fmaxf(most, __builtin_fabsf(x[e]));
       }
-      for (int d = 32; d >= 1; d >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d, 64));
+      most = wave_all<Max>(most);
       const float scale = block_scale<FMT>(most, &inv);
       if (lane == 0) gptr(a.dst.scales)[side * (a.dst.cap / kBlockTokens) + blk] = scale;
     }

@@ -132,10 +132,8 @@ __device__ __forceinline__ void store_tail(const RQ_GLOBAL uint16_t* kt, int n_t
                                                __builtin_fabsf(widen_t<BF16>(v[p][i] >> 16))));
     }
   }
-  for (int d = 32; d >= 1; d >>= 1) {
-    km = __builtin_fmaxf(km, __shfl_xor(km, d, 64));
-    vm = __builtin_fmaxf(vm, __shfl_xor(vm, d, 64));
-  }
+  km = wave_all<Max>(km);
+  vm = wave_all<Max>(vm);
   if (lane == 0) {
     red[wave] = km;
     red[8 + wave] = vm;
@@ -255,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
           most = __builtin_fmaxf(most, __builtin_fabsf(widen_t<true>(raw[k][i] & 0xffffu)));
           most = __builtin_fmaxf(most, __builtin_fabsf(widen_t<true>(raw[k][i] >> 16)));
         }
-      most = __builtin_fmaxf(most, __shfl_xor(most, 32, 64));
+      most = half_all<Max>(most);
       const int e = most > 0.0f ? __builtin_amdgcn_frexp_expf(most) : 0;
 #pragma unroll
       for (int k = 0; k < D / 16; ++k)
@@ -396,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
     // (the same in every lane; scales of zero have no unit to follow)
     const bool grow = sv > 0.0f && (unit2 == 0.0f || sv * unit2 > 128.0f);
     if (grow || __any(top > m + 8.0f)) {
-      top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
+      top = half_all<Max>(top);
       const float mn = __builtin_fmaxf(m, top);
       float by = exp2_f(m - mn);
       m = mn;
@@ -476,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
     work(blk, buf);
   }
 
-  l += __shfl_xor(l, 32, 64);
+  l = half_all<Sum>(l);
   const float to_value = unit2 == 0.0f ? 0.0f : 1.0f / (unit2 * kValueUnit<FMT>);
   if (a.splits > 1) {
     if (row >= a.row_tiles * 16) return;

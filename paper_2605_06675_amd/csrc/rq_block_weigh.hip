@@ -77,7 +77,7 @@ __device__ __forceinline__ float tail_keys(const RQ_GLOBAL uint16_t* kt, int n_t
     for (int k = 0; k < D / 16; ++k) f[k] = as_h8(raw[k]);
     return 1.0f;
   }
-  for (int d = 32; d >= 1; d >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d, 64));
+  most = wave_all<Max>(most);
   const int e = most > 0.0f ? __builtin_amdgcn_frexp_expf(most) : 0;
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) f[k] = bf16_scaled(raw[k], e);
