@@ -142,21 +142,35 @@ __device__ __forceinline__ void add_values(const ValueBlock<D>& v, const f4 s[QT
   }
 }
 
-// The tail's values, divided by a power of two that brings the largest below 1
-// (fp16 holds the others to 2^-25 of it), as a block of that scale.  Rows from
-// n_tail on count as zero.
-template <int FMT, int D, bool BF16, int QT>
-__device__ __forceinline__ void add_tail(const RQ_GLOBAL uint16_t* vt, int n_tail, const f4 s[QT][2],
-                                         Running<D> st[QT]) {
-  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+// The tail's values of this lane, as load_values has a block's; rows from n_tail on
+// count as zero.
+template <int D>
+struct TailValues {
   uint32_t w[D / 32][8];      // [two channels][token]
-  float most = 0.0f;
+};
+
+template <int D>
+__device__ __forceinline__ void load_tail(const RQ_GLOBAL uint16_t* vt, int n_tail, TailValues<D>* t) {
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int tok = 16 * (j >> 2) + 4 * g + (j & 3);
-      w[c][j] = tok < n_tail ? *(const RQ_GLOBAL uint32_t*)(vt + tok * D + (D / 16) * r + 2 * c) : 0u;
+      t->w[c][j] = tok < n_tail ? *(const RQ_GLOBAL uint32_t*)(vt + tok * D + (D / 16) * r + 2 * c) : 0u;
+    }
+}
+
+// The tail's values, divided by a power of two that brings the largest below 1
+// (fp16 holds the others to 2^-25 of it), as a block of that scale.
+template <int FMT, int D, bool BF16, int QT>
+__device__ __forceinline__ void add_tail(const TailValues<D>& t, const f4 s[QT][2], Running<D> st[QT]) {
+  const auto& w = t.w;
+  float most = 0.0f;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
       most = __builtin_fmaxf(most, __builtin_fmaxf(__builtin_fabsf(widen_t<BF16>(w[c][j] & 0xffffu)),
                                                    __builtin_fabsf(widen_t<BF16>(w[c][j] >> 16))));
     }
@@ -359,6 +373,8 @@ __global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch 
   }
   if (lo <= full && full < hi && (full - lo) % 4 == wave) {
     const RQ_GLOBAL uint16_t* kt = gptr(a.c.tail) + (size_t)unit * 2 * kBlockTokens * D;
+    TailValues<D> tv;          // (on their way while the keys are)
+    load_tail<D>(kt + kBlockTokens * D, total % kBlockTokens, &tv);
     f4 s[QT][2];
 #pragma unroll
     for (int n = 0; n < QT; ++n) {
@@ -367,7 +383,7 @@ __global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch 
       keep(s[n], n, full);
       probabilities<D>(&st[n], s[n]);
     }
-    add_tail<FMT, D, BF16, QT>(kt + kBlockTokens * D, total % kBlockTokens, s, st);
+    add_tail<FMT, D, BF16, QT>(tv, s, st);
   }
 
 #pragma unroll

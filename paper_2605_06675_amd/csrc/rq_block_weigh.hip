@@ -84,6 +84,16 @@ __device__ __forceinline__ float tail_keys(const RQ_GLOBAL uint16_t* kt, int n_t
   return __builtin_amdgcn_ldexpf(1.0f, e);
 }
 
+// One step of the sums at the kernel's end, with the lane that a move names: it
+// differs in bit d, and in lower bits that later steps add up all the same.
+template <int d, int MOVE>
+__device__ __forceinline__ void halve(float x[32], int col) {
+  const bool upper = col & d;
+#pragma unroll
+  for (int i = 0; i < d; ++i)
+    x[i] = (upper ? x[i + d] : x[i]) + moved<MOVE>(upper ? x[i] : x[i + d]);
+}
+
 // What a score needs of its row.
 struct RowInfo {
   float qs, m, inv, slope;
@@ -263,12 +273,15 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
 #pragma unroll
   for (int i = 0; i < 32; ++i) x[i] = sum[i >> 4][i & 15];
 #pragma unroll
-  for (int d = 16; d >= 1; d >>= 1) {
-    const bool upper = col & d;
-#pragma unroll
-    for (int i = 0; i < d; ++i)
-      x[i] = (upper ? x[i + d] : x[i]) + __shfl_xor(upper ? x[i] : x[i + d], d, 64);
+  for (int i = 0; i < 16; ++i) {
+    const u2 p = __builtin_bit_cast(u2, __builtin_amdgcn_permlane16_swap(
+        __float_as_uint(x[i]), __float_as_uint(x[i + 16]), false, false));
+    x[i] = __uint_as_float(p.x) + __uint_as_float(p.y);
   }
+  halve<8, 0x128>(x, col);
+  halve<4, 0x141>(x, col);
+  halve<2, 0x4e>(x, col);
+  halve<1, 0xb1>(x, col);
   const int slot = slot0 + (col & 16) * 2 + 8 * ((col & 15) >> 2) + 4 * hl + (col & 3);
   if (slot < total) {
     if (a.row_parts > 1)
