@@ -511,10 +511,12 @@ def make_block_cache(format, dtype, n_layers, batch, n_kv_heads, n_q_heads,
             setattr(c, name, _tptr(t))
         import torch
         c._device = given[0].device
+        c._calls = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
         c._lengths = torch.int32
-        # (the inputs' type, then the outputs')
-        c._types = (torch.bfloat16 if dtype == RQ_BF16 else torch.float16,
-                    torch.float32, torch.float16, torch.bfloat16)
+        # (the inputs' type, and the outputs')
+        c._type = torch.bfloat16 if dtype == RQ_BF16 else torch.float16,
+        c._out_types = {torch.float32: RQ_F32, torch.float16: RQ_F16,
+                        torch.bfloat16: RQ_BF16}
         counters = torch.zeros(sizes[5] // 4, dtype=torch.int32, device=c._device)
         # calls may come on any stream
         torch.cuda.current_stream(c._device).synchronize()
@@ -542,17 +544,18 @@ assert _QUERY.size == C.sizeof(RqBlockQuery)
 def _block_call(cache, stream, f, *args):
     """Launch on the given stream, or the current one of the cache's device,
     with that device current."""
-    import torch
     device = cache._device
+    current, raw_stream = cache._calls
     if stream is None:
-        s = torch._C._cuda_getCurrentRawStream(device.index)
+        s = raw_stream(device.index)
     elif stream.device != device:
         raise ValueError(f"the stream is on {stream.device}, the cache on {device}")
     else:
         s = stream.cuda_stream
-    if torch.cuda.current_device() == device.index:
+    if current() == device.index:
         status = f(*args, s)
     else:
+        import torch
         with torch.cuda.device(device):
             status = f(*args, s)
     if status != RQ_OK:
@@ -568,7 +571,7 @@ def _block_rows(cache, t, what, heads, n, dtypes):
     if t.device != cache._device:
         raise ValueError(f"{what} is on {t.device}, the cache on {cache._device}")
     if t.dtype not in dtypes:
-        raise ValueError(f"{what} has dtype {t.dtype}, expected {dtypes[0]}")
+        raise ValueError(f"{what} has dtype {t.dtype}, expected {next(iter(dtypes))}")
     sb, sh, st, sd = t.stride()
     if sd != 1:
         raise ValueError(f"the rows of {what} must be contiguous")
@@ -598,8 +601,8 @@ def rq_block_append(cache, layer, past, k, v, new_len=None, stream=None):
     """k, v: torch [batch][n_kv_heads][n_new][head_dim] in the cache's dtype
     (any strides, contiguous rows); past, new_len: device int32 [batch]."""
     n = k.shape[2] if k.dim() == 4 else -1
-    rk = _block_rows(cache, k, "k", cache.n_kv_heads, n, cache._types[:1])
-    rv = _block_rows(cache, v, "v", cache.n_kv_heads, n, cache._types[:1])
+    rk = _block_rows(cache, k, "k", cache.n_kv_heads, n, cache._type)
+    rv = _block_rows(cache, v, "v", cache.n_kv_heads, n, cache._type)
     if past is None:
         raise ValueError("past is missing")
     _block_call(cache, stream, lib().rq_block_append, C.byref(cache), layer,
@@ -633,17 +636,17 @@ def rq_block_attention(cache, layer, past, q, out, ws, new_len=None,
     if past is None:
         raise ValueError("past is missing")
     if slopes is not None and (slopes.device != cache._device
-                               or slopes.dtype != cache._types[1]
+                               or cache._out_types.get(slopes.dtype) != RQ_F32
                                or slopes.shape != (cache.n_q_heads,)
                                or not slopes.is_contiguous()):
         raise ValueError(f"slopes must be float32 [{cache.n_q_heads}] on the cache's device")
-    rq_ = _block_rows(cache, q, "q", cache.n_q_heads, n, cache._types[:1])
-    ro = _block_rows(cache, out, "out", cache.n_q_heads, n, cache._types[1:])
+    rq_ = _block_rows(cache, q, "q", cache.n_q_heads, n, cache._type)
+    ro = _block_rows(cache, out, "out", cache.n_q_heads, n, cache._out_types)
     a = _QUERY.pack(
         n, cache.capacity if max_tokens is None else max_tokens,
         _block_lengths(cache, past, "past"),
         _block_lengths(cache, new_len, "new_len"), *rq_, *ro,
-        (RQ_F32, RQ_F16, RQ_BF16)[cache._types.index(out.dtype, 1) - 1],
+        cache._out_types[out.dtype],
         cache.head_dim ** -0.5 if scale is None else scale, cap, window,
         0 if slopes is None else slopes.data_ptr(), 1 if accumulate else 0)
     _block_call(cache, stream, lib().rq_block_attention, C.byref(cache), layer,
