@@ -762,7 +762,8 @@ class BlockCache:
 
     def append(self, layer, k, v, new_len=None, stream=None):
         """Append k, v ([batch][n_kv_heads][n][head_dim]); new_len: how many
-        of the n rows each sequence takes."""
+        of the n rows each sequence takes.  Where `bound` would pass the
+        capacity, the lengths are read (a wait) before it is refused."""
         self._room(layer, k.shape[2], stream)
         rq_block_append(self.desc, layer, self.lengths[layer], k, v, new_len,
                         stream)
