@@ -169,12 +169,13 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
     // each.  us with four / two rounds: 32 units of 2000 tokens, 1000 rows 103 / 95,
     // 8 of 32000 and 400 rows 147 / 136, 2 of 8000 and 400 rows 39 / 41; 32 of 8192
     // and 2036 rows, window of 2000: 278 / 305.
-    int64_t parts = (a->window ? 8 : 4) * (int64_t)rq::device_cus() / (u * ((a->max_tokens + 255) / 256));
-    parts = std::min(parts, (rows + 63) / 128);
-    p.row_parts = (int)std::max<int64_t>(parts, 1);
+    // (A window needs no more workspace than none: the size counts its parts.)
+    const int64_t round = 2 * (int64_t)rq::device_cus(), wgs = u * ((a->max_tokens + 255) / 256);
+    const int64_t most = std::max<int64_t>(std::min(4 * round / wgs, (rows + 63) / 128), 1);
+    p.row_parts = (int)(a->window ? most : std::max<int64_t>(std::min(2 * round / wgs, most), 1));
     p.queries = tiles * 16 * c->head_dim * sizeof(uint16_t);
     p.factors = tiles * 16 * sizeof(float);
-    if (p.row_parts > 1) p.sums = (uint64_t)p.row_parts * u * a->max_tokens * sizeof(float);
+    if (most > 1) p.sums = (uint64_t)most * u * a->max_tokens * sizeof(float);
   }
   return p;
 }

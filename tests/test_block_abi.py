@@ -196,3 +196,19 @@ def test_oracle_unit_attention_and_eviction():
     assert list(u.evict(7, 2, 3, w).pos) == [0, 1, 9, 20, 67, 68, 69]
     np.testing.assert_array_equal(to.tail[0][2], u.values(0)[9])
     assert u.evict(100, 2, 3).length == 70
+
+
+def test_a_window_needs_no_more_workspace():
+    """The size without a window serves every window, whatever the plans."""
+    rng = np.random.default_rng(5)
+    for _ in range(4000):
+        H, G = int(rng.integers(1, 9)), int(rng.integers(1, 17))
+        cap = 32 * int(2 ** rng.uniform(0, 12))
+        c = desc(batch=int(2 ** rng.uniform(0, 6)), n_kv_heads=H, n_q_heads=H * G, capacity=cap,
+                 head_dim=int(rng.choice([64, 128])))
+        most = int(rng.integers(1, cap + 1))
+        n = int(min(most, 2 ** rng.uniform(0, 13)))
+        for acc in (False, True):
+            whole = rq.rq_block_attention_workspace(c, n, most, acc)
+            for window in (1, int(2 ** rng.uniform(0, 17))):
+                assert rq.rq_block_attention_workspace(c, n, most, acc, window) <= whole
