@@ -127,7 +127,9 @@ struct Plan {
 // least four blocks each.  Where the new tokens are few beside the cached ones,
 // sequences may differ in length and a round's workgroups with them: one split
 // more (4 sequences, 8 kv-heads of 4 heads, 512 tokens over 8192: 358 us
-// unsplit, 366 in two; lengths from 2048 to 8192: 289 and 250).
+// unsplit, 366 in two; lengths from 2048 to 8192: 289 and 250).  Up to eight blocks
+// a split saves less than its merging launch takes (192 tiles of 143 tokens 14.2
+// us, in two splits 22.6).
 Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
   Plan p{};
   const int64_t G = c->n_q_heads / c->n_kv_heads, u = (int64_t)units(c);
@@ -141,7 +143,7 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
   int64_t s;
   if (p.prompt) {
     s = 2 * (int64_t)rq::device_cus() / (u * ((a->n_new * G + 127) / 128));
-    s = std::min(s, (blocks + 3) / 4);
+    s = blocks > 8 ? std::min(s, (blocks + 3) / 4) : 1;
     if (s <= 1 && a->max_tokens >= 4 * (int64_t)a->n_new && blocks >= 128) s = 2;
   } else {
     const bool two = (a->accumulate && c->batch > 1) || (p.row_tiles > 1 && u > 64);
