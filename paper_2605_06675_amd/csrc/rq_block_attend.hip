@@ -10,6 +10,10 @@
 // lanes.  Every code is exact in fp16; a block's key scale multiplies the
 // fp32 scores, its value scale the probabilities.  These are split into an
 // fp16 pair hi + lo (22 bits), in units that keep p * scale below 2^15.
+//
+// Long contexts are bound by memory: 32 units of 32768 tokens (268 MB) 47 us, 5.7
+// TB/s where a plain read reaches 7.  Short ones by a chain of latencies (1001
+// tokens 7.8 us): lengths, codes, the four waves' sums, parts, ticket, merge.
 #include "rq_block.h"
 
 namespace rq {

@@ -462,7 +462,8 @@ __global__ void __launch_bounds__(kSelThreads) block_select_part_kernel(BlockEvi
   ((RQ_GLOBAL u2*)(count + side * level + (size_t)part * kBins))[tid] = c;
 }
 
-// One wave a (unit, K or V, block of the new cache).
+// One wave a (unit, K or V, block of the new cache).  128 units to 2048 tokens
+// (137 MB): 26 us, the rate of a copy.
 template <int FMT, int D, bool BF16>
 __global__ void __launch_bounds__(256) block_gather_kernel(BlockEvictLaunch a) {
   constexpr int kChunks = D / 8, kRows = 64 / kChunks, kLoads = kBlockTokens / kRows;

@@ -14,8 +14,8 @@
 // P' is rounded to fp16 (2^-11, an eighth of a bf16 output's own rounding); for
 // fp16 and fp32 outputs (EXACT) it is a pair hi + lo, a quarter more time.
 //
-// Two prompts of 4096 tokens (8 kv-heads of 4 heads, 128 channels, e4m3): 335 us,
-// 820 TFLOP/s; capped 390; fp16 430.  Neither unit bounds it alone: a wave's tile
+// Two prompts of 4096 tokens (8 kv-heads of 4 heads, 128 channels, e4m3): 323 us,
+// 850 TFLOP/s; capped 385; fp16 418.  Neither unit bounds it alone: a wave's tile
 // is 440 vector instructions (96 of them, capped, exponentials and reciprocals)
 // and 1024 cycles of the matrix unit, with two waves a SIMD; capped the units are
 // 64 and 29 % busy.  Workgroups of 256 rows (half the conversions) took 513 us
