@@ -486,8 +486,8 @@ rq_status rq_block_attention_workspace(const rq_block_cache* c,
  * the tail's numbers, as fp16 relative to the largest of their row or block);
  * probabilities times the value scale are rounded to 22 bits relative to the
  * largest.  Calls of more than 32 query rows a kv-head (n_new times the heads
- * of a group) round them to 11 bits where the output is bf16, and take a cap's
- * tanh to 2^-22 of the cap unless the output is fp32, and for the weights.
+ * of a group) take a cap's tanh to 2^-22 of the cap unless the output is fp32,
+ * and for the weights.
  * ws: device scratch, 16-byte aligned, contents arbitrary; calls that share
  * it must not overlap.  Asynchronous. */
 rq_status rq_block_attention(const rq_block_cache* c, int32_t layer,

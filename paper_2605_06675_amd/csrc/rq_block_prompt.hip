@@ -11,8 +11,9 @@
 //
 // A block's value scale goes into the exponent: P' = 2^(x - m + log2(by)),
 // by = value scale * unit, and the row's sum takes the block's sum of P' / by.
-// P' is rounded to fp16 (2^-11, an eighth of a bf16 output's own rounding); for
-// fp16 and fp32 outputs (EXACT) it is a pair hi + lo, a quarter more time.
+// P' is an fp16 pair hi + lo (22 bits), whatever the output's type: as fp16 alone
+// a call of many rows would answer otherwise than one of few, by 2^-12 of the
+// result before its rounding, and be a quarter faster.
 //
 // Two prompts of 4096 tokens (8 kv-heads of 4 heads, 128 channels, e4m3): 323 us,
 // 850 TFLOP/s; capped 385; fp16 418.  Neither unit bounds it alone: a wave's tile
@@ -178,7 +179,7 @@ __device__ __forceinline__ void store_tail(const RQ_GLOBAL uint16_t* kt, int n_t
   }
 }
 
-template <int FMT, int D, bool BF16, bool EXACT>
+template <int FMT, int D, bool BF16>
 __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLaunch a) {
   __shared__ __align__(16) uint8_t sh_k[2][kTile * D * 2];
   __shared__ __align__(16) uint8_t sh_v[2][kTile * D * 2];
@@ -351,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
     const bool masked = a.window || slot0 + kTile - 1 > past + wave_first;
     // scores are s f + off; a mask needs them formed (f may be 0)
     float f[2] = {tks[0] * qs, tks[1] * qs}, off = 0.0f;
-    const bool fine = EXACT && a.out_dtype == RQ_F32;      // tanh to fp32
+    const bool fine = a.out_dtype == RQ_F32;      // tanh to fp32
     if (a.cap != 0.0f && !fine) {
       // cap tanh(x) = cap - 2 cap / (1 + e^(2x)): off by 2^-22 cap, which the
       // output's rounding hides
@@ -432,13 +433,12 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
     auto form = [&](int t, int i) {
       const float x = exp2_f(__builtin_fmaf(s[t][2 * i], f[t], -c[t]));
       const float y = exp2_f(__builtin_fmaf(s[t][2 * i + 1], f[t], -c[t]));
-      if constexpr (EXACT) {
-        const h2 p = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x, y));
-        hi2[t][i] = as_u32(p);
-        lo2[t][i] = as_u32((h2){(_Float16)(x - (float)p.x), (_Float16)(y - (float)p.y)});
-      } else {
-        hi2[t][i] = as_u32((h2){(_Float16)x, (_Float16)y});
-      }
+      const h2 p = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x, y));
+      hi2[t][i] = as_u32(p);
+      float xl, yl;      // what the halves leave of x and y, exactly
+      asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(xl) : "v"(p), "v"(x));
+      asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(yl) : "v"(p), "v"(y));
+      lo2[t][i] = as_u32((h2){(_Float16)xl, (_Float16)yl});
       // (of the fp32 numbers: where by is small, fp16 loses P' but the sum
       // must not)
       sum[t] += x;
@@ -451,10 +451,8 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
       const int g = j / (D / 32), c2 = j % (D / 32);
       const h8 ph = as_h8((u4){hi2[t][4 * g], hi2[t][4 * g + 1], hi2[t][4 * g + 2], hi2[t][4 * g + 3]});
       o[c2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph, o[c2], 0, 0, 0);
-      if constexpr (EXACT) {
-        const h8 pl = as_h8((u4){lo2[t][4 * g], lo2[t][4 * g + 1], lo2[t][4 * g + 2], lo2[t][4 * g + 3]});
-        o[c2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl, o[c2], 0, 0, 0);
-      }
+      const h8 pl = as_h8((u4){lo2[t][4 * g], lo2[t][4 * g + 1], lo2[t][4 * g + 2], lo2[t][4 * g + 3]});
+      o[c2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pl, o[c2], 0, 0, 0);
     };
     constexpr int kSteps = D / 16;
 #pragma unroll
@@ -520,10 +518,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
 template <int FMT, int D, bool BF16>
 hipError_t launch(const BlockAttendLaunch& a, hipStream_t s) {
   const dim3 grid((unsigned)((a.n * a.G + kRows - 1) / kRows * a.splits) * a.c.B * a.c.H);
-  if (a.out_dtype != RQ_BF16)
-    hipLaunchKernelGGL((block_prompt_kernel<FMT, D, BF16, true>), grid, dim3(kThreads), 0, s, a);
-  else
-    hipLaunchKernelGGL((block_prompt_kernel<FMT, D, BF16, false>), grid, dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((block_prompt_kernel<FMT, D, BF16>), grid, dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -457,6 +457,32 @@ def test_attend_repeats_bit_for_bit():
     assert torch.equal(w1[~torch.isnan(w1)], r.c.weights[~torch.isnan(w1)])
 
 
+def between_roundings(o, want, tol):
+    """Every output is a rounding of some number within tol of want."""
+    lo, hi = (torch.from_numpy(x).to(o.dtype).double() for x in (want - tol, want + tol))
+    o = o.cpu().double()
+    return bool(((lo <= o) & (o <= hi)).all())
+
+
+@both
+@types
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompt_probabilities_hold_22_bits(fmt, dtype, D):
+    """Queries of zero: a 16-bit output is the values' mean, rounded once, with
+    as little before that as fp32 outputs show."""
+    r = Rig(fmt, dtype, D=D, cap=160)
+    r.append(150)
+    n, q = 40, torch.zeros(2, 4, 40, D, dtype=r.dt)
+    o = r.attend(n, q=q, out=r.dt).cpu()
+    for b in range(2):
+        for h in range(2):
+            V = r.u[b][h].values(1).astype(np.float64)
+            want = np.stack([V[:150 - n + 1 + i].mean(0) for i in range(n)])
+            tol = 6 * 2.0 ** -22 * np.abs(V).max()
+            for g in range(2):
+                assert between_roundings(o[b, 2 * h + g], want, tol), (b, h)
+
+
 # ----------------------------------------------------------------- eviction
 def evict(r, keep, sink, recent, weight=None):
     """Evicts r's cache; returns a rig around the new one, checked."""
