@@ -458,7 +458,8 @@ typedef struct rq_block_query {
   rq_block_rows out;       /* the same shape in out_dtype                  */
   int32_t out_dtype;       /* RQ_F32, RQ_F16 or RQ_BF16                    */
   float scale;             /* of the scores                                */
-  float cap;               /* scores become cap * tanh(score / cap); 0: no */
+  float cap;               /* scores become cap * tanh(score / cap), at
+                              most 2^100; 0: no                            */
   int32_t window;          /* a query sees keys less than window positions
                               before it; 0: all                            */
   const float* slopes;     /* device [n_q_heads]: slope * (distance in
@@ -485,9 +486,9 @@ rq_status rq_block_attention_workspace(const rq_block_cache* c,
  * Accuracy: scores, softmax and sums are fp32 on exact operands (queries, and
  * the tail's numbers, as fp16 relative to the largest of their row or block);
  * probabilities times the value scale are rounded to 22 bits relative to the
- * largest.  Calls of more than 32 query rows a kv-head (n_new times the heads
- * of a group) take a cap's tanh to 2^-22 of the cap unless the output is fp32,
- * and for the weights.
+ * largest.  A cap's tanh is taken to 2^-21 of itself; in calls of more than 32
+ * query rows a kv-head (n_new times the heads of a group) with 16-bit output
+ * and caps up to 64 to 2^-22 of 1.
  * ws: device scratch, 16-byte aligned, contents arbitrary; calls that share
  * it must not overlap.  Asynchronous. */
 rq_status rq_block_attention(const rq_block_cache* c, int32_t layer,

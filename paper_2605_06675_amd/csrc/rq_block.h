@@ -71,6 +71,7 @@ struct BlockAttendLaunch {
   Divider by_G, by_splits;
   float qscale;            // scale * log2(e); scale / cap where scores are capped
   float cap;               // cap * log2(e), or 0
+  int fine;                // many rows: the cap's tanh relative to itself
   int window;
   const float* slopes;     // [H * G] or NULL
   int accumulate;

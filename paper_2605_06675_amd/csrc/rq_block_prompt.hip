@@ -352,10 +352,8 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
     const bool masked = a.window || slot0 + kTile - 1 > past + wave_first;
     // scores are s f + off; a mask needs them formed (f may be 0)
     float f[2] = {tks[0] * qs, tks[1] * qs}, off = 0.0f;
-    const bool fine = a.out_dtype == RQ_F32;      // tanh to fp32
-    if (a.cap != 0.0f && !fine) {
-      // cap tanh(x) = cap - 2 cap / (1 + e^(2x)): off by 2^-22 cap, which the
-      // output's rounding hides
+    if (a.cap != 0.0f && !a.fine) {
+      // cap tanh(x) = cap - 2 cap / (1 + e^(2x)): off by 2^-22 cap
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const float e2 = f[t] * 2.8853900817779268f;
@@ -365,12 +363,12 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
       }
       off = a.cap;
     }
-    if (far || masked || (fine && a.cap != 0.0f)) {
+    if (far || masked || a.fine) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[t][i] = __builtin_fmaf(s[t][i], f[t], off);
-        if (fine && a.cap != 0.0f) {
+        if (a.fine) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[t][i] = a.cap * tanh_f(s[t][i]);
         }

@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       float f = ks[t] * r.qs, off = 0.0f;      // scores are s f + off
-      if (a.cap != 0.0f) {
+      if (a.cap != 0.0f && !a.fine) {
         // cap tanh(x) = cap - 2 cap / (1 + e^(2x)), off by 2^-22 cap
         const float e2 = f * 2.8853900817779268f;
 #pragma unroll
@@ -233,9 +233,13 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
         f = 2.0f * a.cap;
         off = a.cap;
       }
-      if (far || masked) {
+      if (far || masked || a.fine) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[t][i] = __builtin_fmaf(s[t][i], f, off);
+        if (a.fine) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[t][i] = a.cap * tanh_f(s[t][i]);
+        }
         f = 1.0f;
         off = 0.0f;
         if (far) {

@@ -105,6 +105,13 @@ def test_attention_refusals(kw, status):
                                        None) == status
 
 
+def test_cap_refusals():
+    L, c = rq.lib(), desc()
+    for cap in (float("nan"), -1e-30, 2.0 ** 100 * 1.01, 1e38):
+        assert L.rq_block_attention(C.byref(c), 0, C.byref(query(cap=cap)), P, 1 << 40, None) == rq.RQ_EINVAL
+        assert b"cap" in L.rq_last_error()
+
+
 def test_attention_workspace_refusals():
     L, c = rq.lib(), desc()
     need = rq.rq_block_attention_workspace(c, 2, 96, True)

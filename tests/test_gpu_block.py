@@ -483,6 +483,36 @@ def test_prompt_probabilities_hold_22_bits(fmt, dtype, D):
                 assert between_roundings(o[b, 2 * h + g], want, tol), (b, h)
 
 
+@pytest.mark.parametrize("cap", [20.0, 300.0, 1e4, 1e6, 1e9, 1e30])
+@pytest.mark.parametrize("n,dtype,out", [(1, "bf16", "fp32"), (40, "bf16", "bf16"), (40, "bf16", "fp32"),
+                                         (70, "fp16", "fp16")])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attend_large_caps(cap, n, dtype, out, D):
+    """A capped score errs relative to itself, not to the cap: where the cap is
+    far above the scores, the result is that of none."""
+    r = Rig("e4m3", dtype, D=D, cap=192)
+    r.append(130)
+    q = (r.randn(2, 4, n, D) * 2).to(r.dt)
+    before = r.weights()
+    o = r.attend(n, q=q, cap=cap, accumulate=True, out={**DT, "fp32": (0, torch.float32)}[out][1])
+    after, o, scale = r.weights(), o.cpu(), D ** -0.5
+    for b in range(2):
+        for h in range(2):
+            u = block.Unit(r.u[b][h].fmt, D, None)
+            u.__dict__.update({**r.u[b][h].__dict__, "weight": np.zeros(130)})
+            qq = q[b, 2 * h:2 * h + 2].float().numpy().transpose(1, 0, 2)
+            want = u.attend(qq, scale, cap, accumulate=True)
+            ratio, big = r.bounds(b, h, qq, scale, 0.0, None)
+            # tanh to 2^-21 of itself, the score not above the row's sum of |q k|
+            K = np.abs(u.values(0).astype(np.float64))
+            ratio = ratio + 2 * 2.0 ** -21 * scale * (np.abs(qq.astype(np.float64)) @ K.T).max(-1)
+            got = o[b, 2 * h:2 * h + 2].transpose(0, 1)
+            assert between_roundings(got, want, (ratio[..., None] + 2.0 ** -21) * big), (b, h)
+            add = after[b, h, :130] - before[b, h, :130]
+            tol = ratio.max() * u.weight + 2.0 ** -24 * (after[b, h, :130] + 2 * n * u.weight)
+            assert (np.abs(add - u.weight) <= tol + 1e-30).all(), (b, h)
+
+
 # ----------------------------------------------------------------- eviction
 def evict(r, keep, sink, recent, weight=None):
     """Evicts r's cache; returns a rig around the new one, checked."""
