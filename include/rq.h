@@ -457,7 +457,9 @@ typedef struct rq_block_query {
   rq_block_rows q;         /* [batch][n_q_heads][n_new][head_dim] in dtype */
   rq_block_rows out;       /* the same shape in out_dtype                  */
   int32_t out_dtype;       /* RQ_F32, RQ_F16 or RQ_BF16                    */
-  float scale;             /* of the scores                                */
+  float scale;             /* of the scores; with the largest |q|, the
+                              largest |k| and head_dim (over the cap, if
+                              any) at most 2^126                           */
   float cap;               /* scores become cap * tanh(score / cap), at
                               most 2^100; 0: no                            */
   int32_t window;          /* a query sees keys less than window positions

@@ -294,6 +294,11 @@ __device__ __forceinline__ void value_pairs(uint32_t a, uint32_t b, uint32_t out
 __device__ __forceinline__ h8 as_h8(u4 x) { return __builtin_bit_cast(h8, x); }
 __device__ __forceinline__ b8 as_b8(u4 x) { return __builtin_bit_cast(b8, x); }
 
+// A row's maximum before it has seen a token: below all scores.
+constexpr float kNoScore = -3.0e38f;
+// Scores (log2) from here on are rounded before their row's maximum is subtracted.
+constexpr float kLargeScore = 0x1p12f;
+
 __device__ __forceinline__ float exp2_f(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // tanh to about two units in the last place.  Below 0.8 the fraction

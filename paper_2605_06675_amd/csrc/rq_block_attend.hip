@@ -63,7 +63,7 @@ __device__ __forceinline__ void rescale(Running<D>* st, float by) {
 // exceeds the reference by more than 8 (log2).
 template <int D>
 __device__ __forceinline__ void probabilities(Running<D>* st, f4 s[2]) {
-  float top = -3.0e38f;
+  float top = kNoScore;
 #pragma unroll
   for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -242,10 +242,10 @@ __device__ __forceinline__ void merge_tile(const BlockAttendLaunch& a, const Par
     const bool on = row < rows;
     // this lane has the maxima and sums of splits col, col + kCols, ..
     f2 ml[kEach];
-    float m = -1.0e30f, l = 0.0f;
+    float m = kNoScore, l = 0.0f;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      ml[i] = (f2){-1.0e30f, 0.0f};
+      ml[i] = (f2){kNoScore, 0.0f};
       if (on && col + i * kCols < a.splits) ml[i] = parts.load_ml(col + i * kCols, row);
     }
 #pragma unroll
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch 
     load_queries<D, BF16>(a, b, h, 16 * n + r, past, nnew, &q[n]);
 #pragma unroll
     for (int e = 0; e < D / 16; ++e) st[n].o[e] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
-    st[n].m = -1.0e30f;
+    st[n].m = kNoScore;
     st[n].l = 0.0f;
     st[n].unit = 0.0f;
   }
@@ -473,7 +473,7 @@ __device__ __forceinline__ void merge_row(const BlockAttendLaunch& a, int grow, 
   const size_t base = ((size_t)unit * a.row_tiles + rt) * a.splits;
   const RQ_GLOBAL float* ml = gptr(a.part_ml) + (base * 16 + row) * 2;
   const RQ_GLOBAL float* o = gptr(a.part) + (base * 16 + row) * D + col * 4;
-  float m = -1.0e30f;
+  float m = kNoScore;
   for (int s = lane; s < a.splits; s += 64) m = __builtin_fmaxf(m, ml[s * 32]);
   m = wave_all<Max>(m);
   float l = 0.0f;
@@ -514,7 +514,7 @@ __global__ void __launch_bounds__(256) block_merge_rows_kernel(BlockAttendLaunch
   const size_t base = ((size_t)unit * a.row_tiles + (grow >> 4)) * a.splits;
   const RQ_GLOBAL f2* ml = (const RQ_GLOBAL f2*)(gptr(a.part_ml) + (base * 16 + row) * 2);
   const RQ_GLOBAL float* o = gptr(a.part) + (base * 16 + row) * D + col * 4;
-  float m = -1.0e30f, l = 0.0f;
+  float m = kNoScore, l = 0.0f;
   f4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
   for (int s = 0; s < a.splits; ++s) m = __builtin_fmaxf(m, ml[s * 16].x);
@@ -565,7 +565,7 @@ __global__ void __launch_bounds__(256) block_merge_weigh_kernel(BlockAttendLaunc
   for (int row = threadIdx.x >> 4; row < rows; row += 16) {
     if (a.splits > 1) {
       const RQ_GLOBAL float* ml = gptr(a.part_ml) + (((size_t)unit * a.row_tiles + (row >> 4)) * a.splits * 16 + (row & 15)) * 2;
-      float m = -1.0e30f, l = 0.0f;
+      float m = kNoScore, l = 0.0f;
       for (int s = lane; s < a.splits; s += 16) m = __builtin_fmaxf(m, ml[s * 32]);
       m = row_all<Max>(m);
       for (int s = lane; s < a.splits; s += 16)

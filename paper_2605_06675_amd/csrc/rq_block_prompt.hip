@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
   for (int c = 0; c < D / 32; ++c)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[c][i] = 0.0f;
-  float m = -1.0e30f, l = 0.0f, unit2 = 0.0f;
+  float m = kNoScore, l = 0.0f, unit2 = 0.0f;
   const bool far = a.slopes || a.window;
 
   float tks[2], tvs[2];               // scales of a tile's blocks
@@ -391,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
       off = 0.0f;
     }
     // the running maximum (moved when a score exceeds it by 8) and unit
-    float top = -3.0e38f;
+    float top = kNoScore;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       float x = s[t][0];
@@ -418,6 +418,19 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) o[c] *= by;
     }
+    // (Scores this large differ from their maximum by more than an exponent
+    // holds through its rounding alone, and swallow log2(by): the difference is
+    // taken of rounded ones, and first.)
+    float reference = m - off;
+    if (__any(__builtin_fabsf(m) > kLargeScore && m > kNoScore)) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[t][i] = __builtin_fmaf(s[t][i], f[t], off) - m;
+        f[t] = 1.0f;
+      }
+      reference = 0.0f;
+    }
     // Probabilities of the second block are formed between the first one's
     // products.
     float by[2], c[2], sum[2] = {0.0f, 0.0f};
@@ -426,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
     for (int t = 0; t < 2; ++t) {
       // (codes under a scale of zero are zero: any factor serves)
       by[t] = tvs[t] > 0.0f ? __builtin_fmaxf(tvs[t] * unit2, 0x1p-80f) : 1.0f;
-      c[t] = m - __builtin_amdgcn_logf(by[t]) - off;
+      c[t] = reference - __builtin_amdgcn_logf(by[t]);
     }
     auto form = [&](int t, int i) {
       const float x = exp2_f(__builtin_fmaf(s[t][2 * i], f[t], -c[t]));

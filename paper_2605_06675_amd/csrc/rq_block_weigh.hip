@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
 #pragma unroll
     for (int i = 0; i < kShare / 8; ++i) raw[i] = (u4){0u, 0u, 0u, 0u};
     // (a row behind the last adds exp2(-3e38) * 0)
-    info.m = 3.0e38f;
+    info.m = -kNoScore;
     info.qs = info.inv = info.slope = 0.0f;
     info.token = info.pos = 0;
     if (row >= rows) return;
@@ -222,6 +222,7 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
         s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key[t][k], q, s[t], 0, 0, 0);
     }
     const bool masked = a.window || slot0 + kWaveTokens - 1 > past + over(row0, a.by_G);
+    const bool large = __any(__builtin_fabsf(r.m) > kLargeScore && r.m < -kNoScore);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       float f = ks[t] * r.qs, off = 0.0f;      // scores are s f + off
@@ -233,7 +234,7 @@ __global__ void __launch_bounds__(256, 2) block_weigh_kernel(BlockAttendLaunch a
         f = 2.0f * a.cap;
         off = a.cap;
       }
-      if (far || masked || a.fine) {
+      if (far || masked || a.fine || large) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[t][i] = __builtin_fmaf(s[t][i], f, off);
         if (a.fine) {

@@ -513,6 +513,85 @@ def test_attend_large_caps(cap, n, dtype, out, D):
             assert (np.abs(add - u.weight) <= tol + 1e-30).all(), (b, h)
 
 
+@both
+@pytest.mark.parametrize("n,G", [(1, 1), (5, 2), (30, 2), (40, 4)])
+@pytest.mark.parametrize("window", [0, 1])
+def test_attend_scores_far_below_zero(fmt, n, G, window):
+    """Scores of -1.4e31, alike for all tokens a row sees: of the unfinished
+    block its mean, behind a window of one the token itself."""
+    if not window and n > 31:
+        n = 31
+    r = Rig(fmt, "bf16", G=G, cap=64)
+    k, v = r.kv(n)
+    k[:] = 2.0 ** 50
+    r.append(n, kv=(k, v))
+    o = torch.full((2, 2 * G, n, 128), 7.5, device="cuda")
+    ws = torch.empty(rq.rq_block_attention_workspace(r.c.desc, n, 64, True), dtype=torch.uint8, device="cuda")
+    q = torch.full((2, 2 * G, n, 128), -2.0 ** 50, dtype=r.dt, device="cuda")
+    rq.rq_block_attention(r.c.desc, 0, ints([0, 0]), q, o, ws, max_tokens=64, window=window, accumulate=True)
+    o, w = o.cpu().double().numpy(), r.weights()
+    for b in range(2):
+        for h in range(2):
+            V = r.u[b][h].values(1).astype(np.float64)
+            seen = [V[i:i + 1] if window else V[:i + 1] for i in range(n)]
+            want = np.stack([x.mean(0) for x in seen])
+            for g in range(G):
+                assert np.abs(o[b, h * G + g] - want).max() <= 8 * 2.0 ** -22 * np.abs(V).max()
+            add = G * (np.ones(n) if window else np.cumsum(1 / np.arange(n, 0, -1.0))[::-1])
+            np.testing.assert_allclose(w[b, h, :n], add, rtol=1e-5)
+
+
+@pytest.mark.parametrize("fmt,most", [("int8", 127.0), ("e4m3", 448.0)])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("n", [1, 7, 40])
+def test_attend_equal_scores_of_any_size(fmt, most, sign, n):
+    """Keys alike, whose codes and scale are exact, and scores of 2^33 and more:
+    still the mean of values whose blocks' scales differ."""
+    r = Rig(fmt, "bf16", cap=256)
+    for size in (1.0, 100.0, 0.01, 1.0):
+        k, v = r.kv(50)
+        k[:] = most * 2.0 ** 10
+        r.append(50, kv=(k, (v * size).to(r.dt)))
+    q = torch.full((2, 4, n, 128), sign * 2.0 ** 10, dtype=r.dt)
+    o = r.attend(n, q=q, scale=1.0, accumulate=True).cpu().double().numpy()
+    for b in range(2):
+        for h in range(2):
+            V = r.u[b][h].values(1).astype(np.float64)
+            want = np.stack([V[:201 - n + i].mean(0) for i in range(n)])
+            for g in range(2):
+                assert np.abs(o[b, 2 * h + g] - want).max() <= 6 * 2.0 ** -22 * np.abs(V).max()
+            np.testing.assert_allclose(r.weights()[b, h, :200 - n], 2 * sum(1 / (201 - n + i) for i in range(n)),
+                                       rtol=1e-5)
+
+
+@both
+@pytest.mark.parametrize("dtype,size,scale", [("bf16", 2.0 ** 17, 1.0), ("bf16", 2.0 ** 17, -1.0),
+                                              ("fp16", 2.0 ** 5, 2.0 ** 20)])
+@pytest.mark.parametrize("n", [1, 7, 40])
+def test_attend_large_scores_pick_one_token(fmt, dtype, size, scale, n):
+    """Scores of 2^32 and more: the values of the largest, wherever it leads by
+    more than the products' rounding."""
+    r = Rig(fmt, dtype, cap=256)
+    k, v = r.kv(200)
+    r.append(200, kv=((k.float() * size).to(r.dt), v))
+    q = (r.randn(2, 4, n, 128) * size).to(r.dt)
+    o = r.attend(n, q=q, scale=scale, accumulate=True).cpu().double().numpy()
+    sure = 0
+    for b in range(2):
+        for h in range(2):
+            K, V = (r.u[b][h].values(s).astype(np.float64) for s in (0, 1))
+            for g in range(2):
+                for i in range(n):
+                    qq = q[b, 2 * h + g, i].double().numpy()
+                    seen = K[:201 - n + i]
+                    x, err = scale * (seen @ qq), np.abs(scale) * (np.abs(seen) @ np.abs(qq)).max() * 2.0 ** -16
+                    top = np.argsort(x)[-2:]
+                    if x[top[1]] - x[top[0]] > err + 100:
+                        sure += 1
+                        assert np.abs(o[b, 2 * h + g, i] - V[top[1]]).max() <= 2.0 ** -20 * np.abs(V).max()
+    assert sure >= 4 * n
+
+
 # ----------------------------------------------------------------- eviction
 def evict(r, keep, sink, recent, weight=None):
     """Evicts r's cache; returns a rig around the new one, checked."""
