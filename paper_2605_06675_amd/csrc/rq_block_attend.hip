@@ -14,6 +14,8 @@
 // Long contexts are bound by memory: 32 units of 32768 tokens (268 MB) 47 us, 5.7
 // TB/s where a plain read reaches 7.  Short ones by a chain of latencies (1001
 // tokens 7.8 us): lengths, codes, the four waves' sums, parts, ticket, merge.
+#include <algorithm>
+
 #include "rq_block.h"
 
 namespace rq {
@@ -618,9 +620,9 @@ hipError_t launch(const BlockAttendLaunch& a, hipStream_t s) {
   const int rows = a.n * a.G;
   if (a.scores) {
     // 1024 tokens a workgroup (one more where a window begins inside one)
-    int tokens = a.max_tokens;
-    if (a.window && a.window + a.n < tokens) tokens = a.window + a.n;
-    const int parts = (tokens + 1023) / 1024 + (a.window ? 1 : 0);
+    int64_t tokens = a.max_tokens;
+    if (a.window) tokens = std::min(tokens, (int64_t)a.window + a.n);
+    const int parts = (int)((tokens + 1023) / 1024) + (a.window ? 1 : 0);
     hipLaunchKernelGGL((block_merge_weigh_kernel<D>), dim3((a.splits > 1 ? rows : 0) + parts, a.c.B * a.c.H),
                        dim3(256), 0, s, a);
     return hipGetLastError();

@@ -592,6 +592,16 @@ def test_attend_large_scores_pick_one_token(fmt, dtype, size, scale, n):
     assert sure >= 4 * n
 
 
+@pytest.mark.parametrize("n,L", [(1, 90), (1, 1900), (5, 1900), (40, 300)])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 3, 2 ** 30])
+def test_attend_windows_beyond_every_position(n, L, window):
+    """No limit, written as a window: results and weights of none."""
+    r = Rig("int8", "bf16", G=2, D=64, cap=2048)
+    r.append(L)
+    r.attend(n, window=window, accumulate=True)
+    r.attend(n, window=window, max_tokens=2048, accumulate=True)
+
+
 # ----------------------------------------------------------------- eviction
 def evict(r, keep, sink, recent, weight=None):
     """Evicts r's cache; returns a rig around the new one, checked."""
