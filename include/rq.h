@@ -510,7 +510,7 @@ rq_status rq_block_evict_workspace(const rq_block_cache* src, int32_t keep,
  * their positions and weights.  Kept values are code * scale in fp32 (or the
  * tail's 16-bit numbers), quantized again in dst's blocks, and rounded to
  * dtype where they land in dst's tail.  new_lengths: device int32 [batch],
- * receives min(L, keep).  n_sink + n_recent <= keep.  ws: device scratch,
+ * receives min(L, keep); no part of lengths.  n_sink + n_recent <= keep.  ws: device scratch,
  * 16-byte aligned, contents arbitrary.  src is left as it was.
  * Asynchronous. */
 rq_status rq_block_evict(const rq_block_cache* src, const rq_block_cache* dst,

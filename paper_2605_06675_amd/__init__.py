@@ -662,8 +662,8 @@ def rq_block_evict_workspace(cache, keep):
 def rq_block_evict(src, dst, layer, lengths, keep, new_lengths, ws, n_sink=4,
                    n_recent=32, stream=None):
     """Shrink one layer of src into dst; lengths, new_lengths: device int32
-    [batch]; ws: device byte tensor of at least rq_block_evict_workspace
-    bytes."""
+    [batch], not the same memory; ws: device byte tensor of at least
+    rq_block_evict_workspace bytes."""
     if lengths is None or new_lengths is None:
         raise ValueError("lengths and new_lengths are needed")
     if dst._device != src._device:

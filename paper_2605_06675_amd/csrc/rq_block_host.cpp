@@ -370,6 +370,9 @@ rq_status rq_block_evict(const rq_block_cache* src, const rq_block_cache* dst, i
     return fail(RQ_ESMALLWS, "workspace %llu bytes < %llu needed", (unsigned long long)ws_bytes,
                 (unsigned long long)need);
   if (!ws || unaligned(ws)) return fail(RQ_EINVAL, "the workspace is NULL or not 16-byte aligned");
+  const uintptr_t from = reinterpret_cast<uintptr_t>(lengths), to = reinterpret_cast<uintptr_t>(new_lengths);
+  if ((from > to ? from - to : to - from) < src->batch * sizeof(int32_t))
+    return fail(RQ_EINVAL, "lengths and new_lengths overlap (the lengths are read to the end)");
   rq::BlockEvictLaunch a{};
   a.src = layer_of(src, layer);
   a.dst = layer_of(dst, layer);

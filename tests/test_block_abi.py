@@ -146,6 +146,17 @@ def test_evict_refusals():
     assert call(size=need - 1) == rq.RQ_ESMALLWS
 
 
+def test_evict_refuses_lengths_that_it_would_overwrite():
+    """Every workgroup reads the lengths until the last launch."""
+    L, src = rq.lib(), desc()
+    dst = desc(**{n: P * (i + 9) for i, n in enumerate(("codes", "scales", "tail", "positions", "weights"))})
+    need = rq.rq_block_evict_workspace(src, 40)
+    for lengths, new in ((P, P), (P, P + 4), (P + 8, P)):
+        assert L.rq_block_evict(C.byref(src), C.byref(dst), 0, lengths, 40, 4, 8, new, P, need,
+                                None) == rq.RQ_EINVAL
+        assert b"lengths" in L.rq_last_error()
+
+
 def test_python_refusals_need_no_device():
     with pytest.raises(ValueError):
         rq.make_block_cache(rq.RQ_INT8, rq.RQ_BF16, 1, 1, 1, 1, 64, 32,
