@@ -440,11 +440,22 @@ rq_status rq_block_sizes(const rq_block_cache* c, uint64_t* codes_bytes,
  * do not fit the capacity are dropped.  Codes every block that becomes full,
  * keeps the rest in the tail, sets the new slots' positions (one more than
  * the slot before; 0 in an empty sequence) and their weights to 0.  The
- * caller adds the new tokens to its lengths.  Asynchronous. */
+ * caller adds the new tokens to its lengths (rq_block_advance, where some may
+ * not fit).  Asynchronous. */
 rq_status rq_block_append(const rq_block_cache* c, int32_t layer,
                           const int32_t* past, int32_t n_new,
                           const int32_t* new_len, const rq_block_rows* k,
                           const rq_block_rows* v, rq_stream stream);
+
+/* Lengths after an append of n_new rows with new_len (as above): lengths
+ * (device int32 [batch], values in 0..capacity) grow by the tokens that fit.
+ * Each of past (the lengths before), fitting (how many fit) and dropped (how
+ * many do not) receives int32 [batch]; NULL: not wanted.  An attention call
+ * with past and fitting for new_len leaves dropped tokens out.  Asynchronous. */
+rq_status rq_block_advance(const rq_block_cache* c, int32_t* lengths,
+                           int32_t n_new, const int32_t* new_len,
+                           int32_t* past, int32_t* fitting, int32_t* dropped,
+                           rq_stream stream);
 
 /* What an attention call asks of one layer. */
 typedef struct rq_block_query {

@@ -30,8 +30,9 @@ EXPORTS = ("rq_version", "rq_last_error", "rq_cache_sizes", "rq_region_offset",
            "rq_sensitivity_workspace", "rq_sensitivity", "rq_cap_weights",
            "rq_fallback_beta", "rq_decode_static_bytes",
            "rq_decode_attention_static", "rq_read_probe", "rq_decode_step",
-           "rq_block_sizes", "rq_block_append", "rq_block_attention_workspace",
-           "rq_block_attention", "rq_block_evict_workspace", "rq_block_evict")
+           "rq_block_sizes", "rq_block_append", "rq_block_advance",
+           "rq_block_attention_workspace", "rq_block_attention",
+           "rq_block_evict_workspace", "rq_block_evict")
 RQ_TURBO_TABLE_FLOATS = 8 * 2 * 256
 
 
@@ -125,6 +126,7 @@ def lib():
         sig.update({
             "rq_block_sizes": (i32, [pb] + [pu64] * 6),
             "rq_block_append": (i32, [pb, i32, vp, i32, vp, vp, vp, vp]),
+            "rq_block_advance": (i32, [pb, vp, i32, vp, vp, vp, vp, vp]),
             "rq_block_attention_workspace": (i32, [pb, pq, pu64]),
             "rq_block_attention": (i32, [pb, i32, vp, vp, u64, vp]),
             "rq_block_evict_workspace": (i32, [pb, i32, pu64]),
@@ -611,6 +613,20 @@ def rq_block_append(cache, layer, past, k, v, new_len=None, stream=None):
                 _ROWS.pack(*rv))
 
 
+def rq_block_advance(cache, lengths, n_new, new_len=None, past=None,
+                     fitting=None, dropped=None, stream=None):
+    """lengths grow by the tokens of an append that fit; all device int32
+    [batch]."""
+    if lengths is None:
+        raise ValueError("lengths is missing")
+    _block_call(cache, stream, lib().rq_block_advance, C.byref(cache),
+                _block_lengths(cache, lengths, "lengths"), n_new,
+                _block_lengths(cache, new_len, "new_len"),
+                _block_lengths(cache, past, "past"),
+                _block_lengths(cache, fitting, "fitting"),
+                _block_lengths(cache, dropped, "dropped"))
+
+
 def rq_block_attention_workspace(cache, n_new, max_tokens=None,
                                  accumulate=False, window=0):
     """Workspace bytes of an attention call (a call with a window needs no
@@ -683,8 +699,10 @@ class BlockCache:
     each other by the caller's events.  All can be captured into a graph
     (evict with a given `into`).  A captured call is planned for the whole
     capacity; its replays move the lengths on, and drop tokens that do not
-    fit.  From then on the layer's `bound` is the capacity, and a call that
-    appends to it outside a graph may wait to read the lengths."""
+    fit: these are not attended and do not attend (their rows of `out` are left
+    as they were, or 0 where the call made it).  From then on the layer's
+    `bound` is the capacity, and a call that appends to it outside a graph may
+    wait to read the lengths."""
 
     def __init__(self, format, dtype, n_layers, batch, n_kv_heads, n_q_heads,
                  head_dim, capacity, device="cuda", weights=False):
@@ -705,6 +723,11 @@ class BlockCache:
                                    device=device)
         self.bound = [0] * n_layers
         self._replayed = set()      # layers that a graph appends to
+        # of the tokens appended last: those before, those that fitted and those
+        # that did not; layers where it may be any
+        self._last = torch.zeros(n_layers, 3, batch, dtype=torch.int32,
+                                 device=device)
+        self._drops = set()
         self._ws = None
         self._held = []             # workspaces that a graph writes to
 
@@ -731,12 +754,13 @@ class BlockCache:
 
     def _grow(self, layer, n, new_len, stream):
         import torch
-        s, capturing = self._on(stream)
-        with torch.cuda.stream(s):
-            row = self.lengths[layer]
-            row += n if new_len is None else new_len.clamp(0, n)
-            if capturing:
-                row.clamp_(max=self.desc.capacity)
+        row = self.lengths[layer]
+        if layer in self._drops:
+            rq_block_advance(self.desc, row, n, new_len,
+                             *self._last[layer].unbind(), stream=stream)
+        else:
+            with torch.cuda.stream(self._on(stream)[0]):
+                row += n if new_len is None else new_len.clamp(0, n)
         if layer not in self._replayed:
             self.bound[layer] += n
 
@@ -747,6 +771,7 @@ class BlockCache:
         s, capturing = self._on(stream)
         if capturing:
             self._replayed.add(layer)
+            self._drops.add(layer)
             self.bound[layer] = capacity
             return capacity
         held = self.bound[layer]
@@ -790,8 +815,10 @@ class BlockCache:
         import torch
         s, capturing = self._on(stream)
         with torch.cuda.stream(s):
-            past = self.lengths[layer] - (q.shape[2] if new_len is None
-                                          else new_len.clamp(0, q.shape[2]))
+            new = q.shape[2] if new_len is None else new_len.clamp(0, q.shape[2])
+            if capturing or layer in self._drops:
+                new = new_len = (new - self._last[layer, 2]).clamp_(min=0)
+            past = self.lengths[layer] - new
         bound = self.desc.capacity if capturing else self.bound[layer]
         return self._attend(layer, past, bound, q, out, new_len, stream, kw)
 
@@ -801,6 +828,10 @@ class BlockCache:
         bound = self._room(layer, k.shape[2], stream)
         past = self.lengths[layer]
         rq_block_append(self.desc, layer, past, k, v, new_len, stream)
+        if layer in self._drops:
+            self._grow(layer, k.shape[2], new_len, stream)
+            past, fitting, _ = self._last[layer].unbind()
+            return self._attend(layer, past, bound, q, out, fitting, stream, kw)
         try:
             return self._attend(layer, past, bound, q, out, new_len, stream, kw)
         finally:
@@ -825,4 +856,10 @@ class BlockCache:
                 into._replayed.add(layer)
             into.bound[layer] = (into.desc.capacity if layer in into._replayed
                                  else min(self.bound[layer], keep))
+        if capturing:
+            into._drops.update(range(self.desc.n_layers))
+        if self._drops or into._drops:      # (the last tokens stay the last)
+            with torch.cuda.stream(s):
+                into._last.copy_(self._last)
+            into._drops |= self._drops
         return into

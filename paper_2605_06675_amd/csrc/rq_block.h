@@ -59,6 +59,13 @@ struct BlockAppendLaunch {
   int n;
 };
 
+struct BlockAdvanceLaunch {
+  int32_t* lengths;        // [B], as the following
+  const int32_t* new_len;  // or NULL
+  int32_t *past, *fitting, *dropped;   // each or NULL
+  int B, cap, n;
+};
+
 struct BlockAttendLaunch {
   BlockLayer c;
   const int32_t* past;
@@ -102,6 +109,7 @@ struct BlockEvictLaunch {
 };
 
 hipError_t launch_block_append(const BlockAppendLaunch& a, hipStream_t s);
+hipError_t launch_block_advance(const BlockAdvanceLaunch& a, hipStream_t s);
 hipError_t launch_block_attend(const BlockAttendLaunch& a, hipStream_t s);
 hipError_t launch_block_prompt(const BlockAttendLaunch& a, hipStream_t s);
 hipError_t launch_block_merge(const BlockAttendLaunch& a, hipStream_t s);

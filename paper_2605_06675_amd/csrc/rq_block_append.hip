@@ -85,6 +85,20 @@ __global__ void __launch_bounds__(256) block_append_kernel(BlockAppendLaunch a) 
   }
 }
 
+// A thread a sequence: the rule by which the kernel above drops tokens.
+__global__ void __launch_bounds__(256) block_advance_kernel(BlockAdvanceLaunch a) {
+  const int b = blockIdx.x * 256 + threadIdx.x;
+  if (b >= a.B) return;
+  int past = gptr(a.lengths)[b], nnew = a.new_len ? gptr(a.new_len)[b] : a.n;
+  past = past < 0 ? 0 : (past > a.cap ? a.cap : past);
+  nnew = nnew < 0 ? 0 : (nnew > a.n ? a.n : nnew);
+  const int fit = nnew > a.cap - past ? a.cap - past : nnew;
+  gptr(a.lengths)[b] = past + fit;
+  if (a.past) gptr(a.past)[b] = past;
+  if (a.fitting) gptr(a.fitting)[b] = fit;
+  if (a.dropped) gptr(a.dropped)[b] = nnew - fit;
+}
+
 template <int FMT, int D>
 hipError_t launch(const BlockAppendLaunch& a, hipStream_t s) {
   const dim3 grid((a.n + 4 * kBlockTokens - 1) / (4 * kBlockTokens), 2 * a.c.B * a.c.H);
@@ -96,6 +110,11 @@ hipError_t launch(const BlockAppendLaunch& a, hipStream_t s) {
 }
 
 }  // namespace
+
+hipError_t launch_block_advance(const BlockAdvanceLaunch& a, hipStream_t s) {
+  hipLaunchKernelGGL(block_advance_kernel, dim3((a.B + 255) / 256), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
 
 hipError_t launch_block_append(const BlockAppendLaunch& a, hipStream_t s) {
   if (a.c.fmt == RQ_INT8) return a.c.D == 64 ? launch<RQ_INT8, 64>(a, s) : launch<RQ_INT8, 128>(a, s);

@@ -249,6 +249,19 @@ rq_status rq_block_append(const rq_block_cache* c, int32_t layer, const int32_t*
                   "append launch");
 }
 
+rq_status rq_block_advance(const rq_block_cache* c, int32_t* lengths, int32_t n_new,
+                           const int32_t* new_len, int32_t* past, int32_t* fitting,
+                           int32_t* dropped, rq_stream stream) {
+  rq_status st = check_shape(c);
+  if (st != RQ_OK) return st;
+  if (n_new < 1 || n_new > c->capacity)
+    return fail(RQ_EINVAL, "n_new %d outside 1..%d", n_new, c->capacity);
+  if (!lengths) return fail(RQ_EINVAL, "NULL device pointer");
+  const rq::BlockAdvanceLaunch a{lengths, new_len, past, fitting, dropped, c->batch, c->capacity, n_new};
+  return launched(rq::launch_block_advance(a, reinterpret_cast<hipStream_t>(stream)),
+                  "advance launch");
+}
+
 rq_status rq_block_attention_workspace(const rq_block_cache* c, const rq_block_query* a,
                                        uint64_t* bytes) {
   rq_status st = check_shape(c);

@@ -94,6 +94,15 @@ def test_append_refusals():
     assert L.rq_block_append(C.byref(c), 0, P, 1, None, None, None, None) == rq.RQ_EINVAL
 
 
+def test_advance_refusals():
+    L = rq.lib()
+    assert L.rq_block_advance(None, P, 1, None, None, None, None, None) == rq.RQ_EINVAL
+    assert L.rq_block_advance(C.byref(desc(capacity=100)), P, 1, None, None, None, None, None) == rq.RQ_EINVAL
+    for lengths, n in ((None, 1), (P, 0), (P, 97)):
+        assert L.rq_block_advance(C.byref(desc()), lengths, n, None, None, None, None, None) == rq.RQ_EINVAL
+        assert rq.rq_last_error()
+
+
 @pytest.mark.parametrize("kw,status", [
     (dict(n_new=0), -1), (dict(n_new=97, max_tokens=97), -1), (dict(max_tokens=1), -1),
     (dict(max_tokens=97), -1), (dict(past=None), -1), (dict(q=rows(None)), -1),

@@ -865,6 +865,90 @@ def test_captured_steps_share_the_cache_with_eager_ones():
     r.check()
 
 
+@pytest.mark.parametrize("n", [1, 3, 20])
+@pytest.mark.parametrize("separate", [False, True])
+@pytest.mark.parametrize("padded", [False, True])
+def test_captured_step_stops_at_the_capacity(n, separate, padded):
+    """Replays that reach the capacity: the tokens that fit attend as they would
+    in an eager call, the others neither answer nor add weight."""
+    r = Rig("e4m3", "bf16", B=4, cap=64)
+    r.append(60, [60, 59, 0, 31])
+    given = [n, max(n - 1, 0), n, 1] if padded else [n] * 4
+    k, v = (torch.zeros(4, 2, n, 128, dtype=r.dt, device="cuda") for _ in range(2))
+    q = torch.zeros(4, 4, n, 128, dtype=r.dt, device="cuda")
+    new_len = ints(given) if padded else None
+    out = torch.zeros(4, 4, n, 128, device="cuda")
+
+    def call():
+        if not separate:
+            return r.c.step(0, k, v, q, out, new_len, accumulate=True)
+        r.c.append(0, k, v, new_len)
+        return r.c.attention(0, q, out, new_len, accumulate=True)
+    graph, o = graph_of(call)
+    for turn in range(7):
+        hk, hv = r.kv(n)
+        hq = r.randn(4, 4, n, 128).to(r.dt)
+        k.copy_(hk)
+        v.copy_(hv)
+        q.copy_(hq)
+        out.fill_(7.5)
+        fits = [min(m, 64 - L) for m, L in zip(given, r.lengths())]
+        before = np.nan_to_num(r.weights())
+        graph.replay()
+        torch.cuda.synchronize()
+        r.took(hk, hv, fits)
+        r.compare(hq, o, fits, accumulate=True, before=before)
+        assert r.c.lengths.tolist() == [r.lengths()]
+    r.check()
+    assert r.lengths()[0] == 64
+    # the rows that a call makes for itself hold zeros for such tokens
+    graph, o = graph_of(lambda: r.c.step(0, k, v, q, None, new_len))
+    for turn in range(2):
+        o.fill_(7.5)
+        fits = [min(m, 64 - L) for m, L in zip(given, r.lengths())]
+        graph.replay()
+        torch.cuda.synchronize()
+        r.took(hk, hv, fits)
+        for b in range(4):
+            assert (o[b, :, fits[b]:] == 0).all() and (o[b, :, :fits[b]] != 7.5).all()
+    # an eager call afterwards: the tokens handed last, of which these fitted
+    o = r.c.attention(0, q, out.fill_(7.5), new_len)
+    r.compare(hq, o, fits)
+    # lengths taken back by the caller and an eager append: all of it fits again
+    for b in range(4):
+        for h in range(2):
+            u = r.u[b][h]
+            u.__init__(u.fmt, u.D, u.narrow)
+    r.c.lengths.zero_()
+    hk, hv = r.kv(5)
+    r.append(5, kv=(hk, hv))
+    hq = r.randn(4, 4, 5, 128).to(r.dt)
+    r.compare(hq, r.c.attention(0, hq.cuda(), torch.full((4, 4, 5, 128), 7.5, device="cuda")))
+
+
+def test_advance():
+    """Lengths as the append that drops tokens leaves them, out of range and all."""
+    c = rq.BlockCache(rq.RQ_INT8, rq.RQ_BF16, 1, 300, 1, 1, 64, 64).desc
+    rng = np.random.default_rng(0)
+    for n, given in ((1, False), (64, False), (9, True)):
+        old, new = rng.integers(-3, 70, 300), rng.integers(-2, 12, 300)
+        old[:4] = [-2 ** 31, 2 ** 31 - 1, 64, 0]
+        x = [ints(old)] + [torch.full((300,), 77, dtype=torch.int32, device="cuda") for _ in range(3)]
+        rq.rq_block_advance(c, x[0], n, ints(new) if given else None, *x[1:])
+        past = old.clip(0, 64)
+        asked = new.clip(0, n) if given else np.full(300, n)
+        fit = np.minimum(asked, 64 - past)
+        for got, want in zip(x, (past + fit, past, fit, asked - fit)):
+            np.testing.assert_array_equal(got.cpu().numpy(), want)
+        lengths = ints(old)
+        rq.rq_block_advance(c, lengths, n, ints(new) if given else None)
+        assert torch.equal(lengths, x[0])
+    with pytest.raises(ValueError):
+        rq.rq_block_advance(c, None, 1)
+    with pytest.raises(ValueError):
+        rq.rq_block_advance(c, lengths, 1, past=lengths[:4])
+
+
 def test_captured_attention_and_eviction():
     """A graph that attends, weighs and evicts, replayed over a cache that
     grows by eager calls in between."""
