@@ -717,17 +717,18 @@ class BlockCache:
         for name, size, t in zip(names, sizes, types):
             new = torch.zeros(size // t.itemsize, dtype=t, device=device)
             setattr(self, name, new if name != "weights" or weights else None)
-        self.desc = make_block_cache(*self.shape, capacity,
-                                     **{n: getattr(self, n) for n in names})
         self.lengths = torch.zeros(n_layers, batch, dtype=torch.int32,
                                    device=device)
-        self.bound = [0] * n_layers
-        self._replayed = set()      # layers that a graph appends to
         # of the tokens appended last: those before, those that fitted and those
         # that did not; layers where it may be any
         self._last = torch.zeros(n_layers, 3, batch, dtype=torch.int32,
                                  device=device)
         self._drops = set()
+        # (which waits for the buffers' zeros, these included)
+        self.desc = make_block_cache(*self.shape, capacity,
+                                     **{n: getattr(self, n) for n in names})
+        self.bound = [0] * n_layers
+        self._replayed = set()      # layers that a graph appends to
         self._ws = None
         self._held = []             # workspaces that a graph writes to
 

@@ -1023,6 +1023,29 @@ def test_another_stream_and_shared_workspace_in_order():
     assert to.lengths.tolist() == [[50, 50]]
 
 
+def test_a_new_cache_is_ready_for_any_stream(monkeypatch):
+    """The constructor waits for all that it clears: nothing is left on its
+    stream, however late, when it returns."""
+    held = [torch.full((n,), 77, dtype=torch.int32, device="cuda") for n in (4, 12) for _ in range(64)]
+    del held                                    # memory that the allocator hands out again
+    make = rq.make_block_cache
+
+    def slow(*a, **kw):
+        c = make(*a, **kw)
+        if kw:
+            torch.cuda._sleep(100_000_000)      # what follows on the stream comes late
+        return c
+    monkeypatch.setattr(rq, "make_block_cache", slow)
+    c = rq.BlockCache(rq.RQ_INT8, rq.RQ_BF16, 2, 2, 1, 1, 64, 64)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        copies = [x.clone() for x in (c.lengths, c._last)]
+    side.synchronize()
+    late = not torch.cuda.current_stream().query()
+    torch.cuda.synchronize()
+    assert late and all((x == 0).all() for x in copies)
+
+
 def test_python_refusals():
     r = Rig("int8", "bf16", cap=64)
     r.append(40)
