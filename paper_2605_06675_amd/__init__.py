@@ -815,12 +815,14 @@ class BlockCache:
         rq_block_attention)."""
         import torch
         s, capturing = self._on(stream)
+        bound = self.desc.capacity if capturing else self.bound[layer]
+        if new_len is not None:         # (padding may be more rows than tokens)
+            bound = max(bound, q.shape[2])
         with torch.cuda.stream(s):
             new = q.shape[2] if new_len is None else new_len.clamp(0, q.shape[2])
             if capturing or layer in self._drops:
                 new = new_len = (new - self._last[layer, 2]).clamp_(min=0)
             past = self.lengths[layer] - new
-        bound = self.desc.capacity if capturing else self.bound[layer]
         return self._attend(layer, past, bound, q, out, new_len, stream, kw)
 
     def step(self, layer, k, v, q, out=None, new_len=None, stream=None, **kw):

@@ -989,6 +989,15 @@ def test_padding_does_not_use_up_the_capacity():
         r.append(60, [1, 1])          # 49 + 60 rows, whatever they hold
 
 
+def test_attention_of_more_padded_rows_than_the_cache_holds():
+    r = Rig("int8", "bf16", cap=96)
+    r.append(5, [5, 3])
+    for n in (8, 90):
+        q = r.randn(2, 4, n, 128).to(r.dt)
+        o = torch.full(q.shape, 7.5, device="cuda")
+        r.compare(q, r.c.attention(0, q.cuda(), o, ints([5, 2])), [5, 2])
+
+
 def test_refused_attention_leaves_the_step_s_tokens():
     r = Rig("int8", "bf16", cap=64, weights=False)
     r.append(40)
