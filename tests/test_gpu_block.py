@@ -602,6 +602,79 @@ def test_attend_windows_beyond_every_position(n, L, window):
     r.attend(n, window=window, max_tokens=2048, accumulate=True)
 
 
+def fill(r, L):
+    """Appends L tokens to every sequence; the oracle's blocks at once."""
+    k, v = r.kv(L)
+    r.c.append(r.layer, k.cuda(), v.cuda())
+    full = L // 32 * 32
+    for b in range(r.B):
+        for h in range(r.H):
+            u = r.u[b][h]
+            for s, x in ((0, k), (1, v)):
+                part = [block.quantize(u.fmt, x[b, h, i:i + 32].float().numpy()) for i in range(0, full, 32)]
+                u.codes[s] = np.concatenate([c for c, _ in part])
+                u.scales[s] = np.array([y for _, y in part], np.float32)
+                u.tail[s] = x[b, h, full:].float().numpy()
+            u.pos, u.weight = np.arange(L), np.zeros(L)
+
+
+OPTIONS = [dict(), dict(cap=15.0), dict(window=70), dict(slopes=True), dict(cap=9.0, window=150, slopes=True)]
+
+
+@both
+@pytest.mark.parametrize("B,H,G,n,L", [(1, 8, 2, 100, 301), (2, 8, 4, 33, 160), (4, 4, 3, 90, 90), (3, 1, 8, 70, 500)])
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("bf16", "fp32"), ("fp16", "fp16")])
+@pytest.mark.parametrize("kw", OPTIONS)
+def test_prompt_units_and_options(fmt, B, H, G, n, L, dtype, out, kw):
+    """Prompts of 8 and 16 units and others, several tiles of rows, split and
+    not, 128 channels: outputs of every type, masks and biases, weights."""
+    r = Rig(fmt, dtype, B=B, H=H, G=G, D=128, cap=512)
+    fill(r, L)
+    if "slopes" in kw:
+        kw = {**kw, "slopes": (2.0 ** (-8.0 * np.arange(1, H * G + 1) / (H * G))).astype(np.float32).tolist()}
+    r.attend(n, accumulate=True, out={**DT, "fp32": (0, torch.float32)}[out][1], **kw)
+
+
+@pytest.mark.parametrize("dtype,n,G,L", [("fp16", 512, 16, 4609), ("bf16", 520, 8, 4192), ("fp16", 256, 16, 8100)])
+def test_long_chunks_split_in_two(dtype, n, G, L):
+    """Chunks of many rows behind many tokens, uneven ones, against an fp64
+    product on the device."""
+    B, H, D, cap = 2, 4 if G == 16 else 8, 64, (L + 31) // 32 * 32
+    r = Rig("int8", dtype, B=B, H=H, G=G, D=D, cap=cap)
+    lengths, new = [L, L - 700], [n, n - 90]
+    k, v = (x.cuda() for x in r.kv(L, lengths))
+    r.c.append(0, k, v, ints(lengths))
+    q = r.randn(B, H * G, n, D).to(r.dt).cuda()
+    q[1, :, n - 90:] = math.nan
+    o = r.c.attention(0, q, torch.full(q.shape, 7.5, device="cuda"), ints(new), accumulate=True)
+    codes = r.c.codes.view(torch.int8).view(B, H, 2, cap, D)
+    scales, tail = r.c.scales.view(B, H, 2, cap // 32), r.c.tail.view(B, H, 2, 32, D)
+    for b in range(B):
+        T, m = lengths[b], new[b]
+        full = T // 32 * 32
+        assert (o[b, :, m:] == 7.5).all()
+        hide = torch.arange(T, device="cuda") > torch.arange(T - m, T, device="cuda")[:, None]
+        for h in range(H):
+            K, V = (torch.cat([(codes[b, h, s, :full].float() * scales[b, h, s, :full // 32]
+                                .repeat_interleave(32)[:, None]).double(), tail[b, h, s, :T - full].double()])
+                    for s in (0, 1))
+            add = torch.zeros(T, dtype=torch.float64, device="cuda")
+            worst, big = 0.0, float(V.abs().max())
+            for g in range(G):
+                x = q[b, h * G + g, :m].double()
+                p = torch.softmax((x @ K.T.contiguous() / math.sqrt(D)).masked_fill(hide, -math.inf), -1)
+                add += p.sum(0)
+                a = 1.4427 / math.sqrt(D) * (x.abs() @ K.abs().T.contiguous()).amax(-1)
+                s = (D + 4) * 2.0 ** -24 * a
+                if dtype == "bf16":
+                    s += D * 2.0 ** -25 * 1.4427 / math.sqrt(D) * x.abs().amax(-1) * K.abs().sum(-1).max()
+                ratio = 2 * s * math.log(2) + 2.0 ** -21 + (T / 4 + 64) * 2.0 ** -24
+                worst = max(worst, float(ratio.max()))
+                assert ((o[b, h * G + g, :m].double() - p @ V).abs() <= (ratio[:, None] + 2.0 ** -21) * big).all()
+            w = r.c.weights.view(B, H, cap)[b, h, :T].double()
+            assert ((w - add).abs() <= worst * add + 2.0 ** -24 * (1 + m * G) * add + 1e-30).all()
+
+
 # ----------------------------------------------------------------- eviction
 def evict(r, keep, sink, recent, weight=None):
     """Evicts r's cache; returns a rig around the new one, checked."""
@@ -722,6 +795,32 @@ def test_evict_selection_of_unusual_weights(L, cap, kind):
         order[:sink] = order[L - recent:] = math.inf
         rank = torch.sort(order, stable=True, descending=True)[1][:keep]
         assert torch.equal(pos[h, :keep].long(), torch.sort(rank)[0])
+
+
+@pytest.mark.parametrize("L,cap", [(139_999, 140_000), (262_145, 262_176), (301_003, 301_024)])
+@pytest.mark.parametrize("kind", ["random", "zero", "few", "levels"])
+def test_evict_selection_of_many_parts(L, cap, kind):
+    """More than sixteen parts, and parts of more than one tile."""
+    r = Rig("e4m3", "bf16", B=1, H=2, D=64, cap=cap)
+    c = r.c
+    c.codes.zero_()
+    c.scales.zero_()
+    c.tail.zero_()
+    c.positions.view(2, cap).copy_(torch.arange(cap, dtype=torch.int32).expand(2, -1))
+    c.lengths.fill_(L)
+    w = torch.rand(2, cap, generator=r.g)
+    w = {"random": w, "zero": w * 0, "few": (w < 0.01).float(), "levels": (w * 40).floor()}[kind]
+    c.weights.view(2, cap).copy_(w)
+    keep, sink, recent = L // 7, 5, 77
+    to = c.evict(keep, sink, recent)
+    pos = to.positions.view(2, -1).cpu()
+    assert to.lengths.tolist() == [[keep]]
+    for h in range(2):
+        order = w[h, :L].double()
+        order[:sink] = order[L - recent:] = math.inf
+        rank = torch.sort(order, stable=True, descending=True)[1][:keep]
+        assert torch.equal(pos[h, :keep].long(), torch.sort(rank)[0])
+        assert torch.equal(to.weights.view(2, -1)[h, :keep].cpu(), w[h, pos[h, :keep].long()])
 
 
 def test_evict_parts_of_uneven_sequences():
