@@ -126,10 +126,10 @@ struct Plan {
 // More than two tiles of 16 rows: tiles of 128 rows, two workgroups a CU, at
 // least four blocks each.  Where the new tokens are few beside the cached ones,
 // sequences may differ in length and a round's workgroups with them: one split
-// more (4 sequences, 8 kv-heads of 4 heads, 512 tokens over 8192: 358 us
-// unsplit, 366 in two; lengths from 2048 to 8192: 289 and 250).  Up to eight blocks
-// a split saves less than its merging launch takes (192 tiles of 143 tokens 14.2
-// us, in two splits 22.6).
+// more (4 sequences, 8 kv-heads of 4 heads, 512 tokens over 8192: 426 us
+// unsplit, 440 in two; lengths from 2048 to 8192: 322 and 254).  Up to eight blocks
+// a split saves less than its merging launch takes (256 tiles of 143 tokens 15.3
+// us, in two splits 24.6).
 Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
   Plan p{};
   const int64_t G = c->n_q_heads / c->n_kv_heads, u = (int64_t)units(c);
@@ -158,8 +158,11 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
   }
   if (a->accumulate) {
     p.stats = tiles * 16 * 2 * sizeof(float);
-    // one or two tiles of rows: the scores are kept (4 bytes a row and token) rather
-    // than computed again from the keys (D bytes a token)
+    // one or two tiles of rows: the scores are kept (4 bytes a row and token, out
+    // and back) rather than computed again from the keys, which takes a prompt's
+    // kernels.  us so / with those, 4, 8, 16 and 32 rows: 16 sequences to 8192
+    // tokens 38, 42, 49, 70 / 128 to 131, to 1000 14, 15, 17, 24 / 30 to 32, two to
+    // 8192 15, 16, 18, 27 / 30 to 33.
     const int64_t rows = a->n_new * G;
     if (!p.prompt) {
       p.scores = (uint64_t)u * ((a->max_tokens + rq::kBlockTokens - 1) / rq::kBlockTokens) * rows *
@@ -168,9 +171,9 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
     }
     // else workgroups of 256 tokens, and parts of the rows to fill two rounds (two
     // a CU; windows leave some without rows: four), about 128 rows or more in
-    // each.  us with four / two rounds: 32 units of 2000 tokens, 1000 rows 103 / 95,
-    // 8 of 32000 and 400 rows 147 / 136, 2 of 8000 and 400 rows 39 / 41; 32 of 8192
-    // and 2036 rows, window of 2000: 278 / 305.
+    // each.  us a call with four / two rounds: 32 units of 2000 tokens, 1000 rows
+    // 125 / 118, 8 of 32000 and 400 rows 169 / 159, 2 of 8000 and 400 rows 42 / 41;
+    // 32 of 8192 and 2036 rows, window of 2000: 324 / 428.
     // (A window needs no more workspace than none: the size counts its parts.)
     const int64_t round = 2 * (int64_t)rq::device_cus(), wgs = u * ((a->max_tokens + 255) / 256);
     const int64_t most = std::max<int64_t>(std::min(4 * round / wgs, (rows + 63) / 128), 1);

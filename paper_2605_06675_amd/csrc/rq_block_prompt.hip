@@ -15,13 +15,13 @@
 // a call of many rows would answer otherwise than one of few, by 2^-12 of the
 // result before its rounding, and be a quarter faster.
 //
-// Two prompts of 4096 tokens (8 kv-heads of 4 heads, 128 channels, e4m3): 323 us,
-// 850 TFLOP/s; capped 385; fp16 418.  Neither unit bounds it alone: a wave's tile
-// is 440 vector instructions (96 of them, capped, exponentials and reciprocals)
-// and 1024 cycles of the matrix unit, with two waves a SIMD; capped the units are
-// 64 and 29 % busy.  Workgroups of 256 rows (half the conversions) took 513 us
-// where this one took 501; the conversion between the products of the tile
-// before does not fit the registers.
+// Two prompts of 4096 tokens (8 kv-heads of 4 heads, 128 channels, e4m3): 412 us,
+// 667 TFLOP/s, bf16 as fp16; capped 480.  Neither unit bounds it alone: a wave's
+// tile is, capped, some 500 vector instructions (96 of them exponentials and
+// reciprocals) and 1536 cycles of the matrix unit, with two waves a SIMD; the
+// units are 60 and 37 % busy.  Workgroups of 256 rows (half the conversions) took
+// 2 % longer; the conversion between the products of the tile before does not fit
+// the registers.
 #include "rq_block.h"
 
 namespace rq {
@@ -75,8 +75,8 @@ __device__ __forceinline__ void load_tile(const RQ_GLOBAL uint8_t* kc, const RQ_
   }
 }
 
-// WHOLE: no slot of the tile lies behind the last (without the comparisons the
-// whole call takes 2 % less).
+// WHOLE: no slot of the tile lies behind the last (without the comparisons 512
+// tokens over 8192 take 2 % less, capped prompts 1 % more).
 template <int FMT, int D, bool WHOLE>
 __device__ __forceinline__ void store_tile(const TileLoad& t, int slot0, int slots, uint8_t* sk,
                                            uint8_t* sv) {
@@ -189,8 +189,9 @@ __global__ void __launch_bounds__(kThreads, 2) block_prompt_kernel(BlockAttendLa
   const int col = lane & 31, hl = lane >> 5;
   // Two workgroups share a SIMD, a wave each.  The wave in the odd slot (the low
   // bit of hardware register 4) goes first, so that one's products meet the
-  // other's exponentials: 512 tokens over 8192 in chunks 332 -> 322 us, 4096 of 64
-  // channels 205 -> 197, uncapped 128 channels 327 -> 323.
+  // other's exponentials: 509 tokens over up to 8192, with weights, 411 -> 381 us,
+  // 4096 uncapped ones 436 -> 431, fp16 440 -> 432; capped 488 -> 490, 64 channels
+  // alike.
   if (__builtin_amdgcn_s_getreg(4 | (3 << 11)) & 1) __builtin_amdgcn_s_setprio(1);
   // workgroups go round the XCDs: where the units are a multiple of eight, a
   // unit's tiles share an L2; the tiles that see most tokens go first

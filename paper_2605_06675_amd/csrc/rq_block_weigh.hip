@@ -10,7 +10,7 @@
 // workgroups are few, several share the rows, and a small launch adds their sums
 // in order: the result does not depend on scheduling.
 //
-// 32 units of up to 8192 tokens, 2036 rows: 117 us.  A wave's 32 rows are 512
+// 32 units of up to 8192 tokens, 2036 rows: 116 us.  A wave's 32 rows are 512
 // cycles of products and 600 of exponentials and sums, two waves a SIMD; a
 // workgroup takes 70 us, 4 of them to begin, and the last round is half empty.
 #include "rq_block.h"
