@@ -1048,6 +1048,32 @@ def test_advance():
         rq.rq_block_advance(c, lengths, 1, past=lengths[:4])
 
 
+@pytest.mark.parametrize("n", [1, 3])
+def test_eviction_after_dropped_tokens(n):
+    """The last tokens stay the last: in the smaller cache, too, those that did
+    not fit are left out of what follows; the next append has room for all."""
+    r = Rig("int8", "bf16", cap=64)
+    r.append(63, [63, 20])
+    k, v = (torch.zeros(2, 2, n, 128, dtype=r.dt, device="cuda") for _ in range(2))
+    graph, _ = graph_of(lambda: r.c.append(0, k, v))
+    for turn in range(2):
+        hk, hv = r.kv(n)
+        k.copy_(hk)
+        v.copy_(hv)
+        fits = [min(n, 64 - L) for L in r.lengths()]
+        graph.replay()
+        r.took(hk, hv, fits)
+    assert fits == [0, n]
+    to = evict(r, 40, 4, 16)
+    q = r.randn(2, 4, n, 128).to(r.dt)
+    out = torch.full((2, 4, n, 128), 7.5, device="cuda")
+    to.compare(q, to.c.attention(0, q.cuda(), out), fits)
+    to.append(3)
+    to.check()
+    q = r.randn(2, 4, 3, 128).to(r.dt)
+    to.compare(q, to.c.attention(0, q.cuda()))
+
+
 def test_captured_attention_and_eviction():
     """A graph that attends, weighs and evicts, replayed over a cache that
     grows by eager calls in between."""
