@@ -450,8 +450,9 @@ rq_status rq_block_append(const rq_block_cache* c, int32_t layer,
 /* Lengths after an append of n_new rows with new_len (as above): lengths
  * (device int32 [batch], values in 0..capacity) grow by the tokens that fit.
  * Each of past (the lengths before), fitting (how many fit) and dropped (how
- * many do not) receives int32 [batch]; NULL: not wanted.  An attention call
- * with past and fitting for new_len leaves dropped tokens out.  Asynchronous. */
+ * many do not) receives int32 [batch]; NULL: not wanted.  The arrays must not
+ * overlap.  An attention call with past and fitting for new_len leaves dropped
+ * tokens out.  Asynchronous. */
 rq_status rq_block_advance(const rq_block_cache* c, int32_t* lengths,
                            int32_t n_new, const int32_t* new_len,
                            int32_t* past, int32_t* fitting, int32_t* dropped,

@@ -69,6 +69,12 @@ rq_status check_buffers(const rq_block_cache* c, int32_t layer) {
   return RQ_OK;
 }
 
+// Two arrays of n int32 (none overlaps NULL).
+bool overlap(const int32_t* a, const int32_t* b, int32_t n) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && (x > y ? x - y : y - x) < n * sizeof(int32_t);
+}
+
 uint64_t units(const rq_block_cache* c) { return (uint64_t)c->batch * c->n_kv_heads; }
 
 rq::BlockLayer layer_of(const rq_block_cache* c, int32_t layer) {
@@ -260,6 +266,10 @@ rq_status rq_block_advance(const rq_block_cache* c, int32_t* lengths, int32_t n_
   if (n_new < 1 || n_new > c->capacity)
     return fail(RQ_EINVAL, "n_new %d outside 1..%d", n_new, c->capacity);
   if (!lengths) return fail(RQ_EINVAL, "NULL device pointer");
+  const int32_t* arrays[] = {lengths, new_len, past, fitting, dropped};
+  for (int i = 0; i < 5; ++i)
+    for (int j = 0; j < i; ++j)
+      if (overlap(arrays[i], arrays[j], c->batch)) return fail(RQ_EINVAL, "two of the arrays overlap");
   const rq::BlockAdvanceLaunch a{lengths, new_len, past, fitting, dropped, c->batch, c->capacity, n_new};
   return launched(rq::launch_block_advance(a, reinterpret_cast<hipStream_t>(stream)),
                   "advance launch");
@@ -386,8 +396,7 @@ rq_status rq_block_evict(const rq_block_cache* src, const rq_block_cache* dst, i
     return fail(RQ_ESMALLWS, "workspace %llu bytes < %llu needed", (unsigned long long)ws_bytes,
                 (unsigned long long)need);
   if (!ws || unaligned(ws)) return fail(RQ_EINVAL, "the workspace is NULL or not 16-byte aligned");
-  const uintptr_t from = reinterpret_cast<uintptr_t>(lengths), to = reinterpret_cast<uintptr_t>(new_lengths);
-  if ((from > to ? from - to : to - from) < src->batch * sizeof(int32_t))
+  if (overlap(lengths, new_lengths, src->batch))
     return fail(RQ_EINVAL, "lengths and new_lengths overlap (the lengths are read to the end)");
   rq::BlockEvictLaunch a{};
   a.src = layer_of(src, layer);

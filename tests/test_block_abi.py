@@ -103,6 +103,18 @@ def test_advance_refusals():
         assert rq.rq_last_error()
 
 
+def test_advance_refuses_overlapping_arrays():
+    L, c = rq.lib(), desc()
+    for i in range(5):
+        for j in range(5):
+            if i == j:
+                continue
+            a = [P * (k + 1) for k in range(5)]
+            a[i] = a[j] + (4 if i < j else 8)          # three int32 each
+            assert L.rq_block_advance(C.byref(c), a[0], 1, *a[1:], None) == rq.RQ_EINVAL
+            assert b"overlap" in L.rq_last_error()
+
+
 @pytest.mark.parametrize("kw,status", [
     (dict(n_new=0), -1), (dict(n_new=97, max_tokens=97), -1), (dict(max_tokens=1), -1),
     (dict(max_tokens=97), -1), (dict(past=None), -1), (dict(q=rows(None)), -1),
