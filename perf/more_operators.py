@@ -364,7 +364,7 @@ def _verify(s):
             r = torch.where(no[:, None], left, r)
             mass = torch.where(no, left.sum(-1), mass)
         else:
-            mass = torch.where(no, mass - rx, mass)
+            mass = torch.where(no, (mass - rx).clamp(min=0), mass)
             r[rows, x] = torch.where(no, torch.zeros_like(rx), rx)
         r = torch.where(yes[:, None], target[:, i].double(), r)
         mass = torch.where(yes, torch.ones_like(mass), mass)
@@ -546,7 +546,7 @@ def _exact_verify(c, s):
                     r = torch.relu(r / mass - q) if mass > 0 else r * 0
                     mass = float(r.sum())
                 else:
-                    mass -= float(r[x])
+                    mass = max(0.0, mass - float(r[x]))
                     r = r.clone()
                     r[x] = 0
         if not float(r.sum()) > 0:
