@@ -531,6 +531,153 @@ rq_status rq_block_evict(const rq_block_cache* src, const rq_block_cache* dst,
                          int32_t* new_lengths, void* ws, uint64_t ws_bytes,
                          rq_stream stream);
 
+/* ------------------------------------------------------------------------
+ * Speculative decoding over the block-scaled cache: a draft proposes a tree of
+ * tokens for every sequence, the target runs them all in one step, and the
+ * longest path that its probabilities accept is kept.  A step lays the tree out
+ * (rq_tree_mask), attends in every layer (rq_block_tree_attention), verifies
+ * (rq_tree_verify) and appends the path's keys and values to all layers
+ * (rq_block_accept).  A drafted token's keys and values stay outside the cache
+ * until then: an append codes full blocks, which cannot be taken back.
+ *
+ * The drafted tokens ("nodes") of a sequence are numbered so that parents come
+ * before their children.  parents[b][i] is a node before i, or -1: node i
+ * follows the last cached token itself.  (For verification node 0 is the root: a
+ * token that is accepted already, as the one that the step before drew last.)
+ * Of n_nodes rows a sequence uses the first new_len[b] (device int32 [batch];
+ * NULL: all); the others may hold anything, and their outputs are left as they
+ * were.  Values of device arrays outside the stated range are taken as the
+ * nearest inside. */
+#define RQ_MAX_NODES 1024
+
+/* Lay out trees: mask (device uint32 [batch][n_nodes][ceil(n_nodes / 32)])
+ * says in bit j % 32 of word j / 32 of row i that node i sees node j, its
+ * ancestors and itself; depth (device int32 [batch][n_nodes]; NULL: not wanted)
+ * counts its ancestors among the nodes.  parents: device int32
+ * [batch][n_nodes].  1 <= n_nodes <= RQ_MAX_NODES, batch <= 65535.  The arrays
+ * must not overlap.  Asynchronous. */
+rq_status rq_tree_mask(int32_t batch, int32_t n_nodes, const int32_t* parents,
+                       const int32_t* new_len, uint32_t* mask, int32_t* depth,
+                       rq_stream stream);
+
+/* What a tree's attention call asks of one layer. */
+typedef struct rq_block_tree {
+  int32_t n_nodes;         /* 1..RQ_MAX_NODES                              */
+  int32_t max_tokens;      /* bound on the cached tokens, 0..capacity      */
+  const int32_t* past;     /* device [batch]: cached tokens, 0..max_tokens */
+  const int32_t* new_len;  /* device [batch]: nodes of each sequence
+                              (0..n_nodes), or NULL: n_nodes               */
+  const uint32_t* mask;    /* device [batch][n_nodes][ceil(n_nodes / 32)]:
+                              the nodes that each one sees (rq_tree_mask's,
+                              or any other, bits of later nodes among them;
+                              bits from new_len on count as 0)             */
+  const int32_t* depth;    /* device [batch][n_nodes], 0..n_nodes - 1: needed
+                              where there is a window or slopes            */
+  rq_block_rows q;         /* [batch][n_q_heads][n_nodes][head_dim] and    */
+  rq_block_rows k, v;      /* [batch][n_kv_heads][n_nodes][head_dim] in
+                              dtype                                        */
+  rq_block_rows out;       /* the shape of q in out_dtype                  */
+  int32_t out_dtype;       /* RQ_F32, RQ_F16 or RQ_BF16                    */
+  float scale, cap;        /* as rq_block_query, which see                 */
+  int32_t window;
+  const float* slopes;
+} rq_block_tree;
+
+/* Workspace bytes of rq_block_tree_attention for n_nodes, max_tokens and
+ * window of *t (its pointers may be NULL).  Host only. */
+rq_status rq_block_tree_attention_workspace(const rq_block_cache* c,
+                                            const rq_block_tree* t,
+                                            uint64_t* bytes);
+
+/* Attention of a tree's nodes over the cached tokens and the nodes that each
+ * sees:
+ *   out[b][j][i] = softmax(x) V,
+ *   x = f(scale * q[b][j][i] . K) - slope_j * (p_i - p)
+ * over the slots t < past (K = K_hat_t, p = p_t) and the nodes a of the mask's
+ * row i (K = k[b][.][a], p = p_a), where p_i - p < window.  A node's position
+ * is that of the last cached token (-1 in an empty cache) + 1 + its depth.  A
+ * row that sees nothing is 0.  The cache is left as it was, its accumulated
+ * weights too: which nodes stay is not known yet.  Accuracy, ws and counters
+ * as rq_block_attention.  Asynchronous. */
+rq_status rq_block_tree_attention(const rq_block_cache* c, int32_t layer,
+                                  const rq_block_tree* t, void* ws,
+                                  uint64_t ws_bytes, rq_stream stream);
+
+/* Drafted trees, the probabilities they are verified against, and the results.
+ * Rows of probabilities are contiguous and may begin at any element. */
+typedef struct rq_tree_draft {
+  int32_t batch;            /* 1..65535                                    */
+  int32_t n_nodes;          /* 1..RQ_MAX_NODES                             */
+  int32_t vocab;            /* entries of a row, 1..2^24                   */
+  int32_t dtype;            /* of target and draft: RQ_F32, RQ_F16, RQ_BF16 */
+  const int32_t* tokens;    /* device [batch][n_nodes], 0..vocab - 1 (a
+                               root's is not read for a result)            */
+  const int32_t* parents;   /* device [batch][n_nodes]                     */
+  const int32_t* new_len;   /* device [batch], or NULL                     */
+  const void* target;       /* [batch][n_nodes][vocab]: row i, what follows
+                               node i under the target                     */
+  int64_t target_stride_batch, target_stride_node;   /* elements          */
+  const void* draft;        /* the same shape: row i, what node i's children
+                               were drawn from, each by itself; or NULL: they
+                               were not drawn (the likeliest tokens, say)  */
+  int64_t draft_stride_batch, draft_stride_node;
+  const float* uniforms;    /* device [batch][n_nodes], in [0, 1): node i's
+                               test; a root's draws the last token         */
+  int32_t n_path;           /* room in path: 1..n_nodes                    */
+  int32_t* path;            /* device [batch][n_path]: the accepted nodes in
+                               order, the root first; -1 behind them       */
+  int32_t* count;           /* device [batch]: how many (0 where new_len is) */
+  int32_t* next;            /* device [batch]: the token drawn behind the
+                               path (-1 where new_len is 0)                */
+} rq_tree_draft;
+
+/* Workspace bytes of rq_tree_verify (pointers of *d may be NULL).  Host
+ * only. */
+rq_status rq_tree_verify_workspace(const rq_tree_draft* d, uint64_t* bytes);
+
+/* Verify drafted trees.  From the root, the children of the last accepted
+ * node are tested in order.  With r the target's row of that node, s = 1:
+ * child c of token x is accepted where u_c * q(x) * s < r(x), q being the
+ * draft's row of the node (1 without a draft).  A rejected one leaves
+ *   r <- max(0, r / s - q), s <- sum of r    (with a draft)
+ *   s <- max(0, s - r(x)), r(x) <- 0         (without)
+ * to the next (a residual without mass accepts none).  Where none is accepted,
+ * or the path is full (the node's children are not tested then), the token
+ * next is the first one whose running sum of r exceeds u_0 times the whole sum
+ * (the last of r > 0 where rounding leaves none); r without mass is replaced by
+ * the target's row.  Tokens of a path and next so follow the target's
+ * distribution whatever the draft.
+ * Products, quotients and sums are fp64.  Probabilities must be finite and not
+ * negative; their sum is taken as 1 (rounded ones serve).  ws: device scratch,
+ * 16-byte aligned, contents arbitrary; calls that share it must not overlap.
+ * Asynchronous. */
+rq_status rq_tree_verify(const rq_tree_draft* d, void* ws, uint64_t ws_bytes,
+                         rq_stream stream);
+
+/* A device tensor [n_layers][batch][n_kv_heads][n_nodes][head_dim] whose rows
+ * are contiguous and may begin at any element; strides in elements. */
+typedef struct rq_block_layers {
+  void* data;
+  int64_t stride_layer, stride_batch, stride_head, stride_token;
+} rq_block_layers;
+
+/* Append a path of drafted tokens to every layer: in layer l, sequence b takes
+ * the rows k[l][b][.][path[b][j]] and v, j < count[b], as rq_block_append does.
+ * lengths: device int32 [n_layers][batch], tokens held before.  path: device
+ * int32 [batch][n_path], nodes 0..n_nodes - 1; count: device int32 [batch],
+ * 0..n_path (as rq_tree_verify leaves them).  Tokens that do not fit the
+ * capacity are dropped.  new_lengths: device int32 [n_layers][batch], receives
+ * the lengths after it; it may be lengths itself.  Each of past (the lengths
+ * before), fitting (how many fitted) and dropped (how many did not) receives
+ * int32 [n_layers][batch]; NULL: not wanted.  The arrays must not overlap
+ * otherwise.  Asynchronous. */
+rq_status rq_block_accept(const rq_block_cache* c, const int32_t* lengths,
+                          int32_t n_nodes, int32_t n_path, const int32_t* path,
+                          const int32_t* count, const rq_block_layers* k,
+                          const rq_block_layers* v, int32_t* new_lengths,
+                          int32_t* past, int32_t* fitting, int32_t* dropped,
+                          rq_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

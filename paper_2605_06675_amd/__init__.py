@@ -22,6 +22,7 @@ RQ_KIVI, RQ_QUAROT, RQ_TURBO, RQ_RTN, RQ_KIVI_RTN = 0, 1, 2, 3, 4
 RQ_F16, RQ_BF16, RQ_F32 = 0, 1, 2
 RQ_INT8, RQ_E4M3 = 0, 1
 RQ_MAX_KV_HEADS = 32
+RQ_MAX_NODES = 1024
 
 EXPORTS = ("rq_version", "rq_last_error", "rq_cache_sizes", "rq_region_offset",
            "rq_quantize_kv", "rq_decode_workspace", "rq_decode_attention",
@@ -32,7 +33,9 @@ EXPORTS = ("rq_version", "rq_last_error", "rq_cache_sizes", "rq_region_offset",
            "rq_decode_attention_static", "rq_read_probe", "rq_decode_step",
            "rq_block_sizes", "rq_block_append", "rq_block_advance",
            "rq_block_attention_workspace", "rq_block_attention",
-           "rq_block_evict_workspace", "rq_block_evict")
+           "rq_block_evict_workspace", "rq_block_evict", "rq_tree_mask",
+           "rq_block_tree_attention_workspace", "rq_block_tree_attention",
+           "rq_tree_verify_workspace", "rq_tree_verify", "rq_block_accept")
 RQ_TURBO_TABLE_FLOATS = 8 * 2 * 256
 
 
@@ -75,6 +78,35 @@ class RqBlockQuery(C.Structure):
                 ("out_dtype", C.c_int32), ("scale", C.c_float),
                 ("cap", C.c_float), ("window", C.c_int32),
                 ("slopes", C.c_void_p), ("accumulate", C.c_int32)]
+
+
+class RqBlockTree(C.Structure):
+    _fields_ = [("n_nodes", C.c_int32), ("max_tokens", C.c_int32),
+                ("past", C.c_void_p), ("new_len", C.c_void_p),
+                ("mask", C.c_void_p), ("depth", C.c_void_p),
+                ("q", RqBlockRows), ("k", RqBlockRows), ("v", RqBlockRows),
+                ("out", RqBlockRows), ("out_dtype", C.c_int32),
+                ("scale", C.c_float), ("cap", C.c_float),
+                ("window", C.c_int32), ("slopes", C.c_void_p)]
+
+
+class RqTreeDraft(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_nodes", C.c_int32),
+                ("vocab", C.c_int32), ("dtype", C.c_int32),
+                ("tokens", C.c_void_p), ("parents", C.c_void_p),
+                ("new_len", C.c_void_p), ("target", C.c_void_p),
+                ("target_stride_batch", C.c_int64),
+                ("target_stride_node", C.c_int64), ("draft", C.c_void_p),
+                ("draft_stride_batch", C.c_int64),
+                ("draft_stride_node", C.c_int64), ("uniforms", C.c_void_p),
+                ("n_path", C.c_int32), ("path", C.c_void_p),
+                ("count", C.c_void_p), ("next", C.c_void_p)]
+
+
+class RqBlockLayers(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_layer", C.c_int64),
+                ("stride_batch", C.c_int64), ("stride_head", C.c_int64),
+                ("stride_token", C.c_int64)]
 
 
 _lib = None
@@ -132,6 +164,16 @@ def lib():
             "rq_block_evict_workspace": (i32, [pb, i32, pu64]),
             "rq_block_evict": (i32, [pb, pb, i32, vp, i32, i32, i32, vp, vp,
                                      u64, vp]),
+        })
+        pt, pd_ = C.POINTER(RqBlockTree), C.POINTER(RqTreeDraft)
+        sig.update({
+            "rq_tree_mask": (i32, [i32, i32, vp, vp, vp, vp, vp]),
+            "rq_block_tree_attention_workspace": (i32, [pb, pt, pu64]),
+            "rq_block_tree_attention": (i32, [pb, i32, vp, vp, u64, vp]),
+            "rq_tree_verify_workspace": (i32, [pd_, pu64]),
+            "rq_tree_verify": (i32, [vp, vp, u64, vp]),
+            "rq_block_accept": (i32, [pb, vp, i32, i32, vp, vp, vp, vp, vp, vp,
+                                      vp, vp, vp]),
         })
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -539,15 +581,24 @@ def rq_block_sizes(cache):
 # filling ctypes structures takes, where a call takes ten microseconds)
 _ROWS = struct.Struct("@Pqqq")
 _QUERY = struct.Struct("@iiPPPqqqPqqqiffiPi4x")
+_TREE = struct.Struct("@iiPPPPPqqqPqqqPqqqPqqqiffiP")
+_DRAFT = struct.Struct("@iiiiPPPPqqPqqPiPPP")
+_LAYERS = struct.Struct("@Pqqqq")
 assert _ROWS.size == C.sizeof(RqBlockRows)
 assert _QUERY.size == C.sizeof(RqBlockQuery)
+assert _TREE.size == C.sizeof(RqBlockTree)
+assert _DRAFT.size == C.sizeof(RqTreeDraft)
+assert _LAYERS.size == C.sizeof(RqBlockLayers)
 
 
 def _block_call(cache, stream, f, *args):
     """Launch on the given stream, or the current one of the cache's device,
     with that device current."""
-    device = cache._device
-    current, raw_stream = cache._calls
+    _device_call(cache._device, cache._calls, stream, f, *args)
+
+
+def _device_call(device, calls, stream, f, *args):
+    current, raw_stream = calls
     if stream is None:
         s = raw_stream(device.index)
     elif stream.device != device:
@@ -591,6 +642,14 @@ def _block_lengths(cache, t, what):
             or t.shape != (cache.batch,) or not t.is_contiguous():
         raise ValueError(f"{what} must be int32 [{cache.batch}] on the cache's device")
     return t.data_ptr()
+
+
+def _block_slopes(cache, slopes):
+    if slopes is not None and (slopes.device != cache._device
+                               or cache._out_types.get(slopes.dtype) != RQ_F32
+                               or slopes.shape != (cache.n_q_heads,)
+                               or not slopes.is_contiguous()):
+        raise ValueError(f"slopes must be float32 [{cache.n_q_heads}] on the cache's device")
 
 
 def _block_ws(cache, ws):
@@ -651,11 +710,7 @@ def rq_block_attention(cache, layer, past, q, out, ws, new_len=None,
     n = q.shape[2] if q.dim() == 4 else -1
     if past is None:
         raise ValueError("past is missing")
-    if slopes is not None and (slopes.device != cache._device
-                               or cache._out_types.get(slopes.dtype) != RQ_F32
-                               or slopes.shape != (cache.n_q_heads,)
-                               or not slopes.is_contiguous()):
-        raise ValueError(f"slopes must be float32 [{cache.n_q_heads}] on the cache's device")
+    _block_slopes(cache, slopes)
     rq_ = _block_rows(cache, q, "q", cache.n_q_heads, n, cache._type)
     ro = _block_rows(cache, out, "out", cache.n_q_heads, n, cache._out_types)
     a = _QUERY.pack(
@@ -667,6 +722,168 @@ def rq_block_attention(cache, layer, past, q, out, ws, new_len=None,
         0 if slopes is None else slopes.data_ptr(), 1 if accumulate else 0)
     _block_call(cache, stream, lib().rq_block_attention, C.byref(cache), layer,
                 a, *_block_ws(cache, ws))
+
+
+# ------------------------------------------------------ trees of drafted tokens
+def _tree_array(t, what, device, *shape, dtype=None):
+    """Pointer of a contiguous tensor (int32 by default)."""
+    import torch
+    dtype = torch.int32 if dtype is None else dtype
+    if t.dtype is not dtype or t.device != device or t.shape != shape \
+            or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous {dtype} {list(shape)} on {device}")
+    return t.data_ptr()
+
+
+def _tree_call(device, stream, f, *args):
+    import torch
+    if device.type != "cuda":
+        raise ValueError(f"the tensors are on {device}, not on a GPU")
+    calls = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    _device_call(device, calls, stream, f, *args)
+
+
+def rq_tree_mask(parents, mask, depth=None, new_len=None, stream=None):
+    """Which nodes each drafted token sees.  parents: device int32
+    [batch][n_nodes]; mask: int32 [batch][n_nodes][ceil(n_nodes / 32)], 32 nodes a
+    word; depth: int32 [batch][n_nodes] (both are written); new_len: int32
+    [batch]."""
+    if parents.dim() != 2:
+        raise ValueError(f"parents has shape {tuple(parents.shape)}, expected two axes")
+    B, n = parents.shape
+    at = parents.device
+    _tree_call(at, stream, lib().rq_tree_mask, B, n,
+               _tree_array(parents, "parents", at, B, n),
+               0 if new_len is None else _tree_array(new_len, "new_len", at, B),
+               _tree_array(mask, "mask", at, B, n, (n + 31) // 32),
+               0 if depth is None else _tree_array(depth, "depth", at, B, n))
+
+
+def rq_block_tree_attention_workspace(cache, n_nodes, max_tokens=None, window=0):
+    """Workspace bytes of a tree's attention call."""
+    a = RqBlockTree(n_nodes, cache.capacity if max_tokens is None else max_tokens)
+    a.window = int(window)
+    v = C.c_uint64()
+    _check(lib().rq_block_tree_attention_workspace(C.byref(cache), C.byref(a),
+                                                   C.byref(v)))
+    return v.value
+
+
+def rq_block_tree_attention(cache, layer, past, q, k, v, mask, out, ws,
+                            depth=None, new_len=None, max_tokens=None,
+                            scale=None, cap=0.0, window=0, slopes=None,
+                            stream=None):
+    """Attention of drafted tokens over the cached ones and each other: q: torch
+    [batch][n_q_heads][n_nodes][head_dim], k, v: [batch][n_kv_heads][n_nodes]
+    [head_dim] in the cache's dtype; out: q's shape in float32, float16 or
+    bfloat16 (all any strides, contiguous rows); mask, depth: rq_tree_mask's
+    (depth where there is a window or slopes); past: device int32 [batch], cached
+    tokens; max_tokens: bound on them (the capacity by default); the rest as
+    rq_block_attention."""
+    n = q.shape[2] if q.dim() == 4 else -1
+    if past is None:
+        raise ValueError("past is missing")
+    _block_slopes(cache, slopes)
+    B, at = cache.batch, cache._device
+    rq_ = _block_rows(cache, q, "q", cache.n_q_heads, n, cache._type)
+    rk = _block_rows(cache, k, "k", cache.n_kv_heads, n, cache._type)
+    rv = _block_rows(cache, v, "v", cache.n_kv_heads, n, cache._type)
+    ro = _block_rows(cache, out, "out", cache.n_q_heads, n, cache._out_types)
+    a = _TREE.pack(
+        n, cache.capacity if max_tokens is None else max_tokens,
+        _block_lengths(cache, past, "past"),
+        _block_lengths(cache, new_len, "new_len"),
+        _tree_array(mask, "mask", at, B, n, (n + 31) // 32),
+        0 if depth is None else _tree_array(depth, "depth", at, B, n),
+        *rq_, *rk, *rv, *ro, cache._out_types[out.dtype],
+        cache.head_dim ** -0.5 if scale is None else scale, cap, window,
+        0 if slopes is None else slopes.data_ptr())
+    _block_call(cache, stream, lib().rq_block_tree_attention, C.byref(cache),
+                layer, a, *_block_ws(cache, ws))
+
+
+def rq_tree_verify_workspace(batch, n_nodes, vocab):
+    """Workspace bytes of rq_tree_verify."""
+    d = RqTreeDraft(batch, n_nodes, vocab)
+    v = C.c_uint64()
+    _check(lib().rq_tree_verify_workspace(C.byref(d), C.byref(v)))
+    return v.value
+
+
+def _tree_rows(t, what, shape, dtype, device):
+    """Pointer and strides of probabilities [batch][n_nodes][vocab]."""
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        raise ValueError(f"{what} must be {dtype} {list(shape)} on {device}")
+    sb, sn, sv = t.stride()
+    if sv != 1 and shape[2] > 1:
+        raise ValueError(f"the rows of {what} must be contiguous")
+    return t.data_ptr(), sb, sn
+
+
+def rq_tree_verify(tokens, parents, target, draft, uniforms, path, count, next,
+                   ws, new_len=None, stream=None):
+    """Verify drafted trees.  tokens, parents: device int32 [batch][n_nodes];
+    target: float32, float16 or bfloat16 [batch][n_nodes][vocab], the target's
+    probabilities behind each node; draft: the draft's, of its type and shape (both
+    any strides, contiguous rows), or None: the drafted tokens were not drawn;
+    uniforms: float32 [batch][n_nodes] in [0, 1); new_len: int32 [batch].
+    Receives path: int32 [batch][room], the accepted nodes; count: int32 [batch];
+    next: int32 [batch], the token drawn behind them.  ws: device byte tensor of at
+    least rq_tree_verify_workspace bytes."""
+    import torch
+    if target.dim() != 3 or path.dim() != 2:
+        raise ValueError("target must have three axes and path two")
+    types = {torch.float32: RQ_F32, torch.float16: RQ_F16, torch.bfloat16: RQ_BF16}
+    if target.dtype not in types:
+        raise ValueError(f"target has dtype {target.dtype}")
+    (B, n, V), at = target.shape, target.device
+    if ws.device != at or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous tensor on {at}")
+    d = _DRAFT.pack(
+        B, n, V, types[target.dtype], _tree_array(tokens, "tokens", at, B, n),
+        _tree_array(parents, "parents", at, B, n),
+        0 if new_len is None else _tree_array(new_len, "new_len", at, B),
+        *_tree_rows(target, "target", (B, n, V), target.dtype, at),
+        *((0, 0, 0) if draft is None
+          else _tree_rows(draft, "draft", (B, n, V), target.dtype, at)),
+        _tree_array(uniforms, "uniforms", at, B, n, dtype=torch.float32),
+        path.shape[1], _tree_array(path, "path", at, B, path.shape[1]),
+        _tree_array(count, "count", at, B), _tree_array(next, "next", at, B))
+    _tree_call(at, stream, lib().rq_tree_verify, d, ws.data_ptr(),
+               ws.numel() * ws.element_size())
+
+
+def rq_block_accept(cache, lengths, path, count, k, v, new_lengths, past=None,
+                    fitting=None, dropped=None, stream=None):
+    """Append a path of drafted tokens to every layer.  lengths: device int32
+    [n_layers][batch], tokens held; path: int32 [batch][room] and count: int32
+    [batch], as rq_tree_verify leaves them; k, v: torch [n_layers][batch]
+    [n_kv_heads][n_nodes][head_dim] in the cache's dtype (any strides, contiguous
+    rows).  new_lengths (lengths itself, or another tensor), past, fitting and
+    dropped are written, as by rq_block_advance, each int32 [n_layers][batch]."""
+    L, B, at = cache.n_layers, cache.batch, cache._device
+    if path.dim() != 2:
+        raise ValueError("path must have two axes")
+    n = k.shape[3] if k.dim() == 5 else -1
+    shape = (L, B, cache.n_kv_heads, n, cache.head_dim)
+    packed = []
+    for t, what in ((k, "k"), (v, "v")):
+        if t.shape != shape or t.device != at or t.dtype not in cache._type:
+            raise ValueError(f"{what} must be {cache._type[0]} {list(shape)} on {at}")
+        if t.stride(4) != 1:
+            raise ValueError(f"the rows of {what} must be contiguous")
+        packed.append(_LAYERS.pack(t.data_ptr(), *t.stride()[:4]))
+
+    def each(t, what):
+        return 0 if t is None else _tree_array(t, what, at, L, B)
+    if lengths is None or new_lengths is None:
+        raise ValueError("lengths and new_lengths are needed")
+    _block_call(cache, stream, lib().rq_block_accept, C.byref(cache),
+                each(lengths, "lengths"), n, path.shape[1],
+                _tree_array(path, "path", at, B, path.shape[1]),
+                _tree_array(count, "count", at, B), *packed,
+                each(new_lengths, "new_lengths"), each(past, "past"),
+                each(fitting, "fitting"), each(dropped, "dropped"))
 
 
 def rq_block_evict_workspace(cache, keep):
@@ -688,6 +905,50 @@ def rq_block_evict(src, dst, layer, lengths, keep, new_lengths, ws, n_sink=4,
                 layer, _block_lengths(src, lengths, "lengths"), keep, n_sink,
                 n_recent, _block_lengths(src, new_lengths, "new_lengths"),
                 *_block_ws(src, ws))
+
+
+class DraftTree:
+    """Drafted tokens of one step: which of them each one sees, and, verified,
+    which are accepted.  parents: device int32 [batch][n_nodes] (a node's parent
+    comes before it; node 0 is the root); new_len: device int32 [batch], how many
+    of the nodes each sequence uses."""
+
+    def __init__(self, parents, new_len=None, stream=None):
+        import torch
+        B, n = parents.shape
+        self.parents, self.new_len = parents, new_len
+        s = torch.cuda.current_stream(parents.device) if stream is None else stream
+        with torch.cuda.stream(s):
+            # (rows that no sequence uses hold zeros)
+            self.mask = torch.zeros(B, n, (n + 31) // 32, dtype=torch.int32,
+                                    device=parents.device)
+            self.depth = torch.zeros_like(parents)
+        self._results = self._ws = None
+        self.layout(stream)
+
+    def layout(self, stream=None):
+        """Lay out again what parents and new_len hold now."""
+        rq_tree_mask(self.parents, self.mask, self.depth, self.new_len, stream)
+
+    def verify(self, tokens, target, uniforms, draft=None, room=None, stream=None):
+        """(path, count, next) of rq_tree_verify: the accepted nodes ([batch]
+        [room]; at most n_nodes), how many, and the token drawn behind them.  The
+        tensors are this tree's own: a later call writes them again."""
+        import torch
+        B, n = self.parents.shape
+        room = n if room is None else room
+        s = torch.cuda.current_stream(target.device) if stream is None else stream
+        need = rq_tree_verify_workspace(B, n, target.shape[-1])
+        with torch.cuda.stream(s):
+            if self._ws is None or self._ws.numel() < need:
+                self._ws = torch.empty(need, dtype=torch.uint8, device=target.device)
+            if self._results is None or self._results[0].shape[1] != room:
+                self._results = tuple(
+                    torch.empty(shape, dtype=torch.int32, device=target.device)
+                    for shape in ((B, room), (B,), (B,)))
+        rq_tree_verify(tokens, self.parents, target, draft, uniforms,
+                       *self._results, self._ws, self.new_len, stream)
+        return self._results
 
 
 class BlockCache:
@@ -721,7 +982,7 @@ class BlockCache:
                                    device=device)
         # of the tokens appended last: those before, those that fitted and those
         # that did not; layers where it may be any
-        self._last = torch.zeros(n_layers, 3, batch, dtype=torch.int32,
+        self._last = torch.zeros(3, n_layers, batch, dtype=torch.int32,
                                  device=device)
         self._drops = set()
         # (which waits for the buffers' zeros, these included)
@@ -758,15 +1019,16 @@ class BlockCache:
         row = self.lengths[layer]
         if layer in self._drops:
             rq_block_advance(self.desc, row, n, new_len,
-                             *self._last[layer].unbind(), stream=stream)
+                             *self._last[:, layer].unbind(), stream=stream)
         else:
             with torch.cuda.stream(self._on(stream)[0]):
                 row += n if new_len is None else new_len.clamp(0, n)
         if layer not in self._replayed:
             self.bound[layer] += n
 
-    def _room(self, layer, n, stream):
-        """Bound on the tokens after n more."""
+    def _room(self, layer, n, stream, read=None):
+        """Bound on the tokens after n more (read: the lengths, where they are
+        on the host already)."""
         import torch
         capacity = self.desc.capacity
         s, capturing = self._on(stream)
@@ -778,7 +1040,7 @@ class BlockCache:
         held = self.bound[layer]
         if held + n > capacity:          # (an upper bound: padding counts)
             with torch.cuda.stream(s):
-                held = int(self.lengths[layer].max())
+                held = int((self.lengths if read is None else read)[layer].max())
             if held + n > capacity:
                 raise ValueError(f"tokens {held} + {n} exceed the capacity "
                                  f"{capacity}")
@@ -821,7 +1083,7 @@ class BlockCache:
         with torch.cuda.stream(s):
             new = q.shape[2] if new_len is None else new_len.clamp(0, q.shape[2])
             if capturing or layer in self._drops:
-                new = new_len = (new - self._last[layer, 2]).clamp_(min=0)
+                new = new_len = (new - self._last[2, layer]).clamp_(min=0)
             past = self.lengths[layer] - new
         return self._attend(layer, past, bound, q, out, new_len, stream, kw)
 
@@ -833,12 +1095,49 @@ class BlockCache:
         rq_block_append(self.desc, layer, past, k, v, new_len, stream)
         if layer in self._drops:
             self._grow(layer, k.shape[2], new_len, stream)
-            past, fitting, _ = self._last[layer].unbind()
+            past, fitting, _ = self._last[:, layer].unbind()
             return self._attend(layer, past, bound, q, out, fitting, stream, kw)
         try:
             return self._attend(layer, past, bound, q, out, new_len, stream, kw)
         finally:
             self._grow(layer, k.shape[2], new_len, stream)
+
+    def tree_attention(self, layer, q, k, v, tree, out=None, stream=None, **kw):
+        """Attention of drafted tokens (tree: a DraftTree; q: [batch][n_q_heads]
+        [n_nodes][head_dim], k, v: [batch][n_kv_heads][n_nodes][head_dim]; scale,
+        cap, window, slopes as rq_block_attention) over the layer's tokens and each
+        other.  The cache is left as it was: accept appends what is verified."""
+        import torch
+        s, capturing = self._on(stream)
+        bound = self.desc.capacity if capturing else self.bound[layer]
+        ws = self._workspace(rq_block_tree_attention_workspace(
+            self.desc, q.shape[2], bound, kw.get("window", 0)), stream)
+        if out is None:
+            with torch.cuda.stream(s):
+                out = torch.zeros_like(q) if tree.new_len is not None else torch.empty_like(q)
+        rq_block_tree_attention(self.desc, layer, self.lengths[layer], q, k, v,
+                                tree.mask, out, ws, tree.depth, tree.new_len,
+                                bound, stream=stream, **kw)
+        return out
+
+    def accept(self, k, v, path, count, stream=None):
+        """Append verified drafted tokens to every layer: the rows of k, v
+        ([n_layers][batch][n_kv_heads][n_nodes][head_dim]) that path ([batch][room])
+        names, count ([batch]) of each sequence (DraftTree.verify's).  `bound` grows
+        by path's room: where it would pass the capacity, the lengths are read (a
+        wait) before the call is refused."""
+        import torch
+        room, read = path.shape[1], None
+        s, capturing = self._on(stream)
+        if not capturing and max(self.bound) + room > self.desc.capacity:
+            with torch.cuda.stream(s):
+                read = self.lengths.cpu()
+        bounds = [self._room(layer, room, stream, read)
+                  for layer in range(self.desc.n_layers)]
+        past, fitting, dropped = self._last.unbind()
+        rq_block_accept(self.desc, self.lengths, path, count, k, v, self.lengths,
+                        past, fitting, dropped, stream)
+        self.bound = bounds
 
     def evict(self, keep, n_sink=4, n_recent=32, into=None, stream=None):
         """Shrink every layer to at most `keep` tokens a sequence: into

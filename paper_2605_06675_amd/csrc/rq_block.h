@@ -95,6 +95,28 @@ struct BlockAttendLaunch {
   float* sums;             // and, of more than one, [part][unit][token] sums
 };
 
+// A tree of drafted tokens that attends over the cache and itself: past tokens
+// are cached, the call's own rows are not.
+struct BlockTreeLaunch : BlockAttendLaunch {
+  BlockRows k, v;          // [B][H][n][D]
+  const uint32_t* mask;    // [B][n][words]: the nodes that each one sees
+  const int32_t* depth;    // [B][n], where positions matter
+  int words;
+  int most;                // bound on the cached tokens (max_tokens: that and n)
+};
+
+// The accepted path's rows of every layer.
+struct BlockAcceptLaunch {
+  BlockLayer c;            // of layer 0
+  int layers, n, n_path;
+  const int32_t* lengths;  // [layers][B], as new_lengths to dropped
+  const int32_t* path;     // [B][n_path]
+  const int32_t* count;    // [B]
+  BlockRows k, v;          // of layer 0
+  int64_t k_layer, v_layer;
+  int32_t *new_lengths, *past, *fitting, *dropped;   // the last three or NULL
+};
+
 struct BlockEvictLaunch {
   BlockLayer src, dst;
   const int32_t* lengths;
@@ -114,6 +136,9 @@ hipError_t launch_block_attend(const BlockAttendLaunch& a, hipStream_t s);
 hipError_t launch_block_prompt(const BlockAttendLaunch& a, hipStream_t s);
 hipError_t launch_block_merge(const BlockAttendLaunch& a, hipStream_t s);
 hipError_t launch_block_weigh(const BlockAttendLaunch& a, hipStream_t s);
+hipError_t launch_tree_attend(const BlockTreeLaunch& a, hipStream_t s);
+hipError_t launch_tree_rows(const BlockTreeLaunch& a, hipStream_t s);
+hipError_t launch_block_accept(const BlockAcceptLaunch& a, hipStream_t s);
 hipError_t launch_block_evict(const BlockEvictLaunch& a, hipStream_t s);
 
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
@@ -123,6 +148,7 @@ typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 // callers' rows may begin at any element
 typedef u4 u4_any __attribute__((aligned(2)));
 typedef u2 u2_any __attribute__((aligned(2)));
+typedef uint32_t u1_any __attribute__((aligned(2)));
 typedef f4 f4_any __attribute__((aligned(4)));
 
 // Memory that no kernel writes while this one runs: uniform addresses are
@@ -154,6 +180,16 @@ __device__ __forceinline__ int over(int x, Divider d) {
 __device__ __forceinline__ int part_from(int n, int i, int parts, Divider by_parts) {
   const int each = over(n, by_parts), more = n - each * parts;
   return each * i + (i < more ? i : more);
+}
+
+// The lengths that a launch's rows attend with.  A tree's nodes are not cached:
+// past does not count them, and is bounded by itself.
+template <class Launch>
+constexpr bool kIsTree = __is_same(Launch, BlockTreeLaunch);
+template <class Launch>
+__device__ __forceinline__ void launch_lengths(const Launch& a, int b, int* past, int* nnew) {
+  block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, past, nnew);
+  if constexpr (kIsTree<Launch>) *past = *past < a.most ? *past : a.most;
 }
 
 // Blocks that rows first..last (tokens of the call) see: [lo, hi).
@@ -350,6 +386,28 @@ __device__ __forceinline__ void store_out(const BlockAttendLaunch& a, int b, int
   }
 }
 
+// The position of a tree's nodes of depth 0, and a node's depth.
+__device__ __forceinline__ int tree_base(const BlockTreeLaunch& a, int unit, int past) {
+  return past > 0 ? gptr(a.c.positions)[(size_t)unit * a.c.cap + past - 1] + 1 : 0;
+}
+__device__ __forceinline__ int node_depth(const BlockTreeLaunch& a, int b, int node) {
+  const int d = gptr(a.depth)[(size_t)b * a.n + node];
+  return d < 0 ? 0 : (d < a.n ? d : a.n - 1);
+}
+
+// Which nodes 32 d..32 d + 31 node i sees, of nnew.
+__device__ __forceinline__ uint32_t node_mask(const BlockTreeLaunch& a, int b, int i, int d, int nnew) {
+  const int left = nnew - 32 * d;
+  if (left <= 0) return 0u;
+  const uint32_t w = gptr(a.mask)[((size_t)b * a.n + i) * a.words + d];
+  return left < 32 ? w & ((1u << left) - 1u) : w;
+}
+
+// Row i of a tree's own keys or values in head h.
+__device__ __forceinline__ const RQ_GLOBAL uint16_t* node_row(const BlockRows& x, int b, int h, int i) {
+  return gptr(static_cast<const uint16_t*>(x.p)) + b * x.sb + h * x.sh + i * x.st;
+}
+
 // A tile of 16 query rows as one wave holds it: lane (r = lane & 15,
 // g = lane >> 4) has, of row r, the channels 64 c + 16 g + 8 f + 0..7 in
 // operand 2 c + f.
@@ -367,8 +425,8 @@ struct QueryTile {
 // fp16 queries are used as they are; bf16 rows are scaled by a power of two to
 // magnitudes below 1, which fp16 holds exactly down to 2^-14 of the row's
 // largest element and to 2^-25 of it below.
-template <int D, bool BF16>
-__device__ __forceinline__ void load_queries(const BlockAttendLaunch& a, int b, int h, int row,
+template <int D, bool BF16, class Launch>
+__device__ __forceinline__ void load_queries(const Launch& a, int b, int h, int row,
                                              int past, int nnew, QueryTile<D>* t) {
   const int g = (threadIdx.x & 63) >> 4;
   t->token = over(row, a.by_G);
@@ -412,8 +470,12 @@ __device__ __forceinline__ void load_queries(const BlockAttendLaunch& a, int b, 
   t->slope = a.slopes ? gptr(a.slopes)[h * a.G + t->head] * 1.4426950408889634f : 0.0f;
   t->pos = 0;
   if (a.slopes || a.window) {
-    const int slot = past + t->token;
-    t->pos = gptr(a.c.positions)[(size_t)(b * a.c.H + h) * a.c.cap + (slot < a.c.cap ? slot : 0)];
+    if constexpr (kIsTree<Launch>) {
+      t->pos = tree_base(a, b * a.c.H + h, past) + node_depth(a, b, t->token);
+    } else {
+      const int slot = past + t->token;
+      t->pos = gptr(a.c.positions)[(size_t)(b * a.c.H + h) * a.c.cap + (slot < a.c.cap ? slot : 0)];
+    }
   }
 }
 
@@ -458,13 +520,13 @@ __device__ __forceinline__ void key_products(const KeyBlock<D>& t, const QueryTi
   }
 }
 
-// The same for the tail's 16-bit keys, on the matrix cores' own 16-bit type
-// (the query rows are read again: as bf16 they need no scaling).  Rows from
-// n_tail on hold anything; their products are masked.
-template <int D, bool BF16>
-__device__ __forceinline__ void tail_products(const BlockAttendLaunch& a, int b, int h,
-                                              const RQ_GLOBAL uint16_t* kt, const QueryTile<D>& q,
-                                              f4 s[2]) {
+// The same for the 16-bit keys of the tail or of a tree's nodes (key(row, channel)
+// loads eight of a row 0..31), on the matrix cores' own 16-bit type (the query rows
+// are read again: as bf16 they need no scaling).  Rows behind the last hold
+// anything; their products are masked.
+template <int D, bool BF16, class Key>
+__device__ __forceinline__ void tail_products(const BlockAttendLaunch& a, int b, int h, Key key,
+                                              const QueryTile<D>& q, f4 s[2]) {
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   const RQ_GLOBAL uint16_t* qp = gptr(static_cast<const uint16_t*>(a.q.p)) + b * a.q.sb +
                                  (int64_t)(h * a.G + q.head) * a.q.sh + q.token * a.q.st;
@@ -478,7 +540,7 @@ __device__ __forceinline__ void tail_products(const BlockAttendLaunch& a, int b,
       if (q.valid) qr = *(const RQ_GLOBAL u4_any*)(qp + ch);
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      const u4 kr = *(const RQ_GLOBAL u4*)(kt + (16 * m + r) * D + ch);
+      const u4 kr = key(16 * m + r, ch);
       if constexpr (BF16)
         s[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_b8(kr), as_b8(qr), s[m], 0, 0, 0);
       else
@@ -488,12 +550,12 @@ __device__ __forceinline__ void tail_products(const BlockAttendLaunch& a, int b,
 }
 
 // Scores in log2 units from products: scale, cap, distance bias, mask.
-// slot0: the slot of the block's first token.  masked: some token of the block
-// may be hidden from some row.
+// slot0: the slot of the block's first token.  end: the last slot that the row
+// sees.  masked: some token of the block may be hidden from some row.
 template <int D>
 __device__ __forceinline__ void block_scores(const BlockAttendLaunch& a, const QueryTile<D>& q,
                                              const RQ_GLOBAL int32_t* positions, float factor,
-                                             int slot0, int past, bool masked, f4 s[2]) {
+                                             int slot0, int end, bool masked, f4 s[2]) {
   const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
   for (int m = 0; m < 2; ++m) s[m] *= factor;
@@ -514,13 +576,45 @@ __device__ __forceinline__ void block_scores(const BlockAttendLaunch& a, const Q
       }
   }
   if (masked) {
-    const int last = past + q.token - slot0;
+    const int last = end - slot0;
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (16 * m + 4 * g + i > last) s[m][i] = -__builtin_inff();
   }
+}
+
+// The same of a tree's nodes 32 d..32 d + 31; base: tree_base.
+template <int D>
+__device__ __forceinline__ void node_scores(const BlockTreeLaunch& a, const QueryTile<D>& q, int b,
+                                            int d, int nnew, int base, f4 s[2]) {
+  const int g = (threadIdx.x & 63) >> 4;
+  const uint32_t seen = q.valid ? node_mask(a, b, q.token, d, nnew) : 0u;
+#pragma unroll
+  for (int m = 0; m < 2; ++m) s[m] *= a.qscale;
+  if (a.cap != 0.0f) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[m][i] = a.cap * tanh_f(s[m][i]);
+  }
+  if (a.slopes || a.window) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int node = 32 * d + 16 * m + 4 * g + i;
+        const int away = q.pos - base - node_depth(a, b, node < nnew ? node : nnew - 1);
+        s[m][i] = __builtin_fmaf(-q.slope, (float)away, s[m][i]);
+        if (a.window && away >= a.window) s[m][i] = -__builtin_inff();
+      }
+  }
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (!((seen >> (16 * m + 4 * g + i)) & 1u)) s[m][i] = -__builtin_inff();
 }
 
 }  // namespace rq

@@ -148,22 +148,22 @@ __device__ __forceinline__ void add_values(const ValueBlock<D>& v, const f4 s[QT
   }
 }
 
-// The tail's values of this lane, as load_values has a block's; rows from n_tail on
-// count as zero.
+// The values of this lane of the tail or of a tree's nodes (value(row, channel) loads
+// two of a row), as load_values has a block's; rows from n_tail on count as zero.
 template <int D>
 struct TailValues {
   uint32_t w[D / 32][8];      // [two channels][token]
 };
 
-template <int D>
-__device__ __forceinline__ void load_tail(const RQ_GLOBAL uint16_t* vt, int n_tail, TailValues<D>* t) {
+template <int D, class Value>
+__device__ __forceinline__ void load_tail(Value value, int n_tail, TailValues<D>* t) {
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int tok = 16 * (j >> 2) + 4 * g + (j & 3);
-      t->w[c][j] = tok < n_tail ? *(const RQ_GLOBAL uint32_t*)(vt + tok * D + (D / 16) * r + 2 * c) : 0u;
+      t->w[c][j] = tok < n_tail ? value(tok, (D / 16) * r + 2 * c) : 0u;
     }
 }
 
@@ -293,9 +293,11 @@ __device__ __forceinline__ void merge_tile(const BlockAttendLaunch& a, const Par
   }
 }
 
-// QT tiles of 16 rows hold all rows of a unit.
-template <int FMT, int D, bool BF16, int QT>
-__global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch a) {
+// QT tiles of 16 rows hold all rows of a unit.  A tree (Launch) has its own rows'
+// blocks of 32 nodes behind the cached ones.
+template <int FMT, int D, bool BF16, int QT, class Launch>
+__global__ void __launch_bounds__(256, 2) block_attend_kernel(Launch a) {
+  constexpr bool kTree = kIsTree<Launch>;
   constexpr int kStride = D + 4;           // floats of a row in LDS
   __shared__ float sh_o[4][16 * kStride];
   __shared__ float sh_ml[4][16][2];
@@ -305,11 +307,13 @@ __global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch 
   const int split = blockIdx.x, unit = blockIdx.y;
   const int b = over(unit, a.c.by_H), h = unit - b * a.c.H;
   int past, nnew;
-  block_lengths(a.past, a.new_len, b, a.n, a.max_tokens, &past, &nnew);
+  launch_lengths(a, b, &past, &nnew);
   if (nnew == 0) return;
-  const int total = past + nnew, full = total / kBlockTokens;
+  const int total = kTree ? past : past + nnew, full = total / kBlockTokens;
   int lo_all, hi_all;                      // block `full` is the tail
   seen_blocks(past, 0, nnew - 1, a.window, &lo_all, &hi_all);
+  const int cached = (past + kBlockTokens - 1) / kBlockTokens;
+  if constexpr (kTree) hi_all = cached + (nnew + kBlockTokens - 1) / kBlockTokens;   // blocks from `cached` on are nodes
   const int lo = lo_all + part_from(hi_all - lo_all, split, a.splits, a.by_splits);
   const int hi = lo_all + part_from(hi_all - lo_all, split + 1, a.splits, a.by_splits);
 
@@ -331,12 +335,12 @@ __global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch 
   const RQ_GLOBAL float* vs = ks + a.c.cap / kBlockTokens;
   const RQ_GLOBAL int32_t* pos = gptr(a.c.positions) + (size_t)unit * a.c.cap;
   // blocks below all_seen lie wholly before every row
-  const int all_seen = a.window ? 0 : (past + 1) / kBlockTokens;
+  const int all_seen = a.window ? 0 : (kTree ? past : past + 1) / kBlockTokens;
   // scores kept for the weights: this lane's row, 4 tokens of each half block
   const int rows = a.n * a.G;
   RQ_GLOBAL float* kept = gptr(a.scores) + ((size_t)unit * ((a.max_tokens + kBlockTokens - 1) / kBlockTokens) * rows + r) * kBlockTokens + 4 * g;
   auto keep = [&](const f4 s[2], int n, int blk) {
-    if (a.scores && 16 * n + r < rows)
+    if (!kTree && a.scores && 16 * n + r < rows)
 #pragma unroll
       for (int m = 0; m < 2; ++m)
         *(RQ_GLOBAL f4*)(kept + ((size_t)blk * rows + 16 * n) * kBlockTokens + 16 * m) = s[m];
@@ -348,7 +352,8 @@ __global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch 
     key_products<FMT, D, QT>(k, q, s);
 #pragma unroll
     for (int n = 0; n < QT; ++n) {
-      block_scores<D>(a, q[n], pos, k.scale * q[n].qs, blk * kBlockTokens, past, blk >= all_seen, s[n]);
+      block_scores<D>(a, q[n], pos, k.scale * q[n].qs, blk * kBlockTokens, kTree ? past - 1 : past + q[n].token,
+                      blk >= all_seen, s[n]);
       keep(s[n], n, blk);
       probabilities<D>(&st[n], s[n]);
     }
@@ -377,19 +382,43 @@ __global__ void __launch_bounds__(256, 2) block_attend_kernel(BlockAttendLaunch 
       blk = b2;
     }
   }
-  if (lo <= full && full < hi && (full - lo) % 4 == wave) {
+  if (lo <= full && full < hi && (!kTree || full < cached) && (full - lo) % 4 == wave) {
     const RQ_GLOBAL uint16_t* kt = gptr(a.c.tail) + (size_t)unit * 2 * kBlockTokens * D;
+    const RQ_GLOBAL uint16_t* vt = kt + kBlockTokens * D;
     TailValues<D> tv;          // (on their way while the keys are)
-    load_tail<D>(kt + kBlockTokens * D, total % kBlockTokens, &tv);
+    load_tail<D>([&](int row, int ch) { return *(const RQ_GLOBAL uint32_t*)(vt + row * D + ch); },
+                 total % kBlockTokens, &tv);
     f4 s[QT][2];
 #pragma unroll
     for (int n = 0; n < QT; ++n) {
-      tail_products<D, BF16>(a, b, h, kt, q[n], s[n]);
-      block_scores<D>(a, q[n], pos, a.qscale, full * kBlockTokens, past, true, s[n]);
+      tail_products<D, BF16>(a, b, h, [&](int row, int ch) { return *(const RQ_GLOBAL u4*)(kt + row * D + ch); }, q[n], s[n]);
+      block_scores<D>(a, q[n], pos, a.qscale, full * kBlockTokens, kTree ? past - 1 : past + q[n].token, true, s[n]);
       keep(s[n], n, full);
       probabilities<D>(&st[n], s[n]);
     }
     add_tail<FMT, D, BF16, QT>(tv, s, st);
+  }
+  if constexpr (kTree) {
+    int base = 0;
+    if (hi > cached && (a.slopes || a.window)) base = tree_base(a, unit, past);
+    for (int blk = lo < cached ? cached : lo; blk < hi; ++blk) {
+      if ((blk - lo) % 4 != wave) continue;
+      const int d = blk - cached, left = nnew - d * kBlockTokens, n_rows = left < kBlockTokens ? left : kBlockTokens;
+      const RQ_GLOBAL uint16_t* kn = node_row(a.k, b, h, d * kBlockTokens);
+      const RQ_GLOBAL uint16_t* vn = node_row(a.v, b, h, d * kBlockTokens);
+      TailValues<D> tv;
+      load_tail<D>([&](int row, int ch) { return (uint32_t)*(const RQ_GLOBAL u1_any*)(vn + row * a.v.st + ch); }, n_rows, &tv);
+      f4 s[QT][2];
+#pragma unroll
+      for (int n = 0; n < QT; ++n) {
+        tail_products<D, BF16>(a, b, h, [&](int row, int ch) {
+          return (u4)*(const RQ_GLOBAL u4_any*)(kn + (row < n_rows ? row : n_rows - 1) * a.k.st + ch);
+        }, q[n], s[n]);
+        node_scores<D>(a, q[n], b, d, nnew, base, s[n]);
+        probabilities<D>(&st[n], s[n]);
+      }
+      add_tail<FMT, D, BF16, QT>(tv, s, st);
+    }
   }
 
 #pragma unroll
@@ -604,9 +633,28 @@ template <int FMT, int D, bool BF16>
 void launch(const BlockAttendLaunch& a, hipStream_t s) {
   const dim3 grid(a.splits, a.c.B * a.c.H);
   if (a.row_tiles == 1)
-    hipLaunchKernelGGL((block_attend_kernel<FMT, D, BF16, 1>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((block_attend_kernel<FMT, D, BF16, 1, BlockAttendLaunch>), grid, dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((block_attend_kernel<FMT, D, BF16, 2>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((block_attend_kernel<FMT, D, BF16, 2, BlockAttendLaunch>), grid, dim3(256), 0, s, a);
+}
+
+template <int FMT, int D, bool BF16>
+void launch(const BlockTreeLaunch& a, hipStream_t s) {
+  const dim3 grid(a.splits, a.c.B * a.c.H);
+  if (a.row_tiles == 1)
+    hipLaunchKernelGGL((block_attend_kernel<FMT, D, BF16, 1, BlockTreeLaunch>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((block_attend_kernel<FMT, D, BF16, 2, BlockTreeLaunch>), grid, dim3(256), 0, s, a);
+}
+
+template <int FMT, int D>
+hipError_t launch(const BlockTreeLaunch& a, hipStream_t s) {
+  if (a.c.is_bf16)
+    launch<FMT, D, true>(a, s);
+  else
+    launch<FMT, D, false>(a, s);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || a.tickets ? e : launch_block_merge(a, s);
 }
 
 template <int FMT, int D>
@@ -645,6 +693,11 @@ static hipError_t merge(const BlockAttendLaunch& a, hipStream_t s) {
 hipError_t launch_block_merge(const BlockAttendLaunch& a, hipStream_t s) {
   if (a.splits == 1) return hipSuccess;
   return a.c.D == 64 ? merge<64>(a, s) : merge<128>(a, s);
+}
+
+hipError_t launch_tree_attend(const BlockTreeLaunch& a, hipStream_t s) {
+  if (a.c.fmt == RQ_INT8) return a.c.D == 64 ? launch<RQ_INT8, 64>(a, s) : launch<RQ_INT8, 128>(a, s);
+  return a.c.D == 64 ? launch<RQ_E4M3, 64>(a, s) : launch<RQ_E4M3, 128>(a, s);
 }
 
 hipError_t launch_block_attend(const BlockAttendLaunch& a, hipStream_t s) {

@@ -6,8 +6,11 @@
 
 #include "rq_block.h"
 #include "rq_internal.h"
+#include "rq_tree.h"
 
 namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
 
 rq_status fail(rq_status code, const char* fmt, ...) {
   char buf[512];
@@ -100,6 +103,37 @@ rq::BlockRows rows_of(const rq_block_rows* r) {
   return rq::BlockRows{r->data, r->stride_batch, r->stride_head, r->stride_token};
 }
 
+// A tree's options, as check_query has a query's.
+rq_status check_tree(const rq_block_cache* c, const rq_block_tree* t) {
+  if (!t) return fail(RQ_EINVAL, "tree is NULL");
+  if (t->n_nodes < 1 || t->n_nodes > RQ_MAX_NODES)
+    return fail(RQ_EINVAL, "n_nodes %d outside 1..%d", t->n_nodes, RQ_MAX_NODES);
+  if (t->max_tokens < 0 || t->max_tokens > c->capacity)
+    return fail(RQ_EINVAL, "max_tokens %d outside 0..%d", t->max_tokens, c->capacity);
+  if (t->window < 0) return fail(RQ_EINVAL, "window %d must be >= 0", t->window);
+  return RQ_OK;
+}
+
+// The factor of the products in scores: log2 units, or over the cap.
+rq_status check_scale(float scale, float cap, float* qscale) {
+  if (!std::isfinite(scale)) return fail(RQ_EINVAL, "scale is not finite");
+  // (beyond, scores over the cap leave the normal numbers)
+  if (!(cap >= 0.0f && cap <= 0x1p100f)) return fail(RQ_EINVAL, "cap must be in 0..2^100 (0: none)");
+  *qscale = cap > 0.0f ? scale / cap : scale * kLog2e;
+  if (!std::isfinite(*qscale))
+    return fail(RQ_EINVAL, "scale %g and cap %g leave the fp32 range", scale, cap);
+  return RQ_OK;
+}
+
+rq_status check_workspace(const void* ws, uint64_t bytes, uint64_t need) {
+  if (bytes < need)
+    return fail(RQ_ESMALLWS, "workspace %llu bytes < %llu needed", (unsigned long long)bytes,
+                (unsigned long long)need);
+  if (need && (!ws || unaligned(ws)))
+    return fail(RQ_EINVAL, "the workspace is NULL or not 16-byte aligned");
+  return RQ_OK;
+}
+
 rq_status check_query(const rq_block_cache* c, const rq_block_query* a) {
   if (!a) return fail(RQ_EINVAL, "query is NULL");
   if (a->n_new < 1 || a->n_new > c->capacity)
@@ -189,6 +223,40 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
     if (most > 1) p.sums = (uint64_t)most * u * a->max_tokens * sizeof(float);
   }
   return p;
+}
+
+// A tree's nodes attend to all cached blocks and the blocks of nodes behind them.
+Plan plan_tree(const rq_block_cache* c, const rq_block_tree* t) {
+  Plan p{};
+  const int64_t G = c->n_q_heads / c->n_kv_heads, u = (int64_t)units(c);
+  p.row_tiles = (int)((t->n_nodes * G + 15) / 16);
+  p.prompt = p.row_tiles > 2;
+  int64_t blocks = (t->max_tokens + rq::kBlockTokens - 1) / rq::kBlockTokens;
+  if (t->window) blocks = std::min<int64_t>(blocks, (int64_t)t->window / rq::kBlockTokens + 2);
+  blocks += (t->n_nodes + rq::kBlockTokens - 1) / rq::kBlockTokens;
+  int64_t s;
+  if (p.prompt) {
+    s = (int64_t)rq::device_cus() / (u * ((t->n_nodes * G + 63) / 64));
+    s = std::min(s, (blocks + 7) / 8);
+  } else {
+    s = (p.row_tiles == 2 && u > 64 ? 2 : 1) * (int64_t)rq::device_cus() / u;
+    s = std::min(s, (blocks + 3) / 4);
+  }
+  p.splits = (int)std::max<int64_t>(s, 1);
+  if (p.splits > 1) {
+    const uint64_t tiles = (uint64_t)u * p.row_tiles;
+    p.part = tiles * p.splits * 16 * c->head_dim * sizeof(float);
+    p.part_ml = tiles * p.splits * 16 * 2 * sizeof(float);
+  }
+  return p;
+}
+
+// The last workgroup of a tile adds its splits where they are few: a launch
+// less, but one workgroup's loads.  us with / without, splits x rows: 8 x 4
+// 8.5 / 9.4, 8 x 8 44.2 / 45.4 (32 units of 32768 tokens), 2 x 4 15.4 / 16.5,
+// 32 x 4 10.8 / 9.3, 16 x 16 18.7 / 18.1, 32 x 8 15.0 / 12.5.
+bool use_tickets(const Plan& p, const rq_block_cache* c, int rows) {
+  return !p.prompt && p.splits > 1 && p.splits <= rq::kTicketSplits && p.splits * rows <= 100 && c->counters;
 }
 
 // Calls of many rows form cap tanh(x) as cap - 2 cap / (1 + e^(2x)), which errs by
@@ -295,23 +363,15 @@ rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_bl
   if (!q->past || !q->q.data || !q->out.data) return fail(RQ_EINVAL, "NULL device pointer");
   if (q->out_dtype != RQ_F32 && q->out_dtype != RQ_F16 && q->out_dtype != RQ_BF16)
     return fail(RQ_EINVAL, "unknown output dtype %d", q->out_dtype);
-  if (!std::isfinite(q->scale)) return fail(RQ_EINVAL, "scale is not finite");
-  // (beyond, scores over the cap leave the normal numbers)
-  if (!(q->cap >= 0.0f && q->cap <= 0x1p100f))
-    return fail(RQ_EINVAL, "cap must be in 0..2^100 (0: none)");
+  float qscale;
+  st = check_scale(q->scale, q->cap, &qscale);
+  if (st != RQ_OK) return st;
   if (q->accumulate && !c->weights) return fail(RQ_EINVAL, "the cache keeps no weights");
-  const float log2e = 1.4426950408889634f;
-  const float qscale = q->cap > 0.0f ? q->scale / q->cap : q->scale * log2e;
-  if (!std::isfinite(qscale))
-    return fail(RQ_EINVAL, "scale %g and cap %g leave the fp32 range", q->scale, q->cap);
   const Plan p = plan_attention(c, q);
   if ((double)p.row_tiles * p.splits * units(c) > 2.0e9)
     return fail(RQ_EUNSUPPORTED, "more than 2e9 tiles of 16 query rows");
-  if (ws_bytes < p.bytes())
-    return fail(RQ_ESMALLWS, "workspace %llu bytes < %llu needed", (unsigned long long)ws_bytes,
-                (unsigned long long)p.bytes());
-  if (p.bytes() && (!ws || unaligned(ws)))
-    return fail(RQ_EINVAL, "the workspace is NULL or not 16-byte aligned");
+  st = check_workspace(ws, ws_bytes, p.bytes());
+  if (st != RQ_OK) return st;
   rq::BlockAttendLaunch a{};
   a.c = layer_of(c, layer);
   a.past = q->past;
@@ -327,7 +387,7 @@ rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_bl
   a.by_G = rq::divider(a.G);
   a.by_splits = rq::divider(p.splits);
   a.qscale = qscale;
-  a.cap = q->cap * log2e;
+  a.cap = q->cap * kLog2e;
   a.fine = q->cap > kSmallCap || (q->cap > 0.0f && q->out_dtype == RQ_F32);
   a.window = q->window;
   a.slopes = q->slopes;
@@ -347,17 +407,118 @@ rq_status rq_block_attention(const rq_block_cache* c, int32_t layer, const rq_bl
   a.sums = reinterpret_cast<float*>(take(p.sums));
   a.row_parts = p.row_parts;
   a.by_parts = rq::divider(std::max(p.row_parts, 1));
-  // The last workgroup of a tile adds its splits where they are few: a launch
-  // less, but one workgroup's loads.  us with / without, splits x rows: 8 x 4
-  // 8.5 / 9.4, 8 x 8 44.2 / 45.4 (32 units of 32768 tokens), 2 x 4 15.4 / 16.5,
-  // 32 x 4 10.8 / 9.3, 16 x 16 18.7 / 18.1, 32 x 8 15.0 / 12.5.
-  a.tickets = !p.prompt && p.splits > 1 && p.splits <= rq::kTicketSplits &&
-              p.splits * a.n * a.G <= 100 && a.c.counters && !a.accumulate;
+  a.tickets = use_tickets(p, c, a.n * a.G) && !a.accumulate;
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = p.prompt ? rq::launch_block_prompt(a, s) : rq::launch_block_attend(a, s);
   if (e == hipSuccess && p.prompt) e = rq::launch_block_merge(a, s);
   if (e == hipSuccess && a.accumulate && !a.scores) e = rq::launch_block_weigh(a, s);
   return launched(e, "attention launch");
+}
+
+rq_status rq_block_tree_attention_workspace(const rq_block_cache* c, const rq_block_tree* t,
+                                            uint64_t* bytes) {
+  rq_status st = check_shape(c);
+  if (st != RQ_OK) return st;
+  st = check_tree(c, t);
+  if (st != RQ_OK) return st;
+  if (!bytes) return fail(RQ_EINVAL, "bytes is NULL");
+  *bytes = plan_tree(c, t).bytes();
+  return ok();
+}
+
+rq_status rq_block_tree_attention(const rq_block_cache* c, int32_t layer, const rq_block_tree* t,
+                                  void* ws, uint64_t ws_bytes, rq_stream stream) {
+  rq_status st = check_buffers(c, layer);
+  if (st != RQ_OK) return st;
+  st = check_tree(c, t);
+  if (st != RQ_OK) return st;
+  if (!t->past || !t->mask || !t->q.data || !t->k.data || !t->v.data || !t->out.data)
+    return fail(RQ_EINVAL, "NULL device pointer");
+  if ((t->window || t->slopes) && !t->depth)
+    return fail(RQ_EINVAL, "a window and slopes need the nodes' depths");
+  if (t->out_dtype != RQ_F32 && t->out_dtype != RQ_F16 && t->out_dtype != RQ_BF16)
+    return fail(RQ_EINVAL, "unknown output dtype %d", t->out_dtype);
+  float qscale;
+  st = check_scale(t->scale, t->cap, &qscale);
+  if (st != RQ_OK) return st;
+  const Plan p = plan_tree(c, t);
+  st = check_workspace(ws, ws_bytes, p.bytes());
+  if (st != RQ_OK) return st;
+  rq::BlockTreeLaunch a{};
+  a.c = layer_of(c, layer);
+  a.past = t->past;
+  a.new_len = t->new_len;
+  a.q = rows_of(&t->q);
+  a.k = rows_of(&t->k);
+  a.v = rows_of(&t->v);
+  a.out = rows_of(&t->out);
+  a.out_dtype = t->out_dtype;
+  a.G = c->n_q_heads / c->n_kv_heads;
+  a.n = t->n_nodes;
+  a.most = t->max_tokens;
+  a.max_tokens = t->max_tokens + t->n_nodes;
+  a.mask = t->mask;
+  a.words = (t->n_nodes + 31) / 32;
+  a.depth = t->depth;
+  a.row_tiles = p.row_tiles;
+  a.splits = p.splits;
+  a.by_G = rq::divider(a.G);
+  a.by_splits = rq::divider(p.splits);
+  a.qscale = qscale;
+  a.cap = t->cap * kLog2e;
+  a.fine = t->cap > kSmallCap || (t->cap > 0.0f && t->out_dtype == RQ_F32);
+  a.window = t->window;
+  a.slopes = t->slopes;
+  a.part = static_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.part);
+  a.tickets = use_tickets(p, c, a.n * a.G);
+  const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  return launched(p.prompt ? rq::launch_tree_rows(a, s) : rq::launch_tree_attend(a, s),
+                  "tree attention launch");
+}
+
+rq_status rq_block_accept(const rq_block_cache* c, const int32_t* lengths, int32_t n_nodes,
+                          int32_t n_path, const int32_t* path, const int32_t* count,
+                          const rq_block_layers* k, const rq_block_layers* v,
+                          int32_t* new_lengths, int32_t* past, int32_t* fitting, int32_t* dropped,
+                          rq_stream stream) {
+  rq_status st = check_buffers(c, 0);
+  if (st != RQ_OK) return st;
+  if (c->n_layers > 65535) return fail(RQ_EUNSUPPORTED, "more than 65535 layers");
+  if (n_nodes < 1 || n_nodes > RQ_MAX_NODES)
+    return fail(RQ_EINVAL, "n_nodes %d outside 1..%d", n_nodes, RQ_MAX_NODES);
+  if (n_path < 1 || n_path > RQ_MAX_NODES)
+    return fail(RQ_EINVAL, "n_path %d outside 1..%d", n_path, RQ_MAX_NODES);
+  if (!lengths || !new_lengths || !path || !count || !k || !v || !k->data || !v->data)
+    return fail(RQ_EINVAL, "NULL device pointer");
+  const uint64_t word = sizeof(int32_t), all = (uint64_t)c->n_layers * c->batch * word;
+  const struct {
+    const void* p;
+    uint64_t bytes;
+  } arrays[] = {{new_lengths, all}, {past, all}, {fitting, all}, {dropped, all}, {lengths, all},
+                {path, (uint64_t)c->batch * n_path * word}, {count, c->batch * word}};
+  for (int i = 0; i < 7; ++i)
+    for (int j = 0; j < i && j < 4; ++j)       // (the first four are written)
+      if (rq::overlap(arrays[i].p, arrays[i].bytes, arrays[j].p, arrays[j].bytes) &&
+          !(lengths == new_lengths && i == 4 && j == 0))
+        return fail(RQ_EINVAL, "two of the arrays overlap");
+  rq::BlockAcceptLaunch a{};
+  a.c = layer_of(c, 0);
+  a.layers = c->n_layers;
+  a.n = n_nodes;
+  a.n_path = n_path;
+  a.lengths = lengths;
+  a.path = path;
+  a.count = count;
+  a.k = rq::BlockRows{k->data, k->stride_batch, k->stride_head, k->stride_token};
+  a.v = rq::BlockRows{v->data, v->stride_batch, v->stride_head, v->stride_token};
+  a.k_layer = k->stride_layer;
+  a.v_layer = v->stride_layer;
+  a.new_lengths = new_lengths;
+  a.past = past;
+  a.fitting = fitting;
+  a.dropped = dropped;
+  return launched(rq::launch_block_accept(a, reinterpret_cast<hipStream_t>(stream)), "accept launch");
 }
 
 rq_status rq_block_evict_workspace(const rq_block_cache* src, int32_t keep, uint64_t* bytes) {

@@ -1,0 +1,648 @@
+"""Trees of drafted tokens on the GPU against their oracle: layout and verification
+equal, attention within bounds that follow from the arithmetic, the accepted path's
+cache contents bit for bit.
+
+Attention's bounds are those of test_gpu_block, with the nodes' keys and values
+among the cached ones: their numbers, as fp16 relative to the largest of a block of
+32 nodes, add D 2^-25 of (the largest |k|) * (sum of |q|) to a score, and 2^-25 of the
+largest |v| to a value (counted in its 2^-21)."""
+import math
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_06675_amd as rq
+from oracle import block, tree
+from test_gpu_block import DT, Rig, both, graph_of, ints, types
+
+pytestmark = pytest.mark.gpu
+
+
+def some_parents(n, seed, shape="tree"):
+    rng = random.Random(seed)
+    if shape == "chain":
+        return list(range(-1, n - 1))
+    if shape == "star":
+        return [-1] + [0] * (n - 1)
+    if shape == "forest":
+        return [rng.randint(-1, i - 1) if rng.random() < 0.7 else -1 for i in range(n)]
+    return [-1] + [rng.randint(max(0, i // 4 - 2), i - 1) for i in range(1, n)]
+
+
+def signed(w):
+    return torch.from_numpy(np.ascontiguousarray(w).view(np.int32))
+
+
+class Trees(Rig):
+    """A device cache with unused memory full of NaNs, and trees that attend."""
+
+    def nodes(self, n, new=None, size=1.0):
+        k, v = self.kv(n, new, size)
+        return k, v
+
+    def tree_attend(self, n, new=None, shape="tree", seen=None, out=torch.float32, scale=None, cap=0.0, window=0,
+                    slopes=None, size=1.0, seed=1, max_tokens=None, rows=None, call=None):
+        """One call with random nodes, checked against the oracle.  seen: [B] masks of
+        one's own in place of the parents'."""
+        B, H, G, D = self.B, self.H, self.G, self.D
+        m = [n] * B if new is None else new
+        parents = [some_parents(x, seed + b, shape) for b, x in enumerate(m)]
+        seen = [tree.sees(p) if p else np.zeros((0, 0), bool) for p in parents] if seen is None else seen
+        depth = [[len(c) - 1 for c in tree.ancestors(p)] for p in parents]
+        k, v = self.nodes(n, new, size)
+        q = (self.randn(B, H * G, n, D) * size).to(self.dt)
+        words = np.full((B, n, (n + 31) // 32), 0xffffffff, np.uint32)
+        deep = np.full((B, n), 1 << 30, np.int32)
+        for b in range(B):
+            q[b, :, m[b]:] = math.nan
+            words[b, :m[b]] = tree.words(seen[b], n)
+            if m[b] % 32 and m[b] < n:                  # nodes that are none of the sequence's
+                words[b, :m[b], m[b] // 32] |= np.uint32((0xffffffff << (m[b] % 32)) & 0xffffffff)
+            deep[b, :m[b]] = depth[b]
+        held = self.lengths()
+        bound = max(held) if max_tokens is None else max_tokens
+        o = torch.full(q.shape, 7.5, dtype=out, device="cuda")
+        need = rq.rq_block_tree_attention_workspace(self.c.desc, n, bound, window)
+        ws = torch.full((max(16, need),), 0xff, dtype=torch.uint8, device="cuda")
+        dq, dk, dv = (x.cuda() for x in (q, k, v)) if rows is None else rows(q, k, v)
+        args = (self.c.desc, self.layer, ints(held), dq, dk, dv, signed(words).cuda(), o, ws)
+        kw = dict(depth=torch.from_numpy(deep).cuda(), new_len=None if new is None else ints(new), max_tokens=bound,
+                  scale=scale, cap=cap, window=window, slopes=None if slopes is None else torch.tensor(slopes).cuda())
+        print("tree", dict(n=n, new=new, held=held, B=B, H=H, G=G, D=D, cap=cap, window=window), flush=True)
+        (rq.rq_block_tree_attention if call is None else call)(*args, **kw)
+        torch.cuda.synchronize()
+        self.compare_tree(o, q, k, v, m, seen, depth, scale, cap, window, slopes)
+        return o
+
+    def compare_tree(self, o, q, k, v, m, seen, depth, scale=None, cap=0.0, window=0, slopes=None):
+        G, D = self.G, self.D
+        scale = D ** -0.5 if scale is None else scale
+        half = 0.0 if o.dtype == torch.float32 else torch.finfo(o.dtype).eps / 2
+        tiny = 2.0 ** -25 if o.dtype == torch.float16 else 1e-30
+        o = o.cpu().double().numpy()
+        assert np.isfinite(o).all()
+        for b in range(self.B):
+            assert (o[b, :, m[b]:] == 7.5).all()
+            if m[b] == 0:
+                continue
+            for h in range(self.H):
+                u = self.u[b][h]
+                kk, vv = (x[b, h, :m[b]].float().numpy() for x in (k, v))
+                qq = q[b, h * G:(h + 1) * G, :m[b]].float().numpy().transpose(1, 0, 2)
+                sl = None if slopes is None else np.asarray(slopes[h * G:(h + 1) * G])
+                want = tree.attend(u, kk, vv, seen[b], depth[b], qq, scale, cap, window, sl)
+                K = np.abs(np.concatenate([u.values(0), kk]).astype(np.float64))
+                V = np.abs(np.concatenate([u.values(1), vv]).astype(np.float64))
+                aq, f = np.abs(qq.astype(np.float64)), abs(scale) * 1.4427
+                a = f * (aq @ K.T).max(-1)
+                a2 = f * np.maximum(aq.max(-1) * K.sum(-1).max(), aq.sum(-1) * K.max())
+                far = 0.0 if sl is None else 1.4427 * float(np.max(sl)) * (float(u.pos.max()) if u.length else 0.0) + 64
+                s = D * 2.0 ** -24 * a + (2 * D * 2.0 ** -25 * a2 if self.dt == torch.bfloat16 else 0)
+                s = s + 4 * 2.0 ** -24 * (a + far) + (1.4427 * cap * 2.0 ** -21 if cap else 0)
+                ratio = 2 * s * math.log(2) + 2.0 ** -21 + (len(K) / 4 + 64) * 2.0 ** -24
+                got = o[b, h * G:(h + 1) * G, :m[b]].transpose(1, 0, 2)
+                tol = (ratio[..., None] + 2.0 ** -21) * V.max() + half * np.abs(want) + tiny
+                err = np.abs(got - want) / tol
+                assert (err <= 1).all(), (b, h, float(err.max()))
+
+
+# --------------------------------------------------------------------- layout
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 64, 255, 256, 257, 700, 1024])
+@pytest.mark.parametrize("shape", ["tree", "chain", "star", "forest"])
+def test_mask_and_depth(n, shape):
+    B = 3
+    rows = [some_parents(n, 7 * b + n, shape) for b in range(B)]
+    mask = torch.full((B, n, (n + 31) // 32), 5, dtype=torch.int32, device="cuda")
+    depth = torch.full((B, n), 5, dtype=torch.int32, device="cuda")
+    new = [n, max(0, n - 3), n // 2]
+    for lens in (None, new, [0, n + 9, -4]):
+        mask.fill_(5)
+        depth.fill_(5)
+        rq.rq_tree_mask(ints(rows), mask, depth, None if lens is None else ints(lens))
+        got, deep = mask.cpu().numpy().view(np.uint32), depth.cpu().numpy()
+        for b in range(B):
+            m = n if lens is None else min(max(lens[b], 0), n)
+            if m:
+                np.testing.assert_array_equal(got[b, :m], tree.words(tree.sees(rows[b][:m]), n))
+                assert deep[b, :m].tolist() == [len(c) - 1 for c in tree.ancestors(rows[b][:m])]
+            assert (got[b, m:] == 5).all() and (deep[b, m:] == 5).all()
+    without = torch.zeros_like(mask)
+    rq.rq_tree_mask(ints(rows), without)
+    for b in range(B):
+        np.testing.assert_array_equal(without[b].cpu().numpy().view(np.uint32), tree.words(tree.sees(rows[b]), n))
+
+
+def test_mask_takes_parents_out_of_range_as_the_nearest_inside():
+    given = [[5, -7, 1, 9, 3, 1 << 30, -(1 << 30)]]
+    mask = torch.zeros(1, 7, 1, dtype=torch.int32, device="cuda")
+    rq.rq_tree_mask(ints(given), mask)
+    want = tree.words(tree.sees([-1, -1, 1, 2, 3, 4, -1]), 7)
+    np.testing.assert_array_equal(mask[0].cpu().numpy().view(np.uint32), want)
+
+
+# ------------------------------------------------------------------ attention
+@both
+@types
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("L", [0, 1, 31, 32, 33, 100, 700])
+def test_attend_small_trees(fmt, dtype, D, L):
+    r = Trees(fmt, dtype, G=2, D=D, cap=704)
+    if L:
+        r.append(L)
+    for n in (1, 5):
+        r.tree_attend(n)
+
+
+@both
+@types
+@pytest.mark.parametrize("G", [1, 3, 4, 16])
+@pytest.mark.parametrize("n", [2, 9, 13, 16, 31, 33, 64, 70])
+def test_attend_row_counts(fmt, dtype, G, n):
+    """One to four tiles of 16 rows, and tiles of 128, with the last one ragged."""
+    r = Trees(fmt, dtype, B=1, H=2, G=G, D=128 if (n + G) % 2 else 64, cap=256)
+    r.append(170)
+    r.tree_attend(n, out=torch.float32 if n % 2 else r.dt)
+
+
+@pytest.mark.parametrize("n", [200, 1024])
+def test_attend_large_trees(n):
+    r = Trees("e4m3", "bf16", B=1, H=1, G=2, D=64, cap=128)
+    r.append(100)
+    r.tree_attend(n, shape="chain" if n == 200 else "tree")
+
+
+@both
+@pytest.mark.parametrize("n", [6, 21, 50])
+@pytest.mark.parametrize("kw", [dict(cap=20.0), dict(window=1), dict(window=3), dict(window=50), dict(window=4000),
+                                dict(window=2 ** 31 - 1), dict(slopes=[0.5, 0.25, 0.0, 1.0]),
+                                dict(cap=5.0, window=33, slopes=[0.01, 0.02, 0.03, 0.04]), dict(cap=1e30)])
+def test_attend_masks_and_biases(fmt, n, kw):
+    r = Trees(fmt, "bf16", D=64, cap=352)
+    r.append(333)
+    r.tree_attend(n, **kw)
+    r.tree_attend(n, out=torch.bfloat16, **kw)
+
+
+@both
+@pytest.mark.parametrize("n", [7, 45])
+def test_attend_ragged(fmt, n):
+    """Empty caches and trees, rows of NaNs that no sequence uses, bits of nodes that
+    are none, a bound above the lengths."""
+    r = Trees(fmt, "bf16", B=6, G=3, cap=256)
+    r.append(200, [200, 0, 5, 64, 33, 96])
+    new = [n, 0, 1, n - 1, n // 2, 2]
+    r.tree_attend(n, new)
+    r.tree_attend(n, new, out=torch.float16, window=3, max_tokens=256)
+    r.tree_attend(n, [0] * 6)
+
+
+@pytest.mark.parametrize("n", [6, 40])
+def test_attend_any_mask(n):
+    """Masks that no tree gives: nothing seen, all nodes, later ones only.  A row that
+    sees nothing is 0."""
+    r = Trees("int8", "fp16", B=3, G=4, cap=64)
+    r.append(40, [40, 0, 0])
+    rng = np.random.default_rng(n)
+    masks = [np.zeros((n, n), bool), rng.random((n, n)) < 0.3, np.triu(np.ones((n, n), bool), 1)]
+    o = r.tree_attend(n, seen=masks)
+    assert (o[2, :, n - 1] == 0).all() and not (o[0] == 0).any()
+    r.tree_attend(n, seen=masks, window=2, slopes=[0.1] * 8)
+    r.tree_attend(n, seen=[np.zeros((n, n), bool)] * 3, window=1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("n", [5, 60])
+@pytest.mark.parametrize("size", [1e-4, 1.0, 2000.0])
+def test_attend_sizes(dtype, n, size):
+    """Cached and drafted numbers of unlike sizes, both ways."""
+    r = Trees("int8", dtype, cap=256)
+    r.append(64, size=size)
+    r.append(41)
+    r.tree_attend(n, scale=0.05 / size ** 2 if size > 1 else None, size=size)
+    r.tree_attend(n, scale=-0.05)
+
+
+@pytest.mark.parametrize("n", [4, 37])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attend_strided_and_unaligned_rows(n, D):
+    r = Trees("e4m3", "bf16", B=2, H=3, G=3, D=D, cap=128)
+    r.append(77)
+
+    def rows(q, k, v):
+        dq = torch.empty(2, n, 9, D, dtype=r.dt, device="cuda").transpose(1, 2)
+        dq.copy_(q)
+        flat = torch.full((2 * 3 * n * (D + 3) + 1,), math.nan, dtype=r.dt, device="cuda")
+        dk = flat[1:].view(2, 3, n, D + 3)[..., 2:D + 2]
+        dk.copy_(k)
+        dv = torch.empty(n, 3, 2, D + 1, dtype=r.dt, device="cuda")[..., 1:].permute(2, 1, 0, 3)
+        dv.copy_(v)
+        return dq, dk, dv
+    r.tree_attend(n, rows=rows)
+
+
+@both
+@pytest.mark.parametrize("B,L,n", [(1, 4000, 8), (2, 3001, 13), (1, 4000, 40), (16, 300, 8)])
+def test_attend_in_splits(fmt, B, L, n):
+    """Long sequences of few units in many splits (with a ticket, and without), nodes in
+    the last of them."""
+    r = Trees(fmt, "bf16", B=B, H=2 if B < 16 else 8, G=4 if B < 16 else 1, D=128 if B == 1 else 64, cap=4096)
+    r.append(L, [max(0, L - 37 * b) for b in range(B)])
+    r.tree_attend(n)
+    assert (r.c.desc._buffers[-1] == 0).all()                 # the counters
+
+
+def test_attend_is_the_same_every_time_and_leaves_the_cache():
+    r = Trees("e4m3", "bf16", G=4, cap=2048)
+    r.append(1500)
+    before = [x.clone() for x in (r.c.codes, r.c.scales, r.c.tail, r.c.positions, r.c.weights)]
+
+    def thrice(*a, **kw):
+        outs = []
+        for _ in range(3):
+            rq.rq_block_tree_attention(*a, **kw)
+            outs.append(a[7].clone())
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    for n in (7, 33):
+        r.tree_attend(n, call=thrice)
+    after = (r.c.codes, r.c.scales, r.c.tail, r.c.positions, r.c.weights)
+    assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(before, after))
+
+
+# --------------------------------------------------------------- verification
+def probabilities(g, shape, dt, sharp=2.0):
+    return torch.softmax(sharp * torch.randn(*shape, generator=g), -1).to(dt)
+
+
+def verify(parents, tokens, target, draft, u, new=None, room=None, place=None):
+    """One call, checked against the oracle."""
+    B, n, V = target.shape
+    room = n if room is None else room
+    place = (lambda x: x.cuda()) if place is None else place
+    path = torch.full((B, room), 77, dtype=torch.int32, device="cuda")
+    count, last = (torch.full((B,), 77, dtype=torch.int32, device="cuda") for _ in range(2))
+    ws = torch.full((rq.rq_tree_verify_workspace(B, n, V),), 0xff, dtype=torch.uint8, device="cuda")
+    print("verify", (B, n, V), target.dtype, draft is not None, room, flush=True)
+    rq.rq_tree_verify(ints(tokens), ints(parents), place(target), None if draft is None else place(draft),
+                      u.cuda(), path, count, last, ws, None if new is None else ints(new))
+    path, count, last = (x.cpu().tolist() for x in (path, count, last))
+    for b in range(B):
+        m = n if new is None else new[b]
+        if m == 0:
+            assert path[b] == [-1] * room and count[b] == 0 and last[b] == -1
+            continue
+        want, token = tree.verify(parents[b][:m], tokens[b][:m], target[b, :m].double().numpy(),
+                                  None if draft is None else draft[b, :m].double().numpy(), u[b].double().numpy(), room)
+        assert path[b] == want + [-1] * (room - len(want)) and count[b] == len(want), (b, path[b], want)
+        assert last[b] == token, (b, last[b], token)
+    return path, count, last
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("n,V,shape", [(1, 1, "tree"), (2, 2, "chain"), (5, 7, "tree"), (30, 40, "tree"),
+                                       (64, 1000, "star"), (9, 16383, "tree"), (9, 16385, "star"),
+                                       (12, 50001, "chain"), (40, 40000, "tree")])
+def test_verify(dt, drawn, n, V, shape):
+    g = torch.Generator().manual_seed(n * 31 + V)
+    B = 5
+    parents = [some_parents(n, 3 * b + V, shape) for b in range(B)]
+    target = probabilities(g, (B, n, V), dt)
+    draft = (0.6 * target.float() + 0.4 * probabilities(g, (B, n, V), torch.float32)).to(dt)
+    rows = draft.float() if drawn else target.float()
+    tokens = [[int(torch.multinomial(rows[b, max(p, 0)], 1, generator=g)) for p in parents[b]] for b in range(B)]
+    u = torch.rand(B, n, generator=g)
+    verify(parents, tokens, target, draft if drawn else None, u)
+    verify(parents, tokens, target, draft if drawn else None, u * 0.3, room=max(1, n // 3))
+    new = [n, 0, 1, max(1, n - 2), n // 2]
+    target[0, new[0]:], target[4, new[4]:] = math.nan, math.nan         # rows that no sequence uses
+    verify(parents, tokens, target, draft if drawn else None, u, new)
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("shape", ["star", "chain", "tree"])
+def test_verify_many_nodes(drawn, shape):
+    """A thousand siblings with tokens that repeat; a thousand accepted in a row."""
+    n, V = 1024, 300
+    g = torch.Generator().manual_seed(4)
+    target, draft = probabilities(g, (1, n, V), torch.float32), probabilities(g, (1, n, V), torch.float32)
+    parents = [some_parents(n, 2, shape)]
+    tokens = torch.randint(V, (1, n), generator=g).tolist()
+    u = torch.rand(1, n, generator=g) * (0.0 if shape == "chain" else 1.0)
+    verify(parents, tokens, target, draft if drawn else None, u)
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+def test_verify_borders(drawn):
+    """Numbers that all arithmetic holds exactly: a test that is met exactly fails, a sum
+    that is met exactly goes to the next token, and u = 0 takes the first with mass."""
+    V, n = 8, 4
+    row = torch.tensor([0.0, 0.25, 0.125, 0.0, 0.5, 0.125, 0.0, 0.0])
+    other = torch.tensor([0.5, 0.25, 0.25, 0.0, 0.0, 0.0, 0.0, 0.0])
+    cases = []
+    for u in ([0.0, 0.25, 0.125, 0.5], [0.25, 1.0, 0.5, 0.5], [0.375, 0.5, 0.999, 0.25], [0.875, 0.999, 0.999, 0.999],
+              [0.99999994, 0.99999994, 0.99999994, 0.99999994], [0.5, 0.0, 0.0, 0.0]):
+        for tokens in ([0, 1, 2, 4], [0, 1, 1, 1], [0, 3, 0, 5], [0, 4, 4, 1]):
+            for parents in ([-1, 0, 0, 0], [-1, 0, 1, 2], [-1, 0, 0, 2], [-1, -1, 1, 0]):
+                cases.append((u, tokens, parents))
+    B = len(cases)
+    target = row.expand(B, n, V).contiguous()
+    draft = other.expand(B, n, V).contiguous() if drawn else None
+    verify([c[2] for c in cases], [c[1] for c in cases], target, draft, torch.tensor([c[0] for c in cases]))
+
+
+def test_verify_residuals_without_mass():
+    """A draft equal to the target, one sure token that is refused by rounding, rows of
+    zeros: the token comes from the target's row, and is one in any case."""
+    V, n = 40000, 3
+    sure = torch.zeros(V)
+    sure[33333] = 0.9961
+    g = torch.Generator().manual_seed(0)
+    flat = probabilities(g, (V,), torch.float32)
+    u = torch.full((6, n), 0.99999994)
+    target = torch.stack([sure, flat, torch.zeros(V), sure, flat, flat])[:, None].expand(-1, n, -1).contiguous()
+    draft = target.clone()
+    draft[4] *= 1.01                                          # more than the target everywhere
+    tokens = [[0, 33333, 33333]] * 6
+    parents = [[-1, 0, 0]] * 6
+    verify(parents, tokens, target, draft, u)
+    verify(parents, tokens, target, None, u)
+
+
+def test_verify_takes_tokens_and_parents_out_of_range_as_the_nearest_inside():
+    g = torch.Generator().manual_seed(2)
+    V, n = 50, 6
+    target = probabilities(g, (2, n, V), torch.float32)
+    u = torch.zeros(2, n)
+    path, count, last = (torch.zeros(s, dtype=torch.int32, device="cuda") for s in ((2, n), (2,), (2,)))
+    ws = torch.empty(rq.rq_tree_verify_workspace(2, n, V), dtype=torch.uint8, device="cuda")
+    rq.rq_tree_verify(ints([[1 << 30] * n, [-5] * n]), ints([[9] * n, [3, 0, -9, 1, 7, 2]]), target.cuda(), None,
+                      u.cuda(), path, count, last, ws, ints([99, -1]))
+    want, token = tree.verify(list(range(-1, n - 1)), [V - 1] * n, target[0].numpy(), None, u[0].numpy(), n)
+    assert path[0].tolist() == want + [-1] * (n - len(want)) and last[0] == token
+    assert count.tolist() == [len(want), 0] and last[1] == -1
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_verify_strided_and_unaligned_rows(dt):
+    g = torch.Generator().manual_seed(7)
+    B, n, V = 3, 5, 20001
+    parents = [some_parents(n, b) for b in range(B)]
+    target, draft = probabilities(g, (B, n, V), dt), probabilities(g, (B, n, V), dt)
+    tokens = torch.randint(V, (B, n), generator=g).tolist()
+
+    def place(x):
+        flat = torch.full((n * B * (V + 5) + 3,), math.nan, dtype=dt, device="cuda")
+        out = flat[3:].view(n, B, V + 5)[..., 1:V + 1].transpose(0, 1)
+        out.copy_(x)
+        return out
+    verify(parents, tokens, target, draft, torch.rand(B, n, generator=g), place=place)
+    shared = target[:1].expand(B, -1, -1).contiguous()         # one sequence's rows for all
+    verify(parents, tokens, shared, None, torch.rand(B, n, generator=g), place=lambda x: x[:1].cuda().expand(B, -1, -1))
+
+
+# --------------------------------------------------------------------- accept
+class Layers:
+    """One rig a layer, over one cache."""
+
+    def __init__(self, fmt="int8", dtype="bf16", layers=3, B=3, H=2, D=128, cap=128, weights=True):
+        self.r = [Rig(fmt, dtype, B=B, H=H, G=2, D=D, cap=cap, weights=weights, layers=layers, layer=0, seed=5)]
+        for i in range(1, layers):
+            other = Rig(fmt, dtype, B=B, H=H, G=2, D=D, cap=cap, weights=weights, layers=layers, layer=i, seed=5 + i)
+            other.c = self.r[0].c
+            self.r.append(other)
+        self.c, self.layers, self.B, self.H, self.D, self.cap = self.r[0].c, layers, B, H, D, cap
+
+    def append(self, n, new=None):
+        for r in self.r:
+            r.append(n, new)
+
+    def nodes(self, n, new=None):
+        """[layers][B][H][n][D] each."""
+        return (torch.stack(x) for x in zip(*(r.kv(n, new) for r in self.r)))
+
+    def took(self, k, v, paths):
+        for i, r in enumerate(self.r):
+            for b, path in enumerate(paths):
+                for h in range(self.H):
+                    fit = path[:max(0, self.cap - r.u[b][h].length)]
+                    r.u[b][h].append(k[i, b, h, fit].float().numpy(), v[i, b, h, fit].float().numpy())
+
+    def accept(self, n, paths, room=None, place=None):
+        room = n if room is None else room
+        k, v = self.nodes(n)
+        given = [p + [-1] * (room - len(p)) for p in paths]
+        place = (lambda x: x.cuda()) if place is None else place
+        self.c.accept(place(k), place(v), ints(given), ints([len(p) for p in paths]))
+        self.took(k, v, paths)
+        return k, v
+
+    def check(self):
+        torch.cuda.synchronize()
+        for r in self.r:
+            r.check()
+
+
+@both
+@types
+@pytest.mark.parametrize("D", [64, 128])
+def test_accept(fmt, dtype, D):
+    """Paths that stay in the tail, fill a block, fill several, and none at all."""
+    s = Layers(fmt, dtype, D=D, cap=416)
+    s.accept(9, [[0, 3, 8], [0], []])
+    s.check()
+    s.append(31, [31, 30, 5])
+    s.accept(5, [[0, 1], [0, 4, 2], [0, 1, 2, 3, 4]])
+    s.check()
+    s.accept(100, [list(range(0, 100, 2)), list(range(100)), [99, 0, 0, 7]])
+    s.check()
+    s.accept(64, [[63], list(range(64)), list(range(33))])
+    s.check()
+    assert (s.r[0].weights()[:, :, :38] == 0).all()
+
+
+@pytest.mark.parametrize("H", [1, 3, 8, 9, 32])
+def test_accept_head_counts(H):
+    s = Layers("e4m3", "bf16", layers=2, B=2, H=H, D=64, cap=64, weights=False)
+    s.append(30)
+    s.accept(6, [[0, 2, 4], [0, 5]], room=3)
+    s.check()
+
+
+def test_accept_strided_and_unaligned_rows():
+    s = Layers("int8", "fp16", D=64)
+    s.append(30, [30, 31, 1])
+
+    def place(x):
+        L, B, H, n, D = x.shape
+        flat = torch.full((L * B * n * H * (D + 3) + 1,), math.nan, dtype=x.dtype, device="cuda")
+        out = flat[1:].view(B, n, L, H, D + 3)[..., 2:D + 2].permute(2, 0, 3, 1, 4)
+        out.copy_(x)
+        return out
+    s.accept(7, [[0, 6, 3], [2, 1], [5]], place=place)
+    s.check()
+
+
+def test_accept_stops_at_the_capacity_and_clamps():
+    s = Layers("int8", layers=2, B=4, cap=64)
+    s.append(64, [60, 64, 10, 33])
+    k, v = s.nodes(6)
+    held, dk, dv = s.c.lengths.clone(), k.cuda(), v.cuda()
+    new, past, fitting, dropped = (torch.full_like(held, 77) for _ in range(4))
+    path = ints([[0, 1, 2, 3, 4, 5], [0, 1, -1, -1, -1, -1], [9, -3, 2, 0, 0, 0], [0, 0, 0, 0, 0, 0]])
+    rq.rq_block_accept(s.c.desc, held, path, ints([6, 2, 99, -2]), dk, dv, new, past, fitting, dropped)
+    s.took(k, v, [[0, 1, 2, 3], [], [5, 0, 2, 0, 0, 0], []])
+    s.c.lengths.copy_(new)
+    s.check()
+    assert torch.equal(past, held) and new[0].tolist() == [64, 64, 16, 33]
+    assert fitting[1].tolist() == [4, 0, 6, 0] and dropped[1].tolist() == [2, 2, 0, 0]
+    with pytest.raises(ValueError):
+        s.accept(6, [[0], [0], [0], [0]], room=1)          # 64 + 1 > 64
+    # lengths out of range count as the nearest inside, and may be the new ones
+    odd = ints([[1000, -5, 16, 33], [64, 0, 16, 33]])
+    rq.rq_block_accept(s.c.desc, odd, path, ints([1, 0, 0, 0]), dk, dv, odd)
+    assert odd.tolist() == [[64, 0, 16, 33], [64, 0, 16, 33]]
+
+
+# ------------------------------------------------------------------- together
+def test_steps_of_speculative_decoding():
+    """Prompt, then steps of a drafted tree: layout, attention in every layer,
+    verification, the path's append.  The cache and the attention stay the oracle's."""
+    s = Layers("e4m3", "bf16", layers=2, B=3, cap=160, weights=False)
+    s.append(40, [40, 7, 0])
+    g = torch.Generator().manual_seed(3)
+    n, V, new = 9, 500, [9, 4, 6]
+    for step in range(20):
+        parents = [some_parents(n, 10 * step + b) for b in range(3)]
+        layout = rq.DraftTree(ints(parents), ints(new))
+        k, v = s.nodes(n)
+        q = torch.randn(2, 3, 4, n, 128, generator=g).to(torch.bfloat16)
+        seen = [tree.sees(p[:m]) for p, m in zip(parents, new)]
+        depth = [[len(c) - 1 for c in tree.ancestors(p[:m])] for p, m in zip(parents, new)]
+        dk, dv = k.cuda(), v.cuda()
+        for i, r in enumerate(s.r):
+            t = Trees.__new__(Trees)
+            t.__dict__.update(r.__dict__)
+            o = torch.full((3, 4, n, 128), 7.5, dtype=torch.bfloat16, device="cuda")
+            s.c.tree_attention(i, q[i].cuda(), dk[i], dv[i], layout, o)
+            t.compare_tree(o, q[i], k[i], v[i], new, seen, depth)
+        target = probabilities(g, (3, n, V), torch.float32, 1.0)
+        tokens = [[int(torch.multinomial(target[b, max(p, 0)], 1, generator=g)) for p in parents[b]] for b in range(3)]
+        u = torch.rand(3, n, generator=g) * 0.02
+        path, count, last = layout.verify(ints(tokens), target.cuda(), u.cuda())
+        want = [tree.verify(parents[b][:m], tokens[b][:m], target[b, :m].numpy(), None, u[b].numpy(), n)
+                for b, m in enumerate(new)]
+        assert last.tolist() == [w[1] for w in want] and count.tolist() == [len(w[0]) for w in want]
+        s.c.accept(dk, dv, path, count)
+        s.took(k, v, [w[0] for w in want])
+        s.check()
+    assert max(s.r[0].lengths()) > 64
+
+
+def test_a_captured_step_replays():
+    """A whole step in one graph, replayed with new inputs as the sequences grow, with
+    the program's own eager work between; at the capacity tokens are dropped."""
+    s = Layers("int8", "bf16", layers=2, B=2, cap=96, weights=False)
+    s.append(50, [50, 3])
+    n, V = 7, 90
+    g = torch.Generator().manual_seed(6)
+    parents, tokens = ints([some_parents(n, 1), some_parents(n, 2)]), torch.zeros(2, n, dtype=torch.int32, device="cuda")
+    q = torch.zeros(2, 2, 4, n, 128, dtype=torch.bfloat16, device="cuda")
+    k, v = (torch.zeros(2, 2, 2, n, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    o = torch.full((2, 2, 4, n, 128), 7.5, device="cuda")
+    target, u = torch.full((2, n, V), 1.0 / V, device="cuda"), torch.full((2, n), 0.5, device="cuda")
+    layout = rq.DraftTree(parents)
+    results = layout.verify(tokens, target, u)
+    torch.cuda.synchronize()
+    held = s.c.lengths.clone()
+
+    def step():
+        layout.layout()
+        for i in range(2):
+            s.c.tree_attention(i, q[i], k[i], v[i], layout, o[i])
+        layout.verify(tokens, target, u)
+        s.c.accept(k, v, results[0], results[1])
+        return o
+    graph, _ = graph_of(step)
+    assert torch.equal(s.c.lengths, held)
+    for turn in range(40):
+        p = [some_parents(n, 20 * turn + b) for b in range(2)]
+        x = [t.to(torch.bfloat16) for t in (torch.randn(q.shape, generator=g), *s.nodes(n))]
+        t = probabilities(g, (2, n, V), torch.float32)
+        w = [[int(torch.multinomial(t[b, max(i, 0)], 1, generator=g)) for i in p[b]] for b in range(2)]
+        y = torch.rand(2, n, generator=g) * 0.05
+        for dst, src in zip((q, k, v, target, u), (*x, t, y)):
+            dst.copy_(src)
+        parents.copy_(ints(p))
+        tokens.copy_(ints(w))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = [tree.verify(p[b], w[b], t[b].numpy(), None, y[b].numpy(), n) for b in range(2)]
+        assert results[2].tolist() == [a[1] for a in want]
+        for i, r in enumerate(s.r):
+            a = Trees.__new__(Trees)
+            a.__dict__.update(r.__dict__)
+            a.compare_tree(o[i], x[0][i], x[1][i], x[2][i], [n, n], [tree.sees(z) for z in p],
+                           [[len(c) - 1 for c in tree.ancestors(z)] for z in p])
+        s.took(x[1], x[2], [a[0] for a in want])
+        assert s.c.lengths[1].tolist() == s.r[1].lengths()
+    assert s.c.lengths.max() == 96
+
+
+def test_another_stream_and_two_trees_at_once():
+    s = Layers("e4m3", "bf16", layers=1, B=2, cap=256, weights=False)
+    s.append(200)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    n = 12
+    t = Trees.__new__(Trees)
+    t.__dict__.update(s.r[0].__dict__)
+    made = []
+    for stream in (side, torch.cuda.default_stream()):
+        with torch.cuda.stream(stream):
+            p = [some_parents(n, len(made) + b) for b in range(2)]
+            layout = rq.DraftTree(ints(p), stream=stream)
+            k, v = t.nodes(n)
+            q = t.randn(2, 4, n, 128).to(t.dt)
+            o = torch.full(q.shape, 7.5, dtype=torch.float32, device="cuda")
+            made.append((p, k, v, q, o, layout, [x.cuda() for x in (q, k, v)]))
+    for stream, (p, k, v, q, o, layout, d) in zip((side, torch.cuda.default_stream()), made):
+        s.c.tree_attention(0, *d, layout, o, stream=stream)
+        stream.synchronize()
+    for p, k, v, q, o, layout, d in made:
+        t.compare_tree(o, q, k, v, [n, n], [tree.sees(z) for z in p], [[len(c) - 1 for c in tree.ancestors(z)] for z in p])
+
+
+def test_python_refusals():
+    s = Layers("int8", "bf16", layers=2, B=2, cap=64, weights=False)
+    n = 3
+    k, v = (x.cuda() for x in s.nodes(n))
+    q = torch.zeros(2, 4, n, 128, dtype=torch.bfloat16, device="cuda")
+    layout = rq.DraftTree(ints([some_parents(n, 0)] * 2))
+    past, o = ints([0, 0]), torch.zeros_like(q)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    good = dict(past=past, q=q, k=k[0], v=v[0], mask=layout.mask, out=o, ws=ws, depth=layout.depth)
+    for kw in (dict(past=None), dict(past=past.long()), dict(q=q.half()), dict(k=k), dict(k=k[0, :, :, :2]),
+               dict(v=v[0].float()), dict(v=v[0].transpose(2, 3)), dict(mask=layout.mask[:1]), dict(mask=layout.mask.cpu()),
+               dict(depth=layout.depth.long()), dict(out=o.double()), dict(ws=ws.cpu()), dict(out=o[:1].expand(2, -1, -1, -1))):
+        with pytest.raises(ValueError):
+            rq.rq_block_tree_attention(s.c.desc, 0, **{**good, **kw})
+    for kw in (dict(window=-1), dict(max_tokens=65), dict(cap=math.nan), dict(depth=None, window=4)):
+        with pytest.raises(rq.RQError):
+            rq.rq_block_tree_attention(s.c.desc, 0, **{**good, **kw})
+    path, count = ints([[0, 1]] * 2), ints([1, 2])
+    for a in ((k[0], v[0], path, count), (k, v[..., :64], path, count), (k, v, path.long(), count), (k, v, path, count[:1]),
+              (k.float(), v, path, count), (k, v, path.t().contiguous().t(), count), (k.transpose(3, 4), v, path, count)):
+        with pytest.raises(ValueError):
+            s.c.accept(*a)
+    assert s.c.bound == [0, 0] and s.c.lengths.tolist() == [[0, 0]] * 2
+    target, u = torch.ones(2, n, 5, device="cuda"), torch.zeros(2, n, device="cuda")
+    tokens = torch.zeros(2, n, dtype=torch.int32, device="cuda")
+    for a in ((tokens.long(), target, u), (tokens, target.double(), u), (tokens, target, u.double()), (tokens, target, u, target.half()),
+              (tokens, target[..., ::2], u), (tokens, target[0], u), (tokens, target, u, target[:, :2])):
+        with pytest.raises(ValueError):
+            layout.verify(*a)
+    with pytest.raises(rq.RQError):
+        layout.verify(tokens, target, u, room=n + 1)
