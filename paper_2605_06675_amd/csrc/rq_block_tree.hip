@@ -32,15 +32,23 @@ template <int D>
 struct Codes {
   u4 k[D / 32];
   uint32_t v[16];
+  float kscale, vscale;
 };
 
+// (The scales by vector loads, with the codes: a scalar load's wait would be one for
+// the queries' LDS reads too.)
 template <int D>
-__device__ __forceinline__ void load_codes(const RQ_GLOBAL uint8_t* kc, const RQ_GLOBAL uint8_t* vc, int blk, Codes<D>* t) {
+__device__ __forceinline__ void load_keys(const RQ_GLOBAL uint8_t* kc, const RQ_GLOBAL float* ks, int blk, Codes<D>* t) {
   const int lane = threadIdx.x & 63, col = lane & 31, hl = lane >> 5;
   const RQ_GLOBAL uint8_t* k = kc + (uint32_t)(blk * kBlockTokens + col) * D + 16 * hl;
-  const RQ_GLOBAL uint8_t* v = vc + (uint32_t)(blk * kBlockTokens + 4 * hl) * D + D / 32 * col;
 #pragma unroll
   for (int j = 0; j < D / 32; ++j) t->k[j] = *(const RQ_GLOBAL u4*)(k + 32 * j);
+  t->kscale = ks[blk];
+}
+template <int D>
+__device__ __forceinline__ void load_values(const RQ_GLOBAL uint8_t* vc, const RQ_GLOBAL float* vs, int blk, Codes<D>* t) {
+  const int lane = threadIdx.x & 63, col = lane & 31, hl = lane >> 5;
+  const RQ_GLOBAL uint8_t* v = vc + (uint32_t)(blk * kBlockTokens + 4 * hl) * D + D / 32 * col;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const RQ_GLOBAL uint8_t* p = v + (8 * (i >> 2) + (i & 3)) * D;
@@ -49,6 +57,7 @@ __device__ __forceinline__ void load_codes(const RQ_GLOBAL uint8_t* kc, const RQ
     else
       t->v[i] = *(const RQ_GLOBAL uint16_t*)p;
   }
+  t->vscale = vs[blk];
 }
 
 // RT tiles of 32 rows.  The lane's row of tile n, its sums in units of kValueUnit /
@@ -97,13 +106,18 @@ __global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch 
 
   const RQ_GLOBAL uint8_t* kc = gptr(a.c.codes) + (size_t)unit * 2 * a.c.cap * D;
   const RQ_GLOBAL uint8_t* vc = kc + (size_t)a.c.cap * D;
-  // (scales by scalar loads: a vector load's wait would be one for the codes in flight)
-  const RQ_CONSTANT float* ks = cptr(a.c.scales) + (size_t)unit * 2 * (a.c.cap / kBlockTokens);
-  const RQ_CONSTANT float* vs = ks + a.c.cap / kBlockTokens;
+  // (the compiler does not know the zero, and so not that all lanes load alike)
+  int zero = 0;
+  asm volatile("" : "+v"(zero));
+  const RQ_GLOBAL float* ks = gptr(a.c.scales) + (size_t)unit * 2 * (a.c.cap / kBlockTokens) + zero;
+  const RQ_GLOBAL float* vs = ks + a.c.cap / kBlockTokens;
   const RQ_GLOBAL int32_t* pos = gptr(a.c.positions) + (size_t)unit * a.c.cap;
   const int end = hi < full ? hi : full;
-  Codes<D> c0, c1;
-  if (lo + wave < end) load_codes<D>(kc, vc, lo + wave, &c0);
+  Codes<D> c;
+  if (lo + wave < end) {
+    load_keys<D>(kc, ks, lo + wave, &c);
+    load_values<D>(vc, vs, lo + wave, &c);
+  }
 
   // the lane's rows
   Rows<D, RT> st;
@@ -186,13 +200,14 @@ __global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch 
     }
   };
   // Scores, probabilities and their sums of a block of key scale kscale and value
-  // scale vscale (which value(j, x) loads: of the lane's tokens 2 j and 2 j + 1 the
-  // pairs of each channel e).  seen[n]: the tokens that the lane's row sees; at:
-  // the tokens' positions.
-  auto attend = [&](f16v s[RT], float kscale, float vscale, bool masked, const uint32_t seen[RT], auto at, auto value) {
+  // scale vscale_of().  value(j, x): of the lane's tokens 2 j and 2 j + 1 the pairs of
+  // each channel e.  seen[n]: the tokens that the lane's row sees; at:
+  // the tokens' positions; then: called when the keys and their scale are used up.
+  auto attend = [&](f16v s[RT], float kscale, auto vscale_of, bool masked, const uint32_t seen[RT], auto at, auto then, auto value) {
     float f[RT], off = 0.0f;
 #pragma unroll
     for (int n = 0; n < RT; ++n) f[n] = kscale * st.qs[n];
+    then();
     if constexpr (!PLAIN) {
       const bool far = a.slopes || a.window;
       if (a.cap != 0.0f && !a.fine) {
@@ -257,6 +272,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch 
       top[n] = __builtin_fmaxf(kNoScore, __builtin_fmaf(x, f[n], off));
       move |= top[n] > st.m[n] + 8.0f;
     }
+    const float vscale = vscale_of();
     // (the same in every lane; a scale of zero has no unit to follow)
     const bool grow = vscale > 0.0f && (st.unit == 0.0f || vscale * st.unit > 128.0f);
     if (grow || __any(move)) {
@@ -337,32 +353,23 @@ __global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch 
     }
   };
 
-  auto step = [&](const Codes<D>& c, int blk) {
+  int blk = lo + wave;
+  while (blk < end) {
+    // The next block's keys are loaded where this one's are used up, its values where
+    // these are (at the end, the last block's again).
+    const int next = blk + kWaves < end ? blk + kWaves : blk;
     f16v s[RT];
     products([&](int k) {
       const uint32_t x = c.k[k >> 1][2 * (k & 1)], y = c.k[k >> 1][2 * (k & 1) + 1];
       return as_h8((u4){key_pair<FMT>(x, false), key_pair<FMT>(x, true), key_pair<FMT>(y, false), key_pair<FMT>(y, true)});
     }, s);
     const uint32_t all[RT] = {};
-    attend(s, ks[blk], vs[blk], false, all, [&](int t) { return pos[blk * kBlockTokens + t]; },
+    attend(s, c.kscale, [&] { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(c.vscale))); }, false, all,
+           [&](int t) { return pos[blk * kBlockTokens + t]; }, [&] { load_keys<D>(kc, ks, next, &c); },
            [&](int j, uint32_t op[4]) { value_pairs<FMT>(c.v[2 * j], c.v[2 * j + 1], op); });
-  };
-  int blk = lo + wave;
-  if (blk < end) {
-    // the next block's codes are in flight while one is worked on (the last load
-    // repeats the last block)
-    for (;;) {
-      const int b1 = blk + kWaves < end ? blk + kWaves : blk;
-      load_codes<D>(kc, vc, b1, &c1);
-      step(c0, blk);
-      if (b1 == blk) break;
-      blk = b1;
-      const int b2 = blk + kWaves < end ? blk + kWaves : blk;
-      load_codes<D>(kc, vc, b2, &c0);
-      step(c1, blk);
-      if (b2 == blk) break;
-      blk = b2;
-    }
+    load_values<D>(vc, vs, next, &c);
+    if (next == blk) break;
+    blk = next;
   }
 
   // Blocks of 16-bit rows: the tail, then the nodes.  Both sides are divided by a
@@ -422,11 +429,12 @@ __global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch 
 #pragma unroll
     for (int n = 0; n < RT; ++n)
       seen[n] = tail ? (1u << n_rows) - 1u : node_mask(a, b, token[n], blk - cached, nnew);
-    attend(s, __builtin_amdgcn_ldexpf(1.0f, ke), vm > 0.0f ? __builtin_amdgcn_ldexpf(kValueUnit<FMT>, ve) : 0.0f, true, seen,
+    attend(s, __builtin_amdgcn_ldexpf(1.0f, ke),
+           [&] { return vm > 0.0f ? __builtin_amdgcn_ldexpf(kValueUnit<FMT>, ve) : 0.0f; }, true, seen,
            [&](int t) {
              t = t < n_rows ? t : n_rows - 1;
              return tail ? pos[full * kBlockTokens + t] : base + node_depth(a, b, first + t);
-           },
+           }, [] {},
            [&](int j, uint32_t op[4]) {
 #pragma unroll
              for (int e = 0; e < kE; ++e) {
