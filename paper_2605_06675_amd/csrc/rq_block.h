@@ -103,6 +103,7 @@ struct BlockTreeLaunch : BlockAttendLaunch {
   const int32_t* depth;    // [B][n], where positions matter
   int words;
   int most;                // bound on the cached tokens (max_tokens: that and n)
+  int group_rows, waves;   // of a workgroup, where there are more than 16 rows
 };
 
 // The accepted path's rows of every layer.

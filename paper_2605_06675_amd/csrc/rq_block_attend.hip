@@ -640,11 +640,8 @@ void launch(const BlockAttendLaunch& a, hipStream_t s) {
 
 template <int FMT, int D, bool BF16>
 void launch(const BlockTreeLaunch& a, hipStream_t s) {
-  const dim3 grid(a.splits, a.c.B * a.c.H);
-  if (a.row_tiles == 1)
-    hipLaunchKernelGGL((block_attend_kernel<FMT, D, BF16, 1, BlockTreeLaunch>), grid, dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((block_attend_kernel<FMT, D, BF16, 2, BlockTreeLaunch>), grid, dim3(256), 0, s, a);
+  hipLaunchKernelGGL((block_attend_kernel<FMT, D, BF16, 1, BlockTreeLaunch>), dim3(a.splits, a.c.B * a.c.H), dim3(256), 0,
+                     s, a);
 }
 
 template <int FMT, int D>

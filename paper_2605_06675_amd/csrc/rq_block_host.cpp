@@ -225,29 +225,67 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
   return p;
 }
 
-// A tree's nodes attend to all cached blocks and the blocks of nodes behind them.
-Plan plan_tree(const rq_block_cache* c, const rq_block_tree* t) {
-  Plan p{};
-  const int64_t G = c->n_q_heads / c->n_kv_heads, u = (int64_t)units(c);
-  p.row_tiles = (int)((t->n_nodes * G + 15) / 16);
-  p.prompt = p.row_tiles > 2;
-  int64_t blocks = (t->max_tokens + rq::kBlockTokens - 1) / rq::kBlockTokens;
-  if (t->window) blocks = std::min<int64_t>(blocks, (int64_t)t->window / rq::kBlockTokens + 2);
-  blocks += (t->n_nodes + rq::kBlockTokens - 1) / rq::kBlockTokens;
-  int64_t s;
+// A tree's nodes attend to all cached blocks and the blocks of nodes behind them.  Up
+// to 16 rows as any few rows.  More in groups of 32 or 64 rows, workgroups of eight
+// waves (one on a CU) or four (two) that may split the tokens: the plan of the least
+// estimated time, us,
+//   rounds of workgroups * (blocks a wave * block + begin and end) + merge,
+// with a block of 32 / 64 rows measured at 1.9 / 3.1 (half for 64 channels) where two
+// waves share a SIMD, begin and end at 6 / 10, a merge at 4 and its parts' traffic.
+// Groups of 64 convert a code half as often; the kernels with a cap, a window or
+// slopes do not fit the registers so for 128 channels.  us with groups of 32 / 64: 64
+// units of 8192 tokens and 64 rows 39.5 / 44.8, 80 rows 54 / 64, 160 rows 103 / 87, 256
+// rows 123 / 107, of 64 channels 78 / 67, capped 100 / 91; 32 units of 500 tokens and 96
+// rows 13.9 / 20.8.
+struct TreePlan : Plan {
+  int group_rows, waves;
+  uint64_t most;      // bytes whatever the options
+};
+
+TreePlan plan_tree(const rq_block_cache* c, const rq_block_tree* t) {
+  TreePlan p{};
+  const int64_t G = c->n_q_heads / c->n_kv_heads, u = (int64_t)units(c), cus = rq::device_cus();
+  const int64_t rows = t->n_nodes * G;
+  p.row_tiles = (int)((rows + 15) / 16);
+  p.prompt = p.row_tiles > 1;
+  const int64_t nodes = (t->n_nodes + rq::kBlockTokens - 1) / rq::kBlockTokens;
+  const int64_t whole = (t->max_tokens + rq::kBlockTokens - 1) / rq::kBlockTokens + nodes;
+  int64_t blocks = whole;
+  if (t->window) blocks = std::min<int64_t>(blocks, (int64_t)t->window / rq::kBlockTokens + 2 + nodes);
+  int64_t s = 1, most = 1;       // (most: whatever the options)
   if (p.prompt) {
-    s = (int64_t)rq::device_cus() / (u * ((t->n_nodes * G + 63) / 64));
-    s = std::min(s, (blocks + 7) / 8);
+    const bool plain = t->cap == 0.0f && !t->window && !t->slopes;
+    float best = 0.0f;
+    for (int tiles = 1; tiles <= 2; ++tiles)
+      for (int waves = 4; waves <= 8; waves += 4) {
+        const int64_t groups = u * ((rows + 32 * tiles - 1) / (32 * tiles)), slots = cus * 8 / waves;
+        for (int round = 0; round <= 2; ++round) {
+          const int64_t split = std::max<int64_t>(round * slots / groups, 1);
+          most = std::max(most, std::min(split, (whole + waves - 1) / waves));
+          if (tiles == 2 && !plain && c->head_dim == 128) continue;
+          const int64_t n = std::min(split, (blocks + waves - 1) / waves);
+          const int64_t rounds = (groups * n + slots - 1) / slots, each = (blocks + n * waves - 1) / (n * waves);
+          const float us = rounds * (each * (tiles == 1 ? 1.9f : 3.1f) * c->head_dim / 128 + (tiles == 1 ? 6.0f : 10.0f)) +
+                           (n > 1 ? 4.0f + u * rows * n * c->head_dim * 2e-6f : 0.0f);
+          if (best == 0.0f || us < best) {
+            best = us;
+            s = n;
+            p.group_rows = 32 * tiles;
+            p.waves = waves;
+          }
+        }
+      }
   } else {
-    s = (p.row_tiles == 2 && u > 64 ? 2 : 1) * (int64_t)rq::device_cus() / u;
-    s = std::min(s, (blocks + 3) / 4);
+    s = std::max<int64_t>(std::min(cus / u, (blocks + 3) / 4), 1);
+    most = std::max<int64_t>(std::min(cus / u, (whole + 3) / 4), 1);
   }
-  p.splits = (int)std::max<int64_t>(s, 1);
-  if (p.splits > 1) {
-    const uint64_t tiles = (uint64_t)u * p.row_tiles;
-    p.part = tiles * p.splits * 16 * c->head_dim * sizeof(float);
-    p.part_ml = tiles * p.splits * 16 * 2 * sizeof(float);
+  p.splits = (int)s;
+  const uint64_t part = (uint64_t)u * p.row_tiles * 16 * sizeof(float);     // of a split
+  if (s > 1) {
+    p.part = part * s * c->head_dim;
+    p.part_ml = part * s * 2;
   }
+  p.most = most > 1 ? part * most * (c->head_dim + 2) : 0;
   return p;
 }
 
@@ -422,7 +460,7 @@ rq_status rq_block_tree_attention_workspace(const rq_block_cache* c, const rq_bl
   st = check_tree(c, t);
   if (st != RQ_OK) return st;
   if (!bytes) return fail(RQ_EINVAL, "bytes is NULL");
-  *bytes = plan_tree(c, t).bytes();
+  *bytes = plan_tree(c, t).most;
   return ok();
 }
 
@@ -441,8 +479,8 @@ rq_status rq_block_tree_attention(const rq_block_cache* c, int32_t layer, const 
   float qscale;
   st = check_scale(t->scale, t->cap, &qscale);
   if (st != RQ_OK) return st;
-  const Plan p = plan_tree(c, t);
-  st = check_workspace(ws, ws_bytes, p.bytes());
+  const TreePlan p = plan_tree(c, t);
+  st = check_workspace(ws, ws_bytes, p.most);
   if (st != RQ_OK) return st;
   rq::BlockTreeLaunch a{};
   a.c = layer_of(c, layer);
@@ -471,6 +509,8 @@ rq_status rq_block_tree_attention(const rq_block_cache* c, int32_t layer, const 
   a.slopes = t->slopes;
   a.part = static_cast<float*>(ws);
   a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.part);
+  a.group_rows = p.group_rows;
+  a.waves = p.waves;
   a.tickets = use_tickets(p, c, a.n * a.G);
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return launched(p.prompt ? rq::launch_tree_rows(a, s) : rq::launch_tree_attend(a, s),

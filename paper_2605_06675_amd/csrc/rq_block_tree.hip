@@ -23,8 +23,6 @@ namespace {
 
 typedef float f16v __attribute__((ext_vector_type(16)));
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
-
 // The codes of a block as a wave holds them: lane (col = lane & 31, hl = lane >> 5)
 // has of token col the channels 32 j + 16 hl + 0..15 of the keys, and of the values'
 // tokens 8 j + 4 hl + i the channels D / 32 col + 0..D/32-1.
@@ -33,20 +31,24 @@ struct Codes {
   u4 k[D / 32];
   uint32_t v[16];
   float kscale, vscale;
+  int pos;           // token col's position, where positions matter
 };
 
-// (The scales by vector loads, with the codes: a scalar load's wait would be one for
-// the queries' LDS reads too.)
+// (Both scales by vector loads, with the keys: a scalar load's wait would be one for
+// the queries' LDS reads too, one with the values a wait for these where the value
+// scale is first asked for.)
 template <int D>
-__device__ __forceinline__ void load_keys(const RQ_GLOBAL uint8_t* kc, const RQ_GLOBAL float* ks, int blk, Codes<D>* t) {
+__device__ __forceinline__ void load_keys(const RQ_GLOBAL uint8_t* kc, const RQ_GLOBAL float* ks, const RQ_GLOBAL float* vs,
+                                          int blk, Codes<D>* t) {
   const int lane = threadIdx.x & 63, col = lane & 31, hl = lane >> 5;
   const RQ_GLOBAL uint8_t* k = kc + (uint32_t)(blk * kBlockTokens + col) * D + 16 * hl;
 #pragma unroll
   for (int j = 0; j < D / 32; ++j) t->k[j] = *(const RQ_GLOBAL u4*)(k + 32 * j);
   t->kscale = ks[blk];
+  t->vscale = vs[blk];
 }
 template <int D>
-__device__ __forceinline__ void load_values(const RQ_GLOBAL uint8_t* vc, const RQ_GLOBAL float* vs, int blk, Codes<D>* t) {
+__device__ __forceinline__ void load_values(const RQ_GLOBAL uint8_t* vc, int blk, Codes<D>* t) {
   const int lane = threadIdx.x & 63, col = lane & 31, hl = lane >> 5;
   const RQ_GLOBAL uint8_t* v = vc + (uint32_t)(blk * kBlockTokens + 4 * hl) * D + D / 32 * col;
 #pragma unroll
@@ -57,7 +59,13 @@ __device__ __forceinline__ void load_values(const RQ_GLOBAL uint8_t* vc, const R
     else
       t->v[i] = *(const RQ_GLOBAL uint16_t*)p;
   }
-  t->vscale = vs[blk];
+}
+
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+
+// Two bf16 numbers over 2^e, as fp16.
+__device__ __forceinline__ uint32_t halves(uint32_t x, uint32_t y, int e) {
+  return as_u32((h2){(_Float16)__builtin_amdgcn_ldexpf(widen_t<true>(x), -e), (_Float16)__builtin_amdgcn_ldexpf(widen_t<true>(y), -e)});
 }
 
 // RT tiles of 32 rows.  The lane's row of tile n, its sums in units of kValueUnit /
@@ -70,9 +78,9 @@ struct Rows {
 };
 
 // PLAIN: no cap, no window, no slopes.
-template <int FMT, int D, bool BF16, int RT, bool PLAIN>
-__global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch a) {
-  constexpr int kRows = 32 * RT, kStride = D + 4, kE = D / 32, kK = D / 16, kBufs = kWaves / 2;
+template <int FMT, int D, bool BF16, int RT, int kWaves, bool PLAIN>
+__global__ void __launch_bounds__(64 * kWaves, 2) tree_rows_kernel(BlockTreeLaunch a) {
+  constexpr int kThreads = 64 * kWaves, kRows = 32 * RT, kStride = D + 4, kE = D / 32, kK = D / 16, kBufs = kWaves / 2;
   __shared__ __align__(16) float sh_o[kBufs][kRows * kStride];    // first the queries: [tile][operand][lane]
   __shared__ float sh_qs[RT][32];
   __shared__ float sh_m[kWaves][kRows], sh_l[kWaves][kRows];
@@ -113,10 +121,15 @@ __global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch 
   const RQ_GLOBAL float* vs = ks + a.c.cap / kBlockTokens;
   const RQ_GLOBAL int32_t* pos = gptr(a.c.positions) + (size_t)unit * a.c.cap;
   const int end = hi < full ? hi : full;
+  const bool far = !PLAIN && (a.slopes || a.window);
   Codes<D> c;
+  auto next_keys = [&](int blk) {
+    load_keys<D>(kc, ks, vs, blk, &c);
+    if (far) c.pos = pos[blk * kBlockTokens + col];
+  };
   if (lo + wave < end) {
-    load_keys<D>(kc, ks, lo + wave, &c);
-    load_values<D>(vc, vs, lo + wave, &c);
+    next_keys(lo + wave);
+    load_values<D>(vc, lo + wave, &c);
   }
 
   // the lane's rows
@@ -147,41 +160,42 @@ __global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch 
 #pragma unroll
       for (int k = 0; k < kK; ++k) raw[k] = *(const RQ_GLOBAL u4_any*)(p + 32 * (k >> 1) + 8 * (k & 1));
       float qs = __builtin_fabsf(a.qscale);
-      float most = 0.0f;
 #pragma unroll
       for (int k = 0; k < kK; ++k)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          raw[k][i] = valid ? raw[k][i] ^ turn : 0u;
-          most = __builtin_fmaxf(most, __builtin_fabsf(widen_t<true>(raw[k][i] & 0xffffu)));
-          most = __builtin_fmaxf(most, __builtin_fabsf(widen_t<true>(raw[k][i] >> 16)));
-        }
+        for (int i = 0; i < 4; ++i) raw[k][i] = valid ? raw[k][i] ^ turn : 0u;
       if constexpr (BF16) {
-        most = half_all<Max>(most);
-        const int e = most > 0.0f ? __builtin_amdgcn_frexp_expf(most) : 0;
+        us2 most = {0, 0};
 #pragma unroll
         for (int k = 0; k < kK; ++k)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            raw[k][i] = as_u32((h2){(_Float16)__builtin_amdgcn_ldexpf(widen_t<true>(raw[k][i] & 0xffffu), -e),
-                                    (_Float16)__builtin_amdgcn_ldexpf(widen_t<true>(raw[k][i] >> 16), -e)});
+          for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(us2, raw[k][i] & 0x7fff7fffu));
+        const float largest = half_all<Max>(widen_t<true>(most.x > most.y ? most.x : most.y));
+        const int e = largest > 0.0f ? __builtin_amdgcn_frexp_expf(largest) : 0;
+#pragma unroll
+        for (int k = 0; k < kK; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) raw[k][i] = halves(raw[k][i] & 0xffffu, raw[k][i] >> 16, e);
         qs = __builtin_amdgcn_ldexpf(qs, e);
       }
 #pragma unroll
       for (int k = 0; k < kK; ++k) *(u4*)((uint8_t*)sh_o + ((n * kK + k) * 64 + lane) * 16) = raw[k];
       if (hl == 0) sh_qs[n][col] = qs;
     }
+  }
+  __syncthreads();
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int n = 0; n < RT; ++n) {
 #pragma unroll
     for (int e = 0; e < kE; ++e)
 #pragma unroll
       for (int i = 0; i < 16; ++i) st.o[n][e][i] = 0.0f;
     st.m[n] = kNoScore;
     st.l[n] = 0.0f;
+    st.qs[n] = sh_qs[n][col];
   }
   st.unit = 0.0f;
-  __syncthreads();
-#pragma unroll
-  for (int n = 0; n < RT; ++n) st.qs[n] = sh_qs[n][col];
 
   // products of a block's keys with all rows: key(k) is operand k
   auto products = [&](auto key, f16v s[RT]) {
@@ -200,16 +214,15 @@ __global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch 
     }
   };
   // Scores, probabilities and their sums of a block of key scale kscale and value
-  // scale vscale_of().  value(j, x): of the lane's tokens 2 j and 2 j + 1 the pairs of
+  // scale vscale.  value(j, x): of the lane's tokens 2 j and 2 j + 1 the pairs of
   // each channel e.  seen[n]: the tokens that the lane's row sees; at:
-  // the tokens' positions; then: called when the keys and their scale are used up.
-  auto attend = [&](f16v s[RT], float kscale, auto vscale_of, bool masked, const uint32_t seen[RT], auto at, auto then, auto value) {
+  // token col's position; then: called when the keys and their scale are used up.
+  auto attend = [&](f16v s[RT], float kscale, float vscale, bool masked, const uint32_t seen[RT], int at, auto then, auto value) {
     float f[RT], off = 0.0f;
 #pragma unroll
     for (int n = 0; n < RT; ++n) f[n] = kscale * st.qs[n];
     then();
     if constexpr (!PLAIN) {
-      const bool far = a.slopes || a.window;
       if (a.cap != 0.0f && !a.fine) {
         // cap tanh(x) = cap - 2 cap / (1 + e^(2x)): off by 2^-22 cap
 #pragma unroll
@@ -237,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch 
       if (far) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int p = at(8 * (i >> 2) + 4 * hl + (i & 3));
+          const int p = __shfl(at, 8 * (i >> 2) + 4 * hl + (i & 3));
 #pragma unroll
           for (int n = 0; n < RT; ++n) {
             const int away = qpos[n] - p;
@@ -272,7 +285,6 @@ __global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch 
       top[n] = __builtin_fmaxf(kNoScore, __builtin_fmaf(x, f[n], off));
       move |= top[n] > st.m[n] + 8.0f;
     }
-    const float vscale = vscale_of();
     // (the same in every lane; a scale of zero has no unit to follow)
     const bool grow = vscale > 0.0f && (st.unit == 0.0f || vscale * st.unit > 128.0f);
     if (grow || __any(move)) {
@@ -364,17 +376,18 @@ __global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch 
       return as_h8((u4){key_pair<FMT>(x, false), key_pair<FMT>(x, true), key_pair<FMT>(y, false), key_pair<FMT>(y, true)});
     }, s);
     const uint32_t all[RT] = {};
-    attend(s, c.kscale, [&] { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(c.vscale))); }, false, all,
-           [&](int t) { return pos[blk * kBlockTokens + t]; }, [&] { load_keys<D>(kc, ks, next, &c); },
+    attend(s, c.kscale, __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(c.vscale))), false, all,
+           c.pos, [&] { next_keys(next); },
            [&](int j, uint32_t op[4]) { value_pairs<FMT>(c.v[2 * j], c.v[2 * j + 1], op); });
-    load_values<D>(vc, vs, next, &c);
+    load_values<D>(vc, next, &c);
     if (next == blk) break;
     blk = next;
   }
 
-  // Blocks of 16-bit rows: the tail, then the nodes.  Both sides are divided by a
-  // power of two that brings the side's largest number below 1 (fp16 holds the
-  // others to 2^-25 of it).  Rows behind the last repeat it, their values are 0.
+  // Blocks of 16-bit rows: the tail, then the nodes.  fp16 numbers are operands as
+  // they are; both sides of bf16 ones are divided by a power of two that brings the
+  // side's largest below 1 (fp16 holds the others to 2^-25 of it).  Rows behind the
+  // last repeat it, their values are 0.
   for (blk = lo < full ? full : lo; blk < hi; ++blk) {
     if ((blk - lo) % kWaves != wave) continue;
     const bool tail = blk < cached;
@@ -387,61 +400,81 @@ __global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch 
     kt = tail ? kt : node_row(a.k, b, h, first);
     vt = tail ? vt : node_row(a.v, b, h, first);
     const RQ_GLOBAL uint16_t* kp = kt + (col < n_rows ? col : n_rows - 1) * kst + 16 * hl;
-    u4 kr[kK];
-    float km = 0.0f, vm = 0.0f;
-#pragma unroll
-    for (int k = 0; k < kK; ++k) {
-      kr[k] = *(const RQ_GLOBAL u4_any*)(kp + 32 * (k >> 1) + 8 * (k & 1));
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        km = __builtin_fmaxf(km, __builtin_fmaxf(__builtin_fabsf(widen_t<BF16>(kr[k][i] & 0xffffu)),
-                                                 __builtin_fabsf(widen_t<BF16>(kr[k][i] >> 16))));
-    }
-    km = wave_all<Max>(km);
-    const int ke = km > 0.0f ? __builtin_amdgcn_frexp_expf(km) : 0;
-    auto pair = [](uint32_t x, uint32_t y, int e) {
-      return as_u32((h2){(_Float16)__builtin_amdgcn_ldexpf(widen_t<BF16>(x), -e),
-                         (_Float16)__builtin_amdgcn_ldexpf(widen_t<BF16>(y), -e)});
-    };
-    f16v s[RT];
-    products([&](int k) {
-      u4 f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = pair(kr[k][i] & 0xffffu, kr[k][i] >> 16, ke);
-      return as_h8(f);
-    }, s);
-    uint32_t vr[16][kE / 2];               // two channels each
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    // channels kE col + 2 e, + 1 of the lane's token i
+    auto load_two = [&](int i, int e) {
       const int t = 8 * (i >> 2) + 4 * hl + (i & 3);
-      const RQ_GLOBAL uint16_t* vp = vt + (t < n_rows ? t : n_rows - 1) * vst + kE * col;
+      const uint32_t x = *(const RQ_GLOBAL u1_any*)(vt + (t < n_rows ? t : n_rows - 1) * vst + kE * col + 2 * e);
+      return t < n_rows ? x : 0u;
+    };
+    u4 kr[kK];
 #pragma unroll
-      for (int e = 0; e < kE / 2; ++e) {
-        vr[i][e] = *(const RQ_GLOBAL u1_any*)(vp + 2 * e);
-        vr[i][e] = t < n_rows ? vr[i][e] : 0u;
-        vm = __builtin_fmaxf(vm, __builtin_fmaxf(__builtin_fabsf(widen_t<BF16>(vr[i][e] & 0xffffu)),
-                                                 __builtin_fabsf(widen_t<BF16>(vr[i][e] >> 16))));
-      }
-    }
-    vm = wave_all<Max>(vm);
-    const int ve = vm > 0.0f ? __builtin_amdgcn_frexp_expf(vm) : 0;
+    for (int k = 0; k < kK; ++k) kr[k] = *(const RQ_GLOBAL u4_any*)(kp + 32 * (k >> 1) + 8 * (k & 1));
+    // (with two tiles the values are loaded again where they are used: their
+    // registers would not fit beside the probabilities')
+    uint32_t vr[RT == 1 ? 16 : 1][kE / 2];
+    if constexpr (RT == 1)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int e = 0; e < kE / 2; ++e) vr[i][e] = load_two(i, e);
+    auto two = [&](int i, int e) {
+      if constexpr (RT == 1)
+        return vr[i][e];
+      else
+        return load_two(i, e);
+    };
     uint32_t seen[RT];
 #pragma unroll
     for (int n = 0; n < RT; ++n)
       seen[n] = tail ? (1u << n_rows) - 1u : node_mask(a, b, token[n], blk - cached, nnew);
-    attend(s, __builtin_amdgcn_ldexpf(1.0f, ke),
-           [&] { return vm > 0.0f ? __builtin_amdgcn_ldexpf(kValueUnit<FMT>, ve) : 0.0f; }, true, seen,
-           [&](int t) {
-             t = t < n_rows ? t : n_rows - 1;
-             return tail ? pos[full * kBlockTokens + t] : base + node_depth(a, b, first + t);
-           }, [] {},
-           [&](int j, uint32_t op[4]) {
+    int at = 0;
+    if (far) {
+      const int t = col < n_rows ? col : n_rows - 1;
+      at = tail ? pos[full * kBlockTokens + t] : base + node_depth(a, b, first + t);
+    }
+    int ke = 0, ve = 0;
+    float kscale = 1.0f, vscale = kValueUnit<FMT>;
+    if constexpr (BF16) {
+      us2 km = {0, 0}, vm = {0, 0};        // (magnitudes compare as whole numbers)
 #pragma unroll
-             for (int e = 0; e < kE; ++e) {
-               const uint32_t x = vr[2 * j][e / 2], y = vr[2 * j + 1][e / 2];
-               op[e] = e & 1 ? pair(x >> 16, y >> 16, ve) : pair(x & 0xffffu, y & 0xffffu, ve);
-             }
-           });
+      for (int k = 0; k < kK; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) km = __builtin_elementwise_max(km, __builtin_bit_cast(us2, kr[k][i] & 0x7fff7fffu));
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int e = 0; e < kE / 2; ++e) vm = __builtin_elementwise_max(vm, __builtin_bit_cast(us2, two(i, e) & 0x7fff7fffu));
+      const float kmost = wave_all<Max>(widen_t<true>(km.x > km.y ? km.x : km.y));
+      const float vmost = wave_all<Max>(widen_t<true>(vm.x > vm.y ? vm.x : vm.y));
+      ke = kmost > 0.0f ? __builtin_amdgcn_frexp_expf(kmost) : 0;
+      ve = vmost > 0.0f ? __builtin_amdgcn_frexp_expf(vmost) : 0;
+      kscale = __builtin_amdgcn_ldexpf(1.0f, ke);
+      vscale = vmost > 0.0f ? __builtin_amdgcn_ldexpf(kValueUnit<FMT>, ve) : 0.0f;
+    }
+    f16v s[RT];
+    products([&](int k) {
+      if constexpr (BF16) {
+        u4 f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = halves(kr[k][i] & 0xffffu, kr[k][i] >> 16, ke);
+        return as_h8(f);
+      } else {
+        return as_h8(kr[k]);
+      }
+    }, s);
+    attend(s, kscale, vscale, true, seen, at, [] {}, [&](int j, uint32_t op[4]) {
+#pragma unroll
+      for (int e = 0; e < kE / 2; ++e) {
+        const uint32_t x = two(2 * j, e), y = two(2 * j + 1, e);
+        if constexpr (BF16) {
+          op[2 * e] = halves(x & 0xffffu, y & 0xffffu, ve);
+          op[2 * e + 1] = halves(x >> 16, y >> 16, ve);
+        } else {
+          op[2 * e] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+          op[2 * e + 1] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        }
+      }
+    });
   }
 
   // the waves' sums: half of the waves store theirs, the others add
@@ -510,13 +543,21 @@ __global__ void __launch_bounds__(kThreads, 2) tree_rows_kernel(BlockTreeLaunch 
   }
 }
 
+template <int FMT, int D, bool BF16, int RT, int kWaves>
+void launch(const BlockTreeLaunch& a, hipStream_t s) {
+  const dim3 grid((unsigned)((a.n * a.G + 32 * RT - 1) / (32 * RT) * a.splits) * a.c.B * a.c.H), block(64 * kWaves);
+  if (a.cap == 0.0f && !a.window && !a.slopes)
+    hipLaunchKernelGGL((tree_rows_kernel<FMT, D, BF16, RT, kWaves, true>), grid, block, 0, s, a);
+  else if constexpr (D == 64 || RT == 1)
+    hipLaunchKernelGGL((tree_rows_kernel<FMT, D, BF16, RT, kWaves, false>), grid, block, 0, s, a);
+}
+
 template <int FMT, int D, bool BF16>
 void launch(const BlockTreeLaunch& a, hipStream_t s) {
-  const dim3 grid((unsigned)((a.n * a.G + 63) / 64 * a.splits) * a.c.B * a.c.H);
-  if (a.cap == 0.0f && !a.window && !a.slopes)
-    hipLaunchKernelGGL((tree_rows_kernel<FMT, D, BF16, 2, true>), grid, dim3(kThreads), 0, s, a);
+  if (a.group_rows == 32)
+    a.waves == 4 ? launch<FMT, D, BF16, 1, 4>(a, s) : launch<FMT, D, BF16, 1, 8>(a, s);
   else
-    hipLaunchKernelGGL((tree_rows_kernel<FMT, D, BF16, 2, false>), grid, dim3(kThreads), 0, s, a);
+    a.waves == 4 ? launch<FMT, D, BF16, 2, 4>(a, s) : launch<FMT, D, BF16, 2, 8>(a, s);
 }
 
 template <int FMT, int D>
