@@ -20,33 +20,24 @@ constexpr int kRowsOf = 512 / D;
 template <int D>
 constexpr int kLoadsOf = kBlockTokens / kRowsOf<D>;
 
-// Codes a block of unit-side us (unit * 2 + K or V).
-template <int FMT, int D, bool BF16>
-__device__ __forceinline__ void code_block(const BlockLayer& c, size_t us, int blk, const u4 x[kLoadsOf<D>]) {
-  constexpr int kChunks = D / 8, kRows = kRowsOf<D>, kLoads = kLoadsOf<D>;
-  const int lane = threadIdx.x & 63, row0 = lane / kChunks, ch = (lane % kChunks) * 8;
-  float most = 0.0f;
+// The largest magnitude of eight numbers and `most`; their codes.
+template <bool BF16>
+__device__ __forceinline__ float largest_of(u4 x, float most) {
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      most = __builtin_fmaxf(most, __builtin_fabsf(widen_t<BF16>(x[i][w] & 0xffffu)));
-      most = __builtin_fmaxf(most, __builtin_fabsf(widen_t<BF16>(x[i][w] >> 16)));
-    }
-  most = wave_all<Max>(most);
-  float inv;
-  const float scale = block_scale<FMT>(most, &inv);
-  RQ_GLOBAL uint8_t* out = gptr(c.codes) + (us * c.cap + (size_t)blk * kBlockTokens) * D;
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    u2 w;
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-      w[p] = block_codes<FMT>(widen_t<BF16>(x[i][2 * p] & 0xffffu), widen_t<BF16>(x[i][2 * p] >> 16),
-                              widen_t<BF16>(x[i][2 * p + 1] & 0xffffu), widen_t<BF16>(x[i][2 * p + 1] >> 16), inv);
-    __builtin_nontemporal_store(w, (RQ_GLOBAL u2*)(out + (row0 + kRows * i) * D + ch));
+  for (int w = 0; w < 4; ++w) {
+    most = __builtin_fmaxf(most, __builtin_fabsf(widen_t<BF16>(x[w] & 0xffffu)));
+    most = __builtin_fmaxf(most, __builtin_fabsf(widen_t<BF16>(x[w] >> 16)));
   }
-  if (lane == 0) gptr(c.scales)[us * (c.cap / kBlockTokens) + blk] = scale;
+  return most;
+}
+template <int FMT, bool BF16>
+__device__ __forceinline__ void store_codes(u4 x, float inv, RQ_GLOBAL uint8_t* out) {
+  u2 w;
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+    w[p] = block_codes<FMT>(widen_t<BF16>(x[2 * p] & 0xffffu), widen_t<BF16>(x[2 * p] >> 16),
+                            widen_t<BF16>(x[2 * p + 1] & 0xffffu), widen_t<BF16>(x[2 * p + 1] >> 16), inv);
+  __builtin_nontemporal_store(w, (RQ_GLOBAL u2*)out);
 }
 
 // One wave a (unit, K or V, block).
@@ -79,7 +70,16 @@ __global__ void __launch_bounds__(256) block_append_kernel(BlockAppendLaunch a) 
       x[i] = slot < past ? *(const RQ_GLOBAL u4*)(tail + row * D + ch)
                          : __builtin_nontemporal_load((const RQ_GLOBAL u4_any*)(in + (int64_t)(slot - past) * src.st + ch));
     }
-    code_block<FMT, D, BF16>(a.c, (size_t)(unit * 2 + kind), blk, x);
+    float most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) most = largest_of<BF16>(x[i], most);
+    most = wave_all<Max>(most);
+    float inv;
+    const float scale = block_scale<FMT>(most, &inv);
+    RQ_GLOBAL uint8_t* out = gptr(a.c.codes) + ((size_t)(unit * 2 + kind) * a.c.cap + (size_t)blk * kBlockTokens) * D;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) store_codes<FMT, BF16>(x[i], inv, out + (row0 + kRows * i) * D + ch);
+    if (lane == 0) gptr(a.c.scales)[(size_t)(unit * 2 + kind) * (a.c.cap / kBlockTokens) + blk] = scale;
   }
   if (j == 0) {
     // the unfinished block's new rows, after the rows that they may replace
@@ -99,70 +99,100 @@ __global__ void __launch_bounds__(256) block_append_kernel(BlockAppendLaunch a) 
   }
 }
 
-// The rows of an accepted path: a workgroup takes a sequence in one layer, a wave a
-// (kv-head, K or V) at a time, so that the lengths are read by the workgroup that
-// writes them.  A chain of latencies (lengths, path, rows): 32 layers of 16
-// sequences with 8 kv-heads, some four rows of each, in one launch.
-constexpr int kAcceptWaves = 16;
+// The rows of an accepted path.  A workgroup takes a sequence in one layer, all heads and
+// both sides, so that the lengths are read by the workgroup that writes them.  First
+// its waves code the blocks that become full, one (kv-head, side) after the other; then
+// its threads copy the unfinished block's rows, 16 bytes each.
+//
+// A chain of latencies (lengths and path, rows, stores), and of so many small
+// workgroups the launch of their waves: one wave a (kv-head, side) took 16 where eight
+// for all take 12.1 us (32 layers of 16 sequences, 8 kv-heads, some four rows of each).
+constexpr int kAcceptWaves = 8, kAcceptThreads = 64 * kAcceptWaves;
 
 template <int FMT, int D, bool BF16>
-__global__ void __launch_bounds__(64 * kAcceptWaves) block_accept_kernel(BlockAcceptLaunch a) {
+__global__ void __launch_bounds__(kAcceptThreads) block_accept_kernel(BlockAcceptLaunch a) {
   constexpr int kChunks = D / 8, kRows = kRowsOf<D>, kLoads = kLoadsOf<D>;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  __shared__ int node[RQ_MAX_NODES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int b = blockIdx.x, layer = blockIdx.y, at = layer * a.c.B + b;
-  const RQ_GLOBAL int32_t* path = gptr(a.path) + (size_t)b * a.n_path;
-  auto inside = [&](int node) { return node < 0 ? 0 : (node < a.n ? node : a.n - 1); };
-  const int near = inside(path[lane < a.n_path ? lane : a.n_path - 1]);    // node of token `lane`
   int past = gptr(a.lengths)[at], count = gptr(a.count)[b];
+  for (int t = threadIdx.x; t < a.n_path; t += kAcceptThreads) {
+    const int i = gptr(a.path)[(size_t)b * a.n_path + t];
+    node[t] = i < 0 ? 0 : (i < a.n ? i : a.n - 1);
+  }
   past = __builtin_amdgcn_readfirstlane(past < 0 ? 0 : (past < a.c.cap ? past : a.c.cap));
   count = __builtin_amdgcn_readfirstlane(count < 0 ? 0 : (count < a.n_path ? count : a.n_path));
   const int fit = count < a.c.cap - past ? count : a.c.cap - past;
   const int total = past + fit, full = total / kBlockTokens;
-  const int row0 = lane / kChunks, ch = (lane % kChunks) * 8;
-  for (int pair = wave; pair < 2 * a.c.H && fit > 0; pair += waves) {
-    const int kind = pair & 1, h = pair >> 1;
-    const size_t unit = (size_t)at * a.c.H + h;
-    const BlockRows& src = kind ? a.v : a.k;
-    const RQ_GLOBAL uint16_t* in = gptr(static_cast<const uint16_t*>(src.p)) +
-                                   layer * (kind ? a.v_layer : a.k_layer) + b * src.sb + h * src.sh + ch;
-    RQ_GLOBAL uint16_t* tail = gptr(a.c.tail) + (unit * 2 + kind) * kBlockTokens * D;
-    for (int blk = past / kBlockTokens; blk <= full; ++blk) {
-      u4 x[kLoads];
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        // (rows that are no new tokens: the tail's own)
-        const int row = row0 + kRows * i, t = blk * kBlockTokens + row - past;
-        const bool mine = t >= 0 && t < fit;
-        const int node = fit <= 64 ? __shfl(near, t & 63) : inside(path[mine ? t : 0]);
-        const RQ_GLOBAL uint16_t* from = mine ? in + (int64_t)node * src.st : tail + row * D + ch;
-        x[i] = *(const RQ_GLOBAL u4_any*)from;
-      }
-      if (blk < full) {
-        code_block<FMT, D, BF16>(a.c, unit * 2 + kind, blk, x);
-      } else {
-        // the unfinished block (the rows that its own may replace are read)
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-          const int row = row0 + kRows * i, t = blk * kBlockTokens + row - past;
-          if (t >= 0 && t < fit) *(RQ_GLOBAL u4*)(tail + row * D + ch) = x[i];
-        }
-      }
-    }
-    if (kind == 0) {
-      RQ_GLOBAL int32_t* pos = gptr(a.c.positions) + unit * a.c.cap + past;
-      const int next = past > 0 ? pos[-1] + 1 : 0;
-      for (int t = lane; t < fit; t += 64) {
-        pos[t] = next + t;
-        if (a.c.weights) gptr(a.c.weights)[unit * a.c.cap + past + t] = 0.0f;
-      }
-    }
-  }
-  __syncthreads();                       // every wave has read the lengths
+  __syncthreads();                       // (every wave has read the lengths)
   if (threadIdx.x == 0) {
     gptr(a.new_lengths)[at] = total;
     if (a.past) gptr(a.past)[at] = past;
     if (a.fitting) gptr(a.fitting)[at] = fit;
     if (a.dropped) gptr(a.dropped)[at] = count - fit;
+  }
+  if (fit == 0) return;
+  const int pairs = 2 * a.c.H, chunk = threadIdx.x % kChunks;
+  auto rows_of = [&](int pair) {         // the call's rows of a (head, side), at this thread's chunk
+    const BlockRows& src = pair & 1 ? a.v : a.k;
+    return gptr(static_cast<const uint16_t*>(src.p)) + layer * (pair & 1 ? a.v_layer : a.k_layer) + b * src.sb +
+           (pair >> 1) * src.sh + chunk * 8;
+  };
+  auto tail_of = [&](int pair) {
+    return gptr(a.c.tail) + ((size_t)at * pairs + pair) * kBlockTokens * D + chunk * 8;
+  };
+
+  if (full > past / kBlockTokens) {
+    const int row0 = lane / kChunks;
+    for (int pair = wave; pair < pairs; pair += kAcceptWaves) {
+      const size_t us = (size_t)at * pairs + pair;
+      const RQ_GLOBAL uint16_t* in = rows_of(pair);
+      const RQ_GLOBAL uint16_t* tail = tail_of(pair);
+      const int64_t st = pair & 1 ? a.v.st : a.k.st;
+      for (int blk = past / kBlockTokens; blk < full; ++blk) {
+        u4 x[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int row = row0 + kRows * i, t = blk * kBlockTokens + row - past;
+          const RQ_GLOBAL uint16_t* from = t >= 0 ? in + node[t >= 0 ? t : 0] * st : tail + row * D;
+          x[i] = *(const RQ_GLOBAL u4_any*)from;
+        }
+        float most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) most = largest_of<BF16>(x[i], most);
+        float inv;
+        const float scale = block_scale<FMT>(wave_all<Max>(most), &inv);
+        RQ_GLOBAL uint8_t* out = gptr(a.c.codes) + (us * a.c.cap + (size_t)blk * kBlockTokens) * D + chunk * 8;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) store_codes<FMT, BF16>(x[i], inv, out + (row0 + kRows * i) * D);
+        if (lane == 0) gptr(a.c.scales)[us * (a.c.cap / kBlockTokens) + blk] = scale;
+      }
+    }
+    __syncthreads();                     // the rows that the next ones may replace are read
+  }
+
+  const int first = full * kBlockTokens > past ? full * kBlockTokens - past : 0;
+  const int rows = (fit - first) * pairs;               // pair by pair
+  constexpr int kStep = kAcceptThreads / kChunks;       // rows at a time
+  for (int r0 = threadIdx.x / kChunks; r0 < rows; r0 += 4 * kStep) {
+    u4 x[4];
+    RQ_GLOBAL u4* to[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = r0 + i * kStep < rows ? r0 + i * kStep : r0;
+      const int pair = (uint32_t)r / (uint32_t)(fit - first), t = first + r - pair * (fit - first);
+      x[i] = *(const RQ_GLOBAL u4_any*)(rows_of(pair) + node[t] * (pair & 1 ? a.v.st : a.k.st));
+      to[i] = (RQ_GLOBAL u4*)(tail_of(pair) + ((past + t) % kBlockTokens) * D);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i == 0 || r0 + i * kStep < rows) *to[i] = x[i];
+  }
+  for (int i = threadIdx.x; i < a.c.H * fit; i += kAcceptThreads) {
+    const int h = (uint32_t)i / (uint32_t)fit, t = i - h * fit;
+    RQ_GLOBAL int32_t* pos = gptr(a.c.positions) + ((size_t)at * a.c.H + h) * a.c.cap + past;
+    pos[t] = (past > 0 ? pos[-1] + 1 : 0) + t;
+    if (a.c.weights) gptr(a.c.weights)[((size_t)at * a.c.H + h) * a.c.cap + past + t] = 0.0f;
   }
 }
 
@@ -192,7 +222,7 @@ hipError_t launch(const BlockAppendLaunch& a, hipStream_t s) {
 
 template <int FMT, int D>
 hipError_t launch(const BlockAcceptLaunch& a, hipStream_t s) {
-  const dim3 grid(a.c.B, a.layers), block(64 * (2 * a.c.H < kAcceptWaves ? 2 * a.c.H : kAcceptWaves));
+  const dim3 grid(a.c.B, a.layers), block(kAcceptThreads);
   if (a.c.is_bf16)
     hipLaunchKernelGGL((block_accept_kernel<FMT, D, true>), grid, block, 0, s, a);
   else
