@@ -649,8 +649,8 @@ rq_status rq_tree_verify_workspace(const rq_tree_draft* d, uint64_t* bytes);
  * distribution whatever the draft.
  * Products, quotients and sums are fp64.  Probabilities must be finite and not
  * negative; their sum is taken as 1 (rounded ones serve).  ws: device scratch,
- * 16-byte aligned, contents arbitrary; calls that share it must not overlap.
- * Asynchronous. */
+ * 16-byte aligned, zeroed by the caller before its first call, and zero again
+ * after every one; calls that share it must not overlap.  Asynchronous. */
 rq_status rq_tree_verify(const rq_tree_draft* d, void* ws, uint64_t ws_bytes,
                          rq_stream stream);
 

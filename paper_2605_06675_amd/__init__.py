@@ -829,7 +829,8 @@ def rq_tree_verify(tokens, parents, target, draft, uniforms, path, count, next,
     uniforms: float32 [batch][n_nodes] in [0, 1); new_len: int32 [batch].
     Receives path: int32 [batch][room], the accepted nodes; count: int32 [batch];
     next: int32 [batch], the token drawn behind them.  ws: device byte tensor of at
-    least rq_tree_verify_workspace bytes."""
+    least rq_tree_verify_workspace bytes, zeroed before its first call (every call
+    leaves it zero)."""
     import torch
     if target.dim() != 3 or path.dim() != 2:
         raise ValueError("target must have three axes and path two")
@@ -924,6 +925,7 @@ class DraftTree:
                                     device=parents.device)
             self.depth = torch.zeros_like(parents)
         self._results = self._ws = None
+        self._held = []             # tensors that a graph writes to
         self.layout(stream)
 
     def layout(self, stream=None):
@@ -941,11 +943,13 @@ class DraftTree:
         need = rq_tree_verify_workspace(B, n, target.shape[-1])
         with torch.cuda.stream(s):
             if self._ws is None or self._ws.numel() < need:
-                self._ws = torch.empty(need, dtype=torch.uint8, device=target.device)
+                self._ws = torch.zeros(need, dtype=torch.uint8, device=target.device)
             if self._results is None or self._results[0].shape[1] != room:
                 self._results = tuple(
                     torch.empty(shape, dtype=torch.int32, device=target.device)
                     for shape in ((B, room), (B,), (B,)))
+            if torch.cuda.is_current_stream_capturing():
+                self._held.append((self._ws, self._results))
         rq_tree_verify(tokens, self.parents, target, draft, uniforms,
                        *self._results, self._ws, self.new_len, stream)
         return self._results

@@ -16,8 +16,9 @@ struct TreeMaskLaunch {
   int B, n, words;
 };
 
-// Entries of a row that a workgroup takes at once, and the most parts of a row.
-constexpr int kVerifyStep = 16384, kVerifyParts = 64;
+// Entries of a row that a workgroup takes at once, the most parts of a row, and of how
+// many sums over a row the parts are shared.
+constexpr int kVerifyStep = 8192, kVerifyParts = 64, kVerifySums = 16;
 
 struct TreeVerifyLaunch {
   const int32_t *tokens, *parents;   // [B][n]
@@ -27,10 +28,9 @@ struct TreeVerifyLaunch {
   const float* uniforms;             // [B][n]
   int B, n, vocab, dtype, n_path;
   int32_t *path, *count, *next;
-  int part, parts;                   // a row's entries, in parts
-  double* sums;                      // [B][parts]: of the residual
-  double* inverse;                   // [B][n]: 1 / s before each of the node's rejections
-  int32_t* found;                    // [B][4]: last node (-1: no nodes), rejections, path full
+  int part, parts;                   // a row's entries, in parts, a workgroup each
+  uint64_t* slots;                   // [B][kVerifySums][parts]: sums, or 0
+  uint32_t* done;                    // [B]: workgroups that are
 };
 
 // Whether two arrays share memory (none shares with NULL).

@@ -68,23 +68,29 @@ __global__ void __launch_bounds__(kMaskThreads) tree_mask_kernel(TreeMaskLaunch 
 // --------------------------------------------------------------- verification
 // Walk: from the root, the children of the last accepted node in order,
 //   accept child c where u_c q(x) s < r(x);   r <- max(0, r / s - q), s <- sum r
-// (q = 1 and r(x) <- 0, s <- max(0, s - r(x)) without the draft's rows).  A test needs one
-// entry of each row, which all nodes load at once; without the draft's rows the
-// mass before each test is a sum over the earlier siblings, so all tests are
-// decided before the walk.  With them a rejection that leaves a sibling to test
-// needs the residual's sum over a whole row.
+// (q = 1 and r(x) <- 0, s <- max(0, s - r(x)) without the draft's rows).  A test needs
+// one entry of each row, which all nodes load at once; without the draft's rows the
+// mass before each test is a sum over the earlier siblings, so all tests are decided
+// before the walk.  With them a rejection that leaves a sibling to test needs the
+// residual's sum over a whole row, and so does the last token.
 //
-// Every workgroup of a sequence walks by itself, to the same end, and adds its part
-// of the residual that the last token is drawn from; the second kernel finds the
-// part, and in it the token.  All in fp64: the results are decisions, which fp32
-// sums would make otherwise next to a border.
+// A sequence's workgroups, a part of the rows each, all walk by themselves, to the same
+// end.  For a sum each adds its part, puts it where the others see it and waits for
+// theirs; what does not come in time (a workgroup that does not run) it adds itself, in
+// the same order.  So no wait is without an end, and the results are the same either
+// way.  The one whose part holds the last token finds it.  The last to finish clears
+// what was put down.
+//
+// All sums are fp64 in one order: the results are decisions, which fp32 sums would make
+// otherwise next to a border.  Bound by latency: launch, nodes, entries, a row's part,
+// the parts' exchange.
 constexpr int kThreads = 1024, kEach = kVerifyStep / kThreads;
 constexpr int kNone = 1 << 30;
+constexpr int kPolls = 4096;      // some milliseconds
 
 template <int DTYPE>
 struct Prob {
   typedef uint16_t type;
-  static constexpr bool kBf16 = DTYPE == RQ_BF16;
 };
 template <>
 struct Prob<RQ_F32> {
@@ -99,7 +105,7 @@ __device__ __forceinline__ float prob(const RQ_GLOBAL typename Prob<DTYPE>::type
     return widen_t<DTYPE == RQ_BF16>(*p);
 }
 
-// Entries v..v + 15 of a row; zeros behind its end.
+// Entries v..v + 7 of a row; zeros behind its end.
 template <int DTYPE>
 __device__ __forceinline__ void load_probs(const RQ_GLOBAL typename Prob<DTYPE>::type* row, int v, int vocab, float x[kEach]) {
   if (v + kEach <= vocab) {
@@ -111,14 +117,11 @@ __device__ __forceinline__ void load_probs(const RQ_GLOBAL typename Prob<DTYPE>:
         for (int j = 0; j < 4; ++j) x[4 * i + j] = y[j];
       }
     } else {
+      const u4 y = *(const RQ_GLOBAL u4_any*)(row + v);
 #pragma unroll
-      for (int i = 0; i < kEach / 8; ++i) {
-        const u4 y = *(const RQ_GLOBAL u4_any*)(row + v + 8 * i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          x[8 * i + 2 * j] = widen_t<DTYPE == RQ_BF16>(y[j] & 0xffffu);
-          x[8 * i + 2 * j + 1] = widen_t<DTYPE == RQ_BF16>(y[j] >> 16);
-        }
+      for (int j = 0; j < 4; ++j) {
+        x[2 * j] = widen_t<DTYPE == RQ_BF16>(y[j] & 0xffffu);
+        x[2 * j + 1] = widen_t<DTYPE == RQ_BF16>(y[j] >> 16);
       }
     }
   } else {
@@ -134,7 +137,7 @@ struct Residual {
   const RQ_GLOBAL type *target, *draft;
   int rejected;             // with the draft's rows: how many
   const double* inverse;    // 1 / s before each of them (LDS)
-  const int* gone;          // without: the tokens taken out of [.., ..) (LDS),
+  const int* gone;          // without: the tokens taken out (LDS),
   int n_gone;               // how many
 
   __device__ __forceinline__ Residual(const TreeVerifyLaunch& a, int b, int node) {
@@ -161,70 +164,57 @@ struct Residual {
     } else {
       for (int j = 0; j < n_gone; ++j) {
         const int at = gone[j] - v;
+        if (at >= 0 && at < kEach) {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i)
-          if (at == i) r[i] = 0.0;
+          for (int i = 0; i < kEach; ++i)
+            if (at == i) r[i] = 0.0;
+        }
       }
     }
   }
 };
 
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
-  return x;
+// Register moves of doubles (see row_all and its like): CTRL of a lane's row; rows
+// outside ROWS, and lanes without a source, get 0.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved_d(double x) {
+  const u2 w = __builtin_bit_cast(u2, x);
+  return __builtin_bit_cast(double, (u2){(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w.x, CTRL, ROWS, 0xf, true),
+                                         (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w.y, CTRL, ROWS, 0xf, true)});
 }
-
-// The sum over the workgroup, in every thread.
-__device__ __forceinline__ double block_sum(double x, double* lds) {
-  x = wave_sum(x);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-  __syncthreads();
-  double sum = 0.0;
-#pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) sum += lds[w];
-  return sum;
-}
-
-template <int DTYPE, bool DRAFT>
-__device__ __forceinline__ double residual_sum(const Residual<DTYPE, DRAFT>& res, int lo, int hi, int vocab, double* lds) {
-  double sum = 0.0;
-  for (int v = lo + (int)threadIdx.x * kEach; v < hi; v += kVerifyStep) {
-    double r[kEach];
-    res.load(v, vocab, r);
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) sum += r[i];
-  }
-  return block_sum(sum, lds);
-}
-
-// What walk and selection hold of the nodes.
-struct Nodes {
-  int parent[RQ_MAX_NODES], token[RQ_MAX_NODES];
-};
-
-// The tokens of node's children in [lo, hi), into gone.
-__device__ __forceinline__ int gone_tokens(const Nodes& s, int m, int node, int lo, int hi, int* gone, int* count) {
-  if (threadIdx.x == 0) *count = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < m; i += kThreads)
-    if (s.parent[i] == node && s.token[i] >= lo && s.token[i] < hi) gone[atomicAdd(count, 1)] = s.token[i];
-  __syncthreads();
-  return *count;
+// Sums up to each lane, it included.
+__device__ __forceinline__ double wave_scan(double x) {
+  x += moved_d<0x111, 0xf>(x);          // 1, 2, 4 and 8 lanes before, in a row of 16,
+  x += moved_d<0x112, 0xf>(x);
+  x += moved_d<0x114, 0xf>(x);
+  x += moved_d<0x118, 0xf>(x);
+  x += moved_d<0x142, 0xa>(x);          // the last of rows 0 and 2 to the next ones,
+  return x + moved_d<0x143, 0xc>(x);    // the first half's last to the second half
 }
 
 template <int DTYPE, bool DRAFT>
-__global__ void __launch_bounds__(kThreads) tree_walk_kernel(TreeVerifyLaunch a) {
-  __shared__ Nodes s;
-  __shared__ float p[RQ_MAX_NODES], q[RQ_MAX_NODES];   // of a node's token, in its parent's rows
+__global__ void __launch_bounds__(kThreads) tree_verify_kernel(TreeVerifyLaunch a) {
+  __shared__ __align__(16) int parent[RQ_MAX_NODES], token[RQ_MAX_NODES];
+  __shared__ __align__(16) float p[RQ_MAX_NODES], q[RQ_MAX_NODES];   // of a node's token, in its parent's rows
   __shared__ float u[RQ_MAX_NODES];
   __shared__ int child[RQ_MAX_NODES];     // the first child (without a draft: the first accepted one)
   __shared__ int sibling[RQ_MAX_NODES];   // the next one
   __shared__ double inverse[RQ_MAX_NODES];
-  __shared__ double red[kThreads / 64];
-  __shared__ int n_gone;
+  __shared__ double waves[kThreads / 64], sums[kVerifyParts];
+  __shared__ int here[kVerifyParts];
+  __shared__ int n_gone, at_first, at_last;
   const int b = blockIdx.y, part = blockIdx.x, t = threadIdx.x;
+  int up = -1;
+  if (t < a.n) {                          // (at most as many nodes as threads)
+    const size_t at = (size_t)b * a.n + t;
+    int x = gptr(a.tokens)[at];
+    up = t == 0 ? -1 : parent_of(a.parents, b, a.n, t);
+    x = x < 0 ? 0 : (x < a.vocab ? x : a.vocab - 1);
+    parent[t] = up;
+    token[t] = x;
+    u[t] = gptr(a.uniforms)[at];
+    child[t] = sibling[t] = kNone;
+  }
   const int m = node_count(a.new_len, b, a.n);
   RQ_GLOBAL int32_t* path = gptr(a.path) + (size_t)b * a.n_path;
   if (m == 0) {
@@ -232,55 +222,118 @@ __global__ void __launch_bounds__(kThreads) tree_walk_kernel(TreeVerifyLaunch a)
       if (t < a.n_path) path[t] = -1;
       if (t == 0) {
         gptr(a.count)[b] = 0;
-        gptr(a.found)[b * 4] = -1;
+        gptr(a.next)[b] = -1;
       }
     }
     return;
   }
-  const int me = t;                       // (at most as many nodes as threads)
-  if (me < m) {
-    const size_t at = (size_t)b * a.n + me;
-    const int up = me == 0 ? -1 : parent_of(a.parents, b, a.n, me);
-    int x = gptr(a.tokens)[at];
-    x = x < 0 ? 0 : (x < a.vocab ? x : a.vocab - 1);
-    s.parent[me] = up;
-    s.token[me] = x;
-    u[me] = gptr(a.uniforms)[at];
-    child[me] = sibling[me] = kNone;
-    const Residual<DTYPE, DRAFT> row(a, b, up < 0 ? 0 : up);
-    p[me] = prob<DTYPE>(row.target + x);
-    if (DRAFT) q[me] = prob<DTYPE>(row.draft + x);
+  if (t >= m) up = -1;
+  if (up >= 0) {
+    const Residual<DTYPE, DRAFT> row(a, b, up);
+    p[t] = prob<DTYPE>(row.target + token[t]);
+    if (DRAFT) q[t] = prob<DTYPE>(row.draft + token[t]);
   }
   __syncthreads();
-  const int up = me < m ? s.parent[me] : -1;
+  // every earlier node of a thread's, eight at a time (LDS reads are slow one by one)
+  auto earlier = [&](auto f) {
+    if (up >= 0)
+      for (int j0 = 0; j0 < t; j0 += 8) {
+        const u4 a0 = *(const u4*)&parent[j0], a1 = *(const u4*)&parent[j0 + 4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f(j0 + i, (int)(i < 4 ? a0[i & 3] : a1[i & 3]) == up && j0 + i < t, i);
+      }
+  };
   if constexpr (DRAFT) {
+    int before = -1;
+    earlier([&](int j, bool mine, int) { before = mine ? j : before; });
     if (up >= 0) {
-      int before = -1;
-      for (int j = 0; j < me; ++j) before = s.parent[j] == up ? j : before;
       if (before < 0)
-        child[up] = me;
+        child[up] = t;
       else
-        sibling[before] = me;
+        sibling[before] = t;
     }
   } else {
-    if (up >= 0) {
-      // a token that an earlier sibling has is gone by its turn
-      const int x = s.token[me];
-      bool twice = false;
-      for (int j = 0; j < me; ++j) twice |= s.parent[j] == up && s.token[j] == x;
-      q[me] = twice ? 0.0f : p[me];
-    }
-    __syncthreads();
-    if (up >= 0) {
-      double mass = 1.0;
-      for (int j = 0; j < me; ++j) {
-        mass -= s.parent[j] == up ? (double)q[j] : 0.0;
-        mass = mass > 0.0 ? mass : 0.0;
+    // a token that an earlier sibling has is gone by its turn
+    const int x = t < m ? token[t] : 0;
+    bool twice = false;
+    u4 b0, b1;
+    earlier([&](int j, bool mine, int i) {
+      if (i == 0) {
+        b0 = *(const u4*)&token[j];
+        b1 = *(const u4*)&token[j + 4];
       }
-      if ((double)u[me] * mass < (double)q[me]) atomicMin(&child[up], me);
-    }
+      twice |= mine && (int)(i < 4 ? b0[i & 3] : b1[i & 3]) == x;
+    });
+    if (up >= 0) q[t] = twice ? 0.0f : p[t];
+    __syncthreads();
+    double mass = 1.0;      // (below 0 it stays there, and counts as 0)
+    earlier([&](int j, bool mine, int i) {
+      if (i == 0) {
+        b0 = *(const u4*)&q[j];
+        b1 = *(const u4*)&q[j + 4];
+      }
+      mass -= (double)(mine ? __uint_as_float(i < 4 ? b0[i & 3] : b1[i & 3]) : 0.0f);
+    });
+    mass = mass > 0.0 ? mass : 0.0;
+    if (up >= 0 && (double)u[t] * mass < (double)q[t]) atomicMin(&child[up], t);
   }
   __syncthreads();
+
+  // the workgroup's sum of a part, in every thread
+  auto part_sum = [&](const Residual<DTYPE, DRAFT>& res, int i) {
+    const int lo = i * a.part, hi = min(lo + a.part, a.vocab);
+    double sum = 0.0;
+    for (int v = lo + t * kEach; v < hi; v += kVerifyStep) {
+      double r[kEach];
+      res.load(v, a.vocab, r);
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) sum += r[k];
+    }
+    sum = wave_scan(sum);
+    __syncthreads();
+    if ((t & 63) == 63) waves[t >> 6] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) sum += waves[w];
+    return sum;
+  };
+  // All parts' sums, in `sums`, and the whole.  (A sum is not negative: with its sign
+  // set it is no zero, which stands for one that is not there.)
+  int asked = 0;
+  RQ_GLOBAL uint64_t* slots = gptr(a.slots) + (size_t)b * kVerifySums * a.parts;
+  auto all_sums = [&](const Residual<DTYPE, DRAFT>& res) {
+    double mine = part_sum(res, part);
+    mine = mine > 0.0 ? mine : 0.0;       // (no NaN either)
+    const bool shared = asked < kVerifySums;
+    RQ_GLOBAL uint64_t* slot = slots + (size_t)asked * a.parts;
+    ++asked;
+    if (shared && t == 0 && a.parts > 1)
+      __hip_atomic_store(slot + part, __builtin_bit_cast(uint64_t, mine) | 1ull << 63, __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
+    if (t < a.parts) {
+      uint64_t x = 0;
+      if (shared && t != part)
+        for (int i = 0; i < kPolls && x == 0; ++i)
+          x = __hip_atomic_load(slot + t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      sums[t] = t == part ? mine : __builtin_bit_cast(double, x & ~(1ull << 63));
+      here[t] = t == part || x != 0;
+    }
+    __syncthreads();
+    double whole = 0.0;
+    for (int i = 0; i < a.parts; ++i) {
+      if (!here[i]) {                     // (the same in every thread)
+        double sum = part_sum(res, i);
+        sum = sum > 0.0 ? sum : 0.0;
+        if (t == 0) sums[i] = sum;
+        whole += sum;
+      } else {
+        whole += sums[i];
+      }
+    }
+    __syncthreads();
+    return whole;
+  };
 
   // the walk, alike in every thread
   int cur = 0, count = 1, rejected = 0, full = 0;
@@ -312,7 +365,7 @@ __global__ void __launch_bounds__(kThreads) tree_walk_kernel(TreeVerifyLaunch a)
         Residual<DTYPE, DRAFT> res(a, b, cur);
         res.rejected = rejected;
         res.inverse = inverse;
-        mass = residual_sum(res, 0, a.vocab, a.vocab, red);
+        mass = all_sums(res);
       }
     }
     if (c == kNone) break;
@@ -321,98 +374,61 @@ __global__ void __launch_bounds__(kThreads) tree_walk_kernel(TreeVerifyLaunch a)
     if (part == 0 && t == 0) path[count] = c;
     ++count;
   }
+  if (part == 0) {
+    for (int i = count + t; i < a.n_path; i += kThreads) path[i] = -1;
+    if (t == 0) gptr(a.count)[b] = count;
+  }
 
-  Residual<DTYPE, DRAFT> res(a, b, cur);
-  const int lo = part * a.part, hi = min(lo + a.part, a.vocab);
-  res.rejected = rejected;
-  res.inverse = inverse;
-  if (!DRAFT && !full) {
-    res.n_gone = gone_tokens(s, m, cur, lo, hi, sibling, &n_gone);
-    res.gone = sibling;
-  }
-  const double sum = residual_sum(res, lo, hi, a.vocab, red);
-  if (t == 0) gptr(a.sums)[(size_t)b * a.parts + part] = sum;
-  if (part != 0) return;
-  for (int i = count + t; i < a.n_path; i += kThreads) path[i] = -1;
-  for (int i = t; i < rejected; i += kThreads) gptr(a.inverse)[(size_t)b * a.n + i] = inverse[i];
+  // the last token: the first whose running sum exceeds u times the whole
   if (t == 0) {
-    gptr(a.count)[b] = count;
-    RQ_GLOBAL int32_t* found = gptr(a.found) + b * 4;
-    found[0] = cur;
-    found[1] = rejected;
-    found[2] = full;
-  }
-}
-
-// The token: the first whose running sum exceeds u times the whole.
-template <int DTYPE, bool DRAFT>
-__global__ void __launch_bounds__(kThreads) tree_select_kernel(TreeVerifyLaunch a) {
-  __shared__ Nodes s;
-  __shared__ int gone[RQ_MAX_NODES];
-  __shared__ double inverse[RQ_MAX_NODES];
-  __shared__ double sums[kVerifyParts], red[kThreads / 64];
-  __shared__ int n_gone, at_first, at_last;
-  const int b = blockIdx.x, t = threadIdx.x;
-  const int m = node_count(a.new_len, b, a.n);
-  if (m == 0) {
-    if (t == 0) gptr(a.next)[b] = -1;
-    return;
-  }
-  const RQ_GLOBAL int32_t* found = gptr(a.found) + b * 4;
-  const int cur = found[0], full = found[2];
-  Residual<DTYPE, DRAFT> res(a, b, cur);
-  res.rejected = found[1];
-  res.inverse = inverse;
-  res.gone = gone;
-  for (int i = t; i < res.rejected; i += kThreads) inverse[i] = gptr(a.inverse)[(size_t)b * a.n + i];
-  if (!DRAFT && t < m) {
-    s.parent[t] = t == 0 ? -1 : parent_of(a.parents, b, a.n, t);
-    const int x = gptr(a.tokens)[(size_t)b * a.n + t];
-    s.token[t] = x < 0 ? 0 : (x < a.vocab ? x : a.vocab - 1);
-  }
-  if (t < a.parts) sums[t] = gptr(a.sums)[(size_t)b * a.parts + t];
-  if (t == 0) {
+    n_gone = 0;
     at_first = kNone;
     at_last = -1;
   }
   __syncthreads();
-  double whole = 0.0;
-  for (int i = 0; i < a.parts; ++i) whole += sums[i];
-  bool taken = !DRAFT && !full;           // the children's tokens are
-  if (!(whole > 0.0)) {
-    // no mass left: the target's row
-    res.rejected = 0;
-    taken = false;
-    whole = 0.0;
-    for (int i = 0; i < a.parts; ++i) {
-      const int lo = i * a.part;
-      const double sum = residual_sum(res, lo, min(lo + a.part, a.vocab), a.vocab, red);
-      if (t == 0) sums[i] = sum;
-      whole += sum;
-    }
+  Residual<DTYPE, DRAFT> res(a, b, cur);
+  res.rejected = rejected;
+  res.inverse = inverse;
+  if (!DRAFT && !full) {
+    if (t < m && up == cur) sibling[atomicAdd(&n_gone, 1)] = token[t];     // (the children's tokens)
     __syncthreads();
-    if (!(whole > 0.0)) {
-      if (t == 0) gptr(a.next)[b] = 0;
-      return;
+    res.n_gone = n_gone;
+    res.gone = sibling;
+  }
+  double whole = all_sums(res);
+  if (!(whole > 0.0)) {                   // no mass left: the target's row
+    res.rejected = res.n_gone = 0;
+    whole = all_sums(res);
+  }
+  if (a.parts > 1 && t == 0) {
+    // the last of the sequence's workgroups to come here clears the slots
+    __builtin_amdgcn_s_waitcnt(0);        // this one's sums are out
+    RQ_GLOBAL uint32_t* done = gptr(a.done) + b;
+    if (__hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.parts - 1) {
+      const int used = (asked < kVerifySums ? asked : kVerifySums) * a.parts;
+      for (int i = 0; i < used; ++i) __hip_atomic_store(slots + i, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
   }
-  const double bar = (double)gptr(a.uniforms)[(size_t)b * a.n] * whole;
-  int part = -1, last = 0;
+  const double bar = (double)u[0] * whole;
+  int holds = -1, last = 0;
   double before = 0.0, run = 0.0;
   for (int i = 0; i < a.parts; ++i) {
     if (sums[i] > 0.0) last = i;
-    if (part < 0 && run + sums[i] > bar) {
-      part = i;
+    if (holds < 0 && run + sums[i] > bar) {
+      holds = i;
       before = run;
     }
     run += sums[i];
   }
-  if (part < 0) {
-    part = last;
-    before = -1.0;                        // (none exceeds: the last of r > 0)
+  const bool beyond = holds < 0;          // (none exceeds: the last of r > 0)
+  if (beyond) holds = last;
+  if (part != holds) return;
+  if (!(whole > 0.0)) {
+    if (t == 0) gptr(a.next)[b] = 0;
+    return;
   }
   const int lo = part * a.part, hi = min(lo + a.part, a.vocab);
-  if (taken) res.n_gone = gone_tokens(s, m, cur, lo, hi, gone, &n_gone);
   for (int v0 = lo; v0 < hi; v0 += kVerifyStep) {
     const int v = v0 + t * kEach;
     double r[kEach], mine = 0.0;
@@ -424,46 +440,37 @@ __global__ void __launch_bounds__(kThreads) tree_select_kernel(TreeVerifyLaunch 
     }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) mine += r[i];
-    // the sum before this thread's entries
-    double upto = mine;
+    const double upto = wave_scan(mine);
+    __syncthreads();
+    if ((t & 63) == 63) waves[t >> 6] = upto;
+    __syncthreads();
+    double x = before + (upto - mine), all = 0.0;     // the sum before this thread's entries
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const double x = __shfl_up(upto, d);
-      if ((t & 63) >= d) upto += x;
-    }
-    __syncthreads();
-    if ((t & 63) == 63) red[t >> 6] = upto;
-    __syncthreads();
-    double base = before, all = 0.0;
     for (int w = 0; w < kThreads / 64; ++w) {
-      if (w < (t >> 6)) base += red[w];
-      all += red[w];
+      x += w < (t >> 6) ? waves[w] : 0.0;
+      all += waves[w];
     }
-    double x = base + (upto - mine);
     int first = kNone, end = -1;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       x += r[i];
       if (r[i] > 0.0) {
         end = v + i;
-        if (first == kNone && before >= 0.0 && x > bar) first = v + i;
+        if (first == kNone && !beyond && x > bar) first = v + i;
       }
     }
     if (first != kNone) atomicMin(&at_first, first);
     if (end >= 0) atomicMax(&at_last, end);
     __syncthreads();
     if (at_first != kNone) break;
-    if (before >= 0.0) before += all;
+    before += all;
   }
   if (t == 0) gptr(a.next)[b] = at_first != kNone ? at_first : (at_last >= 0 ? at_last : 0);
 }
 
 template <int DTYPE, bool DRAFT>
 hipError_t launch(const TreeVerifyLaunch& a, hipStream_t s) {
-  hipLaunchKernelGGL((tree_walk_kernel<DTYPE, DRAFT>), dim3(a.parts, a.B), dim3(kThreads), 0, s, a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((tree_select_kernel<DTYPE, DRAFT>), dim3(a.B), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((tree_verify_kernel<DTYPE, DRAFT>), dim3(a.parts, a.B), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -40,23 +40,23 @@ rq_status check_draft(const rq_tree_draft* d) {
   return RQ_OK;
 }
 
-// A row's parts, a workgroup each (and one that walks again): of one step of the
-// kernels, or as many steps as leave kVerifyParts.
+// A row's parts, a workgroup each: as many steps of the kernel, at most kVerifyParts,
+// and no more than leave every sequence's workgroups room on the chip together.
 struct VerifyPlan {
   int part, parts;
-  uint64_t sums, inverse, found;   // bytes
-  uint64_t bytes() const { return sums + inverse + found; }
+  uint64_t slots, done;            // bytes
+  uint64_t bytes() const { return slots + done; }
 };
 
 VerifyPlan plan_verify(const rq_tree_draft* d) {
   VerifyPlan p{};
   const int steps = (d->vocab + rq::kVerifyStep - 1) / rq::kVerifyStep;
-  p.part = (steps + rq::kVerifyParts - 1) / rq::kVerifyParts * rq::kVerifyStep;
+  const int most = std::max(std::min({steps, rq::kVerifyParts, rq::device_cus() / d->batch}), 1);
+  p.part = ((d->vocab + most - 1) / most + 15) / 16 * 16;
   p.parts = (d->vocab + p.part - 1) / p.part;
   const uint64_t b = d->batch;
-  p.sums = b * p.parts * sizeof(double);
-  p.inverse = b * d->n_nodes * sizeof(double);
-  p.found = b * 4 * sizeof(int32_t);
+  p.slots = b * rq::kVerifySums * p.parts * sizeof(uint64_t);
+  p.done = b * sizeof(uint32_t);
   return p;
 }
 
@@ -137,9 +137,8 @@ rq_status rq_tree_verify(const rq_tree_draft* d, void* ws, uint64_t ws_bytes, rq
   a.part = p.part;
   a.parts = p.parts;
   uint8_t* w = static_cast<uint8_t*>(ws);
-  a.sums = reinterpret_cast<double*>(w);
-  a.inverse = reinterpret_cast<double*>(w + p.sums);
-  a.found = reinterpret_cast<int32_t*>(w + p.sums + p.inverse);
+  a.slots = reinterpret_cast<uint64_t*>(w);
+  a.done = reinterpret_cast<uint32_t*>(w + p.slots);
   return launched(rq::launch_tree_verify(a, reinterpret_cast<hipStream_t>(stream)), "verification launch");
 }
 

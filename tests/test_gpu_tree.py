@@ -282,11 +282,12 @@ def verify(parents, tokens, target, draft, u, new=None, room=None, place=None):
     place = (lambda x: x.cuda()) if place is None else place
     path = torch.full((B, room), 77, dtype=torch.int32, device="cuda")
     count, last = (torch.full((B,), 77, dtype=torch.int32, device="cuda") for _ in range(2))
-    ws = torch.full((rq.rq_tree_verify_workspace(B, n, V),), 0xff, dtype=torch.uint8, device="cuda")
+    ws = torch.zeros(rq.rq_tree_verify_workspace(B, n, V), dtype=torch.uint8, device="cuda")
     print("verify", (B, n, V), target.dtype, draft is not None, room, flush=True)
     rq.rq_tree_verify(ints(tokens), ints(parents), place(target), None if draft is None else place(draft),
                       u.cuda(), path, count, last, ws, None if new is None else ints(new))
     path, count, last = (x.cpu().tolist() for x in (path, count, last))
+    assert (ws == 0).all()                                  # ready for the next call
     for b in range(B):
         m = n if new is None else new[b]
         if m == 0:
@@ -376,7 +377,7 @@ def test_verify_takes_tokens_and_parents_out_of_range_as_the_nearest_inside():
     target = probabilities(g, (2, n, V), torch.float32)
     u = torch.zeros(2, n)
     path, count, last = (torch.zeros(s, dtype=torch.int32, device="cuda") for s in ((2, n), (2,), (2,)))
-    ws = torch.empty(rq.rq_tree_verify_workspace(2, n, V), dtype=torch.uint8, device="cuda")
+    ws = torch.zeros(rq.rq_tree_verify_workspace(2, n, V), dtype=torch.uint8, device="cuda")
     rq.rq_tree_verify(ints([[1 << 30] * n, [-5] * n]), ints([[9] * n, [3, 0, -9, 1, 7, 2]]), target.cuda(), None,
                       u.cuda(), path, count, last, ws, ints([99, -1]))
     want, token = tree.verify(list(range(-1, n - 1)), [V - 1] * n, target[0].numpy(), None, u[0].numpy(), n)
@@ -646,3 +647,34 @@ def test_python_refusals():
             layout.verify(*a)
     with pytest.raises(rq.RQError):
         layout.verify(tokens, target, u, room=n + 1)
+
+
+@pytest.mark.parametrize("B", [1, 3, 40, 300])
+@pytest.mark.parametrize("V", [8192, 8193, 33333])
+def test_verify_many_rejections_and_sequences(B, V):
+    """Rejections by the dozen (more sums over a row than the workgroups share), and more
+    sequences than a chip holds workgroups."""
+    g = torch.Generator().manual_seed(B + V)
+    n = 30 if B < 100 else 4
+    parents = [some_parents(n, b, "star" if b % 2 == 0 else "tree") for b in range(B)]
+    target = probabilities(g, (B, n, V), torch.float32, 0.5)
+    tokens = torch.stack([torch.randperm(V, generator=g)[:n] for _ in range(B)])
+    draft = 0.05 * target                         # the rest of it on the drafted tokens
+    draft.scatter_add_(2, tokens[:, None].expand(B, n, n), torch.full((B, n, n), 0.95 / n))
+    _, count, _ = verify(parents, tokens.tolist(), target, draft, torch.rand(B, n, generator=g))
+    assert count[0] == 1                          # 29 rejections, or 3
+
+
+def test_verify_gives_the_same_again():
+    """Twenty calls on one workspace, with calls of other sizes between."""
+    g = torch.Generator().manual_seed(1)
+    made = []
+    for B, n, V in ((4, 20, 50000), (9, 5, 20000)):
+        layout = rq.DraftTree(ints([some_parents(n, b) for b in range(B)]))
+        target, draft = (probabilities(g, (B, n, V), torch.float32, 0.3).cuda() for _ in range(2))
+        tokens, u = torch.randint(V, (B, n), generator=g).int().cuda(), torch.rand(B, n, generator=g).cuda()
+        made.append((layout, tokens, target, u, draft))
+    first = [[x.clone() for x in m[0].verify(*m[1:])] for m in made]
+    for _ in range(20):
+        for m, want in zip(made, first):
+            assert all(torch.equal(x, y) for x, y in zip(m[0].verify(*m[1:]), want))
