@@ -31,6 +31,7 @@ struct TreeVerifyLaunch {
   int part, parts;                   // a row's entries, in parts, a workgroup each
   uint64_t* slots;                   // [B][kVerifySums][parts]: sums, or 0
   uint32_t* done;                    // [B]: workgroups that are
+  int spread;                        // 2^spread threads look for a node's siblings
 };
 
 // Whether two arrays share memory (none shares with NULL).

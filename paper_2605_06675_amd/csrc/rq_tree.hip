@@ -213,7 +213,8 @@ __global__ void __launch_bounds__(kThreads) tree_verify_kernel(TreeVerifyLaunch 
     parent[t] = up;
     token[t] = x;
     u[t] = gptr(a.uniforms)[at];
-    child[t] = sibling[t] = kNone;
+    child[t] = kNone;
+    sibling[t] = -1;
   }
   const int m = node_count(a.new_len, b, a.n);
   RQ_GLOBAL int32_t* path = gptr(a.path) + (size_t)b * a.n_path;
@@ -234,18 +235,31 @@ __global__ void __launch_bounds__(kThreads) tree_verify_kernel(TreeVerifyLaunch 
     if (DRAFT) q[t] = prob<DTYPE>(row.draft + token[t]);
   }
   __syncthreads();
-  // every earlier node of a thread's, eight at a time (LDS reads are slow one by one)
+  // Each node's earlier siblings, found by 2^spread threads: every 2^spread-th node
+  // before it is one's, eight at a time (LDS reads are slow one by one).
+  const int spread = a.spread, node = t >> spread, slice = t & ((1 << spread) - 1);
+  const int mother = node < m ? parent[node] : -1;
   auto earlier = [&](auto f) {
-    if (up >= 0)
-      for (int j0 = 0; j0 < t; j0 += 8) {
-        const u4 a0 = *(const u4*)&parent[j0], a1 = *(const u4*)&parent[j0 + 4];
+    if (mother >= 0)
+      for (int j0 = slice; j0 < node; j0 += 8 << spread) {
+        int j[8], of[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f(j0 + i, (int)(i < 4 ? a0[i & 3] : a1[i & 3]) == up && j0 + i < t, i);
+        for (int i = 0; i < 8; ++i) {
+          j[i] = j0 + (i << spread);
+          of[i] = parent[j[i] < node ? j[i] : 0];       // (the root has none)
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (of[i] == mother) f(j[i]);
       }
   };
   if constexpr (DRAFT) {
-    int before = -1;
-    earlier([&](int j, bool mine, int) { before = mine ? j : before; });
+    earlier([&](int j) { atomicMax(&sibling[node], j); });         // (the one before, at first)
+    __syncthreads();
+    const int before = t < m ? sibling[t] : -1;
+    __syncthreads();
+    if (t < m) sibling[t] = kNone;
+    __syncthreads();
     if (up >= 0) {
       if (before < 0)
         child[up] = t;
@@ -254,28 +268,18 @@ __global__ void __launch_bounds__(kThreads) tree_verify_kernel(TreeVerifyLaunch 
     }
   } else {
     // a token that an earlier sibling has is gone by its turn
-    const int x = t < m ? token[t] : 0;
     bool twice = false;
-    u4 b0, b1;
-    earlier([&](int j, bool mine, int i) {
-      if (i == 0) {
-        b0 = *(const u4*)&token[j];
-        b1 = *(const u4*)&token[j + 4];
-      }
-      twice |= mine && (int)(i < 4 ? b0[i & 3] : b1[i & 3]) == x;
-    });
-    if (up >= 0) q[t] = twice ? 0.0f : p[t];
+    const int x = node < m ? token[node] : 0;
+    earlier([&](int j) { twice |= token[j] == x; });
+    const uint64_t group = (2ull << ((1 << spread) - 1)) - 1;      // 2^spread lanes
+    twice = (__ballot(twice) >> (t & 63 & ~((1 << spread) - 1))) & group;
+    if (mother >= 0 && slice == 0) q[node] = twice ? 0.0f : p[node];
     __syncthreads();
-    double mass = 1.0;      // (below 0 it stays there, and counts as 0)
-    earlier([&](int j, bool mine, int i) {
-      if (i == 0) {
-        b0 = *(const u4*)&q[j];
-        b1 = *(const u4*)&q[j + 4];
-      }
-      mass -= (double)(mine ? __uint_as_float(i < 4 ? b0[i & 3] : b1[i & 3]) : 0.0f);
-    });
-    mass = mass > 0.0 ? mass : 0.0;
-    if (up >= 0 && (double)u[t] * mass < (double)q[t]) atomicMin(&child[up], t);
+    double taken = 0.0;
+    earlier([&](int j) { taken += (double)q[j]; });
+    for (int d = 1; d < 1 << spread; d <<= 1) taken += __shfl_xor(taken, d);
+    const double mass = taken < 1.0 ? 1.0 - taken : 0.0;
+    if (mother >= 0 && slice == 0 && (double)u[node] * mass < (double)q[node]) atomicMin(&child[mother], node);
   }
   __syncthreads();
 

@@ -139,6 +139,7 @@ rq_status rq_tree_verify(const rq_tree_draft* d, void* ws, uint64_t ws_bytes, rq
   uint8_t* w = static_cast<uint8_t*>(ws);
   a.slots = reinterpret_cast<uint64_t*>(w);
   a.done = reinterpret_cast<uint32_t*>(w + p.slots);
+  while (a.spread < 6 && (2 << a.spread) * d->n_nodes <= RQ_MAX_NODES) ++a.spread;
   return launched(rq::launch_tree_verify(a, reinterpret_cast<hipStream_t>(stream)), "verification launch");
 }
 
