@@ -37,6 +37,17 @@ __global__ void __launch_bounds__(kMaskThreads) tree_mask_kernel(TreeMaskLaunch 
   const int first = blockIdx.x * kMaskThreads, end = min(first + kMaskThreads, m);
   if (first >= m) return;
   for (int i = threadIdx.x; i < end; i += kMaskThreads) parent[i] = parent_of(a.parents, b, a.n, i);
+  // most words of a row of many are zero: the workgroup's rows first, then its chains
+  RQ_GLOBAL uint32_t* rows = gptr(a.mask) + ((size_t)b * a.n + first) * a.words;
+  if (a.words > 2) {
+    const int all = (end - first) * a.words;
+    for (int i = 4 * threadIdx.x; i < all; i += 4 * kMaskThreads) {
+      if (i + 4 <= all)
+        *(RQ_GLOBAL u4_any*)(rows + i) = (u4){0u, 0u, 0u, 0u};
+      else
+        for (int k = i; k < all; ++k) rows[k] = 0u;
+    }
+  }
   __syncthreads();
   for (int i = threadIdx.x; i < end; i += kMaskThreads) {
     uint32_t w = 0;
@@ -51,16 +62,13 @@ __global__ void __launch_bounds__(kMaskThreads) tree_mask_kernel(TreeMaskLaunch 
   __syncthreads();
   const int i = first + threadIdx.x;
   if (i >= end) return;
-  RQ_GLOBAL uint32_t* row = gptr(a.mask) + ((size_t)b * a.n + i) * a.words;
-  int j = i, count = 0;
-  for (int w = a.words - 1; w >= 0; --w) {
-    uint32_t x = 0;
-    if (j >= w * 32) {         // (never further than this word)
-      x = bits[j];
-      j = leave[j];
-      count += __popc(x);
-    }
-    row[w] = x;
+  RQ_GLOBAL uint32_t* row = rows + threadIdx.x * a.words;
+  int count = 0;
+  if (a.words <= 2)
+    for (int w = 0; w < a.words; ++w) row[w] = 0u;
+  for (int j = i; j >= 0; j = leave[j]) {
+    row[j >> 5] = bits[j];
+    count += __popc(bits[j]);
   }
   if (a.depth) gptr(a.depth)[(size_t)b * a.n + i] = count - 1;
 }
