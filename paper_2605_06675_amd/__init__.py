@@ -725,22 +725,40 @@ def rq_block_attention(cache, layer, past, q, out, ws, new_len=None,
 
 
 # ------------------------------------------------------ trees of drafted tokens
-def _tree_array(t, what, device, *shape, dtype=None):
-    """Pointer of a contiguous tensor (int32 by default)."""
-    import torch
-    dtype = torch.int32 if dtype is None else dtype
-    if t.dtype is not dtype or t.device != device or t.shape != shape \
+class _Torch:
+    """What the calls below need of torch, looked up once (an import statement in
+    each call takes as long as three of its checks)."""
+
+    def __init__(self):
+        import torch
+        self.calls = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+        self.int32, self.float32 = torch.int32, torch.float32
+        self.types = {torch.float32: RQ_F32, torch.float16: RQ_F16,
+                      torch.bfloat16: RQ_BF16}
+
+
+_torch = None
+
+
+def _the_torch():
+    global _torch
+    if _torch is None:
+        _torch = _Torch()
+    return _torch
+
+
+def _tree_array(t, what, device, shape, dtype):
+    """Pointer of a contiguous tensor."""
+    if t.dtype is not dtype or t.shape != shape or t.device != device \
             or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous {dtype} {list(shape)} on {device}")
     return t.data_ptr()
 
 
 def _tree_call(device, stream, f, *args):
-    import torch
     if device.type != "cuda":
         raise ValueError(f"the tensors are on {device}, not on a GPU")
-    calls = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
-    _device_call(device, calls, stream, f, *args)
+    _device_call(device, _the_torch().calls, stream, f, *args)
 
 
 def rq_tree_mask(parents, mask, depth=None, new_len=None, stream=None):
@@ -750,13 +768,13 @@ def rq_tree_mask(parents, mask, depth=None, new_len=None, stream=None):
     [batch]."""
     if parents.dim() != 2:
         raise ValueError(f"parents has shape {tuple(parents.shape)}, expected two axes")
-    B, n = parents.shape
-    at = parents.device
+    shape = B, n = parents.shape
+    at, i32 = parents.device, _the_torch().int32
     _tree_call(at, stream, lib().rq_tree_mask, B, n,
-               _tree_array(parents, "parents", at, B, n),
-               0 if new_len is None else _tree_array(new_len, "new_len", at, B),
-               _tree_array(mask, "mask", at, B, n, (n + 31) // 32),
-               0 if depth is None else _tree_array(depth, "depth", at, B, n))
+               _tree_array(parents, "parents", at, shape, i32),
+               0 if new_len is None else _tree_array(new_len, "new_len", at, (B,), i32),
+               _tree_array(mask, "mask", at, (B, n, (n + 31) // 32), i32),
+               0 if depth is None else _tree_array(depth, "depth", at, shape, i32))
 
 
 def rq_block_tree_attention_workspace(cache, n_nodes, max_tokens=None, window=0):
@@ -784,7 +802,7 @@ def rq_block_tree_attention(cache, layer, past, q, k, v, mask, out, ws,
     if past is None:
         raise ValueError("past is missing")
     _block_slopes(cache, slopes)
-    B, at = cache.batch, cache._device
+    B, at, i32 = cache.batch, cache._device, cache._lengths
     rq_ = _block_rows(cache, q, "q", cache.n_q_heads, n, cache._type)
     rk = _block_rows(cache, k, "k", cache.n_kv_heads, n, cache._type)
     rv = _block_rows(cache, v, "v", cache.n_kv_heads, n, cache._type)
@@ -793,8 +811,8 @@ def rq_block_tree_attention(cache, layer, past, q, k, v, mask, out, ws,
         n, cache.capacity if max_tokens is None else max_tokens,
         _block_lengths(cache, past, "past"),
         _block_lengths(cache, new_len, "new_len"),
-        _tree_array(mask, "mask", at, B, n, (n + 31) // 32),
-        0 if depth is None else _tree_array(depth, "depth", at, B, n),
+        _tree_array(mask, "mask", at, (B, n, (n + 31) // 32), i32),
+        0 if depth is None else _tree_array(depth, "depth", at, (B, n), i32),
         *rq_, *rk, *rv, *ro, cache._out_types[out.dtype],
         cache.head_dim ** -0.5 if scale is None else scale, cap, window,
         0 if slopes is None else slopes.data_ptr())
@@ -831,25 +849,27 @@ def rq_tree_verify(tokens, parents, target, draft, uniforms, path, count, next,
     next: int32 [batch], the token drawn behind them.  ws: device byte tensor of at
     least rq_tree_verify_workspace bytes, zeroed before its first call (every call
     leaves it zero)."""
-    import torch
     if target.dim() != 3 or path.dim() != 2:
         raise ValueError("target must have three axes and path two")
-    types = {torch.float32: RQ_F32, torch.float16: RQ_F16, torch.bfloat16: RQ_BF16}
-    if target.dtype not in types:
-        raise ValueError(f"target has dtype {target.dtype}")
-    (B, n, V), at = target.shape, target.device
+    t, dtype = _the_torch(), target.dtype
+    if dtype not in t.types:
+        raise ValueError(f"target has dtype {dtype}")
+    shape, at, i32 = target.shape, target.device, t.int32
+    B, n, V = shape
+    nodes = B, n
     if ws.device != at or not ws.is_contiguous():
         raise ValueError(f"ws must be a contiguous tensor on {at}")
     d = _DRAFT.pack(
-        B, n, V, types[target.dtype], _tree_array(tokens, "tokens", at, B, n),
-        _tree_array(parents, "parents", at, B, n),
-        0 if new_len is None else _tree_array(new_len, "new_len", at, B),
-        *_tree_rows(target, "target", (B, n, V), target.dtype, at),
+        B, n, V, t.types[dtype], _tree_array(tokens, "tokens", at, nodes, i32),
+        _tree_array(parents, "parents", at, nodes, i32),
+        0 if new_len is None else _tree_array(new_len, "new_len", at, (B,), i32),
+        *_tree_rows(target, "target", shape, dtype, at),
         *((0, 0, 0) if draft is None
-          else _tree_rows(draft, "draft", (B, n, V), target.dtype, at)),
-        _tree_array(uniforms, "uniforms", at, B, n, dtype=torch.float32),
-        path.shape[1], _tree_array(path, "path", at, B, path.shape[1]),
-        _tree_array(count, "count", at, B), _tree_array(next, "next", at, B))
+          else _tree_rows(draft, "draft", shape, dtype, at)),
+        _tree_array(uniforms, "uniforms", at, nodes, t.float32),
+        path.shape[1], _tree_array(path, "path", at, (B, path.shape[1]), i32),
+        _tree_array(count, "count", at, (B,), i32),
+        _tree_array(next, "next", at, (B,), i32))
     _tree_call(at, stream, lib().rq_tree_verify, d, ws.data_ptr(),
                ws.numel() * ws.element_size())
 
@@ -875,14 +895,16 @@ def rq_block_accept(cache, lengths, path, count, k, v, new_lengths, past=None,
             raise ValueError(f"the rows of {what} must be contiguous")
         packed.append(_LAYERS.pack(t.data_ptr(), *t.stride()[:4]))
 
+    i32, layers = cache._lengths, (L, B)
+
     def each(t, what):
-        return 0 if t is None else _tree_array(t, what, at, L, B)
+        return 0 if t is None else _tree_array(t, what, at, layers, i32)
     if lengths is None or new_lengths is None:
         raise ValueError("lengths and new_lengths are needed")
     _block_call(cache, stream, lib().rq_block_accept, C.byref(cache),
                 each(lengths, "lengths"), n, path.shape[1],
-                _tree_array(path, "path", at, B, path.shape[1]),
-                _tree_array(count, "count", at, B), *packed,
+                _tree_array(path, "path", at, (B, path.shape[1]), i32),
+                _tree_array(count, "count", at, (B,), i32), *packed,
                 each(new_lengths, "new_lengths"), each(past, "past"),
                 each(fitting, "fitting"), each(dropped, "dropped"))
 
