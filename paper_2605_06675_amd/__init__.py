@@ -934,7 +934,10 @@ class DraftTree:
     """Drafted tokens of one step: which of them each one sees, and, verified,
     which are accepted.  parents: device int32 [batch][n_nodes] (a node's parent
     comes before it; node 0 is the root); new_len: device int32 [batch], how many
-    of the nodes each sequence uses."""
+    of the nodes each sequence uses.
+
+    The calls of one tree share its tensors: they go to one stream, or follow each
+    other by the caller's events.  All can be captured into a graph."""
 
     def __init__(self, parents, new_len=None, stream=None):
         import torch
@@ -964,16 +967,24 @@ class DraftTree:
         s = torch.cuda.current_stream(target.device) if stream is None else stream
         need = rq_tree_verify_workspace(B, n, target.shape[-1])
         with torch.cuda.stream(s):
-            if self._ws is None or self._ws.numel() < need:
-                self._ws = torch.zeros(need, dtype=torch.uint8, device=target.device)
+            capturing = torch.cuda.is_current_stream_capturing()
+            ws = self._ws
+            if ws is None or ws.numel() < need:
+                if ws is not None:
+                    ws.record_stream(s)
+                ws = torch.zeros(need, dtype=torch.uint8, device=target.device)
+                if not capturing:       # (else its zeros are the graph's work)
+                    self._ws = ws
             if self._results is None or self._results[0].shape[1] != room:
+                for t in self._results or ():
+                    t.record_stream(s)
                 self._results = tuple(
                     torch.empty(shape, dtype=torch.int32, device=target.device)
                     for shape in ((B, room), (B,), (B,)))
-            if torch.cuda.is_current_stream_capturing():
-                self._held.append((self._ws, self._results))
+            if capturing:
+                self._held.append((ws, self._results))
         rq_tree_verify(tokens, self.parents, target, draft, uniforms,
-                       *self._results, self._ws, self.new_len, stream)
+                       *self._results, ws, self.new_len, stream)
         return self._results
 
 

@@ -678,3 +678,86 @@ def test_verify_gives_the_same_again():
     for _ in range(20):
         for m, want in zip(made, first):
             assert all(torch.equal(x, y) for x, y in zip(m[0].verify(*m[1:]), want))
+
+
+def test_captured_verifications_of_one_tree():
+    """Two graphs captured before the tree has verified anything, replayed in either
+    order with eager calls of more memory and less room between."""
+    g = torch.Generator().manual_seed(8)
+    n, B = 6, 3
+    parents = [some_parents(n, b) for b in range(B)]
+    layout = rq.DraftTree(ints(parents))
+    calls = []
+    for V, room in ((20000, 6), (40000, 4), (90000, 6)):
+        x = [torch.zeros(B, n, dtype=torch.int32, device="cuda"), torch.zeros(B, n, V, device="cuda"),
+             torch.zeros(B, n, device="cuda"), torch.zeros(B, n, V, device="cuda")]
+        calls.append((V, room, x))
+    torch.cuda.synchronize()
+    graphs = [graph_of(lambda: layout.verify(*x, room=room)) for V, room, x in calls[:2]]
+    for turn, which in enumerate([2, 1, 0, 1, 2, 0, 0, 1, 2, 2, 1]):
+        V, room, x = calls[which]
+        w = torch.randint(V, (B, n), generator=g).int()
+        t = probabilities(g, (B, n, V), torch.float32, 0.5)
+        d = 0.5 * t                                     # the rest of it on the drafted tokens
+        d.scatter_add_(2, w.long()[:, None].expand(B, n, n), torch.full((B, n, n), 0.5 / n))
+        u = torch.rand(B, n, generator=g) * (0.001 if turn % 2 else 1.0)
+        for dst, src in zip(x, (w, t, u, d)):
+            dst.copy_(src)
+        torch.cuda.synchronize()
+        if which < 2:
+            graphs[which][0].replay()
+            got = graphs[which][1]
+        else:
+            got = layout.verify(*x, room=room)
+        torch.cuda.synchronize()
+        path, count, last = (y.tolist() for y in got)
+        for b in range(B):
+            want, token = tree.verify(parents[b], w[b].tolist(), t[b].double().numpy(), d[b].double().numpy(),
+                                      u[b].double().numpy(), room)
+            assert path[b] == want + [-1] * (room - len(want)) and count[b] == len(want), (turn, b)
+            assert last[b] == token, (turn, b)
+
+
+@pytest.mark.parametrize("window", [0, 100])
+@pytest.mark.parametrize("n", [3, 40])
+def test_attend_at_the_end_of_the_longest_cache(n, window):
+    """Offsets beyond 2^31 bytes: 2^24 slots, zeros but for the last 200 (scores of 0 and
+    values of 0: without a window each adds 1 to a row's sum)."""
+    cap, D, G, some = 1 << 24, 128, 4, 200
+    L = cap - 3
+    c = rq.BlockCache(rq.RQ_INT8, rq.RQ_BF16, 1, 1, 1, G, D, cap)
+    g = torch.Generator().manual_seed(n)
+    at = (L - some) // 32 * 32
+    codes = torch.randint(-127, 128, (2, cap - at, D), generator=g, dtype=torch.int8)
+    scales = 0.01 + 0.02 * torch.rand(2, (cap - at) // 32, generator=g)
+    tail = torch.randn(2, 32, D, generator=g).bfloat16()
+    c.codes.view(torch.int8).view(2, cap, D)[:, at:].copy_(codes)
+    c.scales.view(2, cap // 32)[:, at // 32:].copy_(scales)
+    c.tail.view(2, 32, D).copy_(tail)
+    c.positions.copy_(torch.arange(cap, dtype=torch.int32, device="cuda"))
+    c.lengths.fill_(L)
+    c.bound = [L]
+    K, V = (torch.cat([(codes[i].double() * scales[i].double().repeat_interleave(32)[:, None])[:L // 32 * 32 - at],
+                       tail[i, :L % 32].double()]) for i in range(2))
+    parents = some_parents(n, 1)
+    seen = torch.from_numpy(tree.sees(parents))
+    depth = torch.tensor([len(x) - 1 for x in tree.ancestors(parents)])
+    q, k, v = (torch.randn(1, h, n, D, generator=g).bfloat16() for h in (G, 1, 1))
+    o = torch.full((1, G, n, D), 7.5, device="cuda")
+    c.tree_attention(0, q.cuda(), k.cuda(), v.cuda(), rq.DraftTree(ints([parents])), o, window=window)
+    K, V = torch.cat([K, k[0, 0].double()]), torch.cat([V, v[0, 0].double()])
+    x = q[0].double() @ K.T * D ** -0.5
+    away = depth[:, None] + torch.cat([torch.arange(L - at, 0, -1)[None].expand(n, -1), -depth[None].expand(n, -1)], 1)
+    sees = torch.cat([torch.ones(n, L - at, dtype=torch.bool), seen], 1)
+    if window:
+        sees &= away < window
+    p = torch.where(sees, x, torch.tensor(-math.inf)).exp()
+    want = p @ V / (p.sum(-1, keepdim=True) + (0 if window else at))
+    # as in compare_tree; at least 256 waves share the sum of 2^24 numbers
+    aq, f = q[0].double().abs(), D ** -0.5 * 1.4427
+    a = f * (aq @ K.abs().T).max(-1).values
+    a2 = f * torch.maximum(aq.amax(-1) * K.abs().sum(-1).max(), aq.sum(-1) * K.abs().max())
+    s = D * 2.0 ** -24 * a + 2 * D * 2.0 ** -25 * a2 + 4 * 2.0 ** -24 * (a + 64)
+    ratio = 2 * s * math.log(2) + 2.0 ** -21 + (cap / 32 / 256 + 64) * 2.0 ** -24
+    err = (o.cpu()[0].double() - want).abs() / ((ratio[..., None] + 2.0 ** -21) * V.abs().max())
+    assert float(err.max()) <= 1
