@@ -23,10 +23,9 @@ __device__ __forceinline__ int parent_of(const int32_t* parents, int b, int n, i
 // sees(i) = {i} + sees(parent of i).
 //
 // In two levels of 32 nodes, a word each: a node first follows its parents inside
-// its own word (at most 31 steps), which gives that word's bits and the ancestor
-// where the chain leaves it; a row then goes from word to word by those (at most
-// 31 steps more).  Bound by latency: some 60 dependent LDS reads at worst, where
-// a chain of 1024 nodes followed parent by parent takes 1023.
+// its own word, twice as far a step (5 at most), which gives that word's bits and the
+// ancestor where the chain leaves it; a row then goes from word to word by those (at
+// most 31 steps more).  Bound by latency.
 constexpr int kMaskThreads = 256;
 
 __global__ void __launch_bounds__(kMaskThreads) tree_mask_kernel(TreeMaskLaunch a) {
@@ -49,15 +48,23 @@ __global__ void __launch_bounds__(kMaskThreads) tree_mask_kernel(TreeMaskLaunch 
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < end; i += kMaskThreads) {
-    uint32_t w = 0;
-    int j = i;
-    do {
-      w |= 1u << (j & 31);
-      j = parent[j];
-    } while (j >= (i & ~31));
-    bits[i] = w;
-    leave[i] = j;
+  for (int i0 = 0; i0 < end; i0 += kMaskThreads) {       // (a word's nodes are lanes of one wave)
+    const int i = i0 + threadIdx.x, lane = threadIdx.x & 63;
+    uint32_t w = 1u << (i & 31);
+    int j = i < end ? parent[i] : -1;
+    while (__any(j >= (i & ~31))) {
+      const bool inside = j >= (i & ~31);
+      const uint32_t more = __shfl(w, inside ? j & 63 : lane);
+      const int next = __shfl(j, inside ? j & 63 : lane);
+      if (inside) {
+        w |= more;
+        j = next;
+      }
+    }
+    if (i < end) {
+      bits[i] = w;
+      leave[i] = j;
+    }
   }
   __syncthreads();
   const int i = first + threadIdx.x;
