@@ -98,7 +98,11 @@ __global__ void __launch_bounds__(kMaskThreads) tree_mask_kernel(TreeMaskLaunch 
 //
 // All sums are fp64 in one order: the results are decisions, which fp32 sums would make
 // otherwise next to a border.  Bound by latency: launch, nodes, entries, a row's part,
-// the parts' exchange.
+// the parts' exchange.  So what LDS is read for one by one counts: which first children
+// are accepted is decided by their threads, a walk then reads one word a node; a lane
+// has a part's sum, and scans find the whole and the part of the last token.  us so / one
+// by one: 32 chains of 6 nodes 8.7 / 11.1, four trees of 31 over 100003 tokens 10.9 /
+// 15.8, 16 of 64 without a draft's rows over 131072 9.9 / 14.0.
 constexpr int kThreads = 1024, kEach = kVerifyStep / kThreads;
 constexpr int kNone = 1 << 30;
 constexpr int kPolls = 4096;      // some milliseconds
@@ -161,21 +165,27 @@ struct Residual {
     rejected = n_gone = 0;
   }
 
-  __device__ __forceinline__ void load(int v, int vocab, double r[kEach]) const {
-    float p[kEach], q[kEach];
+  // Rejections j and on.
+  __device__ __forceinline__ void reject(int j, const float q[kEach], double r[kEach]) const {
+    for (; j < rejected; ++j) {
+      const double by = inverse[j];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const double x = r[i] * by - (double)q[i];
+        r[i] = x > 0.0 ? x : 0.0;
+      }
+    }
+  }
+
+  // Entries v..v + 7, and the draft's where it has a part in them.
+  __device__ __forceinline__ void load(int v, int vocab, float q[kEach], double r[kEach]) const {
+    float p[kEach];
     load_probs<DTYPE>(target, v, vocab, p);
     if (DRAFT && rejected) load_probs<DTYPE>(draft, v, vocab, q);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) r[i] = p[i];
     if constexpr (DRAFT) {
-      for (int j = 0; j < rejected; ++j) {
-        const double by = inverse[j];
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-          const double x = r[i] * by - (double)q[i];
-          r[i] = x > 0.0 ? x : 0.0;
-        }
-      }
+      reject(0, q, r);
     } else {
       for (int j = 0; j < n_gone; ++j) {
         const int at = gone[j] - v;
@@ -212,12 +222,13 @@ __global__ void __launch_bounds__(kThreads) tree_verify_kernel(TreeVerifyLaunch 
   __shared__ __align__(16) int parent[RQ_MAX_NODES], token[RQ_MAX_NODES];
   __shared__ __align__(16) float p[RQ_MAX_NODES], q[RQ_MAX_NODES];   // of a node's token, in its parent's rows
   __shared__ float u[RQ_MAX_NODES];
-  __shared__ int child[RQ_MAX_NODES];     // the first child (without a draft: the first accepted one)
+  __shared__ int child[RQ_MAX_NODES];     // the first child, ~ of it where it is rejected (without a draft: the first accepted one)
   __shared__ int sibling[RQ_MAX_NODES];   // the next one
   __shared__ double inverse[RQ_MAX_NODES];
-  __shared__ double waves[kThreads / 64], sums[kVerifyParts];
-  __shared__ int here[kVerifyParts];
+  __shared__ double waves[2][kThreads / 64], sums[64];
+  __shared__ uint64_t there;
   __shared__ int n_gone, at_first, at_last;
+  static_assert(kVerifyParts <= 64, "a lane a part");
   const int b = blockIdx.y, part = blockIdx.x, t = threadIdx.x;
   int up = -1;
   if (t < a.n) {                          // (at most as many nodes as threads)
@@ -228,8 +239,12 @@ __global__ void __launch_bounds__(kThreads) tree_verify_kernel(TreeVerifyLaunch 
     parent[t] = up;
     token[t] = x;
     u[t] = gptr(a.uniforms)[at];
-    child[t] = kNone;
-    sibling[t] = -1;
+    child[t] = sibling[t] = kNone;
+  }
+  if (t == 0) {
+    n_gone = 0;
+    at_first = kNone;
+    at_last = -1;
   }
   const int m = node_count(a.new_len, b, a.n);
   RQ_GLOBAL int32_t* path = gptr(a.path) + (size_t)b * a.n_path;
@@ -254,141 +269,165 @@ __global__ void __launch_bounds__(kThreads) tree_verify_kernel(TreeVerifyLaunch 
   // before it is one's, eight at a time (LDS reads are slow one by one).
   const int spread = a.spread, node = t >> spread, slice = t & ((1 << spread) - 1);
   const int mother = node < m ? parent[node] : -1;
-  auto earlier = [&](auto f) {
+  auto earlier = [&](const auto* values, auto f) {
     if (mother >= 0)
       for (int j0 = slice; j0 < node; j0 += 8 << spread) {
-        int j[8], of[8];
+        int of[8];
+        auto x = *values;
+        decltype(x) value[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          j[i] = j0 + (i << spread);
-          of[i] = parent[j[i] < node ? j[i] : 0];       // (the root has none)
+          const int j = j0 + (i << spread);
+          of[i] = parent[j < node ? j : 0];             // (the root has none)
+          value[i] = values[j < node ? j : 0];
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (of[i] == mother) f(j[i]);
+        for (int i = 0; i < 8; ++i) f(of[i] == mother, j0 + (i << spread), value[i]);
       }
   };
   if constexpr (DRAFT) {
-    earlier([&](int j) { atomicMax(&sibling[node], j); });         // (the one before, at first)
-    __syncthreads();
-    const int before = t < m ? sibling[t] : -1;
-    __syncthreads();
-    if (t < m) sibling[t] = kNone;
-    __syncthreads();
-    if (up >= 0) {
+    int before = -1;
+    earlier(parent, [&](bool is, int j, int) { before = is ? j : before; });
+    for (int d = 1; d < 1 << spread; d <<= 1) before = max(before, __shfl_xor(before, d));
+    if (mother >= 0 && slice == 0) {
       if (before < 0)
-        child[up] = t;
+        child[mother] = (double)u[node] * (double)q[node] < (double)p[node] ? node : ~node;
       else
-        sibling[before] = t;
+        sibling[before] = node;
     }
   } else {
     // a token that an earlier sibling has is gone by its turn
     bool twice = false;
     const int x = node < m ? token[node] : 0;
-    earlier([&](int j) { twice |= token[j] == x; });
+    earlier(token, [&](bool is, int, int y) { twice |= is && y == x; });
     const uint64_t group = (2ull << ((1 << spread) - 1)) - 1;      // 2^spread lanes
     twice = (__ballot(twice) >> (t & 63 & ~((1 << spread) - 1))) & group;
     if (mother >= 0 && slice == 0) q[node] = twice ? 0.0f : p[node];
     __syncthreads();
     double taken = 0.0;
-    earlier([&](int j) { taken += (double)q[j]; });
+    earlier(q, [&](bool is, int, float y) { taken += is ? (double)y : 0.0; });
     for (int d = 1; d < 1 << spread; d <<= 1) taken += __shfl_xor(taken, d);
     const double mass = taken < 1.0 ? 1.0 - taken : 0.0;
     if (mother >= 0 && slice == 0 && (double)u[node] * mass < (double)q[node]) atomicMin(&child[mother], node);
   }
   __syncthreads();
 
+  // A part of one step stays in registers, for the node's next rejection and the last
+  // token: after `applied` rejections, or -1.
+  const int lo = part * a.part, hi = min(lo + a.part, a.vocab);
+  const bool held = a.part <= kVerifyStep;
+  double r[kEach];
+  float q_held[kEach];
+  int applied = -1, turn = 0;
+
   // the workgroup's sum of a part, in every thread
   auto part_sum = [&](const Residual<DTYPE, DRAFT>& res, int i) {
-    const int lo = i * a.part, hi = min(lo + a.part, a.vocab);
     double sum = 0.0;
-    for (int v = lo + t * kEach; v < hi; v += kVerifyStep) {
-      double r[kEach];
-      res.load(v, a.vocab, r);
+    if (held && i == part) {
+      if (applied >= 0) {
+        res.reject(applied, q_held, r);
+      } else if (lo + t * kEach < hi) {
+        res.load(lo + t * kEach, a.vocab, q_held, r);
+      } else {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) r[k] = q_held[k] = 0.0f;
+      }
+      applied = res.rejected;
 #pragma unroll
       for (int k = 0; k < kEach; ++k) sum += r[k];
+    } else {
+      const int end = min(i * a.part + a.part, a.vocab);
+      for (int v = i * a.part + t * kEach; v < end; v += kVerifyStep) {
+        double x[kEach];
+        float y[kEach];
+        res.load(v, a.vocab, y, x);
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) sum += x[k];
+      }
     }
     sum = wave_scan(sum);
-    __syncthreads();
-    if ((t & 63) == 63) waves[t >> 6] = sum;
+    double* each = waves[turn];           // (by turns: those of the last sum may be read still)
+    turn ^= 1;
+    if ((t & 63) == 63) each[t >> 6] = sum;
     __syncthreads();
     sum = 0.0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) sum += waves[w];
-    return sum;
+    for (int w = 0; w < kThreads / 64; ++w) sum += each[w];
+    return sum > 0.0 ? sum : 0.0;         // (no NaN)
   };
-  // All parts' sums, in `sums`, and the whole.  (A sum is not negative: with its sign
-  // set it is no zero, which stands for one that is not there.)
+  // All parts' sums, in `sums`, those up to a lane's part, in `upto`, and the whole.  (A
+  // sum is not negative: with its sign set it is no zero, which stands for one that is
+  // not there.)
   int asked = 0;
+  double upto = 0.0;
   RQ_GLOBAL uint64_t* slots = gptr(a.slots) + (size_t)b * kVerifySums * a.parts;
   auto all_sums = [&](const Residual<DTYPE, DRAFT>& res) {
-    double mine = part_sum(res, part);
-    mine = mine > 0.0 ? mine : 0.0;       // (no NaN either)
+    const double mine = part_sum(res, part);
     const bool shared = asked < kVerifySums;
     RQ_GLOBAL uint64_t* slot = slots + (size_t)asked * a.parts;
     ++asked;
     if (shared && t == 0 && a.parts > 1)
       __hip_atomic_store(slot + part, __builtin_bit_cast(uint64_t, mine) | 1ull << 63, __ATOMIC_RELAXED,
                          __HIP_MEMORY_SCOPE_AGENT);
-    if (t < a.parts) {
-      uint64_t x = 0;
-      if (shared && t != part)
+    if (t < 64) {
+      uint64_t x = t < a.parts && t != part ? 0 : 1ull << 63;
+      if (shared && x == 0)
         for (int i = 0; i < kPolls && x == 0; ++i)
           x = __hip_atomic_load(slot + t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       sums[t] = t == part ? mine : __builtin_bit_cast(double, x & ~(1ull << 63));
-      here[t] = t == part || x != 0;
+      const uint64_t all = __ballot(x != 0);
+      if (t == 0) there = all;
     }
     __syncthreads();
-    double whole = 0.0;
-    for (int i = 0; i < a.parts; ++i) {
-      if (!here[i]) {                     // (the same in every thread)
-        double sum = part_sum(res, i);
-        sum = sum > 0.0 ? sum : 0.0;
-        if (t == 0) sums[i] = sum;
-        whole += sum;
-      } else {
-        whole += sums[i];
-      }
+    const uint64_t missing = ~there;      // (the same in every thread)
+    if (missing) {
+      for (int i = 0; i < a.parts; ++i)
+        if ((missing >> i) & 1) {
+          const double sum = part_sum(res, i);
+          if (t == 0) sums[i] = sum;
+        }
+      __syncthreads();
     }
-    __syncthreads();
-    return whole;
+    upto = wave_scan(sums[t & 63]);
+    return __shfl(upto, 63);
   };
 
   // the walk, alike in every thread
-  int cur = 0, count = 1, rejected = 0, full = 0;
+  int cur = 0, count = 1, rejected = 0;
+  bool full = false;
   if (part == 0 && t == 0) path[0] = 0;
   for (;;) {
-    if (count == a.n_path) {
-      full = 1;
-      break;
-    }
+    full = count == a.n_path;
+    if (full) break;
     int c = child[cur];
-    if constexpr (DRAFT) {
+    if (DRAFT && c < 0) {
+      Residual<DTYPE, DRAFT> res(a, b, cur);
+      res.inverse = inverse;
       double mass = 1.0;
-      rejected = 0;
-      while (c != kNone) {
-        double r = p[c];
-        for (int j = 0; j < rejected; ++j) {
-          r = r * inverse[j] - (double)q[c];
-          r = r > 0.0 ? r : 0.0;
-        }
-        if ((double)u[c] * (double)q[c] * mass < r) break;
+      c = ~c;
+      for (;;) {                          // c is rejected
         if (t == 0) inverse[rejected] = rejected == 0 ? 1.0 : (mass > 0.0 ? 1.0 / mass : 0.0);
-        ++rejected;
+        res.rejected = ++rejected;
         c = sibling[c];
-        __syncthreads();
-        if (c == kNone || mass == 0.0) {      // (no mass: none of the others is accepted)
+        if (c == kNone) break;
+        if (mass == 0.0) {                // (none of the others is accepted)
           c = kNone;
           break;
         }
-        Residual<DTYPE, DRAFT> res(a, b, cur);
-        res.rejected = rejected;
-        res.inverse = inverse;
+        const double by = (double)u[c] * (double)q[c];
+        double left = p[c];
+        __syncthreads();
         mass = all_sums(res);
+        for (int j = 0; j < rejected; ++j) {
+          left = left * inverse[j] - (double)q[c];
+          left = left > 0.0 ? left : 0.0;
+        }
+        if (by * mass < left) break;
       }
     }
     if (c == kNone) break;
     rejected = 0;
+    applied = -1;
     cur = c;
     if (part == 0 && t == 0) path[count] = c;
     ++count;
@@ -399,75 +438,67 @@ __global__ void __launch_bounds__(kThreads) tree_verify_kernel(TreeVerifyLaunch 
   }
 
   // the last token: the first whose running sum exceeds u times the whole
-  if (t == 0) {
-    n_gone = 0;
-    at_first = kNone;
-    at_last = -1;
-  }
-  __syncthreads();
   Residual<DTYPE, DRAFT> res(a, b, cur);
   res.rejected = rejected;
   res.inverse = inverse;
-  if (!DRAFT && !full) {
-    if (t < m && up == cur) sibling[atomicAdd(&n_gone, 1)] = token[t];     // (the children's tokens)
-    __syncthreads();
+  if (!DRAFT && !full && t < m && up == cur) sibling[atomicAdd(&n_gone, 1)] = token[t];     // (the children's tokens)
+  __syncthreads();
+  if (!DRAFT) {
     res.n_gone = n_gone;
     res.gone = sibling;
   }
   double whole = all_sums(res);
   if (!(whole > 0.0)) {                   // no mass left: the target's row
     res.rejected = res.n_gone = 0;
+    applied = -1;
     whole = all_sums(res);
   }
+  // the last of the sequence's workgroups to come here clears the slots, at its end
+  uint32_t ticket = 0;
   if (a.parts > 1 && t == 0) {
-    // the last of the sequence's workgroups to come here clears the slots
     __builtin_amdgcn_s_waitcnt(0);        // this one's sums are out
-    RQ_GLOBAL uint32_t* done = gptr(a.done) + b;
-    if (__hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.parts - 1) {
+    ticket = __hip_atomic_fetch_add(gptr(a.done) + b, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  auto finish = [&] {
+    if (a.parts > 1 && t < 64 && __builtin_amdgcn_readfirstlane(ticket) == (uint32_t)a.parts - 1) {
       const int used = (asked < kVerifySums ? asked : kVerifySums) * a.parts;
-      for (int i = 0; i < used; ++i) __hip_atomic_store(slots + i, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      for (int i = t; i < used; i += 64) __hip_atomic_store(slots + i, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (t == 0) __hip_atomic_store(gptr(a.done) + b, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-  }
+  };
   const double bar = (double)u[0] * whole;
-  int holds = -1, last = 0;
-  double before = 0.0, run = 0.0;
-  for (int i = 0; i < a.parts; ++i) {
-    if (sums[i] > 0.0) last = i;
-    if (holds < 0 && run + sums[i] > bar) {
-      holds = i;
-      before = run;
-    }
-    run += sums[i];
-  }
-  const bool beyond = holds < 0;          // (none exceeds: the last of r > 0)
-  if (beyond) holds = last;
-  if (part != holds) return;
-  if (!(whole > 0.0)) {
-    if (t == 0) gptr(a.next)[b] = 0;
+  const uint64_t parts = ~0ull >> (64 - a.parts);
+  const uint64_t exceed = __ballot(upto > bar) & parts, some = __ballot(sums[t & 63] > 0.0) & parts;
+  const bool beyond = exceed == 0;        // (none exceeds: the last of r > 0)
+  const int holds = beyond ? (some ? 63 - __builtin_clzll(some) : 0) : __builtin_ctzll(exceed);
+  if (part != holds) {
+    finish();
     return;
   }
-  const int lo = part * a.part, hi = min(lo + a.part, a.vocab);
+  double before = holds > 0 ? __shfl(upto, holds - 1) : 0.0;
   for (int v0 = lo; v0 < hi; v0 += kVerifyStep) {
     const int v = v0 + t * kEach;
-    double r[kEach], mine = 0.0;
-    if (v < hi) {
-      res.load(v, a.vocab, r);
-    } else {
+    double mine = 0.0;
+    if (!held) {
+      if (v < hi) {
+        res.load(v, a.vocab, q_held, r);
+      } else {
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) r[i] = 0.0;
+        for (int i = 0; i < kEach; ++i) r[i] = 0.0;
+      }
     }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) mine += r[i];
-    const double upto = wave_scan(mine);
+    const double scan = wave_scan(mine);
+    double* each = waves[turn];
+    turn ^= 1;
+    if ((t & 63) == 63) each[t >> 6] = scan;
     __syncthreads();
-    if ((t & 63) == 63) waves[t >> 6] = upto;
-    __syncthreads();
-    double x = before + (upto - mine), all = 0.0;     // the sum before this thread's entries
+    double x = before + (scan - mine), all = 0.0;     // the sum before this thread's entries
 #pragma unroll
     for (int w = 0; w < kThreads / 64; ++w) {
-      x += w < (t >> 6) ? waves[w] : 0.0;
-      all += waves[w];
+      x += w < (t >> 6) ? each[w] : 0.0;
+      all += each[w];
     }
     int first = kNone, end = -1;
 #pragma unroll
@@ -478,13 +509,16 @@ __global__ void __launch_bounds__(kThreads) tree_verify_kernel(TreeVerifyLaunch 
         if (first == kNone && !beyond && x > bar) first = v + i;
       }
     }
-    if (first != kNone) atomicMin(&at_first, first);
-    if (end >= 0) atomicMax(&at_last, end);
+    // (a wave's first and last, where it has any)
+    const uint64_t firsts = __ballot(first != kNone), ends = __ballot(end >= 0);
+    if (firsts && (t & 63) == __builtin_ctzll(firsts)) atomicMin(&at_first, first);
+    if (ends && (t & 63) == 63 - __builtin_clzll(ends)) atomicMax(&at_last, end);
     __syncthreads();
     if (at_first != kNone) break;
     before += all;
   }
   if (t == 0) gptr(a.next)[b] = at_first != kNone ? at_first : (at_last >= 0 ? at_last : 0);
+  finish();
 }
 
 template <int DTYPE, bool DRAFT>
