@@ -508,27 +508,33 @@ __global__ void __launch_bounds__(64 * kWaves, 2) tree_rows_kernel(BlockTreeLaun
         f(mine + 32 * n * kStride + kE * (8 * (i >> 2) + (i & 3)), x);
       }
   };
-  if (wave < kBufs)
-    each_piece([](float* p, const float* x) {
+  typedef float piece __attribute__((ext_vector_type(kE)));
+  auto in_one = [](const float* x) {
+    piece y;
 #pragma unroll
-      for (int e = 0; e < kE; e += 2) *(f2*)(p + e) = (f2){x[e], x[e + 1]};
-    });
+    for (int e = 0; e < kE; ++e) y[e] = x[e];
+    return y;
+  };
+  if (wave < kBufs) each_piece([&](float* p, const float* x) { *(piece*)p = in_one(x); });
   __syncthreads();
-  if (wave >= kBufs)
-    each_piece([](float* p, const float* x) {
-#pragma unroll
-      for (int e = 0; e < kE; e += 2) *(f2*)(p + e) += (f2){x[e], x[e + 1]};
-    });
-  __syncthreads();
-  for (int i = threadIdx.x; i < kRows * (D / 4); i += kThreads) {
-    const int r = i / (D / 4), ch = 4 * (i % (D / 4)), row = row0 + r;
-    const int tok = over(row, a.by_G);
-    if (tok >= nnew) continue;
+  if (wave >= kBufs) {
+    each_piece([&](float* p, const float* x) { *(piece*)p += in_one(x); });
+  } else if (wave < RT && hl == 0) {       // (nobody else reads these until all are added)
+    const int r = 32 * wave + col;
     float m = sh_m[0][r], l = 0.0f;
 #pragma unroll
     for (int j = 1; j < kWaves; ++j) m = __builtin_fmaxf(m, sh_m[j][r]);
 #pragma unroll
     for (int j = 0; j < kWaves; ++j) l = __builtin_fmaf(sh_l[j][r], exp2_f(sh_m[j][r] - m), l);
+    sh_m[0][r] = m;
+    sh_l[0][r] = l;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < kRows * (D / 4); i += kThreads) {
+    const int r = i / (D / 4), ch = 4 * (i % (D / 4)), row = row0 + r;
+    const int tok = over(row, a.by_G);
+    if (tok >= nnew) continue;
+    const float m = sh_m[0][r], l = sh_l[0][r];
     f4 x = *(const f4*)&sh_o[0][r * kStride + ch];
 #pragma unroll
     for (int j = 1; j < kBufs; ++j) x += *(const f4*)&sh_o[j][r * kStride + ch];
