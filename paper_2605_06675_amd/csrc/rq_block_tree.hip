@@ -127,16 +127,13 @@ __global__ void __launch_bounds__(64 * kWaves, 2) tree_rows_kernel(BlockTreeLaun
     load_keys<D>(kc, ks, vs, blk, &c);
     if (far) c.pos = pos[blk * kBlockTokens + col];
   };
-  if (lo + wave < end) {
-    next_keys(lo + wave);
-    load_values<D>(vc, lo + wave, &c);
-  }
-
   // the lane's rows
   Rows<D, RT> st;
   int token[RT], qpos[RT];
   float slope[RT];
   const int base = PLAIN ? 0 : tree_base(a, unit, past);
+  u4 raw[kK];
+  bool used = false;
 #pragma unroll
   for (int n = 0; n < RT; ++n) {
     const int row = row0 + 32 * n + col;
@@ -151,37 +148,44 @@ __global__ void __launch_bounds__(64 * kWaves, 2) tree_rows_kernel(BlockTreeLaun
       if (a.slopes || a.window) qpos[n] = base + node_depth(a, b, token[n]);
     }
     if (wave == n) {
-      // fp16 queries as they are; bf16 rows over a power of two above their largest
       const RQ_GLOBAL uint16_t* p = gptr(static_cast<const uint16_t*>(a.q.p)) + b * a.q.sb +
                                     (int64_t)(h * a.G + head) * a.q.sh + token[n] * a.q.st + 16 * hl;
-      // (a negative scale turns the queries, so that scores grow with products)
-      const uint32_t turn = a.qscale < 0.0f ? 0x80008000u : 0u;
-      u4 raw[kK];
 #pragma unroll
       for (int k = 0; k < kK; ++k) raw[k] = *(const RQ_GLOBAL u4_any*)(p + 32 * (k >> 1) + 8 * (k & 1));
-      float qs = __builtin_fabsf(a.qscale);
+      used = valid;
+    }
+  }
+  // (behind the queries, which are wanted first)
+  if (lo + wave < end) {
+    next_keys(lo + wave);
+    load_values<D>(vc, lo + wave, &c);
+  }
+  if (wave < RT) {
+    // fp16 queries as they are; bf16 rows over a power of two above their largest
+    // (a negative scale turns the queries, so that scores grow with products)
+    const uint32_t turn = a.qscale < 0.0f ? 0x80008000u : 0u;
+    float qs = __builtin_fabsf(a.qscale);
+#pragma unroll
+    for (int k = 0; k < kK; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) raw[k][i] = used ? raw[k][i] ^ turn : 0u;
+    if constexpr (BF16) {
+      us2 most = {0, 0};
 #pragma unroll
       for (int k = 0; k < kK; ++k)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) raw[k][i] = valid ? raw[k][i] ^ turn : 0u;
-      if constexpr (BF16) {
-        us2 most = {0, 0};
+        for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(us2, raw[k][i] & 0x7fff7fffu));
+      const float largest = half_all<Max>(widen_t<true>(most.x > most.y ? most.x : most.y));
+      const int e = largest > 0.0f ? __builtin_amdgcn_frexp_expf(largest) : 0;
 #pragma unroll
-        for (int k = 0; k < kK; ++k)
+      for (int k = 0; k < kK; ++k)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(us2, raw[k][i] & 0x7fff7fffu));
-        const float largest = half_all<Max>(widen_t<true>(most.x > most.y ? most.x : most.y));
-        const int e = largest > 0.0f ? __builtin_amdgcn_frexp_expf(largest) : 0;
-#pragma unroll
-        for (int k = 0; k < kK; ++k)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) raw[k][i] = halves(raw[k][i] & 0xffffu, raw[k][i] >> 16, e);
-        qs = __builtin_amdgcn_ldexpf(qs, e);
-      }
-#pragma unroll
-      for (int k = 0; k < kK; ++k) *(u4*)((uint8_t*)sh_o + ((n * kK + k) * 64 + lane) * 16) = raw[k];
-      if (hl == 0) sh_qs[n][col] = qs;
+        for (int i = 0; i < 4; ++i) raw[k][i] = halves(raw[k][i] & 0xffffu, raw[k][i] >> 16, e);
+      qs = __builtin_amdgcn_ldexpf(qs, e);
     }
+#pragma unroll
+    for (int k = 0; k < kK; ++k) *(u4*)((uint8_t*)sh_o + ((wave * kK + k) * 64 + lane) * 16) = raw[k];
+    if (hl == 0) sh_qs[wave][col] = qs;
   }
   __syncthreads();
   __builtin_amdgcn_sched_barrier(0);
