@@ -598,7 +598,9 @@ rq_status rq_block_tree_attention_workspace(const rq_block_cache* c,
  * is that of the last cached token (-1 in an empty cache) + 1 + its depth.  A
  * row that sees nothing is 0.  The cache is left as it was, its accumulated
  * weights too: which nodes stay is not known yet.  Accuracy, ws and counters
- * as rq_block_attention.  Asynchronous. */
+ * as rq_block_attention: nodes count in blocks of 32 as the tail does, and a
+ * cap's tanh is the coarser one from 17 query rows a kv-head on.
+ * Asynchronous. */
 rq_status rq_block_tree_attention(const rq_block_cache* c, int32_t layer,
                                   const rq_block_tree* t, void* ws,
                                   uint64_t ws_bytes, rq_stream stream);

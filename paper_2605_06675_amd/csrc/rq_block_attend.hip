@@ -14,6 +14,10 @@
 // Long contexts are bound by memory: 32 units of 32768 tokens (268 MB) 47 us, 5.7
 // TB/s where a plain read reaches 7.  Short ones by a chain of latencies (1001
 // tokens 7.8 us): lengths, codes, the four waves' sums, parts, ticket, merge.
+//
+// A tree of up to 16 rows takes the same way, its own nodes as 16-bit blocks behind the
+// cached ones (3 nodes of 4 heads over 1001 tokens 9.6 us, 4 of 16 sequences
+// over 8192, 270 MB, 47.3).
 #include <algorithm>
 
 #include "rq_block.h"

@@ -1,20 +1,29 @@
 // Attention of a tree's nodes over the block-scaled 8-bit cache and each other, for
-// more than 32 query rows a unit.
+// more than 16 query rows a unit.
 //
 //   out = softmax(f(scale q . k) - slope distance) v
 //
-// A workgroup owns up to 64 rows of a unit (token-major, the heads of a group
-// together); its eight waves take turns at the blocks of 32 tokens, each with all
-// rows, one running maximum and sum, and the next block's codes in flight.  On
-// v_mfma_f32_32x32x16_f16 S^T = K Q^T leaves a lane with 16 tokens of one row, the
-// operand that O^T = V^T P^T wants of it.  Every code is converted to fp16 once for
-// the 64 rows, in the registers of the wave that uses it: nothing is shared but the
-// queries, which are read from LDS, so no barrier separates the waves, and of a
-// SIMD's two one's products meet the other's exponentials.  The cached tokens are
-// before every node: only the tail and the nodes' own blocks are masked.
+// A workgroup owns 32 or 64 rows of a unit (token-major, the heads of a group
+// together) and a part of its tokens; its four or eight waves take turns at the blocks
+// of 32 tokens, each with all rows, one running maximum and sum, and the next block's
+// codes in flight.  On v_mfma_f32_32x32x16_f16 S^T = K Q^T leaves a lane with 16 tokens
+// of one row, the operand that O^T = V^T P^T wants of it.  Every code is converted to
+// fp16 once for the rows, in the registers of the wave that uses it: nothing is shared
+// but the queries, which are read from LDS, so no barrier separates the waves.  The
+// cached tokens are before every node: only the tail and the nodes' own blocks are
+// masked.
 //
 // A block's value scale goes into the exponent, and P' is an fp16 pair hi + lo (22
 // bits), as in the other attention kernels.
+//
+// 16 sequences of 8 kv-heads, 28 rows and up to 8192 tokens (204 MB) take 43 to 51 us,
+// 4 to 4.7 TB/s: memory, and lengths that differ.  256 rows, 64 units of 8192 tokens
+// (69 GFLOP, 104 with P's low halves) 103 to 108 us, 0.65 PFLOP/s (1.0): of a SIMD's
+// cycles the matrix unit has 45 %, the vector unit 41 %, and its two waves hardly
+// overlap them, at a clock that the products lower to 2.0 GHz.  Reads of the queries
+// further ahead, raised priorities and three stages of codes changed nothing.  1001
+// tokens and 32 rows 11.9 us, two launches of latencies: lengths, queries, codes, the
+// waves' sums, parts.
 #include "rq_block.h"
 
 namespace rq {

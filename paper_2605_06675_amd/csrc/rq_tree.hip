@@ -25,7 +25,8 @@ __device__ __forceinline__ int parent_of(const int32_t* parents, int b, int n, i
 // In two levels of 32 nodes, a word each: a node first follows its parents inside
 // its own word, twice as far a step (5 at most), which gives that word's bits and the
 // ancestor where the chain leaves it; a row then goes from word to word by those (at
-// most 31 steps more).  Bound by latency.
+// most 31 steps more).  Bound by the launch and latency: 16 trees of 64 nodes 2.4 us,
+// eight of 1000 3.8, a chain of 1024 8.0 (followed node by node in its words 12.8).
 constexpr int kMaskThreads = 256;
 
 __global__ void __launch_bounds__(kMaskThreads) tree_mask_kernel(TreeMaskLaunch a) {
