@@ -665,14 +665,14 @@ typedef struct rq_block_layers {
 
 /* Append a path of drafted tokens to every layer: in layer l, sequence b takes
  * the rows k[l][b][.][path[b][j]] and v, j < count[b], as rq_block_append does.
- * lengths: device int32 [n_layers][batch], tokens held before.  path: device
- * int32 [batch][n_path], nodes 0..n_nodes - 1; count: device int32 [batch],
- * 0..n_path (as rq_tree_verify leaves them).  Tokens that do not fit the
- * capacity are dropped.  new_lengths: device int32 [n_layers][batch], receives
- * the lengths after it; it may be lengths itself.  Each of past (the lengths
- * before), fitting (how many fitted) and dropped (how many did not) receives
- * int32 [n_layers][batch]; NULL: not wanted.  The arrays must not overlap
- * otherwise.  Asynchronous. */
+ * n_layers <= 65535. lengths: device int32 [n_layers][batch], tokens held
+ * before. path: device int32 [batch][n_path], nodes 0..n_nodes - 1; count:
+ * device int32 [batch], 0..n_path (as rq_tree_verify leaves them). Tokens
+ * that do not fit the capacity are dropped. new_lengths: device int32
+ * [n_layers][batch], receives the lengths after it; it may be lengths
+ * itself. Each of past (the lengths before), fitting (how many fitted) and
+ * dropped (how many did not) receives int32 [n_layers][batch]; NULL: not
+ * wanted. The arrays must not overlap otherwise. Asynchronous. */
 rq_status rq_block_accept(const rq_block_cache* c, const int32_t* lengths,
                           int32_t n_nodes, int32_t n_path, const int32_t* path,
                           const int32_t* count, const rq_block_layers* k,

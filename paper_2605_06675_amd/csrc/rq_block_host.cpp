@@ -524,6 +524,7 @@ rq_status rq_block_accept(const rq_block_cache* c, const int32_t* lengths, int32
                           rq_stream stream) {
   rq_status st = check_buffers(c, 0);
   if (st != RQ_OK) return st;
+  if (c->n_layers > 65535) return fail(RQ_EUNSUPPORTED, "more than 65535 layers");
   if (n_nodes < 1 || n_nodes > RQ_MAX_NODES)
     return fail(RQ_EINVAL, "n_nodes %d outside 1..%d", n_nodes, RQ_MAX_NODES);
   if (n_path < 1 || n_path > RQ_MAX_NODES)
