@@ -18,9 +18,10 @@
 //
 // 16 sequences of 8 kv-heads, 28 rows and up to 8192 tokens (204 MB) take 43 to 51 us,
 // 4 to 4.7 TB/s: memory, and lengths that differ.  256 rows, 64 units of 8192 tokens
-// (69 GFLOP, 104 with P's low halves) 103 to 108 us, 0.65 PFLOP/s (1.0): of a SIMD's
-// cycles the matrix unit has 45 %, the vector unit 41 %, and its two waves hardly
-// overlap them, at a clock that the products lower to 2.0 GHz.  Reads of the queries
+// (69 GFLOP, 104 with P's low halves) 103 to 108 us, 0.65 PFLOP/s (1.0, where a large
+// library product reaches 1.2): the products, at the clock that they leave (2.0 GHz).
+// Without the low halves' 82.5, without the scores' 82.7, but with all loads from the
+// cache 104.5, without exponentials 100.6, queries in registers 98.  Reads of the queries
 // further ahead, raised priorities and three stages of codes changed nothing.  1001
 // tokens and 32 rows 11.9 us, two launches of latencies: lengths, queries, codes, the
 // waves' sums, parts.
