@@ -23,7 +23,7 @@
 // Without the low halves' 82.5, without the scores' 82.7, but with all loads from the
 // cache 104.5, without exponentials 100.6, queries in registers 98.  Reads of the queries
 // further ahead, raised priorities and three stages of codes changed nothing.  1001
-// tokens and 32 rows 11.9 us, two launches of latencies: lengths, queries, codes, the
+// tokens and 32 rows 11.1 us, two launches of latencies: lengths, queries, codes, the
 // waves' sums, parts.
 #include "rq_block.h"
 
