@@ -761,3 +761,40 @@ def test_attend_at_the_end_of_the_longest_cache(n, window):
     ratio = 2 * s * math.log(2) + 2.0 ** -21 + (cap / 32 / 256 + 64) * 2.0 ** -24
     err = (o.cpu()[0].double() - want).abs() / ((ratio[..., None] + 2.0 ** -21) * V.abs().max())
     assert float(err.max()) <= 1
+
+
+def test_verifications_at_once():
+    """Two trees, each with a workgroup for every CU, in graphs on two streams: parts of
+    both wait for parts that do not run yet."""
+    g = torch.Generator().manual_seed(12)
+    B, n, V = 32, 12, 64000
+    made = []
+    for i in range(2):
+        parents = [some_parents(n, 10 * i + b, "star" if b % 2 else "tree") for b in range(B)]
+        w = torch.randint(V, (B, n), generator=g).int()
+        t = probabilities(g, (B, n, V), torch.float32, 0.5)
+        d = 0.3 * t
+        d.scatter_add_(2, w.long()[:, None].expand(B, n, n), torch.full((B, n, n), 0.7 / n))
+        u = torch.rand(B, n, generator=g)
+        layout = rq.DraftTree(ints(parents))
+        x = [y.cuda() for y in (w, t, u, d)]
+        want = [y.tolist() for y in layout.verify(*x)]
+        for b in range(B):
+            path, token = tree.verify(parents[b], w[b].tolist(), t[b].double().numpy(), d[b].double().numpy(),
+                                      u[b].double().numpy(), n)
+            assert want[0][b] == path + [-1] * (n - len(path)) and want[2][b] == token
+        stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            for _ in range(20):
+                got = layout.verify(*x)
+        made.append((graph, stream, got, want, x, layout))
+    for _ in range(3):
+        for graph, stream, got, _, _, _ in made:
+            with torch.cuda.stream(stream):
+                for y in got:
+                    y.fill_(77)
+                graph.replay()
+        torch.cuda.synchronize()
+        for _, _, got, want, _, _ in made:
+            assert [y.tolist() for y in got] == want
