@@ -959,8 +959,10 @@ class DraftTree:
 
     def verify(self, tokens, target, uniforms, draft=None, room=None, stream=None):
         """(path, count, next) of rq_tree_verify: the accepted nodes ([batch]
-        [room]; at most n_nodes), how many, and the token drawn behind them.  The
-        tensors are this tree's own: a later call writes them again."""
+        [room]), how many, and the token drawn behind them.  The tensors are this
+        tree's own: a later call writes them again.  room: n_nodes by default; no
+        path is longer than the tree's depth + 1, and BlockCache.accept plans for
+        the whole room."""
         import torch
         B, n = self.parents.shape
         room = n if room is None else room
@@ -1063,9 +1065,8 @@ class BlockCache:
         if layer not in self._replayed:
             self.bound[layer] += n
 
-    def _room(self, layer, n, stream, read=None):
-        """Bound on the tokens after n more (read: the lengths, where they are
-        on the host already)."""
+    def _room(self, layer, n, stream):
+        """Bound on the tokens after n more."""
         import torch
         capacity = self.desc.capacity
         s, capturing = self._on(stream)
@@ -1077,7 +1078,7 @@ class BlockCache:
         held = self.bound[layer]
         if held + n > capacity:          # (an upper bound: padding counts)
             with torch.cuda.stream(s):
-                held = int((self.lengths if read is None else read)[layer].max())
+                held = int(self.lengths[layer].max())
             if held + n > capacity:
                 raise ValueError(f"tokens {held} + {n} exceed the capacity "
                                  f"{capacity}")
@@ -1161,16 +1162,24 @@ class BlockCache:
         """Append verified drafted tokens to every layer: the rows of k, v
         ([n_layers][batch][n_kv_heads][n_nodes][head_dim]) that path ([batch][room])
         names, count ([batch]) of each sequence (DraftTree.verify's).  `bound` grows
-        by path's room: where it would pass the capacity, the lengths are read (a
-        wait) before the call is refused."""
+        by path's room; where it would pass the capacity, lengths and counts are
+        read (a wait): a call is refused where its counts do not fit, else what the
+        sequences then hold is the bound."""
         import torch
-        room, read = path.shape[1], None
+        room, layers, capacity = path.shape[1], self.desc.n_layers, self.desc.capacity
         s, capturing = self._on(stream)
-        if not capturing and max(self.bound) + room > self.desc.capacity:
+        if capturing:
+            bounds = [self._room(layer, room, stream) for layer in range(layers)]
+        else:
+            bounds = [held + room for held in self.bound]
+        if max(bounds) > capacity:
+            _tree_array(count, "count", self.desc._device, (self.desc.batch,), torch.int32)
             with torch.cuda.stream(s):
-                read = self.lengths.cpu()
-        bounds = [self._room(layer, room, stream, read)
-                  for layer in range(self.desc.n_layers)]
+                held = (self.lengths + count.clamp(0, room)).amax(1).tolist()
+            if max(held) > capacity:
+                raise ValueError(f"tokens {max(held)} exceed the capacity {capacity}")
+            bounds = [capacity if layer in self._replayed else n
+                      for layer, n in enumerate(held)]
         past, fitting, dropped = self._last.unbind()
         rq_block_accept(self.desc, self.lengths, path, count, k, v, self.lengths,
                         past, fitting, dropped, stream)

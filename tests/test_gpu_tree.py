@@ -798,3 +798,36 @@ def test_verifications_at_once():
         torch.cuda.synchronize()
         for _, _, got, want, _, _ in made:
             assert [y.tolist() for y in got] == want
+
+
+def test_accept_fits_by_counts_not_by_room():
+    """A path with more room than is left: what its counts ask for decides, layer by
+    layer, and is the bound then."""
+    s = Layers("int8", layers=2, B=3, cap=64)
+    s.append(50, [50, 40, 0])
+    s.r[1].append(9, [9, 1, 0])                               # the second layer: 59, 41, 0
+    s.accept(12, [[0, 4, 11], [0], []])
+    s.check()
+    assert s.c.bound == [53, 62]                              # (59 + 12 > 64: all were read)
+    s.accept(12, [[7, 3], list(range(12)), [0]])
+    s.check()
+    assert s.c.bound == [55, 64]
+    k, v = (x.cuda() for x in s.nodes(12))
+    path = ints([list(range(12))] * 3)
+    for count in ([1, 0, 0], [0, 12, 0], [99, -5, 0]):        # 65, 65 and 76 in the second layer
+        with pytest.raises(ValueError, match="capacity"):
+            s.c.accept(k, v, path, ints(count))
+    s.check()
+    assert s.c.lengths.tolist() == [s.r[0].lengths(), s.r[1].lengths()]
+    s.accept(12, [[], [3, 4, 5], [6] * 12])
+    s.check()
+    # a graph that appends: the bound stays the capacity, an eager call's counts decide
+    count = ints([0, 1, 0])
+    graph, _ = graph_of(lambda: s.c.accept(k, v, path, count))
+    assert s.c.bound == [64, 64]
+    s.accept(12, [[], [2], [1, 3]])
+    s.check()
+    assert s.c.bound == [64, 64]
+    graph.replay()
+    s.took(k.cpu(), v.cpu(), [[], [0], []])
+    s.check()
