@@ -623,8 +623,8 @@ typedef struct rq_tree_draft {
                                were drawn from, each by itself; or NULL: they
                                were not drawn (the likeliest tokens, say)  */
   int64_t draft_stride_batch, draft_stride_node;
-  const float* uniforms;    /* device [batch][n_nodes], in [0, 1): node i's
-                               test; a root's draws the last token         */
+  const float* uniforms;    /* device [batch][n_nodes], 0..1 (NaN: 0): node
+                               i's test; a root's draws the last token     */
   int32_t n_path;           /* room in path: 1..n_nodes                    */
   int32_t* path;            /* device [batch][n_path]: the accepted nodes in
                                order, the root first; -1 behind them       */

@@ -844,7 +844,7 @@ def rq_tree_verify(tokens, parents, target, draft, uniforms, path, count, next,
     target: float32, float16 or bfloat16 [batch][n_nodes][vocab], the target's
     probabilities behind each node; draft: the draft's, of its type and shape (both
     any strides, contiguous rows), or None: the drafted tokens were not drawn;
-    uniforms: float32 [batch][n_nodes] in [0, 1); new_len: int32 [batch].
+    uniforms: float32 [batch][n_nodes], 0..1; new_len: int32 [batch].
     Receives path: int32 [batch][room], the accepted nodes; count: int32 [batch];
     next: int32 [batch], the token drawn behind them.  ws: device byte tensor of at
     least rq_tree_verify_workspace bytes, zeroed before its first call (every call

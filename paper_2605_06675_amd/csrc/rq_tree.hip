@@ -239,7 +239,8 @@ __global__ void __launch_bounds__(kThreads) tree_verify_kernel(TreeVerifyLaunch 
     x = x < 0 ? 0 : (x < a.vocab ? x : a.vocab - 1);
     parent[t] = up;
     token[t] = x;
-    u[t] = gptr(a.uniforms)[at];
+    const float number = gptr(a.uniforms)[at];
+    u[t] = number > 0.0f ? __builtin_fminf(number, 1.0f) : 0.0f;     // (NaN as 0)
     child[t] = sibling[t] = kNone;
   }
   if (t == 0) {

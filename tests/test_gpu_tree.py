@@ -831,3 +831,33 @@ def test_accept_fits_by_counts_not_by_room():
     graph.replay()
     s.took(k.cpu(), v.cpu(), [[], [0], []])
     s.check()
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+def test_verify_takes_uniforms_out_of_range_as_the_nearest_inside(drawn):
+    """0 and 1; NaN counts as 0.  The first part of a row has no mass."""
+    g = torch.Generator().manual_seed(9)
+    V, n = 20000, 3
+    given = [-1.0, -math.inf, math.nan, 1.0, 2.0, math.inf, 0.25]
+    u = torch.tensor([[a, b, 0.5] for a in given for b in given])
+    B = len(u)
+    target = probabilities(g, (B, n, V), torch.float32, 0.5)
+    target[:, :, :9000] = 0.0
+    target[:, :, V - 1] *= 2.0 ** -40                         # (adds nothing to a sum)
+    draft = target.clone()
+    tokens = torch.randint(9000, V, (B, n), generator=g)
+    draft.scatter_(2, tokens[:, None].expand(B, n, n), 0.9)
+    draft[::2, :, 100] = 0.5
+    tokens[::2, 1] = 100                                      # a token without mass
+    inside = torch.where(u > 0, u.clamp(max=1.0), torch.zeros_like(u))
+    inside[u.isnan()] = 0.0
+    parents = [[-1, 0, 0]] * B
+    results = []
+    for x in (inside, u):
+        path, count, last = (torch.full(s, 77, dtype=torch.int32, device="cuda") for s in ((B, n), (B,), (B,)))
+        ws = torch.zeros(rq.rq_tree_verify_workspace(B, n, V), dtype=torch.uint8, device="cuda")
+        rq.rq_tree_verify(tokens.int().cuda(), ints(parents), target.cuda(), draft.cuda() if drawn else None, x.cuda(),
+                          path, count, last, ws)
+        results.append([y.tolist() for y in (path, count, last)])
+    want = verify(parents, tokens.tolist(), target, draft if drawn else None, inside)
+    assert results[0] == list(want) and results[1] == results[0]
