@@ -104,6 +104,7 @@ struct BlockTreeLaunch : BlockAttendLaunch {
   int words;
   int most;                // bound on the cached tokens (max_tokens: that and n)
   int group_rows, waves;   // of a workgroup, where there are more than 16 rows
+  int plain;               // no cap, window or slopes
 };
 
 // The accepted path's rows of every layer.

@@ -239,6 +239,7 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
 // rows 13.9 / 20.8.
 struct TreePlan : Plan {
   int group_rows, waves;
+  bool plain;         // no options
   uint64_t most;      // bytes whatever the options
 };
 
@@ -248,13 +249,13 @@ TreePlan plan_tree(const rq_block_cache* c, const rq_block_tree* t) {
   const int64_t rows = t->n_nodes * G;
   p.row_tiles = (int)((rows + 15) / 16);
   p.prompt = p.row_tiles > 1;
+  p.plain = t->cap == 0.0f && !t->window && !t->slopes;
   const int64_t nodes = (t->n_nodes + rq::kBlockTokens - 1) / rq::kBlockTokens;
   const int64_t whole = (t->max_tokens + rq::kBlockTokens - 1) / rq::kBlockTokens + nodes;
   int64_t blocks = whole;
   if (t->window) blocks = std::min<int64_t>(blocks, (int64_t)t->window / rq::kBlockTokens + 2 + nodes);
   int64_t s = 1, most = 1;       // (most: whatever the options)
   if (p.prompt) {
-    const bool plain = t->cap == 0.0f && !t->window && !t->slopes;
     float best = 0.0f;
     for (int tiles = 1; tiles <= 2; ++tiles)
       for (int waves = 4; waves <= 8; waves += 4) {
@@ -262,7 +263,7 @@ TreePlan plan_tree(const rq_block_cache* c, const rq_block_tree* t) {
         for (int round = 0; round <= 2; ++round) {
           const int64_t split = std::max<int64_t>(round * slots / groups, 1);
           most = std::max(most, std::min(split, (whole + waves - 1) / waves));
-          if (tiles == 2 && !plain && c->head_dim == 128) continue;
+          if (tiles == 2 && !p.plain && c->head_dim == 128) continue;
           const int64_t n = std::min(split, (blocks + waves - 1) / waves);
           const int64_t rounds = (groups * n + slots - 1) / slots, each = (blocks + n * waves - 1) / (n * waves);
           const float us = rounds * (each * (tiles == 1 ? 1.9f : 3.1f) * c->head_dim / 128 + (tiles == 1 ? 6.0f : 10.0f)) +
@@ -511,6 +512,7 @@ rq_status rq_block_tree_attention(const rq_block_cache* c, int32_t layer, const 
   a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.part);
   a.group_rows = p.group_rows;
   a.waves = p.waves;
+  a.plain = p.plain;
   a.tickets = use_tickets(p, c, a.n * a.G);
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return launched(p.prompt ? rq::launch_tree_rows(a, s) : rq::launch_tree_attend(a, s),

@@ -564,29 +564,26 @@ __global__ void __launch_bounds__(64 * kWaves, 2) tree_rows_kernel(BlockTreeLaun
 }
 
 template <int FMT, int D, bool BF16, int RT, int kWaves>
-void launch(const BlockTreeLaunch& a, hipStream_t s) {
+hipError_t launch(const BlockTreeLaunch& a, hipStream_t s) {
   const dim3 grid((unsigned)((a.n * a.G + 32 * RT - 1) / (32 * RT) * a.splits) * a.c.B * a.c.H), block(64 * kWaves);
-  if (a.cap == 0.0f && !a.window && !a.slopes)
+  if (a.plain)
     hipLaunchKernelGGL((tree_rows_kernel<FMT, D, BF16, RT, kWaves, true>), grid, block, 0, s, a);
   else if constexpr (D == 64 || RT == 1)
     hipLaunchKernelGGL((tree_rows_kernel<FMT, D, BF16, RT, kWaves, false>), grid, block, 0, s, a);
+  else
+    return hipErrorInvalidValue;           // (no plan asks for it)
+  return hipGetLastError();
 }
 
 template <int FMT, int D, bool BF16>
-void launch(const BlockTreeLaunch& a, hipStream_t s) {
-  if (a.group_rows == 32)
-    a.waves == 4 ? launch<FMT, D, BF16, 1, 4>(a, s) : launch<FMT, D, BF16, 1, 8>(a, s);
-  else
-    a.waves == 4 ? launch<FMT, D, BF16, 2, 4>(a, s) : launch<FMT, D, BF16, 2, 8>(a, s);
+hipError_t launch(const BlockTreeLaunch& a, hipStream_t s) {
+  if (a.group_rows == 32) return a.waves == 4 ? launch<FMT, D, BF16, 1, 4>(a, s) : launch<FMT, D, BF16, 1, 8>(a, s);
+  return a.waves == 4 ? launch<FMT, D, BF16, 2, 4>(a, s) : launch<FMT, D, BF16, 2, 8>(a, s);
 }
 
 template <int FMT, int D>
 hipError_t launch(const BlockTreeLaunch& a, hipStream_t s) {
-  if (a.c.is_bf16)
-    launch<FMT, D, true>(a, s);
-  else
-    launch<FMT, D, false>(a, s);
-  const hipError_t e = hipGetLastError();
+  const hipError_t e = a.c.is_bf16 ? launch<FMT, D, true>(a, s) : launch<FMT, D, false>(a, s);
   return e != hipSuccess ? e : launch_block_merge(a, s);
 }
 
