@@ -161,13 +161,17 @@ __device__ __forceinline__ const RQ_CONSTANT T* cptr(const T* p) {
   return (const RQ_CONSTANT T*)p;
 }
 
-// Cached and new tokens of batch entry b, whatever the device arrays hold:
-// 0 <= past, new <= n, past + new <= most.
-__device__ __forceinline__ void block_lengths(const int32_t* past, const int32_t* new_len, int b,
-                                              int n, int most, int* p, int* w) {
+// New tokens of batch entry b, whatever the device array holds: 0 <= new <= n, most.
+__device__ __forceinline__ int new_tokens(const int32_t* new_len, int b, int n, int most) {
   int nw = new_len ? gptr(new_len)[b] : n;
   nw = nw < 0 ? 0 : (nw > n ? n : nw);
-  nw = nw > most ? most : nw;
+  return nw > most ? most : nw;
+}
+
+// Cached and new tokens of batch entry b: 0 <= past, past + new <= most.
+__device__ __forceinline__ void block_lengths(const int32_t* past, const int32_t* new_len, int b,
+                                              int n, int most, int* p, int* w) {
+  const int nw = new_tokens(new_len, b, n, most);
   int ps = gptr(past)[b];
   ps = ps < 0 ? 0 : (ps > most - nw ? most - nw : ps);
   *p = __builtin_amdgcn_readfirstlane(ps);

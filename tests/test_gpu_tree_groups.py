@@ -208,6 +208,41 @@ def test_groups_waves_and_splits(fmt, dtype, kind):
     r.tree_attend(n, shape="forest")
 
 
+@types
+@pytest.mark.parametrize("B,H,G,n,T,splits", [(2, 1, 16, 128, 4600, 16), (4, 4, 8, 64, 4000, 8), (4, 8, 8, 64, 2500, 4),
+                                              (8, 8, 8, 64, 2500, 2)])
+def test_padded_chunks_in_splits(dtype, B, H, G, n, T, splits):
+    """Chunks of cached tokens whose sequences take fewer than n, one none: the splits'
+    parts of the other rows hold NaNs, their outputs are left as they were."""
+    new = [n - 29] + [max(0, n // 2 - 13 * b) for b in range(1, B - 1)] + [0]
+    held = [T + n - 29 * b for b in range(B)]
+    r = Filled("e4m3", dtype, B, H, G, 64, held)
+    past = [x - m for x, m in zip(held, new)]
+    q = r.randn(B, H * G, n, 64).to(r.dt)
+    for b, m in enumerate(new):
+        q[b, :, m:] = math.nan
+    o = torch.full(q.shape, 7.5, device="cuda")
+    need = rq.rq_block_attention_workspace(r.c.desc, n, max(held))
+    ws = torch.full((need,), 0xff, dtype=torch.uint8, device="cuda")
+    dq, dp, dn = q.cuda(), ints(past), ints(new)
+    torch.cuda.synchronize()
+
+    def call(stream=None):
+        rq.rq_block_attention(r.c.desc, 0, dp, dq, o, ws, new_len=dn, max_tokens=max(held), stream=stream)
+    kernels = launches(call)
+    assert "block_merge_rows_kernel" in kernels[1][0]
+    assert kernels[0][1][0] == (n * G + 127) // 128 * B * H * splits
+    call()
+    whole, keys, values = r.u, np.zeros((B, H, n, 64)), np.zeros((B, H, n, 64))
+    r.u = []
+    for b, p in enumerate(past):
+        r.u.append([Held(*(u.x[i][:p] for i in (0, 1)), u.pos[:p]) for u in whole[b]])
+        for h, u in enumerate(whole[b]):
+            keys[b, h, :new[b]], values[b, h, :new[b]] = (u.x[i][p:] for i in (0, 1))
+    r.compare_tree(o, q, torch.from_numpy(keys).float(), torch.from_numpy(values).float(), new,
+                   [np.tril(np.ones((m, m), bool)) for m in new], [list(range(m)) for m in new])
+
+
 def test_the_oracle_s_rows_at_once():
     """attend_at_once against tree.attend."""
     g = np.random.default_rng(3)
