@@ -243,6 +243,36 @@ def test_padded_chunks_in_splits(dtype, B, H, G, n, T, splits):
                    [np.tril(np.ones((m, m), bool)) for m in new], [list(range(m)) for m in new])
 
 
+@pytest.mark.parametrize("n", [4, 40])
+def test_trees_of_two_caches_at_once(n):
+    """Two caches' calls in graphs on two streams, neither waited for before the other
+    starts, with nodes for up to 16 rows and for more."""
+    made = []
+    for i in range(2):
+        r = Filled(("int8", "e4m3")[i], "bf16", 2, 2, 4, 64, [3000, 2000 + 500 * i], seed=i)
+        parents = [some_parents(n, 10 * i + b) for b in range(2)]
+        q, (k, v) = r.randn(2, 8, n, 64).to(r.dt), r.nodes(n)
+        layout = rq.DraftTree(ints(parents))
+        d = [x.cuda() for x in (q, k, v)]
+        o = torch.full(q.shape, 7.5, device="cuda")
+        r.c.tree_attention(0, *d, layout, o)
+        stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            for _ in range(50):
+                r.c.tree_attention(0, *d, layout, o)
+        made.append((r, parents, q, k, v, o, stream, graph, layout, d))
+    for _ in range(3):
+        for r, parents, q, k, v, o, stream, graph, layout, d in made:
+            with torch.cuda.stream(stream):
+                o.fill_(7.5)
+                graph.replay()
+        torch.cuda.synchronize()
+        for r, parents, q, k, v, o, stream, graph, layout, d in made:
+            r.compare_tree(o, q, k, v, [n, n], [tree.sees(p) for p in parents],
+                           [[len(c) - 1 for c in tree.ancestors(p)] for p in parents])
+
+
 def test_the_oracle_s_rows_at_once():
     """attend_at_once against tree.attend."""
     g = np.random.default_rng(3)
