@@ -570,12 +570,16 @@ typedef struct rq_block_tree {
   const uint32_t* mask;    /* device [batch][n_nodes][ceil(n_nodes / 32)]:
                               the nodes that each one sees (rq_tree_mask's,
                               or any other, bits of later nodes among them;
-                              bits from new_len on count as 0)             */
+                              bits from new_len on count as 0).  The q, k
+                              and v of all of a sequence's nodes are finite,
+                              also of those that it hides                  */
   const int32_t* depth;    /* device [batch][n_nodes], 0..n_nodes - 1: needed
                               where there is a window or slopes            */
   rq_block_rows q;         /* [batch][n_q_heads][n_nodes][head_dim] and    */
   rq_block_rows k, v;      /* [batch][n_kv_heads][n_nodes][head_dim] in
-                              dtype                                        */
+                              dtype.  Every node has a row in each: a draft
+                              that grows its tree level by level passes the
+                              earlier nodes' queries again                 */
   rq_block_rows out;       /* the shape of q in out_dtype                  */
   int32_t out_dtype;       /* RQ_F32, RQ_F16 or RQ_BF16                    */
   float scale, cap;        /* as rq_block_query, which see                 */

@@ -794,10 +794,10 @@ def rq_block_tree_attention(cache, layer, past, q, k, v, mask, out, ws,
     """Attention of drafted tokens over the cached ones and each other: q: torch
     [batch][n_q_heads][n_nodes][head_dim], k, v: [batch][n_kv_heads][n_nodes]
     [head_dim] in the cache's dtype; out: q's shape in float32, float16 or
-    bfloat16 (all any strides, contiguous rows); mask, depth: rq_tree_mask's
-    (depth where there is a window or slopes); past: device int32 [batch], cached
-    tokens; max_tokens: bound on them (the capacity by default); the rest as
-    rq_block_attention."""
+    bfloat16 (all any strides, contiguous rows; a sequence's are finite, also where
+    the mask hides a node); mask, depth: rq_tree_mask's (depth where there is a window
+    or slopes); past: device int32 [batch], cached tokens; max_tokens: bound on them
+    (the capacity by default); the rest as rq_block_attention."""
     n = q.shape[2] if q.dim() == 4 else -1
     if past is None:
         raise ValueError("past is missing")
@@ -1144,7 +1144,8 @@ class BlockCache:
         """Attention of drafted tokens (tree: a DraftTree; q: [batch][n_q_heads]
         [n_nodes][head_dim], k, v: [batch][n_kv_heads][n_nodes][head_dim]; scale,
         cap, window, slopes as rq_block_attention) over the layer's tokens and each
-        other.  The cache is left as it was: accept appends what is verified."""
+        other.  A sequence's nodes are finite, also those that no other sees.  The
+        cache is left as it was: accept appends what is verified."""
         import torch
         s, capturing = self._on(stream)
         bound = self.desc.capacity if capturing else self.bound[layer]

@@ -236,7 +236,8 @@ Plan plan_attention(const rq_block_cache* c, const rq_block_query* a) {
 // slopes do not fit the registers so for 128 channels.  us with groups of 32 / 64: 64
 // units of 8192 tokens and 64 rows 39.5 / 44.8, 80 rows 54 / 64, 160 rows 103 / 87, 256
 // rows 123 / 107, of 64 channels 78 / 67, capped 100 / 91; 32 units of 500 tokens and 96
-// rows 13.9 / 20.8.
+// rows 13.9 / 20.8.  (The estimate is that of plain blocks: what options cost, for a cap
+// some 1.3 times the plain block, is not in it.)
 struct TreePlan : Plan {
   int group_rows, waves;
   bool plain;         // no options

@@ -18,8 +18,8 @@
 //
 // 16 sequences of 8 kv-heads, 28 rows and up to 8192 tokens (204 MB) take 43 to 51 us,
 // 4 to 4.7 TB/s: memory, and lengths that differ.  256 rows, 64 units of 8192 tokens
-// (69 GFLOP, 104 with P's low halves) 103 to 108 us, 0.65 PFLOP/s (1.0, where a large
-// library product reaches 1.2): the products, at the clock that they leave (2.0 GHz).
+// (69 GFLOP, 104 with P's low halves) 103 to 113 us from card to card, 0.65 PFLOP/s (1.0,
+// where a large library product reaches 1.2): the products, at the clock that they leave (2.0 GHz).
 // Without the low halves' 82.5, without the scores' 82.7, but with all loads from the
 // cache 104.5, without exponentials 100.6, queries in registers 98.  Reads of the queries
 // further ahead, raised priorities and three stages of codes changed nothing.  1001
@@ -88,6 +88,8 @@ struct Rows {
 };
 
 // PLAIN: no cap, no window, no slopes.
+// Registers of a lane: 32 rows 120 to 190; 64 rows 172 to 189 of 64 channels, and all
+// 256 of 128 channels (up to 3 more in scratch memory) or with options (4 to 12).
 template <int FMT, int D, bool BF16, int RT, int kWaves, bool PLAIN>
 __global__ void __launch_bounds__(64 * kWaves, 2) tree_rows_kernel(BlockTreeLaunch a) {
   constexpr int kThreads = 64 * kWaves, kRows = 32 * RT, kStride = D + 4, kE = D / 32, kK = D / 16, kBufs = kWaves / 2;
